@@ -50,7 +50,7 @@
 extern "C" {
 #endif
 
-#define ACTQKV_VERSION 107
+#define ACTQKV_VERSION 108
 
 enum {
   ACTQKV_OK = 0,
@@ -535,6 +535,87 @@ int actqkv_gather_blocks_cached(const actqkv_shape* shape, int n_windows, const 
  * known size; with the cache kept in host memory (see actqkv_gather_blocks) it carries the local
  * span from one working cache to the next and new blocks back to the host store. */
 int actqkv_copy_bytes(void* dst, const void* src, size_t bytes, void* stream);
+
+/* ---- Paged cache: blocks of a pool, handed out to sequences page by page ------------------------------------------------
+ *
+ * A page is a block of the blocked cache (layouts above), anywhere in a pool:
+ *     k_pages  [n_pages][Hk][Bs][D]     v_pages  [n_pages][Hk][D][Bs]
+ *   pages    device int32 [batch][max_pages]: sequence s has its tokens [i*Bs, (i+1)*Bs) in page pages[s][i].  Entries outside
+ *            [0, n_pages) stand for no page: nothing is written there and nobody sees its tokens.  Sequences may share
+ *            pages that are only read (a common prefix).
+ *   n_ctx    device int32 [batch]: tokens of the sequence, the call's new ones included (clamped to max_pages * Bs).
+ *   row_start  device int32 [batch + 1], not decreasing: sequence s brings the rows row_start[s] .. row_start[s+1] - 1 of q,
+ *            k_new, v_new, out and lse (none, one or many), its last tokens: row row_start[s] + i of m rows is at
+ *            position n_ctx[s] - m + i.  Rows that belong to no sequence are not read and their results not written; a row
+ *            at a negative position (m > n_ctx) is not in the cache and sees nothing.
+ *   n_rows   rows of the arrays (1 .. 2^22); max_new  the most rows a sequence brings (1 .. n_rows; of more, the first
+ *            max_new are taken as all of them).
+ * Of the shape, n_q_heads, n_kv_heads, head_dim, block_size, dtype and softmax_scale are used.  Slots behind a sequence's last
+ * token may hold anything, NaN and infinities included; its own keys and values must be finite.  What lies on the device is
+ * clamped, never trusted: a wrong value gives a wrong result but no out-of-bounds access. */
+
+/* Bytes of workspace of the paged calls that take one, for calls of at most batch sequences, n_rows rows, max_new rows of a
+ * sequence and max_pages pages.  As for the other calls: zero-filled once, and calls that share one ordered on one stream (a graph
+ * that was captured with it is a call). */
+size_t actqkv_paged_workspace_bytes(const actqkv_shape* shape, int batch, int n_rows, int max_new, int max_pages);
+
+/* Keys and values of the new tokens into their pages.
+ *   k_new, v_new  [n_rows][Hk][D], storage dtype.  Only the new tokens' slots are written. */
+int actqkv_paged_append(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* k_new,
+                        const void* v_new, const int32_t* row_start, const int32_t* n_ctx, const int32_t* pages,
+                        int max_pages, void* k_pages, void* v_pages, int n_pages, void* stream);
+
+/* Attention of the new tokens over everything their sequences have in the cache (the new tokens' keys and values
+ * included: actqkv_paged_append comes first): whole prompts, chunks and single tokens, together in one call.
+ *   q        [n_rows][H][D], storage dtype.  Query head h reads KV head h / G.
+ *   The score of a row at position p and a key at position j, with s = scale * <q, k>:
+ *     softcap > 0:  s = softcap * tanh(s / softcap)                      (0: none)
+ *     slopes [H] fp32, may be NULL:  s = s - slopes[h] * |p - j|
+ *   The row sees the positions first <= j < end:
+ *     first = max(0, row_first[row], p - window + 1)    row_first [n_rows] int32, may be NULL (of a document mask: where the
+ *                                                       row's document begins); window 0: none
+ *     end   = min(row_end[row], n_ctx)                  row_end [n_rows] int32 (of a prefix mask: max(p + 1, prefix length));
+ *                                                       NULL: p + 1
+ *   out      [n_rows][H][D] = softmax over the keys seen, times their values; 0 for a row that sees none.
+ *   lse      [n_rows][H] fp32, natural-log sum of exp of the scores (-infinity for a row that sees none); may be NULL.
+ * Errors: EINVAL (null, sizes, softcap negative, infinite or NaN, window < 0), ESHAPE, EALIGN, EWORKSPACE. */
+int actqkv_paged_attention(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q,
+                           const int32_t* row_start, const int32_t* n_ctx, const int32_t* pages, int max_pages,
+                           const void* k_pages, const void* v_pages, int n_pages, float softcap, int window,
+                           const float* slopes, const int32_t* row_first, const int32_t* row_end, void* out, float* lse,
+                           void* workspace, size_t ws_bytes, void* stream);
+
+/* The same, and the account of the attention weight that every cached token has received:
+ *   weights_out[s][hk][j] = weights_in[s][hk][j] + sum of exp(score - lse) over the last weight_rows (>= 1; at least the
+ *            sequence's rows: all of them) rows of sequence s and the G query heads of KV head hk, for the tokens j they see.
+ *   weights_in, weights_out  [batch][Hk][weight_stride] fp32, weight_stride >= max_pages * Bs and a multiple of 4; may be the
+ *            same array.  The first max_pages * Bs entries of a row are written.  Fill them with zero when a sequence begins.
+ *   lse      required.
+ * The sums are taken in an order that depends on the sizes alone: the same call gives the same bits. */
+int actqkv_paged_attention_weights(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q,
+                                   const int32_t* row_start, const int32_t* n_ctx, const int32_t* pages, int max_pages,
+                                   const void* k_pages, const void* v_pages, int n_pages, float softcap, int window,
+                                   const float* slopes, const int32_t* row_first, const int32_t* row_end, void* out,
+                                   float* lse, int weight_rows, const float* weights_in, float* weights_out,
+                                   int64_t weight_stride, void* workspace, size_t ws_bytes, void* stream);
+
+/* Eviction: every KV head of every sequence with more than `budget` tokens keeps, of its n_ctx tokens, the first keep_first, the
+ * last keep_last and, of those between, the budget - keep_first - keep_last with the largest weight (equal weights: the lower
+ * positions; NaN below everything).  The kept tokens keep their order and move to the slots 0 .. budget - 1, keys, values
+ * and weights; a shorter sequence keeps everything.
+ *   weights  [batch][Hk][weight_stride] fp32, weight_stride >= max_pages * Bs.
+ *   to_pages device int32 [batch][to_max_pages]: the pages the kept tokens move to, none of which is a page of `pages`; NULL,
+ *            or the array `pages` itself: in place (to_max_pages = max_pages), for sequences that share no page.
+ *   to_weights  [batch][Hk][to_weight_stride], to_weight_stride >= to_max_pages * Bs; the kept tokens' weights, and 0 up to entry
+ *            to_max_pages * Bs; may be `weights` with the same stride; NULL: not written.
+ *   kept     [batch][Hk][budget] int32: the old positions, ascending; -1 behind the last.
+ *   n_kept   [batch] int32 = min(n_ctx, budget): the n_ctx of the calls that follow.  Not the array n_ctx.
+ *   Afterwards positions are slots: window, slopes and masks of later calls count kept tokens.
+ * Errors: EINVAL (null, keep_first + keep_last > budget, a budget larger than to_max_pages pages), ESHAPE, EALIGN. */
+int actqkv_paged_evict(const actqkv_shape* shape, int batch, const int32_t* n_ctx, const int32_t* pages, int max_pages,
+                       void* k_pages, void* v_pages, int n_pages, const float* weights, int64_t weight_stride,
+                       int keep_first, int keep_last, int budget, const int32_t* to_pages, int to_max_pages,
+                       float* to_weights, int64_t to_weight_stride, int32_t* kept, int32_t* n_kept, void* stream);
 
 /* How an attention call of batch windows of m >= 2 tokens in bf16 is cut up (host only, nothing is launched): cut[0] query rows of
  * a workgroup, cut[1] query tiles of a window and KV head, cut[2] pieces they are in altogether (equal: not cut; the tiles are

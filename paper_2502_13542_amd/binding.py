@@ -89,6 +89,13 @@ SIGNATURES = {
                                          _i, _i, _i, _vp, _vp, _vp]),
     "actqkv_retrieval_attention_windows": (_i, [_shp, _i, _i, _vp, _vp, _vp, _i, _vp, _vp, _vp, _i, _vp, _vp, _vp, _sz,
                                                 _i, _vp]),
+    "actqkv_paged_workspace_bytes": (_sz, [_shp, _i, _i, _i, _i]),
+    "actqkv_paged_append": (_i, [_shp, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _i, _vp, _vp, _i, _vp]),
+    "actqkv_paged_attention": (_i, [_shp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _i, ctypes.c_float, _i, _vp, _vp, _vp,
+                                    _vp, _vp, _vp, _sz, _vp]),
+    "actqkv_paged_attention_weights": (_i, [_shp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _i, ctypes.c_float, _i, _vp, _vp,
+                                            _vp, _vp, _vp, _i, _vp, _vp, _i64, _vp, _sz, _vp]),
+    "actqkv_paged_evict": (_i, [_shp, _i, _vp, _vp, _i, _vp, _vp, _i, _vp, _i64, _i, _i, _i, _vp, _i, _vp, _i64, _vp, _vp, _vp]),
     "actqkv_last_error": (ctypes.c_char_p, []),
     "actqkv_prefill_cut": (_i, [_shp, _i, _i, _i, _i, _vp]),
     "actqkv_version": (_i, []),
@@ -339,3 +346,42 @@ def retrieval_attention(shape: CShape, batch: int, m: int, q, k_cache, v_cache, 
     attend = _calls().retrieval_attention_per_head if per_head else _calls().retrieval_attention
     attend(shape, batch, m, q, k_cache, v_cache, seq_stride, nb_capacity, n_ctx, idx, n_sel, k_cap, out, lse,
            workspace, stream)
+
+
+def paged_workspace_bytes(shape: CShape, batch: int, n_rows: int, max_new: int, max_pages: int) -> int:
+    n = load_library().actqkv_paged_workspace_bytes(ctypes.byref(shape), batch, n_rows, max_new, max_pages)
+    if n == 0:
+        raise ActQKVError(-1, last_error())
+    return n
+
+
+def paged_append(shape: CShape, batch: int, n_rows: int, max_new: int, k_new, v_new, row_start, n_ctx, pages, max_pages: int,
+                 k_pages, v_pages, n_pages: int, stream=None) -> None:
+    _calls().paged_append(shape, batch, n_rows, max_new, k_new, v_new, row_start, n_ctx, pages, max_pages, k_pages, v_pages,
+                          n_pages, stream)
+
+
+def paged_attention(shape: CShape, batch: int, n_rows: int, max_new: int, q, row_start, n_ctx, pages, max_pages: int, k_pages,
+                    v_pages, n_pages: int, out, lse, workspace, softcap: float = 0.0, window: int = 0, slopes=None,
+                    row_first=None, row_end=None, stream=None) -> None:
+    """Attention of a ragged batch's new tokens over its pages; see the header."""
+    _calls().paged_attention(shape, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, k_pages, v_pages, n_pages,
+                             softcap, window, slopes, row_first, row_end, out, lse, workspace, stream)
+
+
+def paged_attention_weights(shape: CShape, batch: int, n_rows: int, max_new: int, q, row_start, n_ctx, pages, max_pages: int,
+                            k_pages, v_pages, n_pages: int, out, lse, weight_rows: int, weights_in, weights_out,
+                            weight_stride: int, workspace, softcap: float = 0.0, window: int = 0, slopes=None,
+                            row_first=None, row_end=None, stream=None) -> None:
+    """The same with the attention weight of every cached token added to its account; see the header."""
+    _calls().paged_attention_weights(shape, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, k_pages, v_pages,
+                                     n_pages, softcap, window, slopes, row_first, row_end, out, lse, weight_rows, weights_in,
+                                     weights_out, weight_stride, workspace, stream)
+
+
+def paged_evict(shape: CShape, batch: int, n_ctx, pages, max_pages: int, k_pages, v_pages, n_pages: int, weights,
+                weight_stride: int, keep_first: int, keep_last: int, budget: int, to_pages, to_max_pages: int, to_weights,
+                to_weight_stride: int, kept, n_kept, stream=None) -> None:
+    """The tokens with the least attention weight leave the cache; see the header."""
+    _calls().paged_evict(shape, batch, n_ctx, pages, max_pages, k_pages, v_pages, n_pages, weights, weight_stride, keep_first,
+                         keep_last, budget, to_pages, to_max_pages, to_weights, to_weight_stride, kept, n_kept, stream)

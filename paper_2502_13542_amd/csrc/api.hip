@@ -6,6 +6,7 @@
 #include <cstdio>
 #include <cstring>
 
+#include "checks.h"
 #include "common.h"
 #include "launch.h"
 #include "select_body.h"
@@ -28,9 +29,7 @@ int hip_status(const char* what) {
   return set_error(ACTQKV_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-static int check_shape(const actqkv_shape* sh) {
+int check_shape(const actqkv_shape* sh) {
   if (sh == nullptr) return set_error(ACTQKV_EINVAL, "shape is NULL");
   if (sh->n_q_heads < 1 || sh->n_kv_heads < 1 || sh->head_dim < 1 || sh->n_rep < 1 ||
       sh->n_init < 0 || sh->n_local < 0)
@@ -57,7 +56,7 @@ static int check_shape(const actqkv_shape* sh) {
   return ACTQKV_OK;
 }
 
-static int check_batch(int batch) {
+int check_batch(int batch) {
   if (batch < 1) return set_error(ACTQKV_EINVAL, "batch %d < 1", batch);
   if (batch > kMaxBatch) return set_error(ACTQKV_ESHAPE, "batch %d > %d", batch, kMaxBatch);
   return ACTQKV_OK;
@@ -73,32 +72,6 @@ static int check_blocks(int nb_capacity, int nb_begin, int k_cap, bool use_k) {
                      nb_capacity - nb_begin);
   return ACTQKV_OK;
 }
-
-#define ACTQKV_REQUIRE_PTR(p)                                                       \
-  do {                                                                              \
-    if ((p) == nullptr) return set_error(ACTQKV_EINVAL, #p " is NULL");             \
-    if (!aligned16(p)) return set_error(ACTQKV_EALIGN, #p " is not 16-byte aligned"); \
-  } while (0)
-#define ACTQKV_REQUIRE_SMALL(p, a)                                                          \
-  do {                                                                                      \
-    if ((p) == nullptr) return set_error(ACTQKV_EINVAL, #p " is NULL");                     \
-    if ((reinterpret_cast<uintptr_t>(p) & ((a)-1)) != 0)                                    \
-      return set_error(ACTQKV_EALIGN, #p " is not %d-byte aligned", int(a));                \
-  } while (0)
-#define ACTQKV_OPTIONAL_SMALL(p, a)                                                         \
-  do {                                                                                      \
-    if ((p) != nullptr && (reinterpret_cast<uintptr_t>(p) & ((a)-1)) != 0)                  \
-      return set_error(ACTQKV_EALIGN, #p " is not %d-byte aligned", int(a));                \
-  } while (0)
-#define ACTQKV_OPTIONAL_PTR(p)                                                                   \
-  do {                                                                                           \
-    if ((p) != nullptr && !aligned16(p)) return set_error(ACTQKV_EALIGN, #p " is not 16-byte aligned"); \
-  } while (0)
-#define ACTQKV_TRY(expr)      \
-  do {                        \
-    int rc_ = (expr);         \
-    if (rc_ != ACTQKV_OK) return rc_; \
-  } while (0)
 
 bool prefill_mfma_supported(const actqkv_shape& sh, int m);
 bool prefill_merge_after(const actqkv_shape& sh, int s_lo);

@@ -12,10 +12,12 @@
 //   s  tensor of the shape's storage type        b  tensor of bf16, whatever the shape says
 //   h  like s, but pinned host memory will do    w  workspace (a size_t parameter follows: its bytes)
 //   p  address (an integer)                      q  stream, None for the current one
+// A string that begins with @ is of a call whose tensors all have to be on the current device (where it launches).
 // A tensor parameter accepts None (the library decides whether it may be NULL).
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <dlfcn.h>
 
@@ -45,6 +47,7 @@ struct Args {
   actqkv_shape shape;
   size_t ws_bytes = 0;
   bool ok = true;
+  bool here = false;               // tensors have to be on the current device
 
   PyObject* next() {
     if (!ok) return nullptr;
@@ -69,6 +72,8 @@ struct Args {
     // (the runtime is asked about every host tensor: an answer kept by address would outlive the tensor)
     if (!t.is_cuda() && !(host_too && t.is_pinned())) {
       ok = raise(ACTQKV_EINVAL, host_too ? "tensor is neither on the GPU nor in pinned host memory" : "tensor is not on the GPU");
+    } else if (here && t.is_cuda() && t.get_device() != c10::hip::current_device()) {
+      ok = raise(ACTQKV_EINVAL, ("tensor is on device " + std::to_string(t.get_device()) + ", not on the current one").c_str());
     } else if (!t.is_contiguous()) {
       ok = raise(ACTQKV_EINVAL, "tensor is not contiguous");
     } else if (!any_type && t.scalar_type() != want) {
@@ -189,6 +194,8 @@ template <typename... P> struct Entry<int(P...)> {
     a.at = args;
     a.end = args + n;
     a.kinds = kinds;
+    a.here = *kinds == '@';
+    a.kinds += a.here;
     const std::tuple<P...> values{Take<P>::from(a)...};    // (in order: a braced list)
     if (a.ok && a.at != a.end) {
       PyErr_SetString(PyExc_TypeError, "too many arguments");
@@ -229,7 +236,11 @@ template <typename... P> struct Entry<int(P...)> {
   X(score_blocks_per_head, "sq")                                 \
   X(select, "q")                                                 \
   X(window_step, "ssssswq")                                      \
-  X(decode_step, "ssssssswq")
+  X(decode_step, "ssssssswq")                                    \
+  X(paged_append, "@ssssq")                                      \
+  X(paged_attention, "@sssswq")                                  \
+  X(paged_attention_weights, "@sssswq")                          \
+  X(paged_evict, "@ssq")
 
 #define ACTQKV_DEFINE(name, kinds)                                                          \
   Entry<decltype(actqkv_##name)> entry_##name;                                              \

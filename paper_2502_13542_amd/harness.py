@@ -901,3 +901,105 @@ class HostCachePrefill:
             attended[g].record(attender)
         return {t: dict(idx=self.idx_all[t], n_sel=self.n_sel_all[t], idx_slots=self.idx_slots_all[t])
                 for t in range(plan.n_windows)}
+
+
+# ---------------------------------------------------------------- a pool of pages
+class PagedRunner:
+    """The calls of a layer whose cache is a pool of pages: the workspace they share, and the checks of sizes that the
+    library, which has pointers only, cannot make.  One stream at a time.
+
+    batch, n_rows, max_new and max_pages are the most that a call brings: sequences, rows of all of them, rows of one,
+    pages of one.  A call's own numbers follow from its tensors: row_start [batch + 1], n_ctx [batch], pages [batch][max_pages];
+    the library's header says what they hold."""
+
+    def __init__(self, shape: LayerShape, batch: int, n_rows: int, max_new: int, max_pages: int, device="cuda"):
+        self.shape, self.batch, self.n_rows, self.max_new, self.max_pages = shape, batch, n_rows, max_new, max_pages
+        self.cs = B.c_shape(shape)
+        ws = B.paged_workspace_bytes(self.cs, batch, n_rows, max_new, max_pages)
+        self.workspace = torch.zeros(ws, dtype=torch.uint8, device=device)
+        self._page = shape.n_kv_heads * shape.block_size * shape.head_dim
+
+    def _table(self, n_ctx, pages, k_pages, v_pages) -> Tuple[int, int, int]:
+        batch, max_pages = pages.shape
+        n_pages = k_pages.shape[0]
+        if batch > self.batch or max_pages > self.max_pages:
+            raise B.ActQKVError(-1, f"{batch} sequences of {max_pages} pages: made for {self.batch} of {self.max_pages}")
+        if n_ctx.numel() != batch:
+            raise B.ActQKVError(-1, f"n_ctx has {n_ctx.numel()} entries for {batch} sequences")
+        if k_pages.numel() != n_pages * self._page or v_pages.numel() != n_pages * self._page:
+            raise B.ActQKVError(-1, "k_pages and v_pages are not pools of pages of this shape")
+        return batch, max_pages, n_pages
+
+    def _rows(self, batch: int, row_start, rows, heads: int, *same) -> Tuple[int, int]:
+        n_rows = rows.shape[0]
+        if row_start.numel() != batch + 1:
+            raise B.ActQKVError(-1, f"row_start has {row_start.numel()} entries for {batch} sequences")
+        if n_rows > self.n_rows:
+            raise B.ActQKVError(-1, f"{n_rows} rows: made for {self.n_rows}")
+        for t in (rows, *same):
+            if t.numel() != n_rows * heads * self.shape.head_dim:
+                raise B.ActQKVError(-1, f"tensor of {t.numel()} elements, expected {n_rows} rows of {heads} heads")
+        return n_rows, min(self.max_new, n_rows)
+
+    def _per_row(self, n: int, *tensors) -> None:
+        for t in tensors:
+            if t is not None and t.numel() != n:
+                raise B.ActQKVError(-1, f"tensor of {t.numel()} elements, expected {n}")
+
+    def append(self, k_new, v_new, row_start, n_ctx, pages, k_pages, v_pages, stream=None) -> None:
+        """Keys and values [n_rows][Hk][D] of the new tokens into their pages."""
+        batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, v_pages)
+        n_rows, max_new = self._rows(batch, row_start, k_new, self.shape.n_kv_heads, v_new)
+        if n_rows == 0:
+            return
+        B.paged_append(self.cs, batch, n_rows, max_new, k_new, v_new, row_start, n_ctx, pages, max_pages, k_pages, v_pages,
+                       n_pages, stream)
+
+    def attend(self, q, row_start, n_ctx, pages, k_pages, v_pages, out, lse=None, softcap: float = 0.0, window: int = 0,
+               slopes=None, row_first=None, row_end=None, stream=None) -> None:
+        """out [n_rows][H][D], and lse [n_rows][H], of the new tokens' queries over the cache."""
+        batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, v_pages)
+        n_rows, max_new = self._rows(batch, row_start, q, self.shape.n_q_heads, out)
+        self._per_row(n_rows, row_first, row_end)
+        self._per_row(n_rows * self.shape.n_q_heads, lse)
+        self._per_row(self.shape.n_q_heads, slopes)
+        if n_rows == 0:
+            return
+        B.paged_attention(self.cs, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, k_pages, v_pages, n_pages,
+                          out, lse, self.workspace, softcap, window, slopes, row_first, row_end, stream)
+
+    def attend_weigh(self, q, row_start, n_ctx, pages, k_pages, v_pages, out, lse, weight_rows: int, weights, weights_out=None,
+                     softcap: float = 0.0, window: int = 0, slopes=None, row_first=None, row_end=None, stream=None) -> None:
+        """attend, and what the last weight_rows rows of every sequence give each cached token added to weights
+        [batch][Hk][max_pages * Bs] (weights_out None: in place)."""
+        batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, v_pages)
+        n_rows, max_new = self._rows(batch, row_start, q, self.shape.n_q_heads, out)
+        weights_out = weights if weights_out is None else weights_out
+        self._per_row(n_rows, row_first, row_end)
+        self._per_row(n_rows * self.shape.n_q_heads, lse)
+        self._per_row(self.shape.n_q_heads, slopes)
+        self._per_row(batch * self.shape.n_kv_heads * weights.shape[-1], weights, weights_out)
+        if n_rows == 0:
+            raise B.ActQKVError(-1, "no rows: there is nothing to weigh")
+        B.paged_attention_weights(self.cs, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, k_pages, v_pages,
+                                  n_pages, out, lse, weight_rows, weights, weights_out, weights.shape[-1], self.workspace,
+                                  softcap, window, slopes, row_first, row_end, stream)
+
+    def evict(self, n_ctx, pages, k_pages, v_pages, weights, keep_first: int, keep_last: int, budget: int, kept, n_kept,
+              to_pages=None, to_weights=None, stream=None) -> None:
+        """Leaves every sequence `budget` tokens per KV head: in place, with the weights, or (to_pages) in other pages, with the
+        weights in to_weights.  kept [batch][Hk][budget], n_kept [batch]."""
+        batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, v_pages)
+        if to_pages is None:
+            to_pages, to_weights = pages, weights if to_weights is None else to_weights
+        rows = batch * self.shape.n_kv_heads
+        self._per_row(rows * weights.shape[-1], weights)
+        self._per_row(rows * budget, kept)
+        self._per_row(batch, n_kept)
+        self._per_row(batch * to_pages.shape[-1], to_pages)
+        to_stride = 0
+        if to_weights is not None:
+            to_stride = to_weights.shape[-1]
+            self._per_row(rows * to_stride, to_weights)
+        B.paged_evict(self.cs, batch, n_ctx, pages, max_pages, k_pages, v_pages, n_pages, weights, weights.shape[-1],
+                      keep_first, keep_last, budget, to_pages, to_pages.shape[-1], to_weights, to_stride, kept, n_kept, stream)

@@ -1,0 +1,398 @@
+"""The calls on a paged cache against a plain fp64 implementation (oracle/paged_oracle.py), on the GPU.
+
+Tolerances are bounds by arithmetic.  e(t) = half a step of type t relative to the value: fp32 2^-24, bf16 2^-8.
+A score is a sum of D products in fp32, each factor exact: off by at most (D + 8) e(fp32) sum |q k| scale, the 8 for the
+scaling, cap, bias and the change to units of log2.  With S the largest such sum of a row (plus the bias, rounded once), a
+probability is off by at most the factor 1 + delta, delta = 2 (D + 16) e(fp32) S + (n + 16) e(fp32) (the sum over n keys, the
+exponential).  So with M = sum p |v|:
+  out   fp32: 2 delta M + 2 e |out|;  bf16: the probabilities enter the product rounded to bf16, e(bf16) M more, and the result is
+        rounded once, e(bf16) |out|.
+  lse   delta + 4 e(fp32) |lse|
+  weights  the sum over the rows of p (delta_row + ...) as above, + 2 e(fp32) per addition of what is there."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged_oracle as po
+from paper_2502_13542_amd import binding as B
+
+from paged_utils import BS, Batch, f64, shape_of
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+E32, E16 = 2.0 ** -24, 2.0 ** -8
+
+SHAPES = {"llama": (32, 8, 128, "bf16"), "g7": (28, 4, 128, "bf16"), "mha64": (3, 3, 64, "bf16"), "g8_64": (8, 1, 64, "bf16"),
+          "fp32_64": (8, 2, 64, "fp32"), "fp32_g3": (6, 2, 128, "fp32"), "g5_64": (10, 2, 64, "bf16"), "fp32_g8": (8, 1, 128, "fp32")}
+BATCHES = {
+    "one": [(1, 1)],
+    "steps": [(1, 127), (1, 128), (1, 129), (1, 1), (0, 5), (1, 700)],
+    "few": [(3, 3), (2, 260), (4, 4), (0, 0), (1, 64)],
+    "chunks": [(130, 130), (1, 300), (64, 321), (0, 10), (200, 513), (1, 1)],
+    "prompt": [(513, 513)],
+    "long_step": [(1, 5003), (1, 2000)],
+    "long_tail": [(17, 3001)],
+}
+FORMS = {
+    "plain": {},
+    "cap": dict(softcap=20.0),
+    "slopes": dict(slopes=True),
+    "cap_slopes": dict(softcap=5.0, slopes=True),
+    "window": dict(window=100),
+    "window1": dict(window=1),
+    "first": dict(first=True),
+    "end": dict(end=True),
+    "all": dict(softcap=30.0, slopes=True, window=300, first=True, end=True),
+}
+
+
+def form_of(b, kind, seed):
+    """The form's arguments on the host."""
+    f = dict(FORMS[kind])
+    rng = np.random.default_rng(seed + 77)
+    pos = b.positions()
+    if f.pop("slopes", False):
+        f["slopes"] = (2.0 ** -(1.0 + np.arange(b.shape.n_q_heads) % 8)).astype(np.float32)
+    if f.pop("first", False):            # documents, rows that see nothing, and values that have to be clamped
+        first = np.maximum(pos - rng.integers(0, 200, b.n_rows), 0)
+        first[rng.random(b.n_rows) < 0.1] = 2 ** 31 - 1
+        first[rng.random(b.n_rows) < 0.1] = -(2 ** 31)
+        f["row_first"] = first
+    if f.pop("end", False):
+        end = np.maximum(pos + 1, rng.integers(0, 400, b.n_rows))
+        end[rng.random(b.n_rows) < 0.1] = 2 ** 31 - 1
+        end[rng.random(b.n_rows) < 0.05] = -5
+        f["row_end"] = end
+    return f
+
+
+def on_device(f):
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device=DEV)
+    g = dict(f)
+    for k in ("row_first", "row_end"):
+        if k in g:
+            g[k] = i32(g[k])
+    if "slopes" in g:
+        g["slopes"] = torch.tensor(g["slopes"], device=DEV)
+    return g
+
+
+def deltas(b, want):
+    d = b.shape.head_dim
+    n = max(b.n_ctx.max(), 1)
+    return (2 * (d + 16) * want["size"] + n + 16) * E32
+
+
+def check_out(b, want, out, lse, rows):
+    delta = deltas(b, want)[rows]
+    got, ref, mass = f64(out)[rows], want["out"][rows], want["mass"][rows]
+    assert np.isfinite(got).all()
+    bound = 2 * delta[..., None] * mass + 2 * E32 * np.abs(ref)
+    if b.shape.dtype == "bf16":
+        bound += E16 * mass + E16 * (np.abs(ref) + 2 * delta[..., None] * mass + E16 * mass)
+    off = np.abs(got - ref) - bound
+    assert (off <= 0).all(), f"out off by {off.max():.3e} more than its bound at {np.unravel_index(off.argmax(), off.shape)}"
+    if lse is not None:
+        got, ref = f64(lse)[rows], want["lse"][rows]
+        none = np.isneginf(ref)
+        assert (np.isneginf(got) == none).all()
+        off = np.abs(got[~none] - ref[~none]) - (delta[~none] + 4 * E32 * np.abs(ref[~none]))
+        assert off.size == 0 or (off <= 0).all(), f"lse off by {off.max():.3e} more than its bound"
+
+
+def run_attention(b, kind="plain", seed=0, weight_rows=0, runner=None):
+    f = form_of(b, kind, seed)
+    r = runner or b.runner()
+    t = b.dev()
+    q = b.q.to(DEV)
+    out = torch.full_like(q, 7.0)
+    lse = torch.full((b.n_rows, b.shape.n_q_heads), 7.0, device=DEV)
+    w = w_out = None
+    if weight_rows:
+        g = torch.Generator().manual_seed(seed + 5)
+        w = torch.rand(b.batch, b.shape.n_kv_heads, b.max_pages * BS, generator=g)
+        w_out = torch.full_like(w, -3.0).to(DEV)
+        r.attend_weigh(q, t["row_start"], t["n_ctx"], t["pages"], t["k_pages"], t["v_pages"], out, lse, weight_rows, w.to(DEV),
+                       w_out, **on_device(f))
+    else:
+        r.attend(q, t["row_start"], t["n_ctx"], t["pages"], t["k_pages"], t["v_pages"], out, lse, **on_device(f))
+    torch.cuda.synchronize()
+    k64, v64 = b.pools64()
+    want = po.attention(f64(b.q), b.row_start, b.n_ctx, b.pages, k64, v64, b.shape.head_dim ** -0.5, weight_rows=weight_rows,
+                        weights=None if w is None else w.double().numpy(), **f)
+    rows = np.arange(b.row_start[0], b.row_start[-1])
+    check_out(b, want, out, lse, rows)
+    nobody = np.setdiff1d(np.arange(b.n_rows), rows)
+    assert (f64(out)[nobody] == 7.0).all() and (f64(lse)[nobody] == 7.0).all(), "rows of nobody were written"
+    if weight_rows:
+        d, n, group = b.shape.head_dim, b.n_ctx.max(), b.shape.group
+        adds = b.max_new * group + 2
+        bound = 2 * (d + 16) * E32 * want["votes_size"] + (n + 32 + 2 * adds) * E32 * want["votes"] + 2 * E32 * np.abs(want["weights"])
+        off = np.abs(f64(w_out) - want["weights"]) - bound
+        assert (off <= 0).all(), f"weights off by {off.max():.3e} more than their bound"
+    return out, lse, w_out, want
+
+
+@pytest.mark.parametrize("shape", list(SHAPES))
+@pytest.mark.parametrize("batch", list(BATCHES))
+def test_attention(shape, batch):
+    b = Batch(shape_of(*SHAPES[shape]), BATCHES[batch], 11, extra_rows=(2, 3))
+    run_attention(b)
+
+
+@pytest.mark.parametrize("kind", [k for k in FORMS if k != "plain"])
+@pytest.mark.parametrize("shape,batch", [("g7", "chunks"), ("g8_64", "chunks"), ("fp32_64", "chunks"), ("llama", "steps"),
+                                         ("fp32_g3", "few"), ("mha64", "few"), ("llama", "long_tail"), ("fp32_g3", "long_tail")])
+def test_attention_forms(shape, batch, kind):
+    b = Batch(shape_of(*SHAPES[shape]), BATCHES[batch], 13, extra_rows=(0, 1), garbage=float("inf"), scale=2.0)
+    run_attention(b, kind, 3)
+
+
+@pytest.mark.parametrize("shape", ["llama", "g7", "g5_64", "mha64", "fp32_64", "fp32_g3"])
+@pytest.mark.parametrize("batch,rows,kind", [("steps", 1, "plain"), ("few", 2, "cap"), ("chunks", 32, "plain"),
+                                             ("chunks", 1000, "all"), ("prompt", 513, "slopes"), ("long_step", 1, "window"),
+                                             ("long_tail", 5, "first"), ("prompt", 64, "end")])
+def test_attention_weights(shape, batch, rows, kind):
+    b = Batch(shape_of(*SHAPES[shape]), BATCHES[batch], 17, extra_rows=(1, 1))
+    run_attention(b, kind, 5, weight_rows=rows)
+
+
+@pytest.mark.parametrize("shape", ["llama", "fp32_64"])
+@pytest.mark.parametrize("batch", ["steps", "chunks", "long_tail"])
+def test_weights_in_place_and_twice_the_same_bits(shape, batch):
+    b = Batch(shape_of(*SHAPES[shape]), BATCHES[batch], 19)
+    r, t, q = b.runner(), b.dev(), b.q.to(DEV)
+    args = (q, t["row_start"], t["n_ctx"], t["pages"], t["k_pages"], t["v_pages"])
+    got = []
+    for _ in range(3):
+        out, lse = torch.zeros_like(q), torch.zeros(b.n_rows, b.shape.n_q_heads, device=DEV)
+        w = torch.ones(b.batch, b.shape.n_kv_heads, b.max_pages * BS, device=DEV)
+        r.attend_weigh(*args, out, lse, 40, w)
+        w2 = torch.empty_like(w)
+        r.attend_weigh(*args, out, lse, 40, torch.ones_like(w), w2)
+        torch.cuda.synchronize()
+        assert torch.equal(w, w2)
+        got.append((out, lse, w))
+    for x in got[1:]:
+        assert all(torch.equal(a, c) for a, c in zip(got[0], x))
+    plain = torch.zeros_like(q)
+    r.attend(*args, plain, None)
+    torch.cuda.synchronize()
+    assert torch.equal(plain, got[0][0]), "the attention of the two calls differs"
+
+
+@pytest.mark.parametrize("shape", ["g7", "fp32_64"])
+def test_pages_of_nobody_inside_a_sequence(shape):
+    """Entries outside the pool are tokens that nobody sees; a page may serve two sequences."""
+    b = Batch(shape_of(*SHAPES[shape]), [(3, 700), (150, 700), (1, 300), (1, 260)], 23)
+    b.pages[0, 1], b.pages[1, 0], b.pages[1, 3], b.pages[2, 0] = -1, b.n_pages, 2 ** 31 - 1, -(2 ** 31)
+    b.pages[3, :2] = b.pages[0, [0, 2]]
+    out, lse, w, want = run_attention(b, weight_rows=2)
+    b.pages[2, :] = -1                            # a whole sequence without pages: its row sees nothing
+    out, lse, w, want = run_attention(b, weight_rows=2)
+    assert np.isneginf(want["lse"][b.row_start[2]]).all()
+
+
+@pytest.mark.parametrize("shape", ["llama", "fp32_64"])
+def test_lengths_that_have_to_be_clamped(shape):
+    b = Batch(shape_of(*SHAPES[shape]), [(5, 200), (3, 130), (40, 256), (2, 256)], 29, garbage=None, extra_entries=0)
+    b.n_ctx = np.array([2 ** 31 - 1, -(2 ** 31), 17, 256])      # more than the pages hold; none; 40 rows of 17 tokens
+    b.pages = np.where(b.pages < 0, 0, b.pages)
+    run_attention(b, weight_rows=3)
+    r, t = b.runner(), b.dev()
+    k0, v0 = b.pools64()
+    r.append(b.k_new.to(DEV), b.v_new.to(DEV), t["row_start"], t["n_ctx"], t["pages"], t["k_pages"], t["v_pages"])
+    b.pages[0] = b.pages[3] = [0, 1]
+    torch.cuda.synchronize()
+    # row_start out of order and out of range: nothing is read or written outside the arrays
+    t["row_start"].copy_(torch.tensor([-(2 ** 31), 2 ** 31 - 1, 3, 1, 2 ** 31 - 1], dtype=torch.int32))
+    guard = torch.full((b.n_rows + 2, b.shape.n_q_heads, b.shape.head_dim), 7.0, dtype=b.q.dtype, device=DEV)
+    r.attend(b.q.to(DEV), t["row_start"], t["n_ctx"], t["pages"], t["k_pages"], t["v_pages"], guard[1:-1], None)
+    torch.cuda.synchronize()
+    assert (guard[0] == 7.0).all() and (guard[-1] == 7.0).all()
+
+
+@pytest.mark.parametrize("shape", list(SHAPES))
+@pytest.mark.parametrize("batch", list(BATCHES))
+def test_append(shape, batch):
+    b = Batch(shape_of(*SHAPES[shape]), BATCHES[batch], 31, extra_rows=(1, 2), garbage=None)
+    if batch == "chunks":
+        b.pages[0, 1] = -1                        # no page: its tokens go nowhere
+    r, t = b.runner(), b.dev()
+    r.append(b.k_new.to(DEV), b.v_new.to(DEV), t["row_start"], t["n_ctx"], t["pages"], t["k_pages"], t["v_pages"])
+    torch.cuda.synchronize()
+    # (rows of nobody lie outside row_start)
+    k, v = po.append(f64(b.k_new), f64(b.v_new), b.row_start, b.n_ctx, b.pages, f64(b.k_pages), f64(b.v_pages))
+    assert np.array_equal(f64(t["k_pages"]), k) and np.array_equal(f64(t["v_pages"]), v)
+
+
+EVICT = [  # sequences, keep_first, keep_last, budget
+    ([(0, 1000)], 4, 100, 300),
+    ([(0, 300), (0, 299), (0, 301), (0, 0), (0, 1), (0, 900)], 0, 0, 300),
+    ([(0, 5000), (0, 140)], 128, 12, 140),        # nothing to choose
+    ([(0, 2500), (0, 700)], 1, 1, 3),
+    ([(0, 300)], 0, 0, 1),
+    ([(0, 4200), (0, 1030)], 7, 33, 1029),
+]
+
+
+@pytest.mark.parametrize("shape", ["llama", "fp32_64", "mha64", "fp32_g3"])
+@pytest.mark.parametrize("case", range(len(EVICT)))
+@pytest.mark.parametrize("kind", ["random", "ties", "flat", "odd"])
+@pytest.mark.parametrize("in_place", [True, False])
+def test_evict(shape, case, kind, in_place):
+    seqs, first, last, budget = EVICT[case]
+    sh = shape_of(*SHAPES[shape])
+    to_max = -(-budget // BS)
+    b = Batch(sh, seqs, 37 + case, spare_pages=2 + len(seqs) * to_max, garbage=None)
+    g = torch.Generator().manual_seed(case)
+    w = torch.rand(b.batch, sh.n_kv_heads, b.max_pages * BS, generator=g)
+    if kind == "ties":
+        w = (w * 5).floor()
+    if kind == "flat":
+        w = torch.full_like(w, 0.25)
+    if kind == "odd":                             # every special value, small ones and negative ones
+        pick = torch.randint(0, 10, w.shape, generator=g)
+        values = torch.tensor([float("nan"), float("inf"), -float("inf"), 0.0, -0.0, 1e-42, -1e-42, -1.0, 3.4e38, 1.0])
+        w = values[pick]
+    r, t = b.runner(), b.dev()
+    kept = torch.full((b.batch, sh.n_kv_heads, budget), -7, dtype=torch.int32, device=DEV)
+    n_kept = torch.full((b.batch,), -7, dtype=torch.int32, device=DEV)
+    wd = w.to(DEV)
+    if in_place:
+        to, to_w = b.pages, wd
+        r.evict(t["n_ctx"], t["pages"], t["k_pages"], t["v_pages"], wd, first, last, budget, kept, n_kept)
+    else:
+        to = np.array([[b.free.pop() for _ in range(to_max)] for _ in seqs])
+        to_w = torch.full((b.batch, sh.n_kv_heads, to_max * BS + 4), 9.0, device=DEV)
+        r.evict(t["n_ctx"], t["pages"], t["k_pages"], t["v_pages"], wd, first, last, budget, kept, n_kept,
+                to_pages=torch.tensor(to, dtype=torch.int32, device=DEV), to_weights=to_w)
+    torch.cuda.synchronize()
+    start_w = w.numpy() if in_place else np.full(to_w.shape, 9.0, np.float32)
+    k2, n2, k, v, ww = po.evict(b.n_ctx, b.pages, f64(b.k_pages), f64(b.v_pages), w.numpy(), first, last, budget, to, start_w)
+    assert np.array_equal(n_kept.cpu().numpy(), n2)
+    assert np.array_equal(kept.cpu().numpy(), k2)
+    assert np.array_equal(to_w.cpu().numpy(), ww, equal_nan=True)
+    assert np.array_equal(f64(t["k_pages"]), k) and np.array_equal(f64(t["v_pages"]), v)
+
+
+@pytest.mark.parametrize("shape", ["g7", "fp32_64"])
+def test_a_cache_in_use(shape):
+    """Prompts in chunks, steps, an eviction, more steps: every call's attention over a dense copy of what the cache holds."""
+    sh = shape_of(*SHAPES[shape])
+    hk, d, hq = sh.n_kv_heads, sh.head_dim, sh.n_q_heads
+    g = torch.Generator().manual_seed(41)
+    td = sh.torch_dtype
+    batch, max_pages, n_pages, budget = 3, 6, 20, 200
+    pages = np.random.default_rng(3).permutation(n_pages)[: batch * max_pages].reshape(batch, max_pages)
+    i32 = lambda a: torch.tensor(np.asarray(a), dtype=torch.int32, device=DEV)
+    from paper_2502_13542_amd import harness as H
+    r = H.PagedRunner(sh, batch, 700, 300, max_pages)
+    kp = torch.full((n_pages, hk, BS, d), float("nan"), dtype=td, device=DEV)      # memory as it comes
+    vp = torch.full((n_pages, hk, d, BS), float("nan"), dtype=td, device=DEV)
+    weights = torch.zeros(batch, hk, max_pages * BS, device=DEV)
+    held = [[[] for _ in range(hk)] for _ in range(batch)]         # what each head's slots hold: (k, v) rows
+    account = np.zeros((batch, hk, max_pages * BS))
+    n_ctx = np.zeros(batch, int)
+    pages_d = i32(pages)
+    for step, news in enumerate([(150, 1, 0), (300, 200, 129), (1, 1, 1), (7, 1, 90), "evict", (1, 1, 1), (130, 1, 3), "evict", (1, 1, 1)]):
+        if news == "evict":
+            kept = torch.zeros(batch, hk, budget, dtype=torch.int32, device=DEV)
+            n_kept = torch.zeros(batch, dtype=torch.int32, device=DEV)
+            chosen_by = weights.cpu().numpy()
+            r.evict(i32(n_ctx), pages_d, kp, vp, weights, 4, 50, budget, kept, n_kept)
+            torch.cuda.synchronize()
+            for s in range(batch):
+                for h in range(hk):
+                    old = po.keep(chosen_by[s, h], n_ctx[s], 4, 50, budget)
+                    assert kept[s, h, : len(old)].cpu().tolist() == old
+                    held[s][h] = [held[s][h][o] for o in old]
+                    account[s, h] = np.concatenate([account[s, h, old], np.zeros(max_pages * BS - len(old))])
+            n_ctx = np.minimum(n_ctx, budget)
+            assert n_kept.cpu().tolist() == n_ctx.tolist()
+            continue
+        n_rows = sum(news)
+        k_new, v_new = (torch.randn(n_rows, hk, d, generator=g).to(td) for _ in range(2))
+        q = torch.randn(n_rows, hq, d, generator=g).to(td)
+        start = np.cumsum([0, *news])
+        n_ctx = n_ctx + np.array(news)
+        out, lse = torch.zeros_like(q, device=DEV), torch.zeros(n_rows, hq, device=DEV)
+        table = (i32(start), i32(n_ctx), pages_d, kp, vp)
+        r.append(k_new.to(DEV), v_new.to(DEV), *table)
+        r.attend_weigh(q.to(DEV), *table, out, lse, 16, weights, softcap=25.0)
+        torch.cuda.synchronize()
+        k64, v64 = np.zeros(kp.shape), np.zeros(vp.shape)
+        for s in range(batch):
+            for h in range(hk):
+                for i in range(start[s], start[s + 1]):
+                    held[s][h].append((f64(k_new[i, h]), f64(v_new[i, h])))
+                for j, (kk, vv) in enumerate(held[s][h]):
+                    k64[pages[s, j // BS], h, j % BS], v64[pages[s, j // BS], h, :, j % BS] = kk, vv
+        want = po.attention(f64(q), start, n_ctx, pages, k64, v64, d ** -0.5, softcap=25.0, weight_rows=16, weights=account)
+        b = type("B", (), dict(shape=sh, n_ctx=n_ctx))
+        check_out(b, want, out, lse, np.arange(n_rows))
+        account = want["weights"]
+        assert np.abs(f64(weights) - account).max() < 1e-4, step
+
+
+@pytest.mark.parametrize("shape", ["llama", "fp32_64"])
+def test_replayed_graph(shape):
+    """Append, attention with weights and eviction in one graph, replayed with other lengths and inputs between eager calls."""
+    sh = shape_of(*SHAPES[shape])
+    b = Batch(sh, [(1, 600), (4, 300), (90, 90)], 43, garbage=None)
+    r, t = b.runner(), b.dev()
+    hk = sh.n_kv_heads
+    q, kn, vn = b.q.to(DEV), b.k_new.to(DEV), b.v_new.to(DEV)
+    budget = 128
+    kept = torch.zeros(3, hk, budget, dtype=torch.int32, device=DEV)
+    n_kept = torch.zeros(3, dtype=torch.int32, device=DEV)
+    to = torch.tensor(b.free[:2] + b.pages[2, :1].tolist(), dtype=torch.int32, device=DEV).reshape(3, 1)
+    spare = torch.zeros_like(t["k_pages"][:3]), torch.zeros_like(t["v_pages"][:3])
+    kp, vp = torch.cat([t["k_pages"], spare[0]]), torch.cat([t["v_pages"], spare[1]])
+    to = torch.arange(b.n_pages, b.n_pages + 3, dtype=torch.int32, device=DEV).reshape(3, 1)
+    out, lse = torch.zeros_like(q), torch.zeros(b.n_rows, sh.n_q_heads, device=DEV)
+    w_in = torch.rand(3, hk, b.max_pages * BS, device=DEV)
+    w_out, to_w = torch.zeros_like(w_in), torch.zeros(3, hk, BS, device=DEV)
+
+    def step():
+        table = (t["row_start"], t["n_ctx"], t["pages"], kp, vp)
+        r.append(kn, vn, *table)
+        r.attend_weigh(q, *table, out, lse, 3, w_in, w_out)
+        r.evict(t["n_ctx"], t["pages"], kp, vp, w_out, 2, 30, budget, kept, n_kept, to_pages=to, to_weights=to_w)
+
+    def state():
+        torch.cuda.synchronize()
+        return [x.clone() for x in (out, lse, w_out, kept, n_kept, kp, vp, to_w)]
+
+    step()
+    state()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for n_ctx in ([600, 300, 90], [130, 299, 90], [5, 4, 90], [600, 17, 95]):
+        t["n_ctx"].copy_(torch.tensor(n_ctx, dtype=torch.int32))
+        q.copy_(torch.randn(q.shape).to(q.dtype))
+        step()
+        want = state()
+        for x in (out, lse, w_out, kept, n_kept, to_w):
+            x.zero_()
+        graph.replay()
+        for a, c in zip(state(), want):
+            assert torch.equal(a, c)
+
+
+def test_one_workspace_for_smaller_calls_and_a_side_stream():
+    sh = shape_of(*SHAPES["llama"])
+    big = Batch(sh, [(200, 900), (1, 2000), (17, 64), (3, 3)], 47)
+    r = big.runner()
+    for seqs in ([(1, 1)], [(200, 900), (1, 2000)], [(1, 2100)], [(16, 2000)], [(1, 5)] * 4, [(40, 40), (0, 3), (180, 1000)]):
+        run_attention(Batch(sh, seqs, 53, extra_entries=0), runner=r)
+    side = torch.cuda.Stream()
+    b = Batch(sh, [(1, 700), (30, 300)], 59)
+    t, q = b.dev(), b.q.to(DEV)
+    out, want = torch.zeros_like(q), torch.zeros_like(q)
+    r.attend(q, t["row_start"], t["n_ctx"], t["pages"], t["k_pages"], t["v_pages"], want)
+    torch.cuda.synchronize()
+    r.attend(q, t["row_start"], t["n_ctx"], t["pages"], t["k_pages"], t["v_pages"], out, stream=side)
+    side.synchronize()
+    assert torch.equal(out, want)
