@@ -106,6 +106,11 @@ struct PagedWeights {
   int64_t stride;
 };
 
+constexpr int kStepWgs = 1024;            // workgroups that a step call is cut into
+bool paged_step_supported(const actqkv_shape& sh, int max_new);
+size_t paged_step_scratch_most(const actqkv_shape& sh, int batch, int max_new, int max_pages);
+int launch_paged_step(const actqkv_shape& sh, const PagedAttn& p, const PagedWeights* weights, const Workspace& ws,
+                      hipStream_t stream);
 size_t paged_workspace_bytes(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages);
 int launch_paged_append(const actqkv_shape& sh, const PagedTable& t, const void* k_new, const void* v_new,
                         void* k_pages, void* v_pages, hipStream_t stream);

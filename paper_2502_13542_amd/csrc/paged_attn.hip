@@ -88,8 +88,8 @@ __global__ __launch_bounds__(kPsThreads) void paged_weights_kernel(PagedAttn p, 
 }
 
 size_t paged_workspace_bytes(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages) {
-  (void)sh; (void)batch; (void)n_rows; (void)max_new; (void)max_pages;
-  return kCounterBytes;
+  (void)n_rows;
+  return kCounterBytes + align_up(paged_step_scratch_most(sh, batch, max_new, max_pages), 256);
 }
 
 template <typename T, int D, bool kCap, bool kBias>
@@ -109,7 +109,7 @@ static void launch_form(const PagedAttn& p, const PagedWeights* w, hipStream_t s
 }
 int launch_paged_attention(const actqkv_shape& sh, const PagedAttn& p, const PagedWeights* weights, const Workspace& ws,
                            hipStream_t stream) {
-  (void)ws;
+  if (paged_step_supported(sh, p.t.max_new)) return launch_paged_step(sh, p, weights, ws, stream);
   if (sh.dtype == ACTQKV_F32) {
     if (sh.head_dim == 64) launch_form<float, 64>(p, weights, stream);
     else launch_form<float, 128>(p, weights, stream);
