@@ -34,6 +34,7 @@
 
 #include "common.h"
 #include "launch.h"
+#include "mfma_util.h"
 #include "select_body.h"
 
 namespace actqkv {
@@ -56,8 +57,6 @@ constexpr int kPfOrderMax = 64;                      // batch entries the queue 
 constexpr int kPfQueueDone = 256;
 static_assert(kPfQueueDone + 1 <= kSeqCounterOffset - kTicketCounters + kSeqCounters, "queue counters");
 
-__device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
-
 // sum += the eight bf16 values of a packed operand (as fp32): four dot products of a pair with
 // (1, 1).  (Written as assembly: the compiler's builtin for this instruction takes the first
 // pair of a packed vector whatever element is asked for.)
@@ -67,28 +66,6 @@ __device__ __forceinline__ void add_bf16x8(float& sum, bf16x8 v, uint32_t ones) 
   asm("v_dot2c_f32_bf16 %0, %1, %2" : "+v"(sum) : "v"(w.y), "v"(ones));
   asm("v_dot2c_f32_bf16 %0, %1, %2" : "+v"(sum) : "v"(w.z), "v"(ones));
   asm("v_dot2c_f32_bf16 %0, %1, %2" : "+v"(sum) : "v"(w.w), "v"(ones));
-}
-
-// 8 fp32 -> 8 bf16 (round to nearest even), packed as an MFMA operand
-__device__ __forceinline__ bf16x8 pack8(float a0, float a1, float a2, float a3, float a4, float a5,
-                                        float a6, float a7) {
-  typedef __attribute__((ext_vector_type(8))) float f32x8;
-  f32x8 v = {a0, a1, a2, a3, a4, a5, a6, a7};
-  return __builtin_convertvector(v, bf16x8);
-}
-
-// A pointer that is the same in all lanes, pinned to scalar registers (so that adding a
-// 32-bit lane offset to it becomes the scalar-base addressing mode of the load).
-__device__ __forceinline__ const char* uniform_ptr(const char* ptr) {
-  const uint64_t v = reinterpret_cast<uint64_t>(ptr);
-  const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(v));
-  const uint32_t hi = __builtin_amdgcn_readfirstlane(uint32_t(v >> 32));
-  return reinterpret_cast<const char*>((uint64_t(hi) << 32) | lo);
-}
-
-// MFMA row -> key row inside a 32-key group: swap bits 2 and 3.
-__device__ __forceinline__ int perm_row(int i) {
-  return (i & ~12) | ((i & 4) << 1) | ((i & 8) >> 1);
 }
 
 struct PfParams {

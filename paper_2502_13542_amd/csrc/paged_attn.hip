@@ -88,34 +88,37 @@ __global__ __launch_bounds__(kPsThreads) void paged_weights_kernel(PagedAttn p, 
 }
 
 size_t paged_workspace_bytes(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages) {
-  (void)n_rows;
-  return kCounterBytes + align_up(paged_step_scratch_most(sh, batch, max_new, max_pages), 256);
+  return kCounterBytes + align_up(std::max(paged_step_scratch_most(sh, batch, max_new, max_pages),
+                                           paged_chunk_scratch_most(sh, batch, n_rows, max_new, max_pages)), 256);
 }
 
 template <typename T, int D, bool kCap, bool kBias>
-static void launch_both(const PagedAttn& p, const PagedWeights* w, hipStream_t stream) {
-  hipLaunchKernelGGL((paged_attention_kernel<T, D, kCap, kBias>), dim3(p.t.n_rows, p.n_q_heads), dim3(kPsThreads), 0, stream, p);
+static void launch_both(const PagedAttn& p, const PagedWeights* w, bool attend, hipStream_t stream) {
+  if (attend) hipLaunchKernelGGL((paged_attention_kernel<T, D, kCap, kBias>), dim3(p.t.n_rows, p.n_q_heads), dim3(kPsThreads), 0, stream, p);
   if (w != nullptr)
     hipLaunchKernelGGL((paged_weights_kernel<T, D, kCap, kBias>), dim3(p.t.max_pages, p.n_kv_heads, p.t.batch),
                        dim3(kPsThreads), 0, stream, p, *w);
 }
 template <typename T, int D>
-static void launch_form(const PagedAttn& p, const PagedWeights* w, hipStream_t stream) {
+static void launch_form(const PagedAttn& p, const PagedWeights* w, bool attend, hipStream_t stream) {
   const bool cap = p.f.cap_in > 0.f, bias = p.f.slopes != nullptr;
-  if (cap && bias) launch_both<T, D, true, true>(p, w, stream);
-  else if (cap) launch_both<T, D, true, false>(p, w, stream);
-  else if (bias) launch_both<T, D, false, true>(p, w, stream);
-  else launch_both<T, D, false, false>(p, w, stream);
+  if (cap && bias) launch_both<T, D, true, true>(p, w, attend, stream);
+  else if (cap) launch_both<T, D, true, false>(p, w, attend, stream);
+  else if (bias) launch_both<T, D, false, true>(p, w, attend, stream);
+  else launch_both<T, D, false, false>(p, w, attend, stream);
 }
 int launch_paged_attention(const actqkv_shape& sh, const PagedAttn& p, const PagedWeights* weights, const Workspace& ws,
                            hipStream_t stream) {
   if (paged_step_supported(sh, p.t.max_new)) return launch_paged_step(sh, p, weights, ws, stream);
+  const bool attend = !paged_chunk_supported(sh);
+  if (!attend)
+    if (int rc = launch_paged_chunk(sh, p, ws, stream)) return rc;
   if (sh.dtype == ACTQKV_F32) {
-    if (sh.head_dim == 64) launch_form<float, 64>(p, weights, stream);
-    else launch_form<float, 128>(p, weights, stream);
+    if (sh.head_dim == 64) launch_form<float, 64>(p, weights, attend, stream);
+    else launch_form<float, 128>(p, weights, attend, stream);
   } else {
-    if (sh.head_dim == 64) launch_form<uint16_t, 64>(p, weights, stream);
-    else launch_form<uint16_t, 128>(p, weights, stream);
+    if (sh.head_dim == 64) launch_form<uint16_t, 64>(p, weights, attend, stream);
+    else launch_form<uint16_t, 128>(p, weights, attend, stream);
   }
   return hip_status("paged attention");
 }
