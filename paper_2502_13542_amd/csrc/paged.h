@@ -114,6 +114,8 @@ int launch_paged_step(const actqkv_shape& sh, const PagedAttn& p, const PagedWei
 bool paged_chunk_supported(const actqkv_shape& sh);
 size_t paged_chunk_scratch_most(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages);
 int launch_paged_chunk(const actqkv_shape& sh, const PagedAttn& p, const Workspace& ws, hipStream_t stream);
+size_t paged_votes_scratch_most(const actqkv_shape& sh);
+int launch_paged_votes(const actqkv_shape& sh, const PagedAttn& p, const PagedWeights& w, const Workspace& ws, hipStream_t stream);
 size_t paged_workspace_bytes(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages);
 int launch_paged_append(const actqkv_shape& sh, const PagedTable& t, const void* k_new, const void* v_new,
                         void* k_pages, void* v_pages, hipStream_t stream);

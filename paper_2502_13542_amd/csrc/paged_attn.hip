@@ -54,73 +54,36 @@ __global__ __launch_bounds__(kPsThreads) void paged_attention_kernel(PagedAttn p
   if (tid == 0 && p.lse != nullptr) p.lse[size_t(row) * p.n_q_heads + head] = (m_run + log2f(l_run)) * kLn2;
 }
 
-template <typename T, int D, bool kCap, bool kBias>
-__global__ __launch_bounds__(kPsThreads) void paged_weights_kernel(PagedAttn p, PagedWeights w) {
-  __shared__ float ql[D];
-  const int t = blockIdx.x, hk = blockIdx.y, s = blockIdx.z, tid = threadIdx.x;
-  const int group = p.n_q_heads / p.n_kv_heads, j = t * kBlock + tid;
-  const PagedSeq seq = paged_seq(p.t, s);
-  const int page = paged_page(p.t, s, t);
-  float sum = 0.f;
-  if (page >= 0) {
-    const T* kp = static_cast<const T*>(p.k_pages) + (size_t(page) * p.n_kv_heads + hk) * (kBlock * D) + size_t(tid) * D;
-    for (int i = max(seq.m - w.rows, 0); i < seq.m; ++i) {
-      const int row = seq.row0 + i, pos = seq.n - seq.m + i;
-      const PagedSpan v = paged_span(p.f, row, pos, seq.n);
-      for (int g = 0; g < group; ++g) {
-        const int head = hk * group + g;
-        const T* qp = static_cast<const T*>(p.q) + (size_t(row) * p.n_q_heads + head) * D;
-        __syncthreads();
-        if (tid < D) ql[tid] = to_f32(qp[tid]);
-        __syncthreads();
-        const float lse = p.lse[size_t(row) * p.n_q_heads + head];
-        if (j >= v.lo && j < v.hi && lse > -INFINITY) {
-          float dot = 0.f;
-          for (int d = 0; d < D; ++d) dot = fmaf(to_f32(kp[d]), ql[d], dot);
-          const float slope = kBias ? p.f.slopes[head] * kLog2e : 0.f;
-          sum += exp2f(paged_score<kCap, kBias>(p.f, dot, slope, abs(pos - j)) - lse * kLog2e);
-        }
-      }
-    }
-  }
-  const size_t at = (size_t(s) * p.n_kv_heads + hk) * w.stride + j;
-  w.out[at] = w.in[at] + sum;
-}
-
 size_t paged_workspace_bytes(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages) {
-  return kCounterBytes + align_up(std::max(paged_step_scratch_most(sh, batch, max_new, max_pages),
-                                           paged_chunk_scratch_most(sh, batch, n_rows, max_new, max_pages)), 256);
+  return kCounterBytes + align_up(std::max({paged_step_scratch_most(sh, batch, max_new, max_pages),
+                                            paged_chunk_scratch_most(sh, batch, n_rows, max_new, max_pages),
+                                            paged_votes_scratch_most(sh)}), 256);
 }
 
-template <typename T, int D, bool kCap, bool kBias>
-static void launch_both(const PagedAttn& p, const PagedWeights* w, bool attend, hipStream_t stream) {
-  if (attend) hipLaunchKernelGGL((paged_attention_kernel<T, D, kCap, kBias>), dim3(p.t.n_rows, p.n_q_heads), dim3(kPsThreads), 0, stream, p);
-  if (w != nullptr)
-    hipLaunchKernelGGL((paged_weights_kernel<T, D, kCap, kBias>), dim3(p.t.max_pages, p.n_kv_heads, p.t.batch),
-                       dim3(kPsThreads), 0, stream, p, *w);
-}
-template <typename T, int D>
-static void launch_form(const PagedAttn& p, const PagedWeights* w, bool attend, hipStream_t stream) {
+template <int D>
+static void launch_form(const PagedAttn& p, hipStream_t stream) {
   const bool cap = p.f.cap_in > 0.f, bias = p.f.slopes != nullptr;
-  if (cap && bias) launch_both<T, D, true, true>(p, w, attend, stream);
-  else if (cap) launch_both<T, D, true, false>(p, w, attend, stream);
-  else if (bias) launch_both<T, D, false, true>(p, w, attend, stream);
-  else launch_both<T, D, false, false>(p, w, attend, stream);
+  auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(p.t.n_rows, p.n_q_heads), dim3(kPsThreads), 0, stream, p);
+  };
+  if (cap && bias) launch(paged_attention_kernel<float, D, true, true>);
+  else if (cap) launch(paged_attention_kernel<float, D, true, false>);
+  else if (bias) launch(paged_attention_kernel<float, D, false, true>);
+  else launch(paged_attention_kernel<float, D, false, false>);
 }
 int launch_paged_attention(const actqkv_shape& sh, const PagedAttn& p, const PagedWeights* weights, const Workspace& ws,
                            hipStream_t stream) {
   if (paged_step_supported(sh, p.t.max_new)) return launch_paged_step(sh, p, weights, ws, stream);
-  const bool attend = !paged_chunk_supported(sh);
-  if (!attend)
-    if (int rc = launch_paged_chunk(sh, p, ws, stream)) return rc;
-  if (sh.dtype == ACTQKV_F32) {
-    if (sh.head_dim == 64) launch_form<float, 64>(p, weights, attend, stream);
-    else launch_form<float, 128>(p, weights, attend, stream);
+  int rc;
+  if (paged_chunk_supported(sh)) {
+    rc = launch_paged_chunk(sh, p, ws, stream);
   } else {
-    if (sh.head_dim == 64) launch_form<uint16_t, 64>(p, weights, attend, stream);
-    else launch_form<uint16_t, 128>(p, weights, attend, stream);
+    if (sh.head_dim == 64) launch_form<64>(p, stream);
+    else launch_form<128>(p, stream);
+    rc = hip_status("paged attention");
   }
-  return hip_status("paged attention");
+  if (rc != ACTQKV_OK || weights == nullptr) return rc;
+  return launch_paged_votes(sh, p, *weights, ws, stream);
 }
 
 }  // namespace actqkv

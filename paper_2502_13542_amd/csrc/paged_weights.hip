@@ -1,0 +1,315 @@
+// The account of the attention weight after a chunk or a prompt: for every cached token, the sum over rows of exp(score - lse).
+//
+// A workgroup of 8 wavefronts takes 128 keys (fp32) or 256 (bf16) of one (sequence, KV head) and walks the voting rows, the G heads of
+// a row side by side.  S = Q K^T with the rows as the first operand and the keys as the second leaves a lane with scores of ONE
+// key, 16 rows of it in its registers: the sum over rows needs no exchange.  A wavefront keeps its keys in registers for the whole
+// walk (straight from memory, each byte read once per 4 wavefronts that do not share it) and reads the rows from LDS, 64 at a
+// time, double buffered, filled without registers in between; four wavefronts take the even 32 rows of each 64, four the odd ones.
+// Beside its products a wavefront has a multiply-add, an exponential and an addition per score, which bound it with them.
+//
+// Where keys alone do not fill the chip, the rows are cut into pieces whose sums a second launch adds up, in order.  Sums of
+// 16 rows are added to the running sum, not single terms: its rounding would pass 1e-6 after some thousand.
+#include "mfma_util.h"
+#include "paged.h"
+
+namespace actqkv {
+
+constexpr int kPwThreads = 512, kPwWaves = kPwThreads / 64;
+constexpr int kPwRows = 64;                      // rows (with a head each) of a step
+constexpr int kPwWgs = 512;                      // workgroups that a call is cut into
+
+// Keys of a wavefront and of a workgroup; 16-byte operands of a row.
+template <typename T, int D> struct PwShape {
+  static constexpr int kGroups = sizeof(T) == 2 ? 2 : 1;          // of 32 keys, per wavefront
+  static constexpr int kKeys = 4 * 32 * kGroups;
+  static constexpr int kRowBytes = D * int(sizeof(T));
+  static constexpr int kSteps = kRowBytes / 32;
+  static __device__ __forceinline__ uint32_t swizzle(int r) { return kRowBytes == 128 ? (r >> 1) & 7 : r & 15; }
+  static __device__ __forceinline__ f32x16 product(const u32x4& a, const u32x4& b, f32x16 c) {
+    if constexpr (sizeof(T) == 2) {
+      return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c, 0, 0, 0);
+      return c;
+    }
+  }
+};
+
+struct PagedVotes {
+  PagedAttn a;
+  PagedWeights w;
+  int key_tiles, pieces;
+  float* part;               // [pair][piece][key_tiles * kKeys], or NULL: one piece
+};
+
+template <typename T, int D, bool kCap, bool kBias>
+__device__ __forceinline__ void votes_body(const PagedVotes& c) {
+  typedef PwShape<T, D> S;
+  constexpr int kG = S::kGroups, kBytes = kPwRows * S::kRowBytes, kPieces = kBytes / 1024 / kPwWaves;
+  constexpr int kRowsOf1k = 1024 / S::kRowBytes, kChunks = S::kRowBytes / 16;
+  constexpr bool kForm = kCap || kBias;
+  __shared__ __attribute__((aligned(16))) char rows_lds[2][kBytes];
+  __shared__ __attribute__((aligned(16))) float lse_lds[2][kPwRows], slope_lds[2][kPwRows];
+  __shared__ __attribute__((aligned(16))) int lo_lds[2][kPwRows], hi_lds[2][kPwRows], pos_lds[2][kPwRows];
+  __shared__ int any_lds[2][2][2], all_lds[2][2][2];               // [stage][32 rows][lo, hi]
+  __shared__ float sum_lds[S::kKeys];
+  const PagedAttn& p = c.a;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, half = lane >> 5, kg = wave & 3, rh = wave >> 2;
+  const int group = p.n_q_heads / p.n_kv_heads;
+  const int hk = blockIdx.x % p.n_kv_heads, rest = blockIdx.x / p.n_kv_heads;
+  const int piece = rest % c.pieces, tile = rest / c.pieces, s = blockIdx.y;
+  const PagedSeq seq = paged_seq(p.t, s);
+  const int key0 = tile * S::kKeys, wkey0 = key0 + kg * 32 * kG;  // the workgroup's first key, this wavefront's
+  const int w0 = seq.n - seq.m;
+
+  // ---- the rows that vote, of those the ones that can see a key of this tile at all
+  int i0 = max(seq.m - c.w.rows, 0), i1 = seq.m;
+  if (p.f.row_end == nullptr) i0 = max(i0, key0 - w0);             // row i sees positions up to w0 + i
+  if (p.f.window > 0) i1 = int(min(int64_t(i1), int64_t(key0) + S::kKeys - 1 + p.f.window - w0));
+  if (key0 >= seq.n) i1 = i0;
+  const int f0 = i0 * group, f1 = max(i1, i0) * group;
+  const int steps = (f1 - f0 + kPwRows - 1) / kPwRows, per = (steps + c.pieces - 1) / c.pieces;
+  const int st0 = piece * per, st1 = min(steps, st0 + per);
+
+  // ---- this wavefront's keys as second operands, and whether their page exists
+  const int page_index = wkey0 / kBlock;
+  const int page = wkey0 < seq.n ? __builtin_amdgcn_readfirstlane(paged_page(p.t, s, page_index)) : -1;
+  u32x4 kreg[kG][S::kSteps];
+  if (page >= 0) {
+    const char* at = static_cast<const char*>(p.k_pages) +
+                     ((size_t(page) * p.n_kv_heads + hk) * kBlock + (wkey0 % kBlock) + n) * S::kRowBytes + 16 * half;
+#pragma unroll
+    for (int gk = 0; gk < kG; ++gk)
+#pragma unroll
+      for (int j = 0; j < S::kSteps; ++j) kreg[gk][j] = *reinterpret_cast<const u32x4*>(at + gk * 32 * S::kRowBytes + j * 32);
+  } else {
+#pragma unroll
+    for (int gk = 0; gk < kG; ++gk)
+#pragma unroll
+      for (int j = 0; j < S::kSteps; ++j) kreg[gk][j] = u32x4{0, 0, 0, 0};
+  }
+
+  // ---- staging of 64 rows: their queries into LDS, and by the first wavefront what else a row has
+  auto fetch = [&](int st, int stage) {
+    const int f = f0 + st * kPwRows;
+    const int first = f / group;
+    const char* base = uniform_ptr(static_cast<const char*>(p.q) +
+                                   (size_t(seq.row0 + first) * p.n_q_heads + hk * group) * S::kRowBytes);
+    const uint32_t row_stride = uint32_t(p.n_q_heads) * S::kRowBytes;
+    const __amdgpu_buffer_rsrc_t src = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, 0x7fffffff, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int r = (kPieces * wave + i) * kRowsOf1k + lane / kChunks;
+      const int fr = min(f + r, f1 - 1), ir = fr / group;          // (rows behind the last repeat it and do not vote)
+      const uint32_t off = uint32_t(ir - first) * row_stride + uint32_t(fr - ir * group) * S::kRowBytes +
+                           ((uint32_t(lane % kChunks) ^ S::swizzle(r)) << 4);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (__attribute__((address_space(3))) void*)(rows_lds[stage] + (kPieces * wave + i) * 1024),
+                                               16, off, 0, 0, 0);
+    }
+  };
+  float my_lse = 0.f, my_slope = 0.f;
+  PagedSpan my_span{0x7fffffff, 0};
+  int my_pos = 0;
+  auto row_read = [&](int st) {
+    const int f = f0 + st * kPwRows + lane;
+    my_span = PagedSpan{0x7fffffff, 0};
+    my_lse = my_slope = 0.f;
+    my_pos = 0;
+    if (f < f1) {
+      const int i = f / group, head = hk * group + (f - i * group), row = seq.row0 + i;
+      my_pos = w0 + i;
+      my_lse = p.lse[size_t(row) * p.n_q_heads + head] * kLog2e;
+      if (kBias) my_slope = p.f.slopes[head] * kLog2e;
+      const PagedSpan v = paged_span(p.f, row, my_pos, seq.n);
+      if (v.hi > v.lo && my_lse > -INFINITY) my_span = v;
+    }
+  };
+  auto row_write = [&](int stage) {
+    lse_lds[stage][lane] = my_span.hi > 0 ? my_lse : 0.f;
+    lo_lds[stage][lane] = my_span.lo;
+    hi_lds[stage][lane] = my_span.hi;
+    if (kBias) {
+      slope_lds[stage][lane] = my_slope;
+      pos_lds[stage][lane] = my_pos;
+    }
+    int lo_any = my_span.lo, hi_any = my_span.hi, lo_all = my_span.lo, hi_all = my_span.hi;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      lo_any = min(lo_any, __shfl_xor(lo_any, d, 64));
+      hi_any = max(hi_any, __shfl_xor(hi_any, d, 64));
+      lo_all = max(lo_all, __shfl_xor(lo_all, d, 64));
+      hi_all = min(hi_all, __shfl_xor(hi_all, d, 64));
+    }
+    if (n == 0) {
+      any_lds[stage][half][0] = lo_any;
+      any_lds[stage][half][1] = hi_any;
+      all_lds[stage][half][0] = lo_all;
+      all_lds[stage][half][1] = hi_all;
+    }
+  };
+  float sum[kG];
+#pragma unroll
+  for (int gk = 0; gk < kG; ++gk) sum[gk] = 0.f;
+  if (st0 < st1) {
+    fetch(st0, 0);
+    if (wave == 0) {
+      row_read(st0);
+      row_write(0);
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  const uint32_t a_off0 = uint32_t(32 * rh + n) * S::kRowBytes + ((uint32_t(half) ^ S::swizzle(n)) << 4);
+  for (int st = st0; st < st1; ++st) {
+    const int stage = (st - st0) & 1;
+    const bool next = st + 1 < st1;
+    if (next && wave == 0) row_read(st + 1);
+    const int lo_any = __builtin_amdgcn_readfirstlane(any_lds[stage][rh][0]), hi_any = __builtin_amdgcn_readfirstlane(any_lds[stage][rh][1]);
+    const int lo_all = __builtin_amdgcn_readfirstlane(all_lds[stage][rh][0]), hi_all = __builtin_amdgcn_readfirstlane(all_lds[stage][rh][1]);
+    const bool visible = page >= 0 && wkey0 < hi_any && wkey0 + 32 * kG > lo_any;
+    const bool masked = wkey0 < lo_all || wkey0 + 32 * kG > hi_all;
+    f32x16 acc[kG];
+    if (visible) {
+#pragma unroll
+      for (int gk = 0; gk < kG; ++gk)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[gk][i] = 0.f;
+      const char* at = rows_lds[stage];
+      u32x4 ring[S::kSteps];
+#pragma unroll
+      for (int j = 0; j < S::kSteps; ++j) ring[j] = *reinterpret_cast<const u32x4*>(at + (a_off0 ^ (uint32_t(j) << 5)));
+#pragma unroll
+      for (int j = 0; j < S::kSteps; ++j)
+#pragma unroll
+        for (int gk = 0; gk < kG; ++gk) acc[gk] = S::product(ring[j], kreg[gk][j], acc[gk]);
+    }
+    if (next) fetch(st + 1, stage ^ 1);
+    if (visible) {
+      // register i is row 32 rh + 8 (i / 4) + 4 half + i % 4, the lane's key wkey0 + 32 gk + n
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const int r0 = 32 * rh + 8 * b + 4 * half;
+        const f32x4 lse = *reinterpret_cast<const f32x4*>(&lse_lds[stage][r0]);
+        f32x4 slope;
+        u32x4 pos;
+        if constexpr (kBias) {
+          slope = *reinterpret_cast<const f32x4*>(&slope_lds[stage][r0]);
+          pos = *reinterpret_cast<const u32x4*>(&pos_lds[stage][r0]);
+        }
+#pragma unroll
+        for (int gk = 0; gk < kG; ++gk)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float x = acc[gk][4 * b + e];
+            if constexpr (kForm) x = paged_score<kCap, kBias>(p.f, x, kBias ? slope[e] : 0.f, kBias ? abs(int(pos[e]) - (wkey0 + 32 * gk + n)) : 0);
+            acc[gk][4 * b + e] = __builtin_amdgcn_exp2f(kForm ? x - lse[e] : fmaf(x, p.f.scale_log2e, -lse[e]));
+          }
+      }
+      if (masked) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const int r0 = 32 * rh + 8 * b + 4 * half;
+          const u32x4 lo = *reinterpret_cast<const u32x4*>(&lo_lds[stage][r0]), hi = *reinterpret_cast<const u32x4*>(&hi_lds[stage][r0]);
+#pragma unroll
+          for (int gk = 0; gk < kG; ++gk) {
+            const int key = wkey0 + 32 * gk + n;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[gk][4 * b + e] = key >= int(lo[e]) && key < int(hi[e]) ? acc[gk][4 * b + e] : 0.f;
+          }
+        }
+      }
+#pragma unroll
+      for (int gk = 0; gk < kG; ++gk) {
+        float t[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) t[i & 3] += acc[gk][i];
+        sum[gk] += (t[0] + t[1]) + (t[2] + t[3]);
+      }
+    }
+    if (next && wave == 0) row_write(stage ^ 1);
+    __builtin_amdgcn_s_waitcnt(0);               // this wavefront's share of the next rows has landed in LDS
+    __syncthreads();
+  }
+  // ---- the two lanes of a key, then the two sets of rows
+#pragma unroll
+  for (int gk = 0; gk < kG; ++gk) sum[gk] = lane_pair<32>(sum[gk], [](float x, float y) { return x + y; });
+  const int mine = kg * 32 * kG + n;
+  if (rh == 1 && half == 0) {
+#pragma unroll
+    for (int gk = 0; gk < kG; ++gk) sum_lds[mine + 32 * gk] = sum[gk];
+  }
+  __syncthreads();
+  if (rh == 1 || half == 1) return;
+  const int pair = s * p.n_kv_heads + hk;
+#pragma unroll
+  for (int gk = 0; gk < kG; ++gk) {
+    const int at = mine + 32 * gk, key = key0 + at;
+    const float v = sum[gk] + sum_lds[at];
+    if (c.part != nullptr) {
+      c.part[(size_t(pair) * c.pieces + piece) * (size_t(c.key_tiles) * S::kKeys) + key] = v;
+    } else if (key < p.t.max_pages * kBlock) {
+      const size_t to = size_t(pair) * c.w.stride + key;
+      c.w.out[to] = c.w.in[to] + v;
+    }
+  }
+}
+template <typename T, int D, bool kCap, bool kBias>
+__global__ __launch_bounds__(kPwThreads) void paged_votes_kernel(PagedVotes c) {
+  votes_body<T, D, kCap, kBias>(c);
+}
+
+// weights_out = weights_in + the pieces, in order: a key a thread.
+constexpr int kVsThreads = 256;
+__global__ __launch_bounds__(kVsThreads) void paged_votes_sum_kernel(PagedVotes c, int keys) {
+  const int key = blockIdx.x * kVsThreads + threadIdx.x, pair = blockIdx.y;
+  if (key >= c.a.t.max_pages * kBlock) return;
+  float v = 0.f;
+  for (int i = 0; i < c.pieces; ++i) v += c.part[(size_t(pair) * c.pieces + i) * keys + key];
+  const size_t to = size_t(pair) * c.w.stride + key;
+  c.w.out[to] = c.w.in[to] + v;
+}
+
+// ---- host side
+static int votes_keys(const actqkv_shape& sh) { return sh.dtype == ACTQKV_F32 ? PwShape<float, 64>::kKeys : PwShape<uint16_t, 64>::kKeys; }
+
+// Pieces hold kPwWgs workgroups' sums and, rounded up, as many again.
+size_t paged_votes_scratch_most(const actqkv_shape& sh) { return size_t(2 * kPwWgs) * votes_keys(sh) * sizeof(float); }
+
+template <typename T, int D>
+static void launch_votes(const PagedVotes& c, hipStream_t stream) {
+  const bool cap = c.a.f.cap_in > 0.f, bias = c.a.f.slopes != nullptr;
+  const dim3 grid(unsigned(c.a.n_kv_heads) * c.key_tiles * c.pieces, c.a.t.batch);
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kPwThreads), 0, stream, c); };
+  if (cap && bias) launch(paged_votes_kernel<T, D, true, true>);
+  else if (cap) launch(paged_votes_kernel<T, D, true, false>);
+  else if (bias) launch(paged_votes_kernel<T, D, false, true>);
+  else launch(paged_votes_kernel<T, D, false, false>);
+}
+
+int launch_paged_votes(const actqkv_shape& sh, const PagedAttn& p, const PagedWeights& w, const Workspace& ws, hipStream_t stream) {
+  PagedVotes c;
+  c.a = p;
+  c.w = w;
+  const int keys = votes_keys(sh);
+  c.key_tiles = (p.t.max_pages * kBlock + keys - 1) / keys;
+  const int64_t items = int64_t(c.key_tiles) * p.n_kv_heads * p.t.batch;
+  const int64_t steps = (int64_t(std::min(w.rows, p.t.max_new)) * (sh.n_q_heads / sh.n_kv_heads) + kPwRows - 1) / kPwRows;
+  c.pieces = int(std::max<int64_t>(1, std::min((kPwWgs + items - 1) / items, steps)));
+  c.part = c.pieces > 1 ? ws.scratch_f32() : nullptr;
+  if (sh.dtype == ACTQKV_F32) {
+    if (sh.head_dim == 64) launch_votes<float, 64>(c, stream);
+    else launch_votes<float, 128>(c, stream);
+  } else {
+    if (sh.head_dim == 64) launch_votes<uint16_t, 64>(c, stream);
+    else launch_votes<uint16_t, 128>(c, stream);
+  }
+  if (c.pieces > 1) {
+    const dim3 grid((p.t.max_pages * kBlock + kVsThreads - 1) / kVsThreads, p.n_kv_heads * p.t.batch);
+    hipLaunchKernelGGL(paged_votes_sum_kernel, grid, dim3(kVsThreads), 0, stream, c, c.key_tiles * keys);
+  }
+  return hip_status("paged attention weights");
+}
+
+}  // namespace actqkv
