@@ -551,7 +551,9 @@ int actqkv_copy_bytes(void* dst, const void* src, size_t bytes, void* stream);
  *   n_rows   rows of the arrays (1 .. 2^22); max_new  the most rows a sequence brings (1 .. n_rows; of more, the first
  *            max_new are taken as all of them).
  * Of the shape, n_q_heads, n_kv_heads, head_dim, block_size, dtype and softmax_scale are used.  Slots behind a sequence's last
- * token may hold anything, NaN and infinities included; its own keys and values must be finite.  What lies on the device is
+ * token may hold anything, NaN and infinities included; its own keys and values must be finite,
+ * and so must, in fp32, 256 times the sum of the absolute values of a channel over the tokens that a row sees (it is taken before it is divided
+ * by that of the exponentials).  What lies on the device is
  * clamped, never trusted: a wrong value gives a wrong result but no out-of-bounds access. */
 
 /* Bytes of workspace of the paged calls that take one, for calls of at most batch sequences, n_rows rows, max_new rows of a

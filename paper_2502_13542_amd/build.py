@@ -14,8 +14,8 @@ NATIVE = os.path.join(HERE, "_native.so")
 
 SOURCES = ["api.hip", "probe.hip", "score.hip", "select.hip", "attn_prefill_f32.hip",
            "attn_prefill_mfma.hip", "attn_decode.hip", "append.hip", "cutoff.hip", "gather.hip",
-           "decode_retrieve.hip", "attn_static.hip", "paged_api.hip", "paged_append.hip", "paged_attn.hip",
-           "paged_chunk.hip", "paged_step.hip", "paged_weights.hip", "paged_evict.hip"]
+           "decode_retrieve.hip", "attn_static.hip", "paged_api.hip", "paged_append.hip", "paged_chunk.hip",
+           "paged_chunk_f32.hip", "paged_step.hip", "paged_weights.hip", "paged_evict.hip"]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
          # packed fp32 instructions are kept out of the generated code

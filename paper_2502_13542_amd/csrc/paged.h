@@ -44,6 +44,41 @@ __device__ __forceinline__ int paged_page(const PagedTable& t, int s, int i) {
   return page >= 0 && page < t.n_pages ? page : -1;
 }
 
+// Of 64 lanes' counts the inclusive sums.
+__device__ __forceinline__ int wave_scan(int v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int below = __shfl_up(v, d, 64);
+    if (lane >= d) v += below;
+  }
+  return v;
+}
+
+// The sequence that query tile `tile` of rows_per rows belongs to, and the tile's number in it (from its last rows on: they see
+// the most keys and start first); false behind the last one.
+__device__ __forceinline__ bool paged_find_tile(const PagedTable& t, int tile, int group, int rows_per, int& s, int& local) {
+  const int lane = threadIdx.x & 63;
+  for (int s0 = 0; s0 < t.batch; s0 += 64) {
+    int n = 0;
+    if (s0 + lane < t.batch) {
+      const PagedSeq q = paged_seq(t, s0 + lane);
+      n = (q.m * group + rows_per - 1) / rows_per;
+    }
+    const int sum = wave_scan(n);
+    const unsigned long long mine = __ballot(tile < sum);
+    if (mine != 0) {
+      const int at = __ffsll(mine) - 1;
+      const int end = __builtin_amdgcn_readlane(sum, at);
+      s = s0 + at;
+      local = end - 1 - tile;
+      return true;
+    }
+    tile -= __builtin_amdgcn_readlane(sum, 63);
+  }
+  return false;
+}
+
 // How scores are formed and which keys a row sees.
 struct PagedForm {
   const int32_t* row_first;  // [n_rows] or NULL
@@ -111,16 +146,14 @@ bool paged_step_supported(const actqkv_shape& sh, int max_new);
 size_t paged_step_scratch_most(const actqkv_shape& sh, int batch, int max_new, int max_pages);
 int launch_paged_step(const actqkv_shape& sh, const PagedAttn& p, const PagedWeights* weights, const Workspace& ws,
                       hipStream_t stream);
-bool paged_chunk_supported(const actqkv_shape& sh);
 size_t paged_chunk_scratch_most(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages);
 int launch_paged_chunk(const actqkv_shape& sh, const PagedAttn& p, const Workspace& ws, hipStream_t stream);
+size_t paged_chunk_f32_scratch_most(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages);
+int launch_paged_chunk_f32(const actqkv_shape& sh, const PagedAttn& p, const Workspace& ws, hipStream_t stream);
 size_t paged_votes_scratch_most(const actqkv_shape& sh);
 int launch_paged_votes(const actqkv_shape& sh, const PagedAttn& p, const PagedWeights& w, const Workspace& ws, hipStream_t stream);
-size_t paged_workspace_bytes(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages);
 int launch_paged_append(const actqkv_shape& sh, const PagedTable& t, const void* k_new, const void* v_new,
                         void* k_pages, void* v_pages, hipStream_t stream);
-int launch_paged_attention(const actqkv_shape& sh, const PagedAttn& p, const PagedWeights* weights, const Workspace& ws,
-                           hipStream_t stream);
 struct PagedEvict {
   PagedTable t;
   void* k_pages;

@@ -3,7 +3,7 @@
 // Work split.  The query rows of a (sequence, KV head) are numbered position by position, the G heads of the KV head side by
 // side; a workgroup of 8 wavefronts takes 256 / KS of them, 32 for KS wavefronts (KS = 1, 2 or 4), which share the keys of every
 // page and merge in LDS at the end.  A workgroup finds its sequence by a scan over row_start.  Where that leaves compute units
-// idle the pages are cut into pieces, a workgroup each, merged by the one that finishes last (chunk_cut).  Workgroups of one KV head
+// idle the pages are cut into pieces, a workgroup each, merged by a second launch (chunk_cut).  Workgroups of one KV head
 // sit on few XCDs (blockIdx % Hk), so that the pages they share stay in those L2s.
 //
 // Data flow per page.  Keys [128][D] and values [D][128] go from HBM straight into LDS (double buffered, 16-byte chunks
@@ -18,6 +18,7 @@
 // none sees is skipped, and the walk is over the union of the spans: a window or documents cost what they cover.
 #include "mfma_util.h"
 #include "paged.h"
+#include "paged_merge.h"
 
 namespace actqkv {
 
@@ -32,44 +33,10 @@ struct PagedChunk {
   PagedAttn a;
   int tiles;                 // query tiles that the launch has workgroups for (a bound)
   int splits;                // pieces of a query tile's pages
-  uint32_t* part;            // [tile][Hk][split][wave][16 * groups + 2][64]
-  unsigned int* counters;    // [tile][Hk]
+  void* part;                // pieces [tile][Hk][split]
 };
-
-// Of 64 lanes' counts the inclusive sums.
-__device__ __forceinline__ int wave_scan(int v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int below = __shfl_up(v, d, 64);
-    if (lane >= d) v += below;
-  }
-  return v;
-}
-
-// The sequence that query tile `tile` of rows_per rows belongs to, and the tile's number in it (from its last rows on: they see
-// the most keys and start first); false behind the last one.
-__device__ __forceinline__ bool paged_find_tile(const PagedTable& t, int tile, int group, int rows_per, int& s, int& local) {
-  const int lane = threadIdx.x & 63;
-  for (int s0 = 0; s0 < t.batch; s0 += 64) {
-    int n = 0;
-    if (s0 + lane < t.batch) {
-      const PagedSeq q = paged_seq(t, s0 + lane);
-      n = (q.m * group + rows_per - 1) / rows_per;
-    }
-    const int sum = wave_scan(n);
-    const unsigned long long mine = __ballot(tile < sum);
-    if (mine != 0) {
-      const int at = __ffsll(mine) - 1;
-      const int end = __builtin_amdgcn_readlane(sum, at);
-      s = s0 + at;
-      local = end - 1 - tile;
-      return true;
-    }
-    tile -= __builtin_amdgcn_readlane(sum, 63);
-  }
-  return false;
-}
+template <int D, int KS>
+using ChunkPiece = PagedPiece<kPcWaves / KS, (D / 32 > KS ? D / 32 / KS : 1), (D / 32 < KS ? D / 32 : KS)>;
 
 // out (and lse) of a lane's share of a row: o[j][4 i + r] is channel (db0 + j) 32 + 8 i + 4 half + r.
 template <int D, int N>
@@ -96,6 +63,7 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
   constexpr int kRows = kPcRows<KS>, kRowGroups = kPcWaves / KS;
   constexpr int kNg = 4 / KS;                    // 32-key groups of a page that are this wavefront's
   constexpr bool kForm = kCap || kBias;
+  typedef ChunkPiece<D, KS> Piece;
   constexpr uint32_t kTileBytes = kPcTileBytes<D>;
   __shared__ __attribute__((aligned(16))) char lds_b[kPcLdsBytes<D>];
   __shared__ int span_lds[2][kPcWaves];
@@ -159,7 +127,11 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
   const int t_first = hi > 0 ? lo / kBlock : 0, n_tiles = hi > 0 ? (hi + kBlock - 1) / kBlock - t_first : 0;
   const int per = max((n_tiles + c.splits - 1) / c.splits, 1);
   const int splits = max((n_tiles + per - 1) / per, 1);
-  if (split >= splits) return;
+  if (split >= splits) {                         // (its place among the pieces says that there is nothing)
+    if (wave < Piece::kWaves)
+      Piece::store_none(Piece::at(c.part, tile * p.n_kv_heads + hk, c.splits, split, wave), -INFINITY, 0.f, lane);
+    return;
+  }
   const int t_begin = t_first + split * per, t_end = min(t_first + n_tiles, t_begin + per);
 
   // ---- fetching a page: each wavefront an eighth of its keys and of its values, 1 KB an instruction
@@ -413,50 +385,19 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
     }
     m_run = m_all;
   }
-  if (splits == 1) {
+  if (c.splits == 1) {
     if (row_ok && has_mine) chunk_store<D, kMine>(p, acc_f, db0, m_run, l_tot, row, head, half);
     return;
   }
-  // ---- the pieces merge through the workspace, in the workgroup that finishes last, in their order
-  constexpr int kWords = 16 * kMine + 2;
-  __shared__ int last_flag;
-  uint32_t* pieces = c.part + (size_t(tile) * p.n_kv_heads + hk) * c.splits * (kPcWaves * kWords * 64) + wave * (kWords * 64) + lane;
-  constexpr size_t kPiece = size_t(kPcWaves) * kWords * 64;
-  if (has_mine) {
-    uint32_t* mine = pieces + split * kPiece;
-#pragma unroll
-    for (int k = 0; k < 16 * kMine; ++k) st_agent(mine + k * 64, __float_as_uint(acc_f[k / 16][k % 16]));
-    st_agent(mine + 16 * kMine * 64, __float_as_uint(m_run));
-    st_agent(mine + (16 * kMine + 1) * 64, __float_as_uint(l_tot));
-  }
-  if (!last_of_group(c.counters + size_t(tile) * p.n_kv_heads + hk, unsigned(splits), &last_flag) || !has_mine) return;
-  float m_all = -INFINITY, l_all = 0.f;
-#pragma unroll
-  for (int k = 0; k < 16 * kMine; ++k) acc_f[k / 16][k % 16] = 0.f;
-  for (int i = 0; i < splits; ++i) {
-    const uint32_t* from = pieces + i * kPiece;
-    uint32_t x[16 * kMine];
-    const uint32_t xm = ld_agent(from + 16 * kMine * 64), xl = ld_agent(from + (16 * kMine + 1) * 64);
-#pragma unroll
-    for (int k = 0; k < 16 * kMine; ++k) x[k] = ld_agent(from + k * 64);
-    const float m_of = __uint_as_float(xm), m_new = fmaxf(m_all, m_of), m_safe = m_new == -INFINITY ? 0.f : m_new;
-    const float a = __builtin_amdgcn_exp2f(m_all - m_safe), b = __builtin_amdgcn_exp2f(m_of - m_safe);
-    l_all = l_all * a + __uint_as_float(xl) * b;
-#pragma unroll
-    for (int k = 0; k < 16 * kMine; ++k) acc_f[k / 16][k % 16] = acc_f[k / 16][k % 16] * a + __uint_as_float(x[k]) * b;
-    m_all = m_new;
-  }
-  if (row_ok) chunk_store<D, kMine>(p, acc_f, db0, m_all, l_all, row, head, half);
+  if (has_mine)
+    Piece::store(Piece::at(c.part, tile * p.n_kv_heads + hk, c.splits, split, wave), acc_f, m_run, l_tot, lane);
 }
-
 template <int D, int KS, bool kCap, bool kBias>
 __global__ __launch_bounds__(kPcThreads) void paged_chunk_kernel(PagedChunk c) {
   chunk_body<D, KS, kCap, kBias>(c);
 }
 
 // ---- host side
-bool paged_chunk_supported(const actqkv_shape& sh) { return sh.dtype == ACTQKV_BF16; }
-
 // The cut of a call: KS, and the pieces of a query tile's pages, by the least time of the busiest compute unit with these
 // figures (us per page and 256, 128, 64 rows; an item's start and end; merging).
 struct ChunkCut {
@@ -469,7 +410,7 @@ static int chunk_tiles(const actqkv_shape& sh, int batch, int n_rows, int max_ne
   return int(std::min(most, int64_t(n_rows) * group / rows + seqs));
 }
 static ChunkCut chunk_cut(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages) {
-  constexpr double kTileUs[] = {3.7, 2.1, 1.5}, kMergeUs[] = {6., 3.5, 2.}, kMergePieceUs[] = {1.1, 0.7, 0.5}, kItemUs = 5.;
+  constexpr double kTileUs[] = {3.7, 2.1, 1.5}, kMergeUs = 4., kMergePieceUs[] = {0.6, 0.3, 0.15}, kItemUs = 5.;
   const double scale = sh.head_dim == 64 ? 0.6 : 1.;
   ChunkCut best{1, 1, 1};
   double least = 0.;
@@ -477,10 +418,10 @@ static ChunkCut chunk_cut(const actqkv_shape& sh, int batch, int n_rows, int max
     const int ks = 1 << i, tiles = chunk_tiles(sh, batch, n_rows, max_new, ks);
     const int64_t items = int64_t(tiles) * sh.n_kv_heads;
     for (int splits = 1; splits <= std::min(kPcMaxSplits, max_pages); ++splits) {
-      if (splits > 1 && (items * splits > kChipCus || items > int64_t(kTicketCounters))) break;
+      if (splits > 1 && items * splits > kChipCus) break;
       const double rounds = std::ceil(double(items) * splits / kChipCus);
       double us = rounds * (std::ceil(double(max_pages) / splits) * kTileUs[i] * scale + kItemUs);
-      if (splits > 1) us += kMergeUs[i] + kMergePieceUs[i] * splits;
+      if (splits > 1) us += kMergeUs + kMergePieceUs[i] * splits;
       if ((i == 0 && splits == 1) || us < least) {
         least = us;
         best = ChunkCut{ks, splits, tiles};
@@ -491,9 +432,9 @@ static ChunkCut chunk_cut(const actqkv_shape& sh, int batch, int n_rows, int max
 }
 // Partial results exist only where all pieces run at once: of at most kChipCus workgroups.
 size_t paged_chunk_scratch_most(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages) {
-  if (!paged_chunk_supported(sh)) return 0;
+  if (sh.dtype != ACTQKV_BF16) return 0;
   const int64_t pieces = std::min<int64_t>(kPcMaxSplits, max_pages) * sh.n_kv_heads * chunk_tiles(sh, batch, n_rows, max_new, 4);
-  return size_t(std::min<int64_t>(kChipCus, pieces)) * kPcWaves * (16 * (sh.head_dim / 32) + 2) * 64 * sizeof(float);
+  return size_t(std::min<int64_t>(kChipCus, pieces)) * (sh.head_dim == 64 ? ChunkPiece<64, 1>::bytes() : ChunkPiece<128, 1>::bytes());
 }
 
 template <int D, int KS>
@@ -506,6 +447,11 @@ static void launch_chunk(const PagedChunk& c, hipStream_t stream) {
   else if (cap) launch(paged_chunk_kernel<D, KS, true, false>);
   else if (bias) launch(paged_chunk_kernel<D, KS, false, true>);
   else launch(paged_chunk_kernel<D, KS, false, false>);
+  if (c.splits > 1) {
+    constexpr int kDb = D / 32;
+    launch_paged_merge<uint16_t, D, kPcWaves / KS, (kDb > KS ? kDb / KS : 1), (kDb < KS ? kDb : KS)>(
+        PagedMerge{c.a, c.tiles, c.splits, c.part}, stream);
+  }
 }
 template <int D>
 static void launch_chunk_ks(int ks, const PagedChunk& c, hipStream_t stream) {
@@ -519,8 +465,7 @@ int launch_paged_chunk(const actqkv_shape& sh, const PagedAttn& p, const Workspa
   c.a = p;
   c.tiles = cut.tiles;
   c.splits = cut.splits;
-  c.part = reinterpret_cast<uint32_t*>(ws.scratch_f32());
-  c.counters = ws.counters();
+  c.part = ws.scratch_f32();
   if (sh.head_dim == 64) launch_chunk_ks<64>(cut.ks, c, stream);
   else launch_chunk_ks<128>(cut.ks, c, stream);
   return hip_status("paged attention (chunks)");

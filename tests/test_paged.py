@@ -396,3 +396,24 @@ def test_one_workspace_for_smaller_calls_and_a_side_stream():
     r.attend(q, t["row_start"], t["n_ctx"], t["pages"], t["k_pages"], t["v_pages"], out, stream=side)
     side.synchronize()
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("shape", ["fp32_64", "fp32_g3"])
+@pytest.mark.parametrize("batch", ["chunks", "steps"])
+def test_fp32_values_near_the_largest(shape, batch):
+    """Values above the largest bf16 in fp32 storage, and keys and queries whose product alone is ordinary."""
+    b = Batch(shape_of(*SHAPES[shape]), BATCHES[batch], 61, garbage=float("nan"))
+    big = 3.4e38
+    g = torch.Generator().manual_seed(9)
+    hk, d = b.shape.n_kv_heads, b.shape.head_dim
+    for s, (_, n) in enumerate(b.seqs):
+        # one per sequence and channel: output sums are taken before they are divided by that of the probabilities, so two of
+        # them, each with a probability above a half of the largest, would not be representable
+        if n:
+            slot = torch.randint(0, min(n, BS), (hk, d, 1), generator=g)
+            b.v_pages[b.pages[s, 0]].scatter_(2, slot, big)
+    b.k_pages *= 2.0 ** -3
+    b.q[::7] = 0
+    b.q[::7, :, 5] = big                                            # one huge channel, against keys that are tiny there
+    b.k_pages[:, :, :, 5] *= 1e-38
+    run_attention(b, "cap" if batch == "chunks" else "plain")
