@@ -22,6 +22,7 @@ struct PagedTable {
   const int32_t* n_ctx;      // [batch]
   const int32_t* pages;      // [batch][max_pages]
   int batch, n_rows, max_new, max_pages, n_pages;
+  int few;                   // (row, query head) pairs of a KV head up to which a sequence is a step kernel's and no other's; 0: none is
 };
 
 // Rows and tokens of a sequence, clamped so that no value on the device leads out of an array.
@@ -55,16 +56,16 @@ __device__ __forceinline__ int wave_scan(int v) {
   return v;
 }
 
-// The sequence that query tile `tile` of rows_per rows belongs to, and the tile's number in it (from its last rows on: they see
-// the most keys and start first); false behind the last one.
+// Query tiles of a sequence.
+__device__ __forceinline__ int paged_tiles(const PagedTable& t, const PagedSeq& q, int group, int rows_per) {
+  return q.m * group > t.few ? (q.m * group + rows_per - 1) / rows_per : 0;
+}
+// The sequence that query tile `tile` belongs to, and the tile's number in it (from its last rows on: they see the most keys
+// and start first); false behind the last one.
 __device__ __forceinline__ bool paged_find_tile(const PagedTable& t, int tile, int group, int rows_per, int& s, int& local) {
   const int lane = threadIdx.x & 63;
   for (int s0 = 0; s0 < t.batch; s0 += 64) {
-    int n = 0;
-    if (s0 + lane < t.batch) {
-      const PagedSeq q = paged_seq(t, s0 + lane);
-      n = (q.m * group + rows_per - 1) / rows_per;
-    }
+    const int n = s0 + lane < t.batch ? paged_tiles(t, paged_seq(t, s0 + lane), group, rows_per) : 0;
     const int sum = wave_scan(n);
     const unsigned long long mine = __ballot(tile < sum);
     if (mine != 0) {
@@ -91,7 +92,10 @@ struct PagedForm {
 // Positions [lo, hi) that a row at position pos of a sequence of n tokens sees (hi <= lo: none).
 struct PagedSpan {
   int lo, hi;
+  // one comparison a key, unsigned: a second one costs scalar registers for its mask, which 32 of them do not have
+  __device__ __forceinline__ uint32_t length() const { return uint32_t(max(hi - lo, 0)); }
 };
+__device__ __forceinline__ bool span_holds(int key_less_lo, uint32_t length) { return uint32_t(key_less_lo) < length; }
 __device__ __forceinline__ PagedSpan paged_span(const PagedForm& f, int row, int pos, int n) {
   PagedSpan v{0, 0};
   if (pos < 0) return v;                         // more rows than tokens: the row is not in the cache
@@ -101,27 +105,75 @@ __device__ __forceinline__ PagedSpan paged_span(const PagedForm& f, int row, int
   return v;
 }
 
-// tanh to 2 units of the last place: below 0.625 x + x^3 times a polynomial in x^2 (least squares, 4e-9 of it), above
+// tanh to 2 units of the last place: up to 0.3 x + x^3 times a polynomial in x^2 (least squares, 1.3e-8 of it), above it
 // 1 - 2 / (e^2x + 1).  (That alone loses, by 1 - 1, as many bits as x is small, and a cap multiplies what is lost: scores of
 // 3 under a cap of 50 would be off by 6e-6.)
-__device__ __forceinline__ float paged_tanh(float x) {
-  const float u = x * x;
-  float g = fmaf(u, -0.00570404f, 0.02063786f);
-  g = fmaf(u, g, -0.05373916f);
-  g = fmaf(u, g, 0.13331432f);
-  g = fmaf(u, g, -0.33333281f);
-  const float small = fmaf(x, u * g, x);
+constexpr float kTanhSmall = 0.3f;
+// A capped score, out * tanh(in * x), as x (b0 + u (b1 + u (b2 + u b3))), u = x x, of a product x in the polynomial's range;
+// or x itself, of a score that was capped already.
+struct CapForm {
+  float b0, b1, b2, b3;
+  __device__ __forceinline__ float factor(float x) const {
+    const float u = x * x;
+    return fmaf(u, fmaf(u, fmaf(u, b3, b2), b1), b0);
+  }
+};
+__device__ __forceinline__ CapForm cap_form(float in, float out) {
+  const float b = in * out, k = in * in;
+  return CapForm{b, -0.333330558f * b * k, 0.133146743f * b * k * k, -0.0503546844f * b * k * k * k};
+}
+__device__ __forceinline__ float paged_tanh(float x, float scale) {
   const float e = __builtin_amdgcn_exp2f(fabsf(x) * (2.f * kLog2e));
-  const float large = copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f), x);
-  return fabsf(x) < 0.625f ? small : large;
+  const float large = copysignf(fmaf(-2.f, __builtin_amdgcn_rcpf(e + 1.f), 1.f), x) * scale;
+  return fabsf(x) <= kTanhSmall ? x * cap_form(1.f, scale).factor(x) : large;
 }
 // The score, in units of log2, from a product of query and key: far = |position of the query - position of the key|, slope in
 // units of log2.
 template <bool kCap, bool kBias>
 __device__ __forceinline__ float paged_score(const PagedForm& f, float product, float slope, int far) {
-  float v = kCap ? f.cap_log2e * paged_tanh(product * f.cap_in) : product * f.scale_log2e;
+  float v = kCap ? paged_tanh(product * f.cap_in, f.cap_log2e) : product * f.scale_log2e;
   if (kBias) v = fmaf(-slope, float(far), v);
   return v;
+}
+// Whether the arguments in * x of a lane's registers, of all lanes, are in the polynomial's range: most of the time, and then a
+// cap is 5 instructions a score, otherwise 17.  (in^6 has to be a number, too: of a cap of thousands none is small.)
+template <int N>
+__device__ __forceinline__ bool cap_is_small(const f32x16 (&x)[N], float in) {
+  float mx = 0.f;
+#pragma unroll
+  for (int g = 0; g < N; ++g)
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(fabsf(x[g][i]), fabsf(x[g][i + 1])), mx);
+  return in >= 1e-5f && __all(mx * in <= kTanhSmall);
+}
+// Their scores.  `ahead`: the query's position less that of the key that off(g, i) = 0 would be of.
+template <bool kCap, bool kBias, int N, typename Off>
+__device__ __forceinline__ void paged_scores(const PagedForm& f, f32x16 (&x)[N], float in, float slope, float ahead, Off off) {
+  if constexpr (kCap) {
+    if (cap_is_small(x, in)) {
+      const CapForm c = cap_form(in, f.cap_log2e);
+#pragma unroll
+      for (int g = 0; g < N; ++g)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[g][i] *= c.factor(x[g][i]);
+    } else {
+#pragma unroll
+      for (int g = 0; g < N; ++g)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[g][i] = paged_tanh(x[g][i] * in, f.cap_log2e);
+    }
+  } else {
+#pragma unroll
+    for (int g = 0; g < N; ++g)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[g][i] *= in;
+  }
+  if constexpr (kBias) {
+#pragma unroll
+    for (int g = 0; g < N; ++g)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[g][i] = fmaf(-slope, fabsf(ahead - float(off(g, i))), x[g][i]);
+  }
 }
 
 struct PagedAttn {

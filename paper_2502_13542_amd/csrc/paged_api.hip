@@ -7,9 +7,18 @@
 namespace actqkv {
 
 // Which kernels a call takes: few rows per sequence or chunks, by the storage type; the votes behind them.
-static int launch_paged_attention(const actqkv_shape& sh, const PagedAttn& p, const PagedWeights* weights, const Workspace& ws,
+static int launch_paged_attention(const actqkv_shape& sh, PagedAttn p, const PagedWeights* weights, const Workspace& ws,
                                   hipStream_t stream) {
   if (paged_step_supported(sh, p.t.max_new)) return launch_paged_step(sh, p, weights, ws, stream);
+  // Sequences of a batch that bring few rows go through the step kernel, in a launch of their own of about 15 us, if they may
+  // be so many that their pages, read for a query tile each, would take longer (2 us a page and workgroup).
+  const int group = sh.n_q_heads / sh.n_kv_heads, few_rows = 16 / group;
+  const int64_t more = std::max<int64_t>(0, int64_t(p.t.n_rows) - int64_t(p.t.batch) * few_rows);
+  const int64_t few_most = p.t.batch - (more + p.t.max_new - 1) / p.t.max_new;
+  if (few_most * p.t.max_pages * sh.n_kv_heads * 2 > int64_t(20) * kChipCus) {
+    ACTQKV_TRY(launch_paged_step(sh, p, nullptr, ws, stream));
+    p.t.few = 16;
+  }
   ACTQKV_TRY(sh.dtype == ACTQKV_F32 ? launch_paged_chunk_f32(sh, p, ws, stream) : launch_paged_chunk(sh, p, ws, stream));
   return weights != nullptr ? launch_paged_votes(sh, p, *weights, ws, stream) : ACTQKV_OK;
 }
@@ -79,7 +88,7 @@ static int attention_call(const char* name, const actqkv_shape* shape, int batch
     return set_error(ACTQKV_EWORKSPACE, "workspace has %zu bytes, %s needs %zu", ws_bytes, name, need);
   const float scale = shape->softmax_scale > 0.f ? shape->softmax_scale : 1.f / std::sqrt(float(shape->head_dim));
   PagedAttn p;
-  p.t = PagedTable{row_start, n_ctx, pages, batch, n_rows, max_new, max_pages, n_pages};
+  p.t = PagedTable{row_start, n_ctx, pages, batch, n_rows, max_new, max_pages, n_pages, 0};
   p.f = PagedForm{row_first, row_end, slopes, window, scale * kLog2e, softcap > 0.f ? scale / softcap : 0.f, softcap * kLog2e};
   p.n_q_heads = shape->n_q_heads;
   p.n_kv_heads = shape->n_kv_heads;
@@ -115,7 +124,7 @@ int actqkv_paged_append(const actqkv_shape* shape, int batch, int n_rows, int ma
   ACTQKV_REQUIRE_PTR(k_new);
   ACTQKV_REQUIRE_PTR(v_new);
   ACTQKV_REQUIRE_SMALL(row_start, 4);
-  const PagedTable t{row_start, n_ctx, pages, batch, n_rows, max_new, max_pages, n_pages};
+  const PagedTable t{row_start, n_ctx, pages, batch, n_rows, max_new, max_pages, n_pages, 0};
   return launch_paged_append(*shape, t, k_new, v_new, k_pages, v_pages, static_cast<hipStream_t>(stream));
 }
 
@@ -174,7 +183,7 @@ int actqkv_paged_evict(const actqkv_shape* shape, int batch, const int32_t* n_ct
   ACTQKV_REQUIRE_SMALL(n_kept, 4);
   if (n_kept == n_ctx) return set_error(ACTQKV_EINVAL, "n_kept must not be n_ctx");
   PagedEvict e;
-  e.t = PagedTable{nullptr, n_ctx, pages, batch, 0, 0, max_pages, n_pages};
+  e.t = PagedTable{nullptr, n_ctx, pages, batch, 0, 0, max_pages, n_pages, 0};
   e.k_pages = k_pages;
   e.v_pages = v_pages;
   e.weights = weights;

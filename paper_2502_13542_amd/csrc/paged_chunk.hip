@@ -62,7 +62,8 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
   constexpr int kDb = D / 32, kKs = D / 16;      // 32-channel groups of the output, 16-channel steps of a score
   constexpr int kRows = kPcRows<KS>, kRowGroups = kPcWaves / KS;
   constexpr int kNg = 4 / KS;                    // 32-key groups of a page that are this wavefront's
-  constexpr bool kForm = kCap || kBias;
+  // a hidden score: finite where it is multiplied by a factor of itself (0 times infinity is no number)
+  constexpr float kHidden = kCap && !kBias ? -1e18f : -INFINITY;
   typedef ChunkPiece<D, KS> Piece;
   constexpr uint32_t kTileBytes = kPcTileBytes<D>;
   __shared__ __attribute__((aligned(16))) char lds_b[kPcLdsBytes<D>];
@@ -80,59 +81,6 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
   s = __builtin_amdgcn_readfirstlane(s);
   qtile = __builtin_amdgcn_readfirstlane(qtile);
   const PagedSeq seq = paged_seq(p.t, s);
-
-  // ---- this lane's row
-  const int row_end = seq.m * group;
-  const int frow0 = qtile * kRows + rg * 32;
-  const bool wave_ok = frow0 < row_end, row_ok = frow0 + n < row_end;
-  const int frow = min(frow0 + n, row_end - 1);
-  const int i_row = frow / group, head = hk * group + (frow - i_row * group);
-  const int row = seq.row0 + i_row, pos = seq.n - seq.m + i_row;
-  PagedSpan v = paged_span(p.f, row, pos, seq.n);
-  if (v.hi <= v.lo) v = PagedSpan{0x7fffffff, 0};
-  const float slope = kBias ? p.f.slopes[head] * kLog2e : 0.f;
-  bf16x8 qreg[kKs];                              // Q^T as B operand: channels 16 ks + 8 half .. + 7
-  {
-    const uint16_t* qp = static_cast<const uint16_t*>(p.q) + (size_t(row) * p.n_q_heads + head) * D + 8 * half;
-#pragma unroll
-    for (int ks = 0; ks < kKs; ++ks) qreg[ks] = as_bf16x8(*reinterpret_cast<const u32x4*>(qp + ks * 16));
-  }
-  // ---- what the wavefront's rows see: any of them [lo_any, hi_any), all of them [lo_all, hi_all); the workgroup's [lo, hi)
-  int lo_any = v.lo, hi_any = v.hi, lo_all = v.lo, hi_all = v.hi;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    lo_any = min(lo_any, __shfl_xor(lo_any, d, 64));
-    hi_any = max(hi_any, __shfl_xor(hi_any, d, 64));
-    lo_all = max(lo_all, __shfl_xor(lo_all, d, 64));
-    hi_all = min(hi_all, __shfl_xor(hi_all, d, 64));
-  }
-  lo_any = __builtin_amdgcn_readfirstlane(lo_any);
-  hi_any = __builtin_amdgcn_readfirstlane(wave_ok ? hi_any : 0);
-  lo_all = __builtin_amdgcn_readfirstlane(lo_all);
-  hi_all = __builtin_amdgcn_readfirstlane(hi_all);
-  if (lane == 0) {
-    span_lds[0][wave] = wave_ok ? lo_any : 0x7fffffff;
-    span_lds[1][wave] = hi_any;
-  }
-  __syncthreads();
-  int lo = 0x7fffffff, hi = 0;
-#pragma unroll
-  for (int w = 0; w < kRowGroups; ++w) {
-    lo = min(lo, span_lds[0][w]);
-    hi = max(hi, span_lds[1][w]);
-  }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  hi = __builtin_amdgcn_readfirstlane(hi);
-  // pages [t_first, t_first + n_tiles), this piece's [t_begin, t_end); pieces that would be empty are none
-  const int t_first = hi > 0 ? lo / kBlock : 0, n_tiles = hi > 0 ? (hi + kBlock - 1) / kBlock - t_first : 0;
-  const int per = max((n_tiles + c.splits - 1) / c.splits, 1);
-  const int splits = max((n_tiles + per - 1) / per, 1);
-  if (split >= splits) {                         // (its place among the pieces says that there is nothing)
-    if (wave < Piece::kWaves)
-      Piece::store_none(Piece::at(c.part, tile * p.n_kv_heads + hk, c.splits, split, wave), -INFINITY, 0.f, lane);
-    return;
-  }
-  const int t_begin = t_first + split * per, t_end = min(t_first + n_tiles, t_begin + per);
 
   // ---- fetching a page: each wavefront an eighth of its keys and of its values, 1 KB an instruction
   constexpr int kLoads = D / 32;
@@ -162,6 +110,9 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (__attribute__((address_space(3))) void*)(dst + kTileBytes + i * 1024), 16, gv[i], 0, 0, 0);
     }
   };
+  // ---- where rows bring no spans of their own the tile's is known from its numbers, and its first page is asked for before
+  // anything of the rows
+  int page = -1, t_begin = 0, t_end = 0;
   // the pages of 64 tiles at a time, one per lane
   int my_page = -1;
   auto page_of = [&](int t) {
@@ -169,6 +120,73 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
     if ((k & 63) == 0) my_page = t + lane < t_end ? paged_page(p.t, s, t + lane) : -1;
     return __builtin_amdgcn_readlane(my_page, k & 63);
   };
+  bool none = false;                             // a piece without pages
+  auto piece_of = [&](int lo, int hi) {          // pages of [lo, hi), this piece's [t_begin, t_end)
+    const int t_first = hi > 0 ? lo / kBlock : 0, n_tiles = hi > 0 ? (hi + kBlock - 1) / kBlock - t_first : 0;
+    const int per = max((n_tiles + c.splits - 1) / c.splits, 1);
+    none = split > 0 && split * per >= n_tiles;
+    t_begin = t_first + split * per;
+    t_end = min(t_first + n_tiles, t_begin + per);
+    if (t_begin < t_end) {
+      page = page_of(t_begin);
+      if (page >= 0) fetch(page, 0);
+    }
+  };
+  const bool arrays = p.f.row_first != nullptr || p.f.row_end != nullptr;
+  if (!arrays) {
+    const int first = qtile * kRows / group, last = (min((qtile + 1) * kRows, seq.m * group) - 1) / group, w0 = seq.n - seq.m;
+    piece_of(p.f.window > 0 ? max(max(w0 + first, 0) - p.f.window + 1, 0) : 0, max(w0 + last + 1, 0));
+  }
+
+  // ---- this lane's row
+  const int row_end = seq.m * group;
+  const int frow0 = qtile * kRows + rg * 32;
+  const bool wave_ok = frow0 < row_end, row_ok = frow0 + n < row_end;
+  const int frow = min(frow0 + n, row_end - 1);
+  const int i_row = frow / group, head = hk * group + (frow - i_row * group);
+  const int row = seq.row0 + i_row, pos = seq.n - seq.m + i_row;
+  PagedSpan v = paged_span(p.f, row, pos, seq.n);
+  const uint32_t v_len = v.length();
+  if (v_len == 0) v = PagedSpan{0x7fffffff, 0};
+  const float slope = kBias ? p.f.slopes[head] * kLog2e : 0.f;
+  bf16x8 qreg[kKs];                              // Q^T as B operand: channels 16 ks + 8 half .. + 7
+  {
+    const uint16_t* qp = static_cast<const uint16_t*>(p.q) + (size_t(row) * p.n_q_heads + head) * D + 8 * half;
+#pragma unroll
+    for (int ks = 0; ks < kKs; ++ks) qreg[ks] = as_bf16x8(*reinterpret_cast<const u32x4*>(qp + ks * 16));
+  }
+  // ---- what the wavefront's rows see: any of them [lo_any, hi_any), all of them [lo_all, hi_all)
+  int lo_any = v.lo, hi_any = v.hi, lo_all = v.lo, hi_all = v.hi;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    lo_any = min(lo_any, __shfl_xor(lo_any, d, 64));
+    hi_any = max(hi_any, __shfl_xor(hi_any, d, 64));
+    lo_all = max(lo_all, __shfl_xor(lo_all, d, 64));
+    hi_all = min(hi_all, __shfl_xor(hi_all, d, 64));
+  }
+  lo_any = __builtin_amdgcn_readfirstlane(lo_any);
+  hi_any = __builtin_amdgcn_readfirstlane(wave_ok ? hi_any : 0);
+  lo_all = __builtin_amdgcn_readfirstlane(lo_all);
+  hi_all = __builtin_amdgcn_readfirstlane(hi_all);
+  if (arrays) {
+    if (lane == 0) {
+      span_lds[0][wave] = wave_ok ? lo_any : 0x7fffffff;
+      span_lds[1][wave] = hi_any;
+    }
+    __syncthreads();
+    int lo = 0x7fffffff, hi = 0;
+#pragma unroll
+    for (int w = 0; w < kRowGroups; ++w) {
+      lo = min(lo, span_lds[0][w]);
+      hi = max(hi, span_lds[1][w]);
+    }
+    piece_of(__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(hi));
+  }
+  if (none) {                                    // (its place among the pieces says that there is nothing)
+    if (wave < Piece::kWaves)
+      Piece::store_none(Piece::at(c.part, tile * p.n_kv_heads + hk, c.splits, split, wave), -INFINITY, 0.f, lane);
+    return;
+  }
 
   f32x16 acc_o[kDb];
 #pragma unroll
@@ -176,11 +194,6 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
 #pragma unroll
     for (int j = 0; j < 16; ++j) acc_o[i][j] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;          // the row's maximum (units of log2), this lane's share of its sum
-  int page = -1;
-  if (t_begin < t_end) {
-    page = page_of(t_begin);
-    if (page >= 0) fetch(page, 0);
-  }
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
 
@@ -251,25 +264,31 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
     if (page_next >= 0) fetch(page_next, stage ^ 1);
     if (visible) {
       // register i of group kb holds key kpos0 + (kb0 + kb) 32 + 16 (i / 8) + 8 half + i % 8
-      if constexpr (kForm) {
-        const float ahead = float(pos - sub0 - 8 * half);
+      CapForm cap;
+      if constexpr (kCap && !kBias) {            // the polynomial goes into the exponents below; beyond its range, and where some are hidden, scores are capped here
+        cap = cap_form(p.f.cap_in, p.f.cap_log2e);
+        const bool small = cap_is_small(acc_s, p.f.cap_in);
+        if (masked || !small) {
 #pragma unroll
-        for (int kb = 0; kb < kNg; ++kb)
+          for (int kb = 0; kb < kNg; ++kb)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float x = kCap ? p.f.cap_log2e * paged_tanh(acc_s[kb][i] * p.f.cap_in) : acc_s[kb][i] * p.f.scale_log2e;
-            if (kBias) x = fmaf(-slope, fabsf(ahead - float(kb * 32 + 16 * (i >> 3) + (i & 7))), x);
-            acc_s[kb][i] = x;
-          }
+            for (int i = 0; i < 16; ++i) {
+              const float x = acc_s[kb][i];
+              acc_s[kb][i] = small ? x * cap.factor(x) : paged_tanh(x * p.f.cap_in, p.f.cap_log2e);
+            }
+          cap = CapForm{1.f, 0.f, 0.f, 0.f};
+        }
       }
+      if constexpr (kBias)
+        paged_scores<kCap, kBias>(p.f, acc_s, kCap ? p.f.cap_in : p.f.scale_log2e, slope, float(pos - sub0 - 8 * half),
+                                  [](int g, int i) { return g * 32 + 16 * (i >> 3) + (i & 7); });
       if (masked) {
+        const int ahead = sub0 + 8 * half - v.lo;
 #pragma unroll
         for (int kb = 0; kb < kNg; ++kb)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int kp = sub0 + kb * 32 + 16 * (i >> 3) + 8 * half + (i & 7);
-            acc_s[kb][i] = kp >= v.lo && kp < v.hi ? acc_s[kb][i] : -INFINITY;
-          }
+          for (int i = 0; i < 16; ++i)
+            acc_s[kb][i] = span_holds(ahead + (kb * 32 + 16 * (i >> 3) + (i & 7)), v_len) ? acc_s[kb][i] : kHidden;
       }
       // ---- online softmax, one row per lane (lanes n and n + 32 share it)
       auto v_read = [&](int j) {
@@ -285,7 +304,8 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) mx = fmaxf(mx, acc_s[kb][i]);
       mx = lane_pair<32>(mx, [](float x, float y) { return fmaxf(x, y); });
-      const float m_tile = kForm ? mx : mx * p.f.scale_log2e;
+      float m_tile = kBias ? mx : mx * p.f.scale_log2e;
+      if constexpr (kCap && !kBias) m_tile = mx == kHidden ? -INFINITY : mx * cap.factor(mx);
       const float m_new = m_tile - m_run > kPcLazyLog2 ? m_tile : m_run;
       const float m_safe = m_new == -INFINITY ? 0.f : m_new;
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_safe);
@@ -297,7 +317,11 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
           for (int i = 0; i < 16; ++i) acc_o[db][i] *= alpha;
         l_run *= alpha;
       }
-      auto prob = [&](float x) { return __builtin_amdgcn_exp2f(kForm ? x - m_safe : x * p.f.scale_log2e - m_safe); };
+      auto prob = [&](float x) {
+        if constexpr (kBias) return __builtin_amdgcn_exp2f(x - m_safe);
+        else if constexpr (kCap) return __builtin_amdgcn_exp2f(fmaf(x, cap.factor(x), -m_safe));
+        else return __builtin_amdgcn_exp2f(fmaf(x, p.f.scale_log2e, -m_safe));
+      };
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc_s[0][i] = prob(acc_s[0][i]);
       __builtin_amdgcn_sched_barrier(0);
@@ -398,8 +422,14 @@ __global__ __launch_bounds__(kPcThreads) void paged_chunk_kernel(PagedChunk c) {
 }
 
 // ---- host side
-// The cut of a call: KS, and the pieces of a query tile's pages, by the least time of the busiest compute unit with these
-// figures (us per page and 256, 128, 64 rows; an item's start and end; merging).
+// The cut of a call: KS, and the pieces of a query tile's pages, by these figures, in us: a page with 256, 128, 64 rows, a tile's start
+// and end, and what pieces cost (a launch, and their way out and back at 4 TB/s).  Whole tiles, dealt out as compute units come
+// free, from the longest on: the busiest unit has no more than an average one, or the longest tile, if tiles differ, and a whole
+// number of rounds if they do not.  (Shares of the pages equal to a page, made by a plan on the device, were slower nearly
+// everywhere: 4 prompts in a row 52 us | 68.  A tile costs 6 us beside its pages, a cut of one 135 KB out and in.)
+//   2 x 2048 rows at 16K tokens, 32 query and 8 KV heads of 128: KS 1 908, 2 1036, 4 1563; 1 x 2048 at 2048 59, 52, 75; 8 x 512 at 512
+//   49, 59, 86; 512 at 512 21.5, 16.6, 14.4; 12 sequences of up to 500 with a window, 28 and 4 heads 291, 259, 354; 4 of up to 777
+//   248, 271, 380; 64 channels, 8192 at 8192 137, 100, 137, with documents 79, 52, 61
 struct ChunkCut {
   int ks, splits, tiles;
 };
@@ -409,19 +439,30 @@ static int chunk_tiles(const actqkv_shape& sh, int batch, int n_rows, int max_ne
   const int64_t most = seqs * ((int64_t(max_new) * group + rows - 1) / rows);
   return int(std::min(most, int64_t(n_rows) * group / rows + seqs));
 }
-static ChunkCut chunk_cut(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages) {
-  constexpr double kTileUs[] = {3.7, 2.1, 1.5}, kMergeUs = 4., kMergePieceUs[] = {0.6, 0.3, 0.15}, kItemUs = 5.;
-  const double scale = sh.head_dim == 64 ? 0.6 : 1.;
+static ChunkCut chunk_cut(const actqkv_shape& sh, const PagedAttn& p) {
+  constexpr double kPageUs[2][3] = {{3.5, 2.0, 1.5}, {2.1, 1.45, 1.0}}, kItemUs = 5.;
+  const PagedTable& t = p.t;
+  // pages of the longest tile and of an average one: of a prompt half of its own on average; of documents a part, nobody knows which
+  double longest = t.max_pages, own = double(t.max_new) / kBlock;
+  if (p.f.window > 0) longest = std::min(longest, p.f.window / double(kBlock) + 2.);
+  double average = longest - std::min(own, longest) / 2.;
+  bool equal = p.f.window > 0 ? longest < t.max_pages : own * 4. < longest;
+  if (p.f.row_first != nullptr) {
+    average = longest / 8.;
+    longest /= 3.;
+    equal = false;
+  }
   ChunkCut best{1, 1, 1};
   double least = 0.;
   for (int i = 0; i < 3; ++i) {
-    const int ks = 1 << i, tiles = chunk_tiles(sh, batch, n_rows, max_new, ks);
+    const int ks = 1 << i, tiles = chunk_tiles(sh, t.batch, t.n_rows, t.max_new, ks);
     const int64_t items = int64_t(tiles) * sh.n_kv_heads;
-    for (int splits = 1; splits <= std::min(kPcMaxSplits, max_pages); ++splits) {
+    const double page = kPageUs[sh.head_dim == 64][i], rounds = double(items) / kChipCus;
+    for (int splits = 1; splits <= std::min(kPcMaxSplits, t.max_pages); ++splits) {
       if (splits > 1 && items * splits > kChipCus) break;
-      const double rounds = std::ceil(double(items) * splits / kChipCus);
-      double us = rounds * (std::ceil(double(max_pages) / splits) * kTileUs[i] * scale + kItemUs);
-      if (splits > 1) us += kMergeUs + kMergePieceUs[i] * splits;
+      double us = std::ceil(longest / splits) * page + kItemUs;
+      if (splits == 1) us = equal ? std::ceil(rounds) * us : std::max(us, rounds * (average * page + kItemUs));
+      else us += 4. + double(items) * splits * (kPcRows<1> / ks) * sh.head_dim * 8. / 4e6;
       if ((i == 0 && splits == 1) || us < least) {
         least = us;
         best = ChunkCut{ks, splits, tiles};
@@ -460,7 +501,7 @@ static void launch_chunk_ks(int ks, const PagedChunk& c, hipStream_t stream) {
   else launch_chunk<D, 4>(c, stream);
 }
 int launch_paged_chunk(const actqkv_shape& sh, const PagedAttn& p, const Workspace& ws, hipStream_t stream) {
-  const ChunkCut cut = chunk_cut(sh, p.t.batch, p.t.n_rows, p.t.max_new, p.t.max_pages);
+  const ChunkCut cut = chunk_cut(sh, p);
   PagedChunk c;
   c.a = p;
   c.tiles = cut.tiles;

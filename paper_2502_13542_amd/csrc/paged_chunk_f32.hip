@@ -56,7 +56,8 @@ __device__ __forceinline__ void chunk_f32_body(const PagedChunkF32& c) {
   const int i_row = frow / group, head = hk * group + (frow - i_row * group);
   const int row = seq.row0 + i_row, pos = seq.n - seq.m + i_row;
   PagedSpan v = paged_span(p.f, row, pos, seq.n);
-  if (v.hi <= v.lo) v = PagedSpan{0x7fffffff, 0};
+  const uint32_t v_len = v.length();
+  if (v_len == 0) v = PagedSpan{0x7fffffff, 0};
   const float slope = kBias ? p.f.slopes[head] * kLog2e : 0.f;
   int lo_any = v.lo, hi_any = v.hi, lo_all = v.lo, hi_all = v.hi;
 #pragma unroll
@@ -100,13 +101,12 @@ __device__ __forceinline__ void chunk_f32_body(const PagedChunkF32& c) {
   // are read together hit all banks.
   auto k_key = [](int r) { return uint32_t(D == 64 ? (r >> 1) & 7 : r & 15); };
   auto v_key = [](int r) { return uint32_t(D == 64 ? (r >> 1) & 7 : (r >> 2) & 3); };
-  uint32_t wk[4], wv[4];                                     // where this lane's pieces go in a part
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int kr = kr0 + i * kKPer, vr = vr0 + i * kVPer;
-    wk[i] = uint32_t(kr) * kKRow + ((uint32_t(kc >> 1) ^ k_key(kr)) << 4) + 8 * (kc & 1);
-    wv[i] = uint32_t(vr) * kVRow + ((uint32_t(vc >> 1) ^ v_key(vr)) << 4) + 8 * (vc & 1);
-  }
+  // where this lane's pieces go in a part: piece i of K is 2 i (64 channels: 4 i) rows on, of V^T 4 i (8 i), which changes other bits of the
+  // key than the lane does
+  const uint32_t wk0 = uint32_t(kr0) * kKRow + ((uint32_t(kc >> 1) ^ k_key(kr0)) << 4) + 8 * (kc & 1);
+  const uint32_t wv0 = uint32_t(vr0) * kVRow + ((uint32_t(vc >> 1) ^ v_key(vr0)) << 4) + 8 * (vc & 1);
+  auto wk = [&](int i) { return (wk0 ^ (uint32_t(2 * i) << 4)) + uint32_t(i * kKPer) * kKRow; };
+  auto wv = [&](int i) { return (wv0 ^ (uint32_t(D == 64 ? 2 * i : 2 * i & 3) << 4)) + uint32_t(i * kVPer) * kVRow; };
   const char* kbase = static_cast<const char*>(p.k_pages);
   const char* vbase = static_cast<const char*>(p.v_pages);
   constexpr uint32_t kPageBytes = uint32_t(kBlock) * D * 4;
@@ -160,11 +160,11 @@ __device__ __forceinline__ void chunk_f32_body(const PagedChunkF32& c) {
       ff_split(xk[i][0], xk[i][1], a);
       ff_split(xk[i][2], xk[i][3], b);
 #pragma unroll
-      for (int j = 0; j < 3; ++j) *reinterpret_cast<u32x2*>(lds + j * kP4Part + wk[i]) = u32x2{a[j], b[j]};
+      for (int j = 0; j < 3; ++j) *reinterpret_cast<u32x2*>(lds + j * kP4Part + wk(i)) = u32x2{a[j], b[j]};
       ff_split(xv[i][0], xv[i][1], a);
       ff_split(xv[i][2], xv[i][3], b);
 #pragma unroll
-      for (int j = 0; j < 3; ++j) *reinterpret_cast<u32x2*>(lds + (3 + j) * kP4Part + wv[i]) = u32x2{a[j], b[j]};
+      for (int j = 0; j < 3; ++j) *reinterpret_cast<u32x2*>(lds + (3 + j) * kP4Part + wv(i)) = u32x2{a[j], b[j]};
     }
   };
   // the pages of 64 of the piece's pages at a time, one per lane; a tile without a page has no visible keys
@@ -284,25 +284,16 @@ __device__ __forceinline__ void chunk_f32_body(const PagedChunkF32& c) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc_s[gg][i] *= scale;
     }
-    if constexpr (kCap || kBias) {
-      const float ahead = float(pos - key0 - 8 * half);
-#pragma unroll
-      for (int gg = 0; gg < kG; ++gg)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float x = kCap ? p.f.cap_log2e * paged_tanh(acc_s[gg][i]) : acc_s[gg][i];
-          if (kBias) x = fmaf(-slope, fabsf(ahead - float(gg * 32 + 16 * (i >> 3) + (i & 7))), x);
-          acc_s[gg][i] = x;
-        }
-    }
+    if constexpr (kCap || kBias)                             // (the scale is in the queries)
+      paged_scores<kCap, kBias>(p.f, acc_s, 1.f, slope, float(pos - key0 - 8 * half),
+                                [](int g, int i) { return g * 32 + 16 * (i >> 3) + (i & 7); });
     if (masked) {
+      const int ahead = key0 + 8 * half - v.lo;
 #pragma unroll
       for (int gg = 0; gg < kG; ++gg)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int kpos = key0 + gg * 32 + 16 * (i >> 3) + 8 * half + (i & 7);
-          acc_s[gg][i] = kpos >= v.lo && kpos < v.hi ? acc_s[gg][i] : -INFINITY;
-        }
+        for (int i = 0; i < 16; ++i)
+          acc_s[gg][i] = span_holds(ahead + (gg * 32 + 16 * (i >> 3) + (i & 7)), v_len) ? acc_s[gg][i] : -INFINITY;
     }
     float mx = acc_s[0][0];
 #pragma unroll

@@ -41,12 +41,13 @@ __global__ __launch_bounds__(kStThreads) void paged_step_kernel(PagedStep st) {
   const int wg = blockIdx.x, hk = blockIdx.y, s = blockIdx.z;
   const int group = p.n_q_heads / p.n_kv_heads;
   const PagedSeq seq = paged_seq(p.t, s);
-  if (seq.m == 0) return;
   const int cols = seq.m * group;
+  if (cols == 0 || cols > 16) return;          // (more: another launch's)
   // ---- this lane's column: columns past the last repeat it, nobody reads what they give
   const int col = min(n, cols - 1), i_row = col / group, row = seq.row0 + i_row, head = hk * group + (col - i_row * group);
   const int pos = seq.n - seq.m + i_row;
   const PagedSpan v = paged_span(p.f, row, pos, seq.n);
+  const uint32_t v_len = v.length();
   const float slope = kBias ? p.f.slopes[head] * kLog2e : 0.f;
   u32x4 qb[S::kQ];
   {
@@ -108,7 +109,7 @@ __global__ __launch_bounds__(kStThreads) void paged_step_kernel(PagedStep st) {
       for (int i = 0; i < 4; ++i) {
         const int kp = kpos0 + S::key_of(j, i, kq);
         const float x = paged_score<kCap, kBias>(p.f, sc[j][i], slope, abs(pos - kp));
-        sc[j][i] = kp >= v.lo && kp < v.hi ? x : -INFINITY;
+        sc[j][i] = span_holds(kp - v.lo, v_len) ? x : -INFINITY;
         mx = fmaxf(mx, sc[j][i]);
       }
       if (score_at != nullptr) *reinterpret_cast<f32x4*>(score_at + kpos0 + S::key_of(j, 0, kq)) = sc[j];

@@ -51,7 +51,7 @@ __device__ __forceinline__ void votes_body(const PagedVotes& c) {
   constexpr bool kForm = kCap || kBias;
   __shared__ __attribute__((aligned(16))) char rows_lds[2][kBytes];
   __shared__ __attribute__((aligned(16))) float lse_lds[2][kPwRows], slope_lds[2][kPwRows];
-  __shared__ __attribute__((aligned(16))) int lo_lds[2][kPwRows], hi_lds[2][kPwRows], pos_lds[2][kPwRows];
+  __shared__ __attribute__((aligned(16))) int lo_lds[2][kPwRows], len_lds[2][kPwRows], pos_lds[2][kPwRows];
   __shared__ int any_lds[2][2][2], all_lds[2][2][2];               // [stage][32 rows][lo, hi]
   __shared__ float sum_lds[S::kKeys];
   const PagedAttn& p = c.a;
@@ -129,7 +129,7 @@ __device__ __forceinline__ void votes_body(const PagedVotes& c) {
   auto row_write = [&](int stage) {
     lse_lds[stage][lane] = my_span.hi > 0 ? my_lse : 0.f;
     lo_lds[stage][lane] = my_span.lo;
-    hi_lds[stage][lane] = my_span.hi;
+    len_lds[stage][lane] = int(my_span.length());
     if (kBias) {
       slope_lds[stage][lane] = my_slope;
       pos_lds[stage][lane] = my_pos;
@@ -211,12 +211,12 @@ __device__ __forceinline__ void votes_body(const PagedVotes& c) {
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
           const int r0 = 32 * rh + 8 * b + 4 * half;
-          const u32x4 lo = *reinterpret_cast<const u32x4*>(&lo_lds[stage][r0]), hi = *reinterpret_cast<const u32x4*>(&hi_lds[stage][r0]);
+          const u32x4 lo = *reinterpret_cast<const u32x4*>(&lo_lds[stage][r0]), len = *reinterpret_cast<const u32x4*>(&len_lds[stage][r0]);
 #pragma unroll
           for (int gk = 0; gk < kG; ++gk) {
             const int key = wkey0 + 32 * gk + n;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[gk][4 * b + e] = key >= int(lo[e]) && key < int(hi[e]) ? acc[gk][4 * b + e] : 0.f;
+            for (int e = 0; e < 4; ++e) acc[gk][4 * b + e] = span_holds(key - int(lo[e]), len[e]) ? acc[gk][4 * b + e] : 0.f;
           }
         }
       }
