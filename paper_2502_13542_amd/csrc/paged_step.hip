@@ -55,15 +55,22 @@ __global__ __launch_bounds__(kStThreads) void paged_step_kernel(PagedStep st) {
 #pragma unroll
     for (int ks = 0; ks < S::kQ; ++ks) qb[ks] = *reinterpret_cast<const u32x4*>(qp + ks * S::kQStep);
   }
-  // ---- the items that any column sees
-  int lo = v.hi > v.lo ? v.lo : 0x7fffffff, hi = v.hi > v.lo ? v.hi : 0;
+  // ---- the items that any column sees: from the numbers alone where rows bring no spans of their own
+  int lo, hi;
+  if (p.f.row_first == nullptr && p.f.row_end == nullptr) {
+    lo = p.f.window > 0 ? max(max(seq.n - seq.m, 0) - p.f.window + 1, 0) : 0;
+    hi = seq.n;
+  } else {
+    lo = v_len != 0 ? v.lo : 0x7fffffff;
+    hi = v_len != 0 ? v.hi : 0;
 #pragma unroll
-  for (int d = 1; d < 16; d <<= 1) {
-    lo = min(lo, __shfl_xor(lo, d, 64));
-    hi = max(hi, __shfl_xor(hi, d, 64));
+    for (int d = 1; d < 16; d <<= 1) {
+      lo = min(lo, __shfl_xor(lo, d, 64));
+      hi = max(hi, __shfl_xor(hi, d, 64));
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
   }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  hi = __builtin_amdgcn_readfirstlane(hi);
   constexpr int kPerPage = kBlock / S::kKeys;
   const int it0 = hi > 0 ? lo / S::kKeys : 0, n_items = hi > 0 ? (hi + S::kKeys - 1) / S::kKeys - it0 : 0;
   const int wgs = min(max((n_items + kStWaves - 1) / kStWaves, 1), st.n_wg);
@@ -246,12 +253,15 @@ bool paged_step_supported(const actqkv_shape& sh, int max_new) { return int64_t(
 
 static int step_keys(const actqkv_shape& sh) { return sh.dtype == ACTQKV_F32 ? 4096 / sh.head_dim : 64; }
 
-// Workgroups per (sequence, KV head).
+// Workgroups per (sequence, KV head): as many as fill the compute units once, and more only where a wavefront still has eight items,
+// which evens out sequences of different length; every one adds a part to merge.  us with 256 | 1024 workgroups, 32 query and 8 KV heads: 1 sequence at 32K tokens 28 | 41, 4 at 8K 24 | 30, 8 at up to 16K 83 | 88, 16
+// at up to 32K 300 | 264 (those take the 1024).
 static int step_workgroups(const actqkv_shape& sh, int batch, int max_pages) {
   const int64_t pairs = int64_t(batch) * sh.n_kv_heads;
   if (pairs > int64_t(kTicketCounters)) return 1;
   const int64_t items = int64_t(max_pages) * (kBlock / step_keys(sh));
-  return int(std::min({(items + kStWaves - 1) / kStWaves, (kStepWgs + pairs - 1) / pairs, int64_t(64)}));
+  const int64_t fill = (kChipCus + pairs - 1) / pairs, even = std::min(items / (8 * kStWaves), (kStepWgs + pairs - 1) / pairs);
+  return int(std::max<int64_t>(1, std::min({std::max(fill, even), (items + kStWaves - 1) / kStWaves, int64_t(64)})));
 }
 static size_t step_part_bytes(const actqkv_shape& sh, int batch, int max_pages) {
   const int n_wg = step_workgroups(sh, batch, max_pages);
