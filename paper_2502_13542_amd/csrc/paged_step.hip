@@ -33,7 +33,7 @@ template <typename T, int D, bool kCap, bool kBias>
 __global__ __launch_bounds__(kStThreads) void paged_step_kernel(PagedStep st) {
   typedef DcShape<T, D> S;
   constexpr int kRow = D + 2;
-  __shared__ float lds[kStWaves * 16 * kRow];
+  __shared__ __attribute__((aligned(16))) float lds[kStWaves * 16 * kRow];
   __shared__ int last_flag;
   const PagedAttn& p = st.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -76,9 +76,8 @@ __global__ __launch_bounds__(kStThreads) void paged_step_kernel(PagedStep st) {
   const int wgs = min(max((n_items + kStWaves - 1) / kStWaves, 1), st.n_wg);
   if (wg >= wgs) return;
   const int pair = s * p.n_kv_heads + hk;
-  float* score_at = nullptr;
-  if (st.scores != nullptr && n < cols && i_row >= seq.m - st.weight_rows)
-    score_at = st.scores + (size_t(pair) * (p.t.max_new * group) + n) * (size_t(p.t.max_pages) * kBlock);
+  float* score_at = st.scores == nullptr ? nullptr : st.scores + size_t(pair) * (p.t.max_new * group) * (size_t(p.t.max_pages) * kBlock);
+  const int vote0 = max(seq.m - st.weight_rows, 0) * group;    // first column whose scores are kept
 
   float m_run = -INFINITY, l_run = 0.f;
   f32x4 acc[D / 16];
@@ -119,7 +118,18 @@ __global__ __launch_bounds__(kStThreads) void paged_step_kernel(PagedStep st) {
         sc[j][i] = span_holds(kp - v.lo, v_len) ? x : -INFINITY;
         mx = fmaxf(mx, sc[j][i]);
       }
-      if (score_at != nullptr) *reinterpret_cast<f32x4*>(score_at + kpos0 + S::key_of(j, 0, kq)) = sc[j];
+    }
+    if (score_at != nullptr) {                 // through LDS, so that a store instruction writes 1 KB in rows of an item's keys
+      float* mine = lds + wave * 16 * kRow;
+#pragma unroll
+      for (int j = 0; j < S::kSubs; ++j)
+        if (n < cols) *reinterpret_cast<f32x4*>(mine + n * S::kKeys + S::key_of(j, 0, kq)) = sc[j];
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      for (int e = vote0 * S::kKeys + lane * 4; e < cols * S::kKeys; e += 256)
+        *reinterpret_cast<f32x4*>(score_at + size_t(e / S::kKeys) * (size_t(p.t.max_pages) * kBlock) + kpos0 + e % S::kKeys) =
+            *reinterpret_cast<const f32x4*>(mine + e);
+      __builtin_amdgcn_wave_barrier();
     }
     const auto larger = [](float x, float y) { return fmaxf(x, y); };
     mx = lane_pair<32>(lane_pair<16>(mx, larger), larger);
