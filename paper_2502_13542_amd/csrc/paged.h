@@ -56,6 +56,20 @@ __device__ __forceinline__ int wave_scan(int v) {
   return v;
 }
 
+// The least and the largest over each half of the lanes, by the data-parallel primitives (through LDS, as a shuffle, a step is 60 ns).
+__device__ __forceinline__ int half_min(int v) {
+  v = min(v, int(lane_xor32<1>(uint32_t(v))));
+  v = min(v, int(lane_xor32<2>(uint32_t(v))));
+  v = min(v, int(lane_xor32<4>(uint32_t(v))));
+  v = min(v, int(lane_xor32<8>(uint32_t(v))));
+  return min(v, int(lane_xor32<16>(uint32_t(v))));
+}
+__device__ __forceinline__ int half_max(int v) { return ~half_min(~v); }
+// What 32 rows see: any of them [lo_any, hi_any), all of them [lo_all, hi_all).
+struct SpanOfRows {
+  int lo_any, hi_any, lo_all, hi_all;
+};
+
 // Query tiles of a sequence.
 __device__ __forceinline__ int paged_tiles(const PagedTable& t, const PagedSeq& q, int group, int rows_per) {
   return q.m * group > t.few ? (q.m * group + rows_per - 1) / rows_per : 0;
@@ -186,6 +200,9 @@ struct PagedAttn {
   void* out;                 // [n_rows][H][D]
   float* lse;                // [n_rows][H] or NULL
 };
+__device__ __forceinline__ SpanOfRows span_of_rows(const PagedSpan& v) {
+  return SpanOfRows{half_min(v.lo), half_max(v.hi), half_max(v.lo), half_min(v.hi)};
+}
 struct PagedWeights {
   int rows;                  // the last so many rows of a sequence count
   const float* in;           // [batch][Hk][stride]

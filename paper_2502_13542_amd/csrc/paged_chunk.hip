@@ -156,18 +156,11 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
     for (int ks = 0; ks < kKs; ++ks) qreg[ks] = as_bf16x8(*reinterpret_cast<const u32x4*>(qp + ks * 16));
   }
   // ---- what the wavefront's rows see: any of them [lo_any, hi_any), all of them [lo_all, hi_all)
-  int lo_any = v.lo, hi_any = v.hi, lo_all = v.lo, hi_all = v.hi;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    lo_any = min(lo_any, __shfl_xor(lo_any, d, 64));
-    hi_any = max(hi_any, __shfl_xor(hi_any, d, 64));
-    lo_all = max(lo_all, __shfl_xor(lo_all, d, 64));
-    hi_all = min(hi_all, __shfl_xor(hi_all, d, 64));
-  }
-  lo_any = __builtin_amdgcn_readfirstlane(lo_any);
-  hi_any = __builtin_amdgcn_readfirstlane(wave_ok ? hi_any : 0);
-  lo_all = __builtin_amdgcn_readfirstlane(lo_all);
-  hi_all = __builtin_amdgcn_readfirstlane(hi_all);
+  const SpanOfRows seen = span_of_rows(v);
+  const int lo_any = __builtin_amdgcn_readfirstlane(seen.lo_any);
+  const int hi_any = __builtin_amdgcn_readfirstlane(wave_ok ? seen.hi_any : 0);
+  const int lo_all = __builtin_amdgcn_readfirstlane(seen.lo_all);
+  const int hi_all = __builtin_amdgcn_readfirstlane(seen.hi_all);
   if (arrays) {
     if (lane == 0) {
       span_lds[0][wave] = wave_ok ? lo_any : 0x7fffffff;

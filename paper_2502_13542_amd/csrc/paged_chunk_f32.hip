@@ -59,18 +59,11 @@ __device__ __forceinline__ void chunk_f32_body(const PagedChunkF32& c) {
   const uint32_t v_len = v.length();
   if (v_len == 0) v = PagedSpan{0x7fffffff, 0};
   const float slope = kBias ? p.f.slopes[head] * kLog2e : 0.f;
-  int lo_any = v.lo, hi_any = v.hi, lo_all = v.lo, hi_all = v.hi;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    lo_any = min(lo_any, __shfl_xor(lo_any, d, 64));
-    hi_any = max(hi_any, __shfl_xor(hi_any, d, 64));
-    lo_all = max(lo_all, __shfl_xor(lo_all, d, 64));
-    hi_all = min(hi_all, __shfl_xor(hi_all, d, 64));
-  }
-  lo_any = __builtin_amdgcn_readfirstlane(lo_any);
-  hi_any = __builtin_amdgcn_readfirstlane(wave_ok ? hi_any : 0);
-  lo_all = __builtin_amdgcn_readfirstlane(lo_all);
-  hi_all = __builtin_amdgcn_readfirstlane(hi_all);
+  const SpanOfRows seen = span_of_rows(v);
+  const int lo_any = __builtin_amdgcn_readfirstlane(seen.lo_any);
+  const int hi_any = __builtin_amdgcn_readfirstlane(wave_ok ? seen.hi_any : 0);
+  const int lo_all = __builtin_amdgcn_readfirstlane(seen.lo_all);
+  const int hi_all = __builtin_amdgcn_readfirstlane(seen.hi_all);
   if (lane == 0) {
     span_lds[0][wave] = wave_ok ? lo_any : 0x7fffffff;
     span_lds[1][wave] = hi_any;

@@ -3,9 +3,12 @@
 // A workgroup of 8 wavefronts takes 128 keys (fp32) or 256 (bf16) of one (sequence, KV head) and walks the voting rows, the G heads of
 // a row side by side.  S = Q K^T with the rows as the first operand and the keys as the second leaves a lane with scores of ONE
 // key, 16 rows of it in its registers: the sum over rows needs no exchange.  A wavefront keeps its keys in registers for the whole
-// walk (straight from memory, each byte read once per 4 wavefronts that do not share it) and reads the rows from LDS, 64 at a
-// time, double buffered, filled without registers in between; four wavefronts take the even 32 rows of each 64, four the odd ones.
-// Beside its products a wavefront has a multiply-add, an exponential and an addition per score, which bound it with them.
+// walk (straight from memory, each byte read once per 4 wavefronts that do not share it) and reads the rows from LDS, 128 at a
+// time, double buffered, filled without registers in between; four wavefronts take the first 64 of them, four the others, in two
+// blocks of 32: the multiply-adds and exponentials of the first between the products of the second.  Those and an addition per
+// score bound it with the products: 2048 rows of each of 2 sequences at 16K tokens, 32 heads, 634 us (813 TFLOP/s); 64 rows a step, a block
+// each, 687; 4 wavefronts a workgroup and two workgroups a compute unit 880 (their registers spill); the last 64 rows of 4
+// sequences at 8K, 28 heads, 35 us, of which the products are 12: two rounds of the chip, each with its first keys and rows to wait for.
 //
 // Where keys alone do not fill the chip, the rows are cut into pieces whose sums a second launch adds up, in order.  Sums of
 // 16 rows are added to the running sum, not single terms: its rounding would pass 1e-6 after some thousand.
@@ -15,7 +18,7 @@
 namespace actqkv {
 
 constexpr int kPwThreads = 512, kPwWaves = kPwThreads / 64;
-constexpr int kPwRows = 64;                      // rows (with a head each) of a step
+constexpr int kPwRows = 128;                     // rows (with a head each) of a step
 constexpr int kPwWgs = 512;                      // workgroups that a call is cut into
 
 // Keys of a wavefront and of a workgroup; 16-byte operands of a row.
@@ -52,7 +55,7 @@ __device__ __forceinline__ void votes_body(const PagedVotes& c) {
   __shared__ __attribute__((aligned(16))) char rows_lds[2][kBytes];
   __shared__ __attribute__((aligned(16))) float lse_lds[2][kPwRows], slope_lds[2][kPwRows];
   __shared__ __attribute__((aligned(16))) int lo_lds[2][kPwRows], len_lds[2][kPwRows], pos_lds[2][kPwRows];
-  __shared__ int any_lds[2][2][2], all_lds[2][2][2];               // [stage][32 rows][lo, hi]
+  __shared__ SpanOfRows seen_lds[2][kPwRows / 32];
   __shared__ float sum_lds[S::kKeys];
   const PagedAttn& p = c.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -91,7 +94,7 @@ __device__ __forceinline__ void votes_body(const PagedVotes& c) {
       for (int j = 0; j < S::kSteps; ++j) kreg[gk][j] = u32x4{0, 0, 0, 0};
   }
 
-  // ---- staging of 64 rows: their queries into LDS, and by the first wavefront what else a row has
+  // ---- staging of the rows of a step: their queries into LDS, and by the first two wavefronts what else a row has
   auto fetch = [&](int st, int stage) {
     const int f = f0 + st * kPwRows;
     const int first = f / group;
@@ -113,7 +116,7 @@ __device__ __forceinline__ void votes_body(const PagedVotes& c) {
   PagedSpan my_span{0x7fffffff, 0};
   int my_pos = 0;
   auto row_read = [&](int st) {
-    const int f = f0 + st * kPwRows + lane;
+    const int f = f0 + st * kPwRows + tid;
     my_span = PagedSpan{0x7fffffff, 0};
     my_lse = my_slope = 0.f;
     my_pos = 0;
@@ -127,108 +130,122 @@ __device__ __forceinline__ void votes_body(const PagedVotes& c) {
     }
   };
   auto row_write = [&](int stage) {
-    lse_lds[stage][lane] = my_span.hi > 0 ? my_lse : 0.f;
-    lo_lds[stage][lane] = my_span.lo;
-    len_lds[stage][lane] = int(my_span.length());
+    lse_lds[stage][tid] = my_span.hi > 0 ? my_lse : 0.f;
+    lo_lds[stage][tid] = my_span.lo;
+    len_lds[stage][tid] = int(my_span.length());
     if (kBias) {
-      slope_lds[stage][lane] = my_slope;
-      pos_lds[stage][lane] = my_pos;
+      slope_lds[stage][tid] = my_slope;
+      pos_lds[stage][tid] = my_pos;
     }
-    int lo_any = my_span.lo, hi_any = my_span.hi, lo_all = my_span.lo, hi_all = my_span.hi;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      lo_any = min(lo_any, __shfl_xor(lo_any, d, 64));
-      hi_any = max(hi_any, __shfl_xor(hi_any, d, 64));
-      lo_all = max(lo_all, __shfl_xor(lo_all, d, 64));
-      hi_all = min(hi_all, __shfl_xor(hi_all, d, 64));
-    }
-    if (n == 0) {
-      any_lds[stage][half][0] = lo_any;
-      any_lds[stage][half][1] = hi_any;
-      all_lds[stage][half][0] = lo_all;
-      all_lds[stage][half][1] = hi_all;
-    }
+    const SpanOfRows seen = span_of_rows(my_span);
+    if (n == 0) seen_lds[stage][2 * wave + half] = seen;
   };
   float sum[kG];
 #pragma unroll
   for (int gk = 0; gk < kG; ++gk) sum[gk] = 0.f;
   if (st0 < st1) {
     fetch(st0, 0);
-    if (wave == 0) {
+    if (wave < kPwRows / 64) {
       row_read(st0);
       row_write(0);
     }
   }
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
-  const uint32_t a_off0 = uint32_t(32 * rh + n) * S::kRowBytes + ((uint32_t(half) ^ S::swizzle(n)) << 4);
+  // a wavefront's rows of a step: two blocks of 32, whose products and exponentials take turns
+  const uint32_t a_off0 = uint32_t(64 * rh + n) * S::kRowBytes + ((uint32_t(half) ^ S::swizzle(n)) << 4);
   for (int st = st0; st < st1; ++st) {
     const int stage = (st - st0) & 1;
     const bool next = st + 1 < st1;
-    if (next && wave == 0) row_read(st + 1);
-    const int lo_any = __builtin_amdgcn_readfirstlane(any_lds[stage][rh][0]), hi_any = __builtin_amdgcn_readfirstlane(any_lds[stage][rh][1]);
-    const int lo_all = __builtin_amdgcn_readfirstlane(all_lds[stage][rh][0]), hi_all = __builtin_amdgcn_readfirstlane(all_lds[stage][rh][1]);
-    const bool visible = page >= 0 && wkey0 < hi_any && wkey0 + 32 * kG > lo_any;
-    const bool masked = wkey0 < lo_all || wkey0 + 32 * kG > hi_all;
-    f32x16 acc[kG];
-    if (visible) {
+    if (next && wave < kPwRows / 64) row_read(st + 1);
+    bool visible[2], masked[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const SpanOfRows seen = seen_lds[stage][2 * rh + b];
+      const int lo_any = __builtin_amdgcn_readfirstlane(seen.lo_any), hi_any = __builtin_amdgcn_readfirstlane(seen.hi_any);
+      const int lo_all = __builtin_amdgcn_readfirstlane(seen.lo_all), hi_all = __builtin_amdgcn_readfirstlane(seen.hi_all);
+      visible[b] = page >= 0 && wkey0 < hi_any && wkey0 + 32 * kG > lo_any;
+      masked[b] = wkey0 < lo_all || wkey0 + 32 * kG > hi_all;
+    }
+    f32x16 acc[2][kG];
+    constexpr int kRing = S::kSteps < 8 ? S::kSteps : 8;         // operands on their way
+    auto row_operand = [&](int b, int j) {
+      return *reinterpret_cast<const u32x4*>(rows_lds[stage] + b * 32 * S::kRowBytes + (a_off0 ^ (uint32_t(j) << 5)));
+    };
+    // register i is row 64 rh + 32 b + 8 (i / 4) + 4 half + i % 4, the lane's key wkey0 + 32 gk + n
+    auto first_row = [&](int b, int q) { return 64 * rh + 32 * b + 8 * q + 4 * half; };
+    auto weight = [&](float x, float lse, float slope, int pos, int gk) {
+      if constexpr (kForm) x = paged_score<kCap, kBias>(p.f, x, slope, kBias ? abs(pos - (wkey0 + 32 * gk + n)) : 0);
+      return __builtin_amdgcn_exp2f(kForm ? x - lse : fmaf(x, p.f.scale_log2e, -lse));
+    };
+    auto weights_of = [&](int b, int q) {        // a quarter of a block's
+      const f32x4 lse = *reinterpret_cast<const f32x4*>(&lse_lds[stage][first_row(b, q)]);
+      f32x4 slope = {0.f, 0.f, 0.f, 0.f};
+      u32x4 pos = {0, 0, 0, 0};
+      if constexpr (kBias) {
+        slope = *reinterpret_cast<const f32x4*>(&slope_lds[stage][first_row(b, q)]);
+        pos = *reinterpret_cast<const u32x4*>(&pos_lds[stage][first_row(b, q)]);
+      }
 #pragma unroll
       for (int gk = 0; gk < kG; ++gk)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[gk][i] = 0.f;
-      const char* at = rows_lds[stage];
-      u32x4 ring[S::kSteps];
+        for (int e = 0; e < 4; ++e) acc[b][gk][4 * q + e] = weight(acc[b][gk][4 * q + e], lse[e], slope[e], int(pos[e]), gk);
+    };
+    auto products = [&](int b, bool beside) {    // of block b; beside them the weights of the block before
+      u32x4 ring[kRing];
 #pragma unroll
-      for (int j = 0; j < S::kSteps; ++j) ring[j] = *reinterpret_cast<const u32x4*>(at + (a_off0 ^ (uint32_t(j) << 5)));
+      for (int j = 0; j < kRing; ++j) ring[j] = row_operand(b, j);
 #pragma unroll
-      for (int j = 0; j < S::kSteps; ++j)
+      for (int gk = 0; gk < kG; ++gk)
 #pragma unroll
-        for (int gk = 0; gk < kG; ++gk) acc[gk] = S::product(ring[j], kreg[gk][j], acc[gk]);
-    }
-    if (next) fetch(st + 1, stage ^ 1);
-    if (visible) {
-      // register i is row 32 rh + 8 (i / 4) + 4 half + i % 4, the lane's key wkey0 + 32 gk + n
+        for (int i = 0; i < 16; ++i) acc[b][gk][i] = 0.f;
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const int r0 = 32 * rh + 8 * b + 4 * half;
-        const f32x4 lse = *reinterpret_cast<const f32x4*>(&lse_lds[stage][r0]);
-        f32x4 slope;
-        u32x4 pos;
-        if constexpr (kBias) {
-          slope = *reinterpret_cast<const f32x4*>(&slope_lds[stage][r0]);
-          pos = *reinterpret_cast<const u32x4*>(&pos_lds[stage][r0]);
-        }
+      for (int j = 0; j < S::kSteps; ++j) {
 #pragma unroll
-        for (int gk = 0; gk < kG; ++gk)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float x = acc[gk][4 * b + e];
-            if constexpr (kForm) x = paged_score<kCap, kBias>(p.f, x, kBias ? slope[e] : 0.f, kBias ? abs(int(pos[e]) - (wkey0 + 32 * gk + n)) : 0);
-            acc[gk][4 * b + e] = __builtin_amdgcn_exp2f(kForm ? x - lse[e] : fmaf(x, p.f.scale_log2e, -lse[e]));
-          }
+        for (int gk = 0; gk < kG; ++gk) acc[b][gk] = S::product(ring[j % kRing], kreg[gk][j], acc[b][gk]);
+        if (j + kRing < S::kSteps) ring[j % kRing] = row_operand(b, j + kRing);
+        if (beside && j % (S::kSteps / 4) == 0) weights_of(0, j / (S::kSteps / 4));
       }
-      if (masked) {
+    };
+    auto add = [&](int b) {
+      if (masked[b]) {
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const int r0 = 32 * rh + 8 * b + 4 * half;
-          const u32x4 lo = *reinterpret_cast<const u32x4*>(&lo_lds[stage][r0]), len = *reinterpret_cast<const u32x4*>(&len_lds[stage][r0]);
+        for (int q = 0; q < 4; ++q) {
+          const u32x4 lo = *reinterpret_cast<const u32x4*>(&lo_lds[stage][first_row(b, q)]);
+          const u32x4 len = *reinterpret_cast<const u32x4*>(&len_lds[stage][first_row(b, q)]);
 #pragma unroll
-          for (int gk = 0; gk < kG; ++gk) {
-            const int key = wkey0 + 32 * gk + n;
+          for (int gk = 0; gk < kG; ++gk)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[gk][4 * b + e] = span_holds(key - int(lo[e]), len[e]) ? acc[gk][4 * b + e] : 0.f;
-          }
+            for (int e = 0; e < 4; ++e)
+              acc[b][gk][4 * q + e] = span_holds(wkey0 + 32 * gk + n - int(lo[e]), len[e]) ? acc[b][gk][4 * q + e] : 0.f;
         }
       }
 #pragma unroll
       for (int gk = 0; gk < kG; ++gk) {
         float t[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < 16; ++i) t[i & 3] += acc[gk][i];
+        for (int i = 0; i < 16; ++i) t[i & 3] += acc[b][gk][i];
         sum[gk] += (t[0] + t[1]) + (t[2] + t[3]);
       }
+    };
+    if (visible[0]) products(0, false);
+    if (next) fetch(st + 1, stage ^ 1);
+    if (visible[0] && visible[1]) {
+      products(1, true);
+      add(0);
+    } else if (visible[0]) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) weights_of(0, q);
+      add(0);
+    } else if (visible[1]) {
+      products(1, false);
     }
-    if (next && wave == 0) row_write(stage ^ 1);
+    if (visible[1]) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) weights_of(1, q);
+      add(1);
+    }
+    if (next && wave < kPwRows / 64) row_write(stage ^ 1);
     __builtin_amdgcn_s_waitcnt(0);               // this wavefront's share of the next rows has landed in LDS
     __syncthreads();
   }
