@@ -571,7 +571,7 @@ int actqkv_paged_append(const actqkv_shape* shape, int batch, int n_rows, int ma
  * included: actqkv_paged_append comes first): whole prompts, chunks and single tokens, together in one call.
  *   q        [n_rows][H][D], storage dtype.  Query head h reads KV head h / G.
  *   The score of a row at position p and a key at position j, with s = scale * <q, k>:
- *     softcap > 0:  s = softcap * tanh(s / softcap)                      (0: none)
+ *     softcap > 0:  s = softcap * tanh(s / softcap)                      (0: none; otherwise 1e-6 .. 1e6)
  *     slopes [H] fp32, may be NULL:  s = s - slopes[h] * |p - j|
  *   The row sees the positions first <= j < end:
  *     first = max(0, row_first[row], p - window + 1)    row_first [n_rows] int32, may be NULL (of a document mask: where the
@@ -580,7 +580,7 @@ int actqkv_paged_append(const actqkv_shape* shape, int batch, int n_rows, int ma
  *                                                       NULL: p + 1
  *   out      [n_rows][H][D] = softmax over the keys seen, times their values; 0 for a row that sees none.
  *   lse      [n_rows][H] fp32, natural-log sum of exp of the scores (-infinity for a row that sees none); may be NULL.
- * Errors: EINVAL (null, sizes, softcap negative, infinite or NaN, window < 0), ESHAPE, EALIGN, EWORKSPACE. */
+ * Errors: EINVAL (null, sizes, softcap outside its range, window < 0), ESHAPE, EALIGN, EWORKSPACE. */
 int actqkv_paged_attention(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q,
                            const int32_t* row_start, const int32_t* n_ctx, const int32_t* pages, int max_pages,
                            const void* k_pages, const void* v_pages, int n_pages, float softcap, int window,

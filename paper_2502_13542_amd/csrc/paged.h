@@ -150,7 +150,7 @@ __device__ __forceinline__ float paged_score(const PagedForm& f, float product, 
   return v;
 }
 // Whether the arguments in * x of a lane's registers, of all lanes, are in the polynomial's range: most of the time, and then a
-// cap is 5 instructions a score, otherwise 17.  (in^6 has to be a number, too: of a cap of thousands none is small.)
+// cap is 5 instructions a score, otherwise 17.  (in^6 has to be a number, too: under a cap of thousands, or of millionths, none is small.)
 template <int N>
 __device__ __forceinline__ bool cap_is_small(const f32x16 (&x)[N], float in) {
   float mx = 0.f;
@@ -158,7 +158,7 @@ __device__ __forceinline__ bool cap_is_small(const f32x16 (&x)[N], float in) {
   for (int g = 0; g < N; ++g)
 #pragma unroll
     for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(fabsf(x[g][i]), fabsf(x[g][i + 1])), mx);
-  return in >= 1e-5f && __all(mx * in <= kTanhSmall);
+  return in >= 1e-5f && in <= 1e5f && __all(mx * in <= kTanhSmall);
 }
 // Their scores.  `ahead`: the query's position less that of the key that off(g, i) = 0 would be of.
 template <bool kCap, bool kBias, int N, typename Off>

@@ -31,6 +31,8 @@ static size_t paged_workspace_bytes(const actqkv_shape& sh, int batch, int n_row
 }
 
 constexpr int kMaxPages = (1 << 30) / kBlock;     // 2^30 tokens: of a sequence, and in the pool
+// Caps: their reciprocal is a number, and no capped score is below what the kernels take for a hidden one.
+constexpr float kLeastCap = 1e-6f, kLargestCap = 1e6f;
 
 static int check_table(const actqkv_shape* shape, int batch, const int32_t* n_ctx, const int32_t* pages, int max_pages,
                        const void* k_pages, const void* v_pages, int n_pages) {
@@ -64,8 +66,8 @@ static int attention_call(const char* name, const actqkv_shape* shape, int batch
   ACTQKV_REQUIRE_PTR(q);
   ACTQKV_REQUIRE_SMALL(row_start, 4);
   ACTQKV_REQUIRE_PTR(out);
-  if (!(softcap >= 0.f) || std::isinf(softcap))
-    return set_error(ACTQKV_EINVAL, "softcap must be 0 (none) or positive and finite");
+  if (softcap != 0.f && !(softcap >= kLeastCap && softcap <= kLargestCap))
+    return set_error(ACTQKV_EINVAL, "softcap must be 0 (none) or between %g and %g", kLeastCap, kLargestCap);
   if (window < 0) return set_error(ACTQKV_EINVAL, "window %d < 0", window);
   ACTQKV_OPTIONAL_SMALL(slopes, 4);
   ACTQKV_OPTIONAL_SMALL(row_first, 4);

@@ -48,7 +48,7 @@ FORMS = {
 
 def form_of(b, kind, seed):
     """The form's arguments on the host."""
-    f = dict(FORMS[kind])
+    f = dict(kind if isinstance(kind, dict) else FORMS[kind])
     rng = np.random.default_rng(seed + 77)
     pos = b.positions()
     if f.pop("slopes", False):
@@ -417,3 +417,13 @@ def test_fp32_values_near_the_largest(shape, batch):
     b.q[::7, :, 5] = big                                            # one huge channel, against keys that are tiny there
     b.k_pages[:, :, :, 5] *= 1e-38
     run_attention(b, "cap" if batch == "chunks" else "plain")
+
+
+@pytest.mark.parametrize("shape", ["llama", "fp32_64", "mha64"])
+@pytest.mark.parametrize("batch", ["few", "chunks"])
+@pytest.mark.parametrize("softcap", [1e-6, 1e-3, 3e4, 1e6])
+def test_smallest_and_largest_caps(shape, batch, softcap):
+    """Caps under which every score is the cap, or none is changed, with queries of zeros among the others."""
+    b = Batch(shape_of(*SHAPES[shape]), BATCHES[batch], 67)
+    b.q[::3] = 0
+    run_attention(b, dict(softcap=softcap), weight_rows=2)

@@ -211,3 +211,10 @@ def test_the_runner_checks_sizes():
     with pytest.raises(B.ActQKVError, match="made for"):
         H.PagedRunner(b.shape, 2, 4, 3, b.max_pages, "cpu").append(**rows, **table)
     r.append(b.k_new[:0], b.v_new[:0], t["row_start"], t["n_ctx"], t["pages"], t["k_pages"], t["v_pages"])   # no rows: nothing to do
+
+
+@pytest.mark.parametrize("softcap", [1e-45, 1e-30, 9e-7, 1.1e6, 3e38])
+def test_caps_out_of_range_are_refused(lib, softcap):
+    """A cap whose reciprocal overflows, or that is so large that a capped score may be below a hidden one's mark."""
+    assert _attend(lib, B.c_shape(LLAMA), softcap=softcap) == -1 and "softcap" in B.last_error()
+    assert _weigh(lib, B.c_shape(LLAMA), softcap=softcap) == -1
