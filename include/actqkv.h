@@ -604,7 +604,7 @@ int actqkv_paged_attention_weights(const actqkv_shape* shape, int batch, int n_r
 /* Eviction: every KV head of every sequence with more than `budget` tokens keeps, of its n_ctx tokens, the first keep_first, the
  * last keep_last and, of those between, the budget - keep_first - keep_last with the largest weight (equal weights: the lower
  * positions; NaN below everything).  The kept tokens keep their order and move to the slots 0 .. budget - 1, keys, values
- * and weights; a shorter sequence keeps everything.
+ * and weights (of a token without a page: as zeros); a shorter sequence keeps everything, in place untouched.
  *   weights  [batch][Hk][weight_stride] fp32, weight_stride >= max_pages * Bs.
  *   to_pages device int32 [batch][to_max_pages]: the pages the kept tokens move to, none of which is a page of `pages`; NULL,
  *            or the array `pages` itself: in place (to_max_pages = max_pages), for sequences that share no page.

@@ -105,6 +105,7 @@ def evict(n_ctx, pages, k_pages, v_pages, weights, keep_first, keep_last, budget
     """Returns kept, n_kept, the two pools and to_weights after the call (pools are read as they were before it)."""
     k, v, w = k_pages.copy(), v_pages.copy(), to_weights.copy()
     batch, heads = weights.shape[:2]
+    in_place = to_pages is pages
     kept = np.full((batch, heads, budget), -1)
     n_kept = np.zeros(batch, int)
     for s in range(batch):
@@ -118,7 +119,8 @@ def evict(n_ctx, pages, k_pages, v_pages, weights, keep_first, keep_last, budget
             kept[s, h, : len(old)] = old
             w[s, h, : len(old)] = weights[s, h, old]
             for t, o in enumerate(old):
-                if to_page[t] >= 0 and page[o] >= 0:
-                    k[to_page[t], h, to_slot[t]] = k_pages[page[o], h, slot[o]]
-                    v[to_page[t], h, :, to_slot[t]] = v_pages[page[o], h, :, slot[o]]
+                if to_page[t] >= 0 and not (in_place and n <= budget):
+                    there = page[o] >= 0
+                    k[to_page[t], h, to_slot[t]] = k_pages[page[o], h, slot[o]] if there else 0.0
+                    v[to_page[t], h, :, to_slot[t]] = v_pages[page[o], h, :, slot[o]] if there else 0.0
     return kept, n_kept, k, v, w

@@ -8,7 +8,8 @@
 //
 // Move: the tokens keep their order, so a token never moves up, and slot t of the new cache is filled from a slot >= t.
 // In place, a workgroup has a slice of the channels of one (sequence, KV head) to itself and walks the new pages in order: it
-// reads everything for some pages, waits, and writes them; nothing that a later step reads lies in them.
+// reads everything for some pages, waits, and writes them; nothing that a later step reads lies in them.  A kept token without a page
+// moves as zeros: what its new slot held before belongs to nobody.
 #include <type_traits>
 
 #include "paged.h"
@@ -161,7 +162,8 @@ __global__ __launch_bounds__(kEmThreads) void paged_evict_move_kernel(PagedEvict
   constexpr int V = Vec<T>::N, kKeySlices = D / V / kEmUnits, kValueSlices = D / kEmRows;
   typedef typename Vec<T>::raw raw_t;
   typedef std::conditional_t<sizeof(T) == 2, uint32_t, u32x2> pair_t;
-  __shared__ int from[kEmPages * kBlock];         // 128 * page + slot of the token that comes to a slot, -1: none
+  __shared__ int from[kEmPages * kBlock];         // 128 * page + slot of the token that comes to a slot, kNone: no token, kGone: one without a page
+  constexpr int kNone = -1, kGone = -2;
   constexpr int kRoles = kKeySlices + kValueSlices + 1;
   const int role = blockIdx.x % kRoles, pair = blockIdx.x / kRoles, s = pair / e.n_kv_heads, hk = pair % e.n_kv_heads, tid = threadIdx.x;
   const int n = paged_tokens(e.t, s), n_kept = min(n, e.budget);
@@ -191,6 +193,7 @@ __global__ __launch_bounds__(kEmThreads) void paged_evict_move_kernel(PagedEvict
     }
     return;
   }
+  if (n <= e.budget && e.to_pages == e.t.pages) return;              // everything is where it belongs
   for (int pg = blockIdx.y * kEmPages; pg * kBlock < n_kept; pg += gridDim.y * kEmPages) {
     int page[kEmPages];
 #pragma unroll
@@ -203,7 +206,7 @@ __global__ __launch_bounds__(kEmThreads) void paged_evict_move_kernel(PagedEvict
     for (int i = tid; i < kEmPages * kBlock; i += kEmThreads) {
       const int t = pg * kBlock + i, pos = t < n_kept ? kept[t] : -1;
       const int at = pos >= 0 ? paged_page(e.t, s, pos / kBlock) : -1;
-      from[i] = at >= 0 ? at * kBlock + pos % kBlock : -1;
+      from[i] = at >= 0 ? at * kBlock + pos % kBlock : pos >= 0 ? kGone : kNone;
     }
     __syncthreads();
     if (role < kKeySlices) {
@@ -215,6 +218,7 @@ __global__ __launch_bounds__(kEmThreads) void paged_evict_move_kernel(PagedEvict
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
           const int src = from[g * kBlock + t0 + i * kTokens];
+          x[g][i] = raw_t{};
           if (src >= 0) x[g][i] = Vec<T>::load_raw(kc + ((size_t(src / kBlock) * e.n_kv_heads + hk) * kBlock + src % kBlock) * D + c);
         }
       __builtin_amdgcn_s_waitcnt(0);
@@ -224,7 +228,7 @@ __global__ __launch_bounds__(kEmThreads) void paged_evict_move_kernel(PagedEvict
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
           const int tk = t0 + i * kTokens;
-          if (page[g] >= 0 && from[g * kBlock + tk] >= 0)
+          if (page[g] >= 0 && from[g * kBlock + tk] != kNone)
             *reinterpret_cast<raw_t*>(kc + ((size_t(page[g]) * e.n_kv_heads + hk) * kBlock + tk) * D + c) = x[g][i];
         }
     } else {
@@ -236,7 +240,9 @@ __global__ __launch_bounds__(kEmThreads) void paged_evict_move_kernel(PagedEvict
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const int src = from[g * kBlock + tk + j];
-          const T* at = vc + ((size_t(src / kBlock) * e.n_kv_heads + hk) * D + d0) * kBlock + src % kBlock;
+          const T* at = vc + ((size_t(max(src, 0) / kBlock) * e.n_kv_heads + hk) * D + d0) * kBlock + max(src, 0) % kBlock;
+#pragma unroll
+          for (int i = 0; i < kEach; ++i) x[g][i][j] = T(0);
           if (src >= 0)
 #pragma unroll
             for (int i = 0; i < kEach; ++i) x[g][i][j] = at[i * kWaves * kBlock];
@@ -245,7 +251,7 @@ __global__ __launch_bounds__(kEmThreads) void paged_evict_move_kernel(PagedEvict
       __syncthreads();
 #pragma unroll
       for (int g = 0; g < kEmPages; ++g) {
-        const bool first = from[g * kBlock + tk] >= 0, second = from[g * kBlock + tk + 1] >= 0;
+        const bool first = from[g * kBlock + tk] != kNone, second = from[g * kBlock + tk + 1] != kNone;
         T* at = vc + ((size_t(max(page[g], 0)) * e.n_kv_heads + hk) * D + d0) * kBlock + tk;
         if (page[g] < 0) continue;
 #pragma unroll

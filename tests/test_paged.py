@@ -427,3 +427,52 @@ def test_smallest_and_largest_caps(shape, batch, softcap):
     b = Batch(shape_of(*SHAPES[shape]), BATCHES[batch], 67)
     b.q[::3] = 0
     run_attention(b, dict(softcap=softcap), weight_rows=2)
+
+
+@pytest.mark.parametrize("shape", ["llama", "fp32_64"])
+@pytest.mark.parametrize("in_place", [True, False])
+def test_evict_with_pages_of_nobody(shape, in_place):
+    """Kept tokens without a page move as zeros, never as what their new slots held; nothing is written where there is no
+    page to move to."""
+    sh = shape_of(*SHAPES[shape])
+    b = Batch(sh, [(0, 900), (0, 700), (0, 100), (0, 513)], 71, spare_pages=10, garbage=None)
+    b.pages[0, [0, 3]], b.pages[1, 1], b.pages[2, 0], b.pages[3, 4] = -1, b.n_pages, -(2 ** 31), 2 ** 31 - 1
+    budget = 290
+    w = torch.rand(4, sh.n_kv_heads, b.max_pages * BS, generator=torch.Generator().manual_seed(1))
+    r, t, wd = b.runner(), b.dev(), w.to(DEV)
+    kept = torch.zeros(4, sh.n_kv_heads, budget, dtype=torch.int32, device=DEV)
+    n_kept = torch.zeros(4, dtype=torch.int32, device=DEV)
+    args = (t["n_ctx"], t["pages"], t["k_pages"], t["v_pages"], wd, 3, 40, budget, kept, n_kept)
+    to, to_w = b.pages, wd
+    if in_place:
+        r.evict(*args)
+    else:
+        to = np.array([[b.free.pop(), b.free.pop(), b.free.pop()], [b.free.pop(), -1, b.free.pop()], [b.free.pop(), b.n_pages, -1],
+                       [-1, b.free.pop(), b.free.pop()]])
+        to_w = torch.full((4, sh.n_kv_heads, 3 * BS), 9.0, device=DEV)
+        r.evict(*args, to_pages=torch.tensor(to, dtype=torch.int32, device=DEV), to_weights=to_w)
+    torch.cuda.synchronize()
+    start = w.numpy() if in_place else np.full(to_w.shape, 9.0, np.float32)
+    k2, n2, k, v, ww = po.evict(b.n_ctx, b.pages, f64(b.k_pages), f64(b.v_pages), w.numpy(), 3, 40, budget, to, start)
+    assert np.array_equal(n_kept.cpu().numpy(), n2) and np.array_equal(kept.cpu().numpy(), k2)
+    assert np.array_equal(to_w.cpu().numpy(), ww)
+    assert np.array_equal(f64(t["k_pages"]), k) and np.array_equal(f64(t["v_pages"]), v)
+
+
+@pytest.mark.parametrize("n,keep", [(9000, 700), (33000, 1500), (40000, 39000)])
+@pytest.mark.parametrize("kind", ["random", "ties", "flat"])
+def test_evict_from_long_sequences(n, keep, kind):
+    """More candidates than a workgroup's registers hold at 8 and at 32 a thread."""
+    sh = shape_of(2, 1, 64, "bf16")
+    b = Batch(sh, [(0, n), (0, keep + 1)], 73, garbage=None)
+    w = torch.rand(2, 1, b.max_pages * BS, generator=torch.Generator().manual_seed(n))
+    w = {"random": w, "ties": (w * 20).floor(), "flat": torch.zeros_like(w)}[kind]
+    r, t, wd = b.runner(), b.dev(), w.to(DEV)
+    kept = torch.zeros(2, 1, keep, dtype=torch.int32, device=DEV)
+    n_kept = torch.zeros(2, dtype=torch.int32, device=DEV)
+    r.evict(t["n_ctx"], t["pages"], t["k_pages"], t["v_pages"], wd, 5, 60, keep, kept, n_kept)
+    torch.cuda.synchronize()
+    k2, n2, k, v, ww = po.evict(b.n_ctx, b.pages, f64(b.k_pages), f64(b.v_pages), w.numpy(), 5, 60, keep, b.pages, w.numpy())
+    assert np.array_equal(kept.cpu().numpy(), k2) and np.array_equal(n_kept.cpu().numpy(), n2)
+    assert np.array_equal(wd.cpu().numpy(), ww)
+    assert np.array_equal(f64(t["k_pages"]), k) and np.array_equal(f64(t["v_pages"]), v)
