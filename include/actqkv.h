@@ -542,19 +542,92 @@ int actqkv_copy_bytes(void* dst, const void* src, size_t bytes, void* stream);
  *     k_pages  [n_pages][Hk][Bs][D]     v_pages  [n_pages][Hk][D][Bs]
  *   pages    device int32 [batch][max_pages]: sequence s has its tokens [i*Bs, (i+1)*Bs) in page pages[s][i].  Entries outside
  *            [0, n_pages) stand for no page: nothing is written there and nobody sees its tokens.  Sequences may share
+ *            pages that are only read (a common prefix); a page that a call writes is one sequence's, once.
+ *   n_ctx    device int32 [batch]: tokens in the cache including the step's token.
+ *   nb_begin, nb_end, scores, score_stride  as in actqkv_score_blocks; scores of the eligible
+ *            blocks are written.  nb_end[s] must not reach the block of position n_ctx[s] - 1.
+ *   k_cap, flags (ACTQKV_SELECT_ENTROPY_TOPK, ACTQKV_DECODE_NO_WAIT), budget_in, theta_rest_sum,
+ *   budget_after, idx, n_sel, theta, budget  as in actqkv_decode_select_attention.
+ *   out, lse, workspace  as in actqkv_retrieval_attention with m = 1.
+ * Results: scores and selection as the two calls give them; the output up to the order of fp32
+ * sums. */
+int actqkv_decode_layer(const actqkv_shape* shape, int batch, const void* q, const void* k_new,
+                        const void* v_new, void* k_cache, void* v_cache, int64_t cache_seq_stride,
+                        void* rep_keys, int64_t rep_seq_stride, int nb_capacity, const int32_t* n_ctx,
+                        int nb_begin, const int32_t* nb_end, float* scores, int64_t score_stride, int k_cap,
+                        int flags, const float* budget_in, const float* theta_rest_sum, float* budget_after,
+                        int32_t* idx, int32_t* n_sel, float* theta, float* budget, void* out, float* lse,
+                        void* workspace, size_t ws_bytes, void* stream);
+
+/* Selected blocks from a block store into a working cache (Sec. 3.1: the cache may be kept
+ * in CPU memory).
+ *   k_store, v_store  the whole context in the blocked cache layouts,
+ *            [batch][nb_store][Hk][Bs][D] and [batch][nb_store][Hk][D][Bs]; any memory the
+ *            device can read in place: pinned host memory (hipHostMalloc) or device memory.
+ *            store_seq_stride = elements between two sequences.
+ *   idx, n_sel, k_cap  as written by actqkv_select (device memory).
+ *   k_cache, v_cache   device working cache of nb_capacity blocks; block idx[s][j], j < n_sel[s],
+ *            is copied to block slot0 + j (slot0 + k_cap <= nb_capacity).  The caller keeps the
+ *            initial tokens in the blocks before slot0 and the local span and the window in the
+ *            blocks from slot0 + k_cap on, i.e. at positions shifted by a multiple of Bs, and
+ *            passes n_ctx in those shifted positions to actqkv_retrieval_attention.
+ *   idx_slots [batch][k_cap] int32, device, may be NULL: slot0 + j for j < n_sel[s], else -1 -
+ *            the selection actqkv_retrieval_attention takes on the working cache.
+ * Entries of idx outside [0, nb_store) are skipped (their idx_slots entry is -1).
+ * Errors: EINVAL (null, slots outside the cache), ESHAPE, EALIGN. */
+int actqkv_gather_blocks(const actqkv_shape* shape, int batch, const void* k_store,
+                         const void* v_store, int64_t store_seq_stride, int nb_store,
+                         const int32_t* idx, const int32_t* n_sel, int k_cap, void* k_cache,
+                         void* v_cache, int64_t cache_seq_stride, int nb_capacity, int slot0,
+                         int32_t* idx_slots, void* stream);
+
+/*
+ * The same for a pass of many windows of one sequence whose slots outlive a window: the n_slots
+ * slots from slot0 on are a cache of the store, least recently used block first out.  A call
+ * serves a group of n_windows windows together (n_windows * k_cap <= 256).
+ *   idx, n_sel  [n_windows][k_cap], [n_windows], as written by actqkv_select (device memory)
+ *   n_slots     2 n_windows k_cap .. 512.  Slots that this group or the one before it uses are never
+ *               overwritten by the call, so the attention of the group before may still be running.
+ *   hereN_lo, hereN_hi, hereN_at  blocks [lo, hi) of the sequence lie in the working cache itself from block
+ *               `at` on, outside the slots, and are copied from there (hi <= lo: none do)
+ *   group       number of the call in the pass: 0, 1, 2, ...
+ *   state       device int32 [nb_store + 2 n_slots + 513]: every entry -2 before group 0, then left alone
+ *   idx_slots   out, [n_windows][k_cap]: the blocks' places in the working cache (-1: none), the selection
+ *               to hand to the attention
+ */
+int actqkv_gather_blocks_cached(const actqkv_shape* shape, int n_windows, const void* k_store, const void* v_store,
+                                int nb_store, const int32_t* idx, const int32_t* n_sel, int k_cap, void* k_cache,
+                                void* v_cache, int nb_capacity, int slot0, int n_slots, int here0_lo, int here0_hi,
+                                int here0_at, int here1_lo, int here1_hi, int here1_at, int group, int32_t* state,
+                                int32_t* idx_slots, void* stream);
+
+/* A plain copy of `bytes` bytes (a multiple of 16; both pointers memory the device can access -
+ * device memory or pinned host memory -, 16-byte aligned, not overlapping) done by one kernel
+ * with 16-byte loads and stores.  Not a step of the method: between device buffers it reads and
+ * writes exactly `bytes` bytes of HBM, which calibrates the hardware traffic counters against a
+ * known size; with the cache kept in host memory (see actqkv_gather_blocks) it carries the local
+ * span from one working cache to the next and new blocks back to the host store. */
+int actqkv_copy_bytes(void* dst, const void* src, size_t bytes, void* stream);
+
+/* ---- Paged cache: blocks of a pool, handed out to sequences page by page ------------------------------------------------
+ *
+ * A page is a block of the blocked cache (layouts above), anywhere in a pool:
+ *     k_pages  [n_pages][Hk][Bs][D]     v_pages  [n_pages][Hk][D][Bs]
+ *   pages    device int32 [batch][max_pages]: sequence s has its tokens [i*Bs, (i+1)*Bs) in page pages[s][i].  Entries outside
+ *            [0, n_pages) stand for no page: nothing is written there and nobody sees its tokens.  Sequences may share
  *            pages that are only read (a common prefix).
  *   n_ctx    device int32 [batch]: tokens of the sequence, the call's new ones included (clamped to max_pages * Bs).
  *   row_start  device int32 [batch + 1], not decreasing: sequence s brings the rows row_start[s] .. row_start[s+1] - 1 of q,
  *            k_new, v_new, out and lse (none, one or many), its last tokens: row row_start[s] + i of m rows is at
  *            position n_ctx[s] - m + i.  Rows that belong to no sequence are not read and their results not written; a row
  *            at a negative position (m > n_ctx) is not in the cache and sees nothing.
- *   n_rows   rows of the arrays (1 .. 2^22); max_new  the most rows a sequence brings (1 .. n_rows; of more, the first
- *            max_new are taken as all of them).
+ *   n_rows   rows of the arrays (1 .. 2^22; of attention, n_rows * H at most 2^28); max_new  the most rows a sequence
+ *            brings (1 .. n_rows; of more, the first max_new are taken as all of them).
  * Of the shape, n_q_heads, n_kv_heads, head_dim, block_size, dtype and softmax_scale are used.  Slots behind a sequence's last
- * token may hold anything, NaN and infinities included; its own keys and values must be finite,
- * and so must, in fp32, 256 times the sum of the absolute values of a channel over the tokens that a row sees (it is taken before it is divided
- * by that of the exponentials).  What lies on the device is
- * clamped, never trusted: a wrong value gives a wrong result but no out-of-bounds access. */
+ * token may hold anything, NaN and infinities included; its own keys and values, queries and slopes must be finite, and so must in
+ * fp32 be a score and 256 times the sum of the absolute values of a channel over the tokens that a row sees (it is taken before it is
+ * divided by that of the exponentials).  What lies on the device is clamped, never trusted: a wrong value gives a wrong result but
+ * no out-of-bounds access. */
 
 /* Bytes of workspace of the paged calls that take one, for calls of at most batch sequences, n_rows rows, max_new rows of a
  * sequence and max_pages pages.  As for the other calls: zero-filled once, and calls that share one ordered on one stream (a graph
@@ -591,7 +664,7 @@ int actqkv_paged_attention(const actqkv_shape* shape, int batch, int n_rows, int
  *   weights_out[s][hk][j] = weights_in[s][hk][j] + sum of exp(score - lse) over the last weight_rows (>= 1; at least the
  *            sequence's rows: all of them) rows of sequence s and the G query heads of KV head hk, for the tokens j they see.
  *   weights_in, weights_out  [batch][Hk][weight_stride] fp32, weight_stride >= max_pages * Bs and a multiple of 4; may be the
- *            same array.  The first max_pages * Bs entries of a row are written.  Fill them with zero when a sequence begins.
+ *            same array.  max_pages * Hk is at most 2^22.  The first max_pages * Bs entries of a row are written.  Fill them with zero when a sequence begins.
  *   lse      required.
  * The sums are taken in an order that depends on the sizes alone: the same call gives the same bits. */
 int actqkv_paged_attention_weights(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q,

@@ -63,6 +63,11 @@ static int attention_call(const char* name, const actqkv_shape* shape, int batch
                           const PagedWeights* weights, void* workspace, size_t ws_bytes, void* stream) {
   ACTQKV_TRY(check_table(shape, batch, n_ctx, pages, max_pages, k_pages, v_pages, n_pages));
   ACTQKV_TRY(check_rows(n_rows, max_new));
+  // (a launch has less than 2^32 threads: 512 for 64 (row, query head) pairs or, of the account, 128 tokens of a KV head)
+  if (int64_t(n_rows) * shape->n_q_heads > 1 << 28)
+    return set_error(ACTQKV_ESHAPE, "%d rows of %d query heads > 2^28", n_rows, shape->n_q_heads);
+  if (weights != nullptr && int64_t(max_pages) * shape->n_kv_heads > 1 << 22)
+    return set_error(ACTQKV_ESHAPE, "weights of %d pages of %d KV heads > 2^22", max_pages, shape->n_kv_heads);
   ACTQKV_REQUIRE_PTR(q);
   ACTQKV_REQUIRE_SMALL(row_start, 4);
   ACTQKV_REQUIRE_PTR(out);

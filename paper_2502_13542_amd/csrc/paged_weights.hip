@@ -69,7 +69,7 @@ __device__ __forceinline__ void votes_body(const PagedVotes& c) {
 
   // ---- the rows that vote, of those the ones that can see a key of this tile at all
   int i0 = max(seq.m - c.w.rows, 0), i1 = seq.m;
-  if (p.f.row_end == nullptr) i0 = max(i0, key0 - w0);             // row i sees positions up to w0 + i
+  if (p.f.row_end == nullptr) i0 = min(max(i0, key0 - w0), seq.m);   // row i sees positions up to w0 + i
   if (p.f.window > 0) i1 = int(min(int64_t(i1), int64_t(key0) + S::kKeys - 1 + p.f.window - w0));
   if (key0 >= seq.n) i1 = i0;
   const int f0 = i0 * group, f1 = max(i1, i0) * group;

@@ -910,7 +910,8 @@ class PagedRunner:
 
     batch, n_rows, max_new and max_pages are the most that a call brings: sequences, rows of all of them, rows of one,
     pages of one.  A call's own numbers follow from its tensors: row_start [batch + 1], n_ctx [batch], pages [batch][max_pages];
-    the library's header says what they hold."""
+    the library's header says what they hold.  What no tensor says is the most rows that a sequence of this call brings: a call
+    that knows it (1 in a decode step) says so in max_new and takes the kernels for it."""
 
     def __init__(self, shape: LayerShape, batch: int, n_rows: int, max_new: int, max_pages: int, device="cuda"):
         self.shape, self.batch, self.n_rows, self.max_new, self.max_pages = shape, batch, n_rows, max_new, max_pages
@@ -930,8 +931,11 @@ class PagedRunner:
             raise B.ActQKVError(-1, "k_pages and v_pages are not pools of pages of this shape")
         return batch, max_pages, n_pages
 
-    def _rows(self, batch: int, row_start, rows, heads: int, *same) -> Tuple[int, int]:
+    def _rows(self, batch: int, row_start, rows, heads: int, max_new, *same) -> Tuple[int, int]:
         n_rows = rows.shape[0]
+        max_new = self.max_new if max_new is None else max_new
+        if not 1 <= max_new <= self.max_new:
+            raise B.ActQKVError(-1, f"max_new {max_new}: made for {self.max_new}")
         if row_start.numel() != batch + 1:
             raise B.ActQKVError(-1, f"row_start has {row_start.numel()} entries for {batch} sequences")
         if n_rows > self.n_rows:
@@ -939,27 +943,27 @@ class PagedRunner:
         for t in (rows, *same):
             if t.numel() != n_rows * heads * self.shape.head_dim:
                 raise B.ActQKVError(-1, f"tensor of {t.numel()} elements, expected {n_rows} rows of {heads} heads")
-        return n_rows, min(self.max_new, n_rows)
+        return n_rows, min(max_new, n_rows)
 
     def _per_row(self, n: int, *tensors) -> None:
         for t in tensors:
             if t is not None and t.numel() != n:
                 raise B.ActQKVError(-1, f"tensor of {t.numel()} elements, expected {n}")
 
-    def append(self, k_new, v_new, row_start, n_ctx, pages, k_pages, v_pages, stream=None) -> None:
+    def append(self, k_new, v_new, row_start, n_ctx, pages, k_pages, v_pages, stream=None, max_new=None) -> None:
         """Keys and values [n_rows][Hk][D] of the new tokens into their pages."""
         batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, v_pages)
-        n_rows, max_new = self._rows(batch, row_start, k_new, self.shape.n_kv_heads, v_new)
+        n_rows, max_new = self._rows(batch, row_start, k_new, self.shape.n_kv_heads, max_new, v_new)
         if n_rows == 0:
             return
         B.paged_append(self.cs, batch, n_rows, max_new, k_new, v_new, row_start, n_ctx, pages, max_pages, k_pages, v_pages,
                        n_pages, stream)
 
     def attend(self, q, row_start, n_ctx, pages, k_pages, v_pages, out, lse=None, softcap: float = 0.0, window: int = 0,
-               slopes=None, row_first=None, row_end=None, stream=None) -> None:
+               slopes=None, row_first=None, row_end=None, stream=None, max_new=None) -> None:
         """out [n_rows][H][D], and lse [n_rows][H], of the new tokens' queries over the cache."""
         batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, v_pages)
-        n_rows, max_new = self._rows(batch, row_start, q, self.shape.n_q_heads, out)
+        n_rows, max_new = self._rows(batch, row_start, q, self.shape.n_q_heads, max_new, out)
         self._per_row(n_rows, row_first, row_end)
         self._per_row(n_rows * self.shape.n_q_heads, lse)
         self._per_row(self.shape.n_q_heads, slopes)
@@ -969,11 +973,11 @@ class PagedRunner:
                           out, lse, self.workspace, softcap, window, slopes, row_first, row_end, stream)
 
     def attend_weigh(self, q, row_start, n_ctx, pages, k_pages, v_pages, out, lse, weight_rows: int, weights, weights_out=None,
-                     softcap: float = 0.0, window: int = 0, slopes=None, row_first=None, row_end=None, stream=None) -> None:
+                     softcap: float = 0.0, window: int = 0, slopes=None, row_first=None, row_end=None, stream=None, max_new=None) -> None:
         """attend, and what the last weight_rows rows of every sequence give each cached token added to weights
         [batch][Hk][max_pages * Bs] (weights_out None: in place)."""
         batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, v_pages)
-        n_rows, max_new = self._rows(batch, row_start, q, self.shape.n_q_heads, out)
+        n_rows, max_new = self._rows(batch, row_start, q, self.shape.n_q_heads, max_new, out)
         weights_out = weights if weights_out is None else weights_out
         self._per_row(n_rows, row_first, row_end)
         self._per_row(n_rows * self.shape.n_q_heads, lse)

@@ -218,3 +218,11 @@ def test_caps_out_of_range_are_refused(lib, softcap):
     """A cap whose reciprocal overflows, or that is so large that a capped score may be below a hidden one's mark."""
     assert _attend(lib, B.c_shape(LLAMA), softcap=softcap) == -1 and "softcap" in B.last_error()
     assert _weigh(lib, B.c_shape(LLAMA), softcap=softcap) == -1
+
+
+def test_calls_of_more_threads_than_a_launch_has_are_refused(lib):
+    wide = B.c_shape(shape_of(256, 256, 64, "bf16"))
+    big = dict(n_rows=(1 << 20) + 1, max_new=1, wsb=1 << 60)
+    assert _attend(lib, wide, **big) == -2 and "2^28" in B.last_error()
+    assert _weigh(lib, wide, **big) == -2
+    assert _weigh(lib, B.c_shape(LLAMA), max_pages=(1 << 19) + 1, stride=1 << 40, wsb=1 << 60) == -2 and "2^22" in B.last_error()
