@@ -42,6 +42,7 @@ FORMS = {
     "window1": dict(window=1),
     "first": dict(first=True),
     "end": dict(end=True),
+    "cap_slopes_end": dict(softcap=8.0, slopes=True, end=True),
     "all": dict(softcap=30.0, slopes=True, window=300, first=True, end=True),
 }
 
@@ -476,3 +477,116 @@ def test_evict_from_long_sequences(n, keep, kind):
     assert np.array_equal(kept.cpu().numpy(), k2) and np.array_equal(n_kept.cpu().numpy(), n2)
     assert np.array_equal(wd.cpu().numpy(), ww)
     assert np.array_equal(f64(t["k_pages"]), k) and np.array_equal(f64(t["v_pages"]), v)
+
+
+# Calls that chunks in bf16 are cut up for in other ways: query heads, KV heads, head size, rows and tokens of the sequences, entries
+# of the table behind the longest one's (the cut goes by the table's width)
+CUTS = [(64, 32, 64, [(100, 120), (99, 99), (1, 3), (100, 130), (70, 70), (100, 100)], 0),      # 256 rows a workgroup
+        (64, 32, 128, [(100, 120), (99, 99), (1, 3), (100, 130), (70, 70), (100, 100)], 0),
+        (64, 8, 64, [(200, 300), (180, 181), (200, 200)], 0),                                   # 128 rows
+        (64, 8, 128, [(200, 300), (180, 181), (200, 200)], 0),
+        (16, 2, 128, [(690, 800)], 22),                                                         # 256 rows, pages in pieces
+        (32, 8, 64, [(166, 500)], 32),
+        (16, 4, 128, [(338, 700)], 5),                                                          # 128 rows, pages in pieces
+        (32, 8, 64, [(81, 400), (80, 160)], 8)]
+
+
+@pytest.mark.parametrize("case", range(len(CUTS)))
+@pytest.mark.parametrize("kind", ["plain", "cap", "cap_slopes_end"])
+def test_attention_in_every_cut(case, kind):
+    hq, hkv, d, seqs, more = CUTS[case]
+    run_attention(Batch(shape_of(hq, hkv, d, "bf16"), seqs, 79, extra_entries=more), kind, 7, weight_rows=50)
+
+
+@pytest.mark.parametrize("shape", ["llama", "g8_64", "fp32_64"])
+@pytest.mark.parametrize("kind", ["plain", "all"])
+def test_steps_and_chunks_of_a_wide_table(shape, kind):
+    """So many pages for sequences of few rows that those take a launch of their own, beside the chunks'."""
+    b = Batch(shape_of(*SHAPES[shape]), [(1, 300), (60, 200), (2, 2), (0, 70), (1, 129), (16, 16), (1, 1), (2, 500)], 83,
+              extra_rows=(1, 2), extra_entries=60 if shape == "llama" else 450)
+    run_attention(b, kind, 9, weight_rows=4)
+
+
+@pytest.mark.parametrize("shape", ["mha64", "fp32_64"])
+def test_more_sequences_than_lanes(shape):
+    rng = np.random.default_rng(5)
+    seqs = [(int(min(m, n)), int(n)) for m, n in zip(rng.integers(0, 30, 150), rng.integers(0, 140, 150))]
+    b = Batch(shape_of(*SHAPES[shape]), seqs, 89, extra_entries=0)
+    run_attention(b, weight_rows=3)
+    r, t = b.runner(), b.dev()
+    r.append(b.k_new.to(DEV), b.v_new.to(DEV), t["row_start"], t["n_ctx"], t["pages"], t["k_pages"], t["v_pages"])
+    torch.cuda.synchronize()
+    k, v = po.append(f64(b.k_new), f64(b.v_new), b.row_start, b.n_ctx, b.pages, *(np.nan_to_num(f64(x)) for x in (b.k_pages, b.v_pages)))
+    assert np.array_equal(np.nan_to_num(f64(t["k_pages"])), k) and np.array_equal(np.nan_to_num(f64(t["v_pages"])), v)
+
+
+@pytest.mark.parametrize("shape", ["llama", "fp32_g3"])
+@pytest.mark.parametrize("seqs", [[(1, 300), (2, 140)], [(150, 300), (3, 140)]])
+def test_pages_past_32_bits(shape, seqs):
+    """A pool of more than 2^32 bytes, and of more than 2^31 elements: the same bits as from a small one."""
+    sh = shape_of(*SHAPES[shape])
+    b = Batch(sh, seqs, 97, garbage=None)
+    r, t = b.runner(), b.dev()
+    page = sh.n_kv_heads * BS * sh.head_dim
+    n_far = 2 ** 31 // page + 40
+    move = torch.tensor([n_far - 1 - 7 * i for i in range(b.n_pages)], device=DEV)     # the last pages of the pool
+    far = dict(t, pages=torch.where(t["pages"] >= 0, move[t["pages"].clamp(min=0).long()].int(), -1).contiguous())
+    for name in ("k_pages", "v_pages"):
+        pool = torch.empty(n_far, *t[name].shape[1:], dtype=t[name].dtype, device=DEV)
+        pool[move] = t[name]
+        far[name] = pool
+    kn, vn, q = b.k_new.to(DEV), b.v_new.to(DEV), b.q.to(DEV)
+    got = []
+    for x in (t, far):
+        table = (x["row_start"], x["n_ctx"], x["pages"], x["k_pages"], x["v_pages"])
+        out, lse = torch.zeros_like(q), torch.zeros(b.n_rows, sh.n_q_heads, device=DEV)
+        w = torch.zeros(b.batch, sh.n_kv_heads, b.max_pages * BS, device=DEV)
+        kept, n_kept = torch.zeros(b.batch, sh.n_kv_heads, 130, dtype=torch.int32, device=DEV), torch.zeros(b.batch, dtype=torch.int32, device=DEV)
+        r.append(kn, vn, *table)
+        r.attend_weigh(q, *table, out, lse, 2, w)
+        r.evict(*table[1:], w, 1, 20, 130, kept, n_kept)
+        torch.cuda.synchronize()
+        got.append((out, lse, w, kept, *((x["k_pages"], x["v_pages"]) if x is t else (x["k_pages"][move], x["v_pages"][move]))))
+    assert all(torch.equal(a, c) for a, c in zip(*got))
+
+
+@pytest.mark.parametrize("shape", ["llama", "fp32_64"])
+def test_two_calls_at_once(shape):
+    """Two runners on two streams over one cache: neither disturbs the other."""
+    sh = shape_of(*SHAPES[shape])
+    calls = [Batch(sh, [(1, 900), (1, 40)], 101), Batch(sh, [(120, 900), (1, 40)], 103)]
+    streams = [torch.cuda.Stream() for _ in calls]
+    prepared = []
+    for b in calls:
+        t, q = b.dev(), b.q.to(DEV)
+        args = (q, t["row_start"], t["n_ctx"], t["pages"], t["k_pages"], t["v_pages"])
+        outs = [torch.zeros_like(q) for _ in range(9)]
+        r = b.runner()
+        r.attend(*args, outs[0])
+        prepared.append((r, args, outs))
+    torch.cuda.synchronize()
+    for i in range(1, 9):
+        for (r, args, outs), stream in zip(prepared, streams):
+            r.attend(*args, outs[i], stream=stream)
+    torch.cuda.synchronize()
+    for _, _, outs in prepared:
+        assert all(torch.equal(o, outs[0]) for o in outs[1:])
+
+
+def test_a_call_that_says_how_many_rows_it_brings():
+    """Decode steps through a runner made for prompts: the kernels for few rows, their results within the same bounds."""
+    sh = shape_of(*SHAPES["llama"])
+    b = Batch(sh, [(1, 300), (1, 129), (1, 1)], 107)
+    from paper_2502_13542_amd import harness as H
+    made_for = H.PagedRunner(sh, 3, 500, 400, b.max_pages)
+    t, q = b.dev(), b.q.to(DEV)
+    args = (q, t["row_start"], t["n_ctx"], t["pages"], t["k_pages"], t["v_pages"])
+    got = []
+    for r, kw in ((b.runner(), {}), (made_for, dict(max_new=1))):
+        out, lse = torch.zeros_like(q), torch.zeros(3, sh.n_q_heads, device=DEV)
+        w = torch.zeros(3, sh.n_kv_heads, b.max_pages * BS, device=DEV)
+        r.attend_weigh(*args, out, lse, 1, w, **kw)
+        torch.cuda.synchronize()
+        got.append((out, lse, w))
+    assert all(torch.equal(a, c) for a, c in zip(*got))
+    run_attention(b, runner=made_for)

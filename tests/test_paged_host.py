@@ -226,3 +226,16 @@ def test_calls_of_more_threads_than_a_launch_has_are_refused(lib):
     assert _attend(lib, wide, **big) == -2 and "2^28" in B.last_error()
     assert _weigh(lib, wide, **big) == -2
     assert _weigh(lib, B.c_shape(LLAMA), max_pages=(1 << 19) + 1, stride=1 << 40, wsb=1 << 60) == -2 and "2^22" in B.last_error()
+
+
+@pytest.mark.parametrize("max_new", [0, -1, 4])
+def test_the_runner_checks_the_rows_a_call_says_it_brings(max_new):
+    b = Batch(shape_of(4, 2, 64, "fp32"), [(2, 40), (3, 200)], 3)
+    r, t = b.runner("cpu"), b.dev("cpu")
+    out, lse, w = torch.zeros_like(b.q), torch.zeros(5, 4), torch.zeros(2, 2, b.max_pages * BS)
+    with pytest.raises(B.ActQKVError, match="max_new"):
+        r.append(b.k_new, b.v_new, **t, max_new=max_new)
+    with pytest.raises(B.ActQKVError, match="max_new"):
+        r.attend(b.q, **t, out=out, max_new=max_new)
+    with pytest.raises(B.ActQKVError, match="max_new"):
+        r.attend_weigh(b.q, **t, out=out, lse=lse, weight_rows=1, weights=w, max_new=max_new)
