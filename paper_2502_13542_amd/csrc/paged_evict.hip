@@ -27,9 +27,14 @@ __device__ __forceinline__ uint32_t evict_key(float w) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
+// base + the lanes of `lanes` before this one.
+__device__ __forceinline__ uint32_t lanes_below(unsigned long long lanes, uint32_t base) {
+  return __builtin_amdgcn_mbcnt_hi(uint32_t(lanes >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(lanes), base));
+}
+
 struct EvictLds {
   uint32_t hist[kEvBins];
-  uint32_t wave_sum[kEvWaves], found[2];
+  uint32_t wave_sum[kEvWaves], found[3];
   uint32_t above[kEvWaves], equal[kEvWaves];
 };
 // The `need` largest of w[lo .. hi), hi - lo > need > 0, to kept[at ..] in order.  A wavefront has kHold * 64 of them in registers, or (kHold
@@ -94,11 +99,17 @@ __device__ __forceinline__ void evict_largest(const float* w, int lo, int hi, ui
       const bool second = before + h0 < need;
       l.found[0] = second ? top - 1 : top;
       l.found[1] = second ? before + h0 : before;
+      l.found[2] = second ? h1 : h0;
     }
     __syncthreads();
     prefix |= l.found[0] << shift;
     mask |= ((1u << bits) - 1u) << shift;
     need -= l.found[1];
+    if (need == l.found[2] && prefix != 0) {                        // the whole bin stays: its last need not be known (the lowest bin also counts lanes without a weight)
+      prefix -= 1;
+      need = 0;
+      break;
+    }
     __syncthreads();
   }
   // ---- positions in order: all above the key, and the first `need` at it
@@ -117,13 +128,17 @@ __device__ __forceinline__ void evict_largest(const float* w, int lo, int hi, ui
     n_above += l.above[i];
     n_equal += l.equal[i];
   }
-  const unsigned long long before = (1ull << lane) - 1;
   each([&](uint32_t key, int i) {
     const unsigned long long a = __ballot(key > prefix), q = __ballot(key == prefix);
-    const uint32_t my_above = n_above + __popcll(a & before), my_equal = n_equal + __popcll(q & before);
-    if (key > prefix || (key == prefix && my_equal < need)) kept[my_above + min(my_equal, need)] = i;
+    const uint32_t my_above = lanes_below(a, n_above);
+    if (q == 0) {                                                    // nearly always
+      if (key > prefix) kept[my_above + min(n_equal, need)] = i;
+    } else {
+      const uint32_t my_equal = lanes_below(q, n_equal);
+      if (key > prefix || (key == prefix && my_equal < need)) kept[my_above + min(my_equal, need)] = i;
+      n_equal += __popcll(q);
+    }
     n_above += __popcll(a);
-    n_equal += __popcll(q);
   });
 }
 
