@@ -16,7 +16,7 @@ namespace actqkv {
 
 constexpr int kP4Threads = 256, kP4Waves = 4, kP4Rows = 32 * kP4Waves;
 constexpr int kP4Part = 8192;                     // one of the three parts of K or V^T of a tile
-constexpr int kP4MaxSplits = 16, kP4Slots = 512;  // pieces of a query tile; workgroups that fill the chip
+constexpr int kP4MaxSplits = 32, kP4Slots = 512;  // pieces of a query tile; workgroups that fill the chip
 
 struct PagedChunkF32 {
   PagedAttn a;
@@ -385,13 +385,35 @@ static int chunk_f32_tiles(const actqkv_shape& sh, int batch, int n_rows, int ma
   const int64_t group = sh.n_q_heads / sh.n_kv_heads, seqs = std::min(batch, n_rows);
   return int(std::min(seqs * ((int64_t(max_new) * group + kP4Rows - 1) / kP4Rows), int64_t(n_rows) * group / kP4Rows + seqs));
 }
-static int chunk_f32_splits(const actqkv_shape& sh, int tiles, int max_pages) {
+// Pieces of a query tile's keys, by these figures, in us: a tile of keys 2.9 (128 channels 3.8), 1.9 times that where two workgroups
+// share a compute unit (of the first rows of a prompt few pieces have keys, and of several sequences some are short); a launch
+// to merge 4, and 0.4 a piece.  8 query and 2 KV heads of 64, us with so many pieces: 2 x 2048 rows at 8192 tokens 1 398, 2 361; 2048
+// at 2048 2 63, 4 46; 2 x 512 at 4096 4 68, 8 63; 4 x 33 at 2000 16 20, 32 23; 128 at 16384 16 63, 32 46, 64 52.
+static int chunk_f32_splits(const actqkv_shape& sh, const PagedAttn& p, int tiles) {
   const int64_t items = int64_t(tiles) * sh.n_kv_heads;
-  return int(std::max<int64_t>(1, std::min({kP4Slots / items, int64_t(kP4MaxSplits), int64_t(max_pages)})));
+  const int keys = 4096 / sh.head_dim;
+  const double tile_us = sh.head_dim == 64 ? 2.9 : 3.8;
+  int64_t longest = int64_t(p.t.max_pages) * (kBlock / keys);
+  if (p.f.window > 0) longest = std::min<int64_t>(longest, (int64_t(p.f.window) + kP4Rows) / keys + 2);
+  if (p.f.row_first != nullptr) longest = (longest + 2) / 3;      // (of documents a part, nobody knows which)
+  const double own = double(p.t.max_new) / keys, average = double(longest) - std::min<double>(own, double(longest)) / 2.;
+  int best = 1;
+  double least = 0.;
+  for (int splits = 1; splits <= std::min<int64_t>(kP4MaxSplits, longest) && (splits == 1 || items * splits <= kP4Slots); ++splits) {
+    const double busy = double(items) * splits * average / double(longest) / kChipCus * (p.t.batch > 1 ? 0.8 : 1.);
+    double us = double((longest + splits - 1) / splits) * tile_us * (1. + 0.9 * std::min(std::max(busy - 1., 0.), 1.));
+    if (splits > 1) us += 4. + 0.4 * splits;
+    if (splits == 1 || us < least) {
+      least = us;
+      best = splits;
+    }
+  }
+  return best;
 }
 size_t paged_chunk_f32_scratch_most(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages) {
   if (sh.dtype != ACTQKV_F32) return 0;
-  const int64_t pieces = std::min<int64_t>(kP4MaxSplits, max_pages) * sh.n_kv_heads * chunk_f32_tiles(sh, batch, n_rows, max_new);
+  const int64_t pieces = std::min<int64_t>(kP4MaxSplits, int64_t(max_pages) * (kBlock / (4096 / sh.head_dim))) * sh.n_kv_heads *
+                         chunk_f32_tiles(sh, batch, n_rows, max_new);
   return size_t(std::min<int64_t>(kP4Slots, pieces)) * (sh.head_dim == 64 ? ChunkPieceF32<64>::bytes() : ChunkPieceF32<128>::bytes());
 }
 
@@ -411,7 +433,7 @@ int launch_paged_chunk_f32(const actqkv_shape& sh, const PagedAttn& p, const Wor
   PagedChunkF32 c;
   c.a = p;
   c.tiles = chunk_f32_tiles(sh, p.t.batch, p.t.n_rows, p.t.max_new);
-  c.splits = chunk_f32_splits(sh, c.tiles, p.t.max_pages);
+  c.splits = chunk_f32_splits(sh, p, c.tiles);
   c.part = ws.scratch_f32();
   if (sh.head_dim == 64) launch_chunk_f32<64>(c, stream);
   else launch_chunk_f32<128>(c, stream);
