@@ -164,15 +164,15 @@ __global__ __launch_bounds__(kEvThreads) void paged_evict_select_kernel(PagedEvi
 }
 
 constexpr int kEmThreads = 256;
-constexpr int kEmPages = 4;                       // new pages of a step
 constexpr int kEmUnits = 8;                       // 16-byte pieces of a key that a workgroup moves
 constexpr int kEmRows = 16;                       // channels of the values that a workgroup moves
 
 // Roles: slices of the keys, slices of the values, the weights.  A step is four pages: 64 KB of keys or half of that
-// of values are in flight in a workgroup, which is what it takes (one page of 8 KB a step: 8 sequences to 4096 of up to 32K tokens 160 us).
+// of values are in flight in a workgroup, which is what a full chip takes (with one page a step 8 sequences to 4096 of up to 32K tokens
+// take 160 us instead of 150).
 // Values: a thread has two neighbouring slots and reads their values one by one, two bytes each; neighbouring lanes' lie in the same
 // few lines, and of a line that holds one kept token all is read.
-template <typename T, int D>
+template <typename T, int D, int kEmPages>
 __global__ __launch_bounds__(kEmThreads) void paged_evict_move_kernel(PagedEvict e) {
   constexpr int V = Vec<T>::N, kKeySlices = D / V / kEmUnits, kValueSlices = D / kEmRows;
   typedef typename Vec<T>::raw raw_t;
@@ -290,17 +290,21 @@ __global__ __launch_bounds__(kEmThreads) void paged_evict_move_kernel(PagedEvict
 
 int launch_paged_evict(const actqkv_shape& sh, const PagedEvict& e, hipStream_t stream) {
   hipLaunchKernelGGL(paged_evict_select_kernel, dim3(sh.n_kv_heads, e.t.batch), dim3(kEvThreads), 0, stream, e);
-  const bool in_place = e.to_pages == e.t.pages;
-  const int groups = in_place ? 1 : std::min((e.budget + kEmPages * kBlock - 1) / (kEmPages * kBlock), 1024);
   const int v = sh.dtype == ACTQKV_F32 ? 4 : 8;
-  const dim3 grid(unsigned(sh.head_dim / v / kEmUnits + sh.head_dim / kEmRows + 1) * e.t.batch * sh.n_kv_heads, groups);
-  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kEmThreads), 0, stream, e); };
+  const unsigned slices = unsigned(sh.head_dim / v / kEmUnits + sh.head_dim / kEmRows + 1) * e.t.batch * sh.n_kv_heads;
+  const int pages = (e.budget + kBlock - 1) / kBlock;
+  const bool in_place = e.to_pages == e.t.pages;
+  // new pages of a step: four, or one where that leaves compute units idle (in place a workgroup walks all of them): 8K tokens of 2
+  // KV heads of 64 in fp32 to 1000, selection included, 16.2 | 13.7 us; 4 sequences 18.4 | 15.7, 16 of 4K 23.0 | 20.8
+  const bool single = !in_place && int64_t(slices) * ((pages + 3) / 4) < 2 * kChipCus;
+  const dim3 grid(slices, in_place ? 1 : std::min(single ? pages : (pages + 3) / 4, 1024));
+  auto launch = [&](auto one, auto four) { hipLaunchKernelGGL(single ? one : four, grid, dim3(kEmThreads), 0, stream, e); };
   if (sh.dtype == ACTQKV_F32) {
-    if (sh.head_dim == 64) launch(paged_evict_move_kernel<float, 64>);
-    else launch(paged_evict_move_kernel<float, 128>);
+    if (sh.head_dim == 64) launch(paged_evict_move_kernel<float, 64, 1>, paged_evict_move_kernel<float, 64, 4>);
+    else launch(paged_evict_move_kernel<float, 128, 1>, paged_evict_move_kernel<float, 128, 4>);
   } else {
-    if (sh.head_dim == 64) launch(paged_evict_move_kernel<uint16_t, 64>);
-    else launch(paged_evict_move_kernel<uint16_t, 128>);
+    if (sh.head_dim == 64) launch(paged_evict_move_kernel<uint16_t, 64, 1>, paged_evict_move_kernel<uint16_t, 64, 4>);
+    else launch(paged_evict_move_kernel<uint16_t, 128, 1>, paged_evict_move_kernel<uint16_t, 128, 4>);
   }
   return hip_status("paged evict");
 }
