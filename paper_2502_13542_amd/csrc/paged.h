@@ -136,6 +136,20 @@ __device__ __forceinline__ CapForm cap_form(float in, float out) {
   const float b = in * out, k = in * in;
   return CapForm{b, -0.333330558f * b * k, 0.133146743f * b * k * k, -0.0503546844f * b * k * k * k};
 }
+// The same with a term less, up to 0.2 (1.3e-7 of it): for bf16 storage, where it is an instruction a score in a loop that vector
+// instructions bound.
+constexpr float kTanhShort = 0.2f;
+struct CapShort {
+  float b0, b1, b2;
+  __device__ __forceinline__ float factor(float x) const {
+    const float u = x * x;
+    return fmaf(u, fmaf(u, b2, b1), b0);
+  }
+};
+__device__ __forceinline__ CapShort cap_short(float in, float out) {
+  const float b = in * out, k = in * in;
+  return CapShort{b, -0.33329646f * b * k, 0.1303653f * b * k * k};
+}
 __device__ __forceinline__ float paged_tanh(float x, float scale) {
   const float e = __builtin_amdgcn_exp2f(fabsf(x) * (2.f * kLog2e));
   const float large = copysignf(fmaf(-2.f, __builtin_amdgcn_rcpf(e + 1.f), 1.f), x) * scale;
@@ -152,19 +166,19 @@ __device__ __forceinline__ float paged_score(const PagedForm& f, float product, 
 // Whether the arguments in * x of a lane's registers, of all lanes, are in the polynomial's range: most of the time, and then a
 // cap is 5 instructions a score, otherwise 17.  (in^6 has to be a number, too: under a cap of thousands, or of millionths, none is small.)
 template <int N>
-__device__ __forceinline__ bool cap_is_small(const f32x16 (&x)[N], float in) {
+__device__ __forceinline__ bool cap_is_small(const f32x16 (&x)[N], float in, float most) {
   float mx = 0.f;
 #pragma unroll
   for (int g = 0; g < N; ++g)
 #pragma unroll
     for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(fabsf(x[g][i]), fabsf(x[g][i + 1])), mx);
-  return in >= 1e-5f && in <= 1e5f && __all(mx * in <= kTanhSmall);
+  return in >= 1e-5f && in <= 1e5f && __all(mx * in <= most);
 }
 // Their scores.  `ahead`: the query's position less that of the key that off(g, i) = 0 would be of.
 template <bool kCap, bool kBias, int N, typename Off>
 __device__ __forceinline__ void paged_scores(const PagedForm& f, f32x16 (&x)[N], float in, float slope, float ahead, Off off) {
   if constexpr (kCap) {
-    if (cap_is_small(x, in)) {
+    if (cap_is_small(x, in, kTanhSmall)) {
       const CapForm c = cap_form(in, f.cap_log2e);
 #pragma unroll
       for (int g = 0; g < N; ++g)

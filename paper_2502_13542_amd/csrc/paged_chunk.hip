@@ -257,10 +257,10 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
     if (page_next >= 0) fetch(page_next, stage ^ 1);
     if (visible) {
       // register i of group kb holds key kpos0 + (kb0 + kb) 32 + 16 (i / 8) + 8 half + i % 8
-      CapForm cap;
+      CapShort cap;
       if constexpr (kCap && !kBias) {            // the polynomial goes into the exponents below; beyond its range, and where some are hidden, scores are capped here
-        cap = cap_form(p.f.cap_in, p.f.cap_log2e);
-        const bool small = cap_is_small(acc_s, p.f.cap_in);
+        cap = cap_short(p.f.cap_in, p.f.cap_log2e);
+        const bool small = cap_is_small(acc_s, p.f.cap_in, kTanhShort);
         if (masked || !small) {
 #pragma unroll
           for (int kb = 0; kb < kNg; ++kb)
@@ -269,7 +269,7 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
               const float x = acc_s[kb][i];
               acc_s[kb][i] = small ? x * cap.factor(x) : paged_tanh(x * p.f.cap_in, p.f.cap_log2e);
             }
-          cap = CapForm{1.f, 0.f, 0.f, 0.f};
+          cap = CapShort{1.f, 0.f, 0.f};
         }
       }
       if constexpr (kBias)
