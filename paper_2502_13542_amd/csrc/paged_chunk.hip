@@ -14,6 +14,9 @@
 // output, and from rounded terms it would have 10 bits.  The rounding of the probabilities costs the output as much as its own
 // (1.66e-3 of it each, 2.3e-3 together); keeping what it leaves as a second term costs half as many products again.
 //
+// Bound by power with whole pages: 2 x 2048 rows at 16K tokens, 32 query and 8 KV heads of 128, 906 to 954 us (1.08 to 1.14 PFLOP/s, the
+// matrix pipe busy in 61 % of the cycles at 1.7 GHz; an 8192^3 library product 1.25 to 1.33), under a cap by vector instructions (21 % more).
+//
 // Every row sees a span of positions.  A page that all rows of a wavefront see whole takes the path without a mask, one that
 // none sees is skipped, and the walk is over the union of the spans: a window or documents cost what they cover.
 #include "mfma_util.h"
@@ -419,7 +422,7 @@ __global__ __launch_bounds__(kPcThreads) void paged_chunk_kernel(PagedChunk c) {
 // and end, and what pieces cost (a launch, and their way out and back at 4 TB/s).  Whole tiles, dealt out as compute units come
 // free, from the longest on: the busiest unit has no more than an average one, or the longest tile, if tiles differ, and a whole
 // number of rounds if they do not.  (Shares of the pages equal to a page, made by a plan on the device, were slower nearly
-// everywhere: 4 prompts in a row 52 us | 68.  A tile costs 6 us beside its pages, a cut of one 135 KB out and in.)
+// everywhere: 2048 rows at 2048 tokens 52 us | 68.  A tile costs 6 us beside its pages, a cut of one 135 KB out and in.)
 //   2 x 2048 rows at 16K tokens, 32 query and 8 KV heads of 128: KS 1 908, 2 1036, 4 1563; 1 x 2048 at 2048 59, 52, 75; 8 x 512 at 512
 //   49, 59, 86; 512 at 512 21.5, 16.6, 14.4; 12 sequences of up to 500 with a window, 28 and 4 heads 291, 259, 354; 4 of up to 777
 //   248, 271, 380; 64 channels, 8192 at 8192 137, 100, 137, with documents 79, 52, 61
