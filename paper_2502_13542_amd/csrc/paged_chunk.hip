@@ -27,6 +27,7 @@ namespace actqkv {
 
 constexpr int kPcThreads = 512, kPcWaves = kPcThreads / 64;
 constexpr int kPcMaxSplits = 32;
+constexpr size_t kPcMostPieces = 512;      // pieces of 256 rows, or as many bytes of smaller ones, that a call leaves to be merged: 69 MB
 template <int KS> constexpr int kPcRows = 32 * kPcWaves / KS;
 template <int D> constexpr int kPcTileBytes = kBlock * D * 2;            // the keys or the values of a page
 template <int D> constexpr int kPcLdsBytes = 2 * 2 * kPcTileBytes<D>;    // 2 stages x (K, V^T)
@@ -423,6 +424,8 @@ __global__ __launch_bounds__(kPcThreads) void paged_chunk_kernel(PagedChunk c) {
 // free, from the longest on: the busiest unit has no more than an average one, or the longest tile, if tiles differ, and a whole
 // number of rounds if they do not.  (Shares of the pages equal to a page, made by a plan on the device, were slower nearly
 // everywhere: 2048 rows at 2048 tokens 52 us | 68.  A tile costs 6 us beside its pages, a cut of one 135 KB out and in.)
+// Pieces may be more than run at once: 22 sequences of up to 215 rows at up to 18K tokens, 8 and 2 heads of 128, 213 us, in at most 256
+// pieces 270; of 64, 144 | 187.
 //   2 x 2048 rows at 16K tokens, 32 query and 8 KV heads of 128: KS 1 908, 2 1036, 4 1563; 1 x 2048 at 2048 59, 52, 75; 8 x 512 at 512
 //   49, 59, 86; 512 at 512 21.5, 16.6, 14.4; 12 sequences of up to 500 with a window, 28 and 4 heads 291, 259, 354; 4 of up to 777
 //   248, 271, 380; 64 channels, 8192 at 8192 137, 100, 137, with documents 79, 52, 61
@@ -435,6 +438,13 @@ static int chunk_tiles(const actqkv_shape& sh, int batch, int n_rows, int max_ne
   const int64_t most = seqs * ((int64_t(max_new) * group + rows - 1) / rows);
   return int(std::min(most, int64_t(n_rows) * group / rows + seqs));
 }
+template <int D>
+static size_t chunk_piece_bytes(int ks) {
+  return ks == 1 ? ChunkPiece<D, 1>::bytes() : ks == 2 ? ChunkPiece<D, 2>::bytes() : ChunkPiece<D, 4>::bytes();
+}
+static size_t chunk_piece_bytes(const actqkv_shape& sh, int ks) {
+  return sh.head_dim == 64 ? chunk_piece_bytes<64>(ks) : chunk_piece_bytes<128>(ks);
+}
 static ChunkCut chunk_cut(const actqkv_shape& sh, const PagedAttn& p) {
   constexpr double kPageUs[2][3] = {{3.5, 2.0, 1.5}, {2.1, 1.45, 1.0}}, kItemUs = 5.;
   const PagedTable& t = p.t;
@@ -443,22 +453,25 @@ static ChunkCut chunk_cut(const actqkv_shape& sh, const PagedAttn& p) {
   if (p.f.window > 0) longest = std::min(longest, p.f.window / double(kBlock) + 2.);
   double average = longest - std::min(own, longest) / 2.;
   bool equal = p.f.window > 0 ? longest < t.max_pages : own * 4. < longest;
+  bool alike = average > 0.8 * longest;          // (pieces of tiles are more so than the tiles)
   if (p.f.row_first != nullptr) {
     average = longest / 8.;
     longest /= 3.;
-    equal = false;
+    equal = alike = false;
   }
   ChunkCut best{1, 1, 1};
   double least = 0.;
   for (int i = 0; i < 3; ++i) {
     const int ks = 1 << i, tiles = chunk_tiles(sh, t.batch, t.n_rows, t.max_new, ks);
-    const int64_t items = int64_t(tiles) * sh.n_kv_heads;
-    const double page = kPageUs[sh.head_dim == 64][i], rounds = double(items) / kChipCus;
+    const double rows = kPcRows<1> / ks, page = kPageUs[sh.head_dim == 64][i];
+    // of several sequences' last tiles half are empty, on average
+    const double likely = t.batch == 1 ? tiles : std::min<double>(tiles, double(t.n_rows) * (sh.n_q_heads / sh.n_kv_heads) / rows + t.batch / 2.);
     for (int splits = 1; splits <= std::min(kPcMaxSplits, t.max_pages); ++splits) {
-      if (splits > 1 && items * splits > kChipCus) break;
+      if (splits > 1 && size_t(tiles) * sh.n_kv_heads * splits * chunk_piece_bytes(sh, ks) > kPcMostPieces * chunk_piece_bytes(sh, 1)) break;
+      const double pieces = likely * sh.n_kv_heads * splits, rounds = pieces / kChipCus;
       double us = std::ceil(longest / splits) * page + kItemUs;
-      if (splits == 1) us = equal ? std::ceil(rounds) * us : std::max(us, rounds * (average * page + kItemUs));
-      else us += 4. + double(items) * splits * (kPcRows<1> / ks) * sh.head_dim * 8. / 4e6;
+      us = equal || (splits > 1 && alike) ? std::ceil(rounds) * us : std::max(us, rounds * (average / splits * page + kItemUs));
+      if (splits > 1) us += 4. + pieces * rows * sh.head_dim * 8. / 4e6;
       if ((i == 0 && splits == 1) || us < least) {
         least = us;
         best = ChunkCut{ks, splits, tiles};
@@ -467,11 +480,13 @@ static ChunkCut chunk_cut(const actqkv_shape& sh, const PagedAttn& p) {
   }
   return best;
 }
-// Partial results exist only where all pieces run at once: of at most kChipCus workgroups.
 size_t paged_chunk_scratch_most(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages) {
   if (sh.dtype != ACTQKV_BF16) return 0;
-  const int64_t pieces = std::min<int64_t>(kPcMaxSplits, max_pages) * sh.n_kv_heads * chunk_tiles(sh, batch, n_rows, max_new, 4);
-  return size_t(std::min<int64_t>(kChipCus, pieces)) * (sh.head_dim == 64 ? ChunkPiece<64, 1>::bytes() : ChunkPiece<128, 1>::bytes());
+  size_t most = 0;
+  for (int ks = 1; ks <= 4; ks *= 2)
+    most = std::max(most, size_t(std::min(kPcMaxSplits, max_pages)) * sh.n_kv_heads * chunk_tiles(sh, batch, n_rows, max_new, ks) *
+                              chunk_piece_bytes(sh, ks));
+  return std::min(most, kPcMostPieces * chunk_piece_bytes(sh, 1));
 }
 
 template <int D, int KS>
