@@ -666,7 +666,7 @@ int actqkv_paged_attention(const actqkv_shape* shape, int batch, int n_rows, int
  *   weights_in, weights_out  [batch][Hk][weight_stride] fp32, weight_stride >= max_pages * Bs and a multiple of 4; may be the
  *            same array.  max_pages * Hk is at most 2^22.  The first max_pages * Bs entries of a row are written.  Fill them with zero when a sequence begins.
  *   lse      required.
- * The sums are taken in an order that depends on the sizes alone: the same call gives the same bits. */
+ * The sums are taken in an order that depends on the sizes and spans alone: the same call gives the same bits. */
 int actqkv_paged_attention_weights(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q,
                                    const int32_t* row_start, const int32_t* n_ctx, const int32_t* pages, int max_pages,
                                    const void* k_pages, const void* v_pages, int n_pages, float softcap, int window,

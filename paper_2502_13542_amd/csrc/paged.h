@@ -152,7 +152,8 @@ __device__ __forceinline__ CapShort cap_short(float in, float out) {
 }
 __device__ __forceinline__ float paged_tanh(float x, float scale) {
   const float e = __builtin_amdgcn_exp2f(fabsf(x) * (2.f * kLog2e));
-  const float large = copysignf(fmaf(-2.f, __builtin_amdgcn_rcpf(e + 1.f), 1.f), x) * scale;
+  float large = copysignf(fmaf(-2.f, __builtin_amdgcn_rcpf(e + 1.f), 1.f), x) * scale;
+  asm volatile("" : "+v"(large));                // (a select, not 64 branches)
   return fabsf(x) <= kTanhSmall ? x * cap_form(1.f, scale).factor(x) : large;
 }
 // The score, in units of log2, from a product of query and key: far = |position of the query - position of the key|, slope in
@@ -164,7 +165,9 @@ __device__ __forceinline__ float paged_score(const PagedForm& f, float product, 
   return v;
 }
 // Whether the arguments in * x of a lane's registers, of all lanes, are in the polynomial's range: most of the time, and then a
-// cap is 5 instructions a score, otherwise 17.  (in^6 has to be a number, too: under a cap of thousands, or of millionths, none is small.)
+// cap is 5 instructions a score, otherwise 17.  Said to be the same for the wavefront: from
+// a branch that might not be, the two ways' 64 scores come to lie beside each other, in scratch (2 x 2048 rows at 8192 tokens with cap and
+// slopes 2120 us instead of 564).  (in^6 has to be a number, too: under a cap of thousands, or of millionths, none is small.)
 template <int N>
 __device__ __forceinline__ bool cap_is_small(const f32x16 (&x)[N], float in, float most) {
   float mx = 0.f;
@@ -172,35 +175,36 @@ __device__ __forceinline__ bool cap_is_small(const f32x16 (&x)[N], float in, flo
   for (int g = 0; g < N; ++g)
 #pragma unroll
     for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(fabsf(x[g][i]), fabsf(x[g][i + 1])), mx);
-  return in >= 1e-5f && in <= 1e5f && __all(mx * in <= most);
+  return __builtin_amdgcn_readfirstlane(int(in >= 1e-5f) & int(in <= 1e5f) & int(__all(mx * in <= most))) != 0;
 }
-// Their scores.  `ahead`: the query's position less that of the key that off(g, i) = 0 would be of.
-template <bool kCap, bool kBias, int N, typename Off>
-__device__ __forceinline__ void paged_scores(const PagedForm& f, f32x16 (&x)[N], float in, float slope, float ahead, Off off) {
+// Their scores.  `ahead`: the query's position less that of the key that off(g, i) = 0 would be of.  `cap`, up to `most` of the
+// argument: the polynomial.
+template <bool kCap, bool kBias, typename Cap, int N, typename Off>
+__device__ __forceinline__ void paged_scores(const PagedForm& f, f32x16 (&x)[N], float in, const Cap& cap, float most, float slope,
+                                             float ahead, Off off) {
+  auto bias = [&](int g, int i) { return kBias ? -slope * fabsf(ahead - float(off(g, i))) : 0.f; };
   if constexpr (kCap) {
-    if (cap_is_small(x, in, kTanhSmall)) {
-      const CapForm c = cap_form(in, f.cap_log2e);
+    if (cap_is_small(x, in, most)) {
+      if (kBias) asm volatile("" : "+v"(ahead));           // (what both branches take of it is not to be taken before them, into 64 registers)
 #pragma unroll
       for (int g = 0; g < N; ++g)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[g][i] *= c.factor(x[g][i]);
+        for (int i = 0; i < 16; ++i) x[g][i] = fmaf(x[g][i], cap.factor(x[g][i]), bias(g, i));
     } else {
+      if (kBias) asm volatile("" : "+v"(ahead));
 #pragma unroll
       for (int g = 0; g < N; ++g)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[g][i] = paged_tanh(x[g][i] * in, f.cap_log2e);
+        for (int i = 0; i < 16; ++i) {
+          x[g][i] = paged_tanh(x[g][i] * in, f.cap_log2e) + bias(g, i);
+          if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (of more at once the two ways of tanh take registers that there are not)
+        }
     }
   } else {
 #pragma unroll
     for (int g = 0; g < N; ++g)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x[g][i] *= in;
-  }
-  if constexpr (kBias) {
-#pragma unroll
-    for (int g = 0; g < N; ++g)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[g][i] = fmaf(-slope, fabsf(ahead - float(off(g, i))), x[g][i]);
+      for (int i = 0; i < 16; ++i) x[g][i] = fmaf(x[g][i], in, bias(g, i));
   }
 }
 

@@ -277,7 +277,8 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
         }
       }
       if constexpr (kBias)
-        paged_scores<kCap, kBias>(p.f, acc_s, kCap ? p.f.cap_in : p.f.scale_log2e, slope, float(pos - sub0 - 8 * half),
+        paged_scores<kCap, kBias>(p.f, acc_s, kCap ? p.f.cap_in : p.f.scale_log2e, cap_short(p.f.cap_in, p.f.cap_log2e), kTanhShort, slope,
+                                  float(pos - sub0 - 8 * half),
                                   [](int g, int i) { return g * 32 + 16 * (i >> 3) + (i & 7); });
       if (masked) {
         const int ahead = sub0 + 8 * half - v.lo;

@@ -279,7 +279,7 @@ __device__ __forceinline__ void chunk_f32_body(const PagedChunkF32& c) {
         for (int i = 0; i < 16; ++i) acc_s[gg][i] *= scale;
     }
     if constexpr (kCap || kBias)                             // (the scale is in the queries)
-      paged_scores<kCap, kBias>(p.f, acc_s, 1.f, slope, float(pos - key0 - 8 * half),
+      paged_scores<kCap, kBias>(p.f, acc_s, 1.f, cap_form(1.f, p.f.cap_log2e), kTanhSmall, slope, float(pos - key0 - 8 * half),
                                 [](int g, int i) { return g * 32 + 16 * (i >> 3) + (i & 7); });
     if (masked) {
       const int ahead = key0 + 8 * half - v.lo;

@@ -10,6 +10,10 @@
 // each, 687; 4 wavefronts a workgroup and two workgroups a compute unit 880 (their registers spill); the last 64 rows of 4
 // sequences at 8K, 28 heads, 35 us, of which the products are 12: two rounds of the chip, each with its first keys and rows to wait for.
 //
+// Rows with spans of their own are walked from the first to the last that sees any of the workgroup's keys (documents, as many rows
+// and tokens as above at 8192: with the attention 239 us instead of 340).  A cap is the polynomial of the attention's where a wavefront's
+// scores are small, a bias two instructions on positions relative to the workgroup's first key.
+//
 // Where keys alone do not fill the chip, the rows are cut into pieces whose sums a second launch adds up, in order.  Sums of
 // 16 rows are added to the running sum, not single terms: its rounding would pass 1e-6 after some thousand.
 #include "mfma_util.h"
@@ -51,10 +55,10 @@ __device__ __forceinline__ void votes_body(const PagedVotes& c) {
   typedef PwShape<T, D> S;
   constexpr int kG = S::kGroups, kBytes = kPwRows * S::kRowBytes, kPieces = kBytes / 1024 / kPwWaves;
   constexpr int kRowsOf1k = 1024 / S::kRowBytes, kChunks = S::kRowBytes / 16;
-  constexpr bool kForm = kCap || kBias;
+  typedef std::conditional_t<sizeof(T) == 2, CapShort, CapForm> Cap;
   __shared__ __attribute__((aligned(16))) char rows_lds[2][kBytes];
-  __shared__ __attribute__((aligned(16))) float lse_lds[2][kPwRows], slope_lds[2][kPwRows];
-  __shared__ __attribute__((aligned(16))) int lo_lds[2][kPwRows], len_lds[2][kPwRows], pos_lds[2][kPwRows];
+  __shared__ __attribute__((aligned(16))) float lse_lds[2][kPwRows], slope_lds[2][kPwRows], ahead_lds[2][kPwRows];
+  __shared__ __attribute__((aligned(16))) int lo_lds[2][kPwRows], len_lds[2][kPwRows];
   __shared__ SpanOfRows seen_lds[2][kPwRows / 32];
   __shared__ float sum_lds[S::kKeys];
   const PagedAttn& p = c.a;
@@ -72,13 +76,31 @@ __device__ __forceinline__ void votes_body(const PagedVotes& c) {
   if (p.f.row_end == nullptr) i0 = min(max(i0, key0 - w0), seq.m);   // row i sees positions up to w0 + i
   if (p.f.window > 0) i1 = int(min(int64_t(i1), int64_t(key0) + S::kKeys - 1 + p.f.window - w0));
   if (key0 >= seq.n) i1 = i0;
+  if ((p.f.row_first != nullptr || p.f.row_end != nullptr) && i1 > i0) {   // of rows with spans of their own from the first to the last that does
+    __shared__ int range[2];
+    if (tid == 0) {
+      range[0] = i1;
+      range[1] = i0;
+    }
+    __syncthreads();
+    for (int i = i0 + tid; i < i1; i += kPwThreads) {
+      const PagedSpan v = paged_span(p.f, seq.row0 + i, w0 + i, seq.n);
+      if (v.hi > max(v.lo, key0) && v.lo < key0 + S::kKeys) {
+        atomicMin(&range[0], i);
+        atomicMax(&range[1], i + 1);
+      }
+    }
+    __syncthreads();
+    i0 = __builtin_amdgcn_readfirstlane(range[0]);
+    i1 = __builtin_amdgcn_readfirstlane(range[1]);
+  }
   const int f0 = i0 * group, f1 = max(i1, i0) * group;
   const int steps = (f1 - f0 + kPwRows - 1) / kPwRows, per = (steps + c.pieces - 1) / c.pieces;
   const int st0 = piece * per, st1 = min(steps, st0 + per);
 
   // ---- this wavefront's keys as second operands, and whether their page exists
   const int page_index = wkey0 / kBlock;
-  const int page = wkey0 < seq.n ? __builtin_amdgcn_readfirstlane(paged_page(p.t, s, page_index)) : -1;
+  const int page = wkey0 < seq.n && st0 < st1 ? __builtin_amdgcn_readfirstlane(paged_page(p.t, s, page_index)) : -1;
   u32x4 kreg[kG][S::kSteps];
   if (page >= 0) {
     const char* at = static_cast<const char*>(p.k_pages) +
@@ -114,18 +136,18 @@ __device__ __forceinline__ void votes_body(const PagedVotes& c) {
   };
   float my_lse = 0.f, my_slope = 0.f;
   PagedSpan my_span{0x7fffffff, 0};
-  int my_pos = 0;
+  float my_ahead = 0.f;                          // its position less the workgroup's first key
   auto row_read = [&](int st) {
     const int f = f0 + st * kPwRows + tid;
     my_span = PagedSpan{0x7fffffff, 0};
     my_lse = my_slope = 0.f;
-    my_pos = 0;
+    my_ahead = 0.f;
     if (f < f1) {
       const int i = f / group, head = hk * group + (f - i * group), row = seq.row0 + i;
-      my_pos = w0 + i;
       my_lse = p.lse[size_t(row) * p.n_q_heads + head] * kLog2e;
       if (kBias) my_slope = p.f.slopes[head] * kLog2e;
-      const PagedSpan v = paged_span(p.f, row, my_pos, seq.n);
+      if (kBias) my_ahead = float(w0 + i - key0);
+      const PagedSpan v = paged_span(p.f, row, w0 + i, seq.n);
       if (v.hi > v.lo && my_lse > -INFINITY) my_span = v;
     }
   };
@@ -135,14 +157,17 @@ __device__ __forceinline__ void votes_body(const PagedVotes& c) {
     len_lds[stage][tid] = int(my_span.length());
     if (kBias) {
       slope_lds[stage][tid] = my_slope;
-      pos_lds[stage][tid] = my_pos;
+      ahead_lds[stage][tid] = my_ahead;
     }
     const SpanOfRows seen = span_of_rows(my_span);
     if (n == 0) seen_lds[stage][2 * wave + half] = seen;
   };
-  float sum[kG];
+  float sum[kG], key_at[kG];                     // key_at: this lane's keys, from the workgroup's first on
 #pragma unroll
-  for (int gk = 0; gk < kG; ++gk) sum[gk] = 0.f;
+  for (int gk = 0; gk < kG; ++gk) {
+    sum[gk] = 0.f;
+    key_at[gk] = float(kg * 32 * kG + 32 * gk + n);
+  }
   if (st0 < st1) {
     fetch(st0, 0);
     if (wave < kPwRows / 64) {
@@ -174,22 +199,42 @@ __device__ __forceinline__ void votes_body(const PagedVotes& c) {
     };
     // register i is row 64 rh + 32 b + 8 (i / 4) + 4 half + i % 4, the lane's key wkey0 + 32 gk + n
     auto first_row = [&](int b, int q) { return 64 * rh + 32 * b + 8 * q + 4 * half; };
-    auto weight = [&](float x, float lse, float slope, int pos, int gk) {
-      if constexpr (kForm) x = paged_score<kCap, kBias>(p.f, x, slope, kBias ? abs(pos - (wkey0 + 32 * gk + n)) : 0);
-      return __builtin_amdgcn_exp2f(kForm ? x - lse : fmaf(x, p.f.scale_log2e, -lse));
-    };
+    const float in = kCap ? p.f.cap_in : p.f.scale_log2e;
+    Cap cap;
+    if constexpr (kCap) {
+      if constexpr (sizeof(T) == 2) cap = cap_short(in, p.f.cap_log2e);
+      else cap = cap_form(in, p.f.cap_log2e);
+    }
+    bool small[2];
     auto weights_of = [&](int b, int q) {        // a quarter of a block's
-      const f32x4 lse = *reinterpret_cast<const f32x4*>(&lse_lds[stage][first_row(b, q)]);
-      f32x4 slope = {0.f, 0.f, 0.f, 0.f};
-      u32x4 pos = {0, 0, 0, 0};
+      if constexpr (kCap) {
+        if (q == 0) small[b] = cap_is_small(acc[b], in, sizeof(T) == 2 ? kTanhShort : kTanhSmall);
+      }
+      f32x4 less = *reinterpret_cast<const f32x4*>(&lse_lds[stage][first_row(b, q)]);
+      f32x4 slope = {0.f, 0.f, 0.f, 0.f}, ahead = {0.f, 0.f, 0.f, 0.f};
       if constexpr (kBias) {
         slope = *reinterpret_cast<const f32x4*>(&slope_lds[stage][first_row(b, q)]);
-        pos = *reinterpret_cast<const u32x4*>(&pos_lds[stage][first_row(b, q)]);
+        ahead = *reinterpret_cast<const f32x4*>(&ahead_lds[stage][first_row(b, q)]);
+      }
+      // of a score's exponent what is not the product's: the bias and the sum over the row's keys
+      auto rest = [&](int e, int gk) { return kBias ? fmaf(-slope[e], fabsf(ahead[e] - key_at[gk]), -less[e]) : -less[e]; };
+      if constexpr (kCap) {
+        if (!small[b]) {
+#pragma unroll
+          for (int gk = 0; gk < kG; ++gk)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              acc[b][gk][4 * q + e] = __builtin_amdgcn_exp2f(paged_tanh(acc[b][gk][4 * q + e] * in, p.f.cap_log2e) + rest(e, gk));
+          return;
+        }
       }
 #pragma unroll
       for (int gk = 0; gk < kG; ++gk)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[b][gk][4 * q + e] = weight(acc[b][gk][4 * q + e], lse[e], slope[e], int(pos[e]), gk);
+        for (int e = 0; e < 4; ++e) {
+          const float x = acc[b][gk][4 * q + e];
+          acc[b][gk][4 * q + e] = __builtin_amdgcn_exp2f(fmaf(x, kCap ? cap.factor(x) : in, rest(e, gk)));
+        }
     };
     auto products = [&](int b, bool beside) {    // of block b; beside them the weights of the block before
       u32x4 ring[kRing];
