@@ -333,6 +333,177 @@ __global__ __launch_bounds__(kVsThreads) void paged_votes_sum_kernel(PagedVotes 
   c.w.out[to] = c.w.in[to] + v;
 }
 
+// ---- few voting rows: so many (row, query head) pairs of a sequence as LDS holds, staged once.  Every wavefront has 32 keys at a time to
+// itself and the next 32 on their way, so that nothing is waited for in common: bound by the reading of the keys.  Attention included, against
+// the kernel above: 35 sequences of up to 19 rows at up to 16K tokens, the last 5 rows counting, 622 | 850 us; 43 of up to 12 under a window
+// of 338 at 15K 52 | 121 (most keys only have their account copied); 4 x 512 rows at 8K, the last 8, 32 and 64 counting, 207 | 219, 218 | 223, 237 | 236.
+constexpr int kPfThreads = 512, kPfWaves = kPfThreads / 64;
+constexpr int kPfBytes = 65536;                  // of rows in LDS; two workgroups a compute unit
+constexpr int kPfWgs = 1024;                     // workgroups that a call is cut into
+template <typename T, int D> constexpr int kPfRows = kPfBytes / PwShape<T, D>::kRowBytes;
+
+template <typename T, int D, bool kCap, bool kBias>
+__device__ __forceinline__ void votes_few_body(const PagedVotes& c) {
+  typedef PwShape<T, D> S;
+  typedef std::conditional_t<sizeof(T) == 2, CapShort, CapForm> Cap;
+  constexpr int kRows = kPfRows<T, D>, kRowsOf1k = 1024 / S::kRowBytes, kChunks = S::kRowBytes / 16;
+  __shared__ __attribute__((aligned(16))) char rows_lds[kPfBytes];
+  __shared__ __attribute__((aligned(16))) float lse_lds[kRows], slope_lds[kBias ? kRows : 4], ahead_lds[kBias ? kRows : 4];
+  __shared__ __attribute__((aligned(16))) int lo_lds[kRows], len_lds[kRows];
+  __shared__ SpanOfRows seen_lds[kRows / 32];
+  const PagedAttn& p = c.a;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, half = lane >> 5;
+  const int group = p.n_q_heads / p.n_kv_heads;
+  const int hk = blockIdx.x % p.n_kv_heads, wg = blockIdx.x / p.n_kv_heads, s = blockIdx.y;
+  const PagedSeq seq = paged_seq(p.t, s);
+  const int w0 = seq.n - seq.m, i0 = max(seq.m - c.w.rows, 0);
+  const int f0 = i0 * group, n_pairs = seq.m * group - f0, blocks = (n_pairs + 31) / 32;
+
+  // ---- the rows, once
+  if (n_pairs > 0) {
+    const char* base = uniform_ptr(static_cast<const char*>(p.q) + (size_t(seq.row0 + i0) * p.n_q_heads + hk * group) * S::kRowBytes);
+    const uint32_t row_stride = uint32_t(p.n_q_heads) * S::kRowBytes;
+    const __amdgpu_buffer_rsrc_t src = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, 0x7fffffff, 0x00020000);
+    for (int piece = wave; piece * kRowsOf1k < blocks * 32; piece += kPfWaves) {
+      const int r = piece * kRowsOf1k + lane / kChunks, fr = min(r, n_pairs - 1), ir = fr / group;   // (rows behind the last repeat it and do not vote)
+      const uint32_t off = uint32_t(ir) * row_stride + uint32_t(fr - ir * group) * S::kRowBytes +
+                           ((uint32_t(lane % kChunks) ^ S::swizzle(r)) << 4);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (__attribute__((address_space(3))) void*)(rows_lds + piece * 1024), 16, off, 0, 0, 0);
+    }
+    for (int r0 = wave * 64; r0 < blocks * 32; r0 += kPfThreads) {
+      const int r = r0 + lane;
+      PagedSpan span{0x7fffffff, 0};
+      float lse = 0.f;
+      if (r < n_pairs) {
+        const int i = i0 + r / group, head = hk * group + r % group, row = seq.row0 + i;
+        const PagedSpan v = paged_span(p.f, row, w0 + i, seq.n);
+        const float l = p.lse[size_t(row) * p.n_q_heads + head] * kLog2e;
+        if (v.hi > v.lo && l > -INFINITY) {
+          span = v;
+          lse = l;
+        }
+        if constexpr (kBias) {
+          slope_lds[r] = p.f.slopes[head] * kLog2e;
+          ahead_lds[r] = float(i);
+        }
+      } else if (kBias && r < blocks * 32) {
+        slope_lds[r] = ahead_lds[r] = 0.f;
+      }
+      const SpanOfRows seen = span_of_rows(span);
+      if (r < blocks * 32) {
+        lse_lds[r] = lse;
+        lo_lds[r] = span.lo;
+        len_lds[r] = int(span.length());
+        if (n == 0) seen_lds[r / 32] = seen;
+      }
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  int lo_any = 0x7fffffff, hi_any = 0;           // what any of them sees
+  for (int b = 0; b < blocks; ++b) {
+    lo_any = min(lo_any, seen_lds[b].lo_any);
+    hi_any = max(hi_any, seen_lds[b].hi_any);
+  }
+  lo_any = __builtin_amdgcn_readfirstlane(lo_any);
+  hi_any = __builtin_amdgcn_readfirstlane(hi_any);
+
+  const int groups = p.t.max_pages * (kBlock / 32), stride = c.key_tiles * kPfWaves;   // (key_tiles: workgroups of a sequence and KV head)
+  const size_t out_row = size_t(s * p.n_kv_heads + hk) * c.w.stride;
+  const char* kp = static_cast<const char*>(p.k_pages);
+  int my_page = -1;
+  auto page_at = [&](int k, int g) {             // the page of key group g, this wavefront's k-th, of those that somebody sees; -1: none
+    if ((k & 63) == 0) {
+      const int mine = g + lane * stride, key = mine * 32;
+      my_page = mine < groups && key < hi_any && key + 32 > lo_any ? paged_page(p.t, s, key / kBlock) : -1;
+    }
+    return __builtin_amdgcn_readlane(my_page, k & 63);
+  };
+  auto load = [&](u32x4 (&to)[S::kSteps], int page, int g) {
+    if (page < 0) return;
+    const char* at = kp + ((size_t(page) * p.n_kv_heads + hk) * kBlock + (g * 32) % kBlock + n) * S::kRowBytes + 16 * half;
+#pragma unroll
+    for (int j = 0; j < S::kSteps; ++j) to[j] = *reinterpret_cast<const u32x4*>(at + j * 32);
+  };
+  const float in = kCap ? p.f.cap_in : p.f.scale_log2e;
+  Cap cap;
+  if constexpr (kCap) {
+    if constexpr (sizeof(T) == 2) cap = cap_short(in, p.f.cap_log2e);
+    else cap = cap_form(in, p.f.cap_log2e);
+  }
+  const uint32_t a_off0 = uint32_t(n) * S::kRowBytes + ((uint32_t(half) ^ S::swizzle(n)) << 4);
+  auto process = [&](const u32x4 (&keys)[S::kSteps], int page, int g) {
+    const int key0 = g * 32;
+    if (page < 0 && c.w.in == c.w.out) return;
+    const float before = half == 0 ? c.w.in[out_row + key0 + n] : 0.f;
+    float sum = 0.f;
+    if (page >= 0) {
+      const float at = float(key0 + n - w0);
+      for (int b = 0; b < blocks; ++b) {
+        const SpanOfRows seen = seen_lds[b];
+        if (key0 >= __builtin_amdgcn_readfirstlane(seen.hi_any) || key0 + 32 <= __builtin_amdgcn_readfirstlane(seen.lo_any)) continue;
+        const bool masked = key0 < __builtin_amdgcn_readfirstlane(seen.lo_all) || key0 + 32 > __builtin_amdgcn_readfirstlane(seen.hi_all);
+        f32x16 acc[1];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[0][i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < S::kSteps; ++j)
+          acc[0] = S::product(*reinterpret_cast<const u32x4*>(rows_lds + b * 32 * S::kRowBytes + (a_off0 ^ (uint32_t(j) << 5))), keys[j], acc[0]);
+        bool small = true;
+        if constexpr (kCap) small = cap_is_small(acc, in, sizeof(T) == 2 ? kTanhShort : kTanhSmall);
+        float t[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {            // register 4 q + e is row 32 b + 8 q + 4 half + e
+          const int r = 32 * b + 8 * q + 4 * half;
+          const f32x4 less = *reinterpret_cast<const f32x4*>(&lse_lds[r]);
+          f32x4 slope = {0.f, 0.f, 0.f, 0.f}, ahead = {0.f, 0.f, 0.f, 0.f};
+          if constexpr (kBias) {
+            slope = *reinterpret_cast<const f32x4*>(&slope_lds[r]);
+            ahead = *reinterpret_cast<const f32x4*>(&ahead_lds[r]);
+          }
+          float w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float x = acc[0][4 * q + e], rest = kBias ? fmaf(-slope[e], fabsf(ahead[e] - at), -less[e]) : -less[e];
+            if constexpr (kCap) w[e] = small ? fmaf(x, cap.factor(x), rest) : paged_tanh(x * in, p.f.cap_log2e) + rest;
+            else w[e] = fmaf(x, in, rest);
+            w[e] = __builtin_amdgcn_exp2f(w[e]);
+          }
+          if (masked) {
+            const u32x4 lo = *reinterpret_cast<const u32x4*>(&lo_lds[r]), len = *reinterpret_cast<const u32x4*>(&len_lds[r]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = span_holds(key0 + n - int(lo[e]), len[e]) ? w[e] : 0.f;
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) t[e] += w[e];
+        }
+        sum += (t[0] + t[1]) + (t[2] + t[3]);
+      }
+      sum = lane_pair<32>(sum, [](float x, float y) { return x + y; });
+    }
+    if (half == 0) c.w.out[out_row + key0 + n] = before + sum;
+  };
+  u32x4 ka[S::kSteps], kb[S::kSteps];
+  int g = wg * kPfWaves + wave;
+  if (g >= groups) return;
+  int pa = page_at(0, g);
+  load(ka, pa, g);
+  for (int k = 0; g < groups; k += 2, g += 2 * stride) {
+    const int pb = g + stride < groups ? page_at(k + 1, g + stride) : -1;
+    load(kb, pb, g + stride);
+    process(ka, pa, g);
+    if (g + stride >= groups) break;
+    pa = g + 2 * stride < groups ? page_at(k + 2, g + 2 * stride) : -1;
+    load(ka, pa, g + 2 * stride);
+    process(kb, pb, g + stride);
+  }
+}
+template <typename T, int D, bool kCap, bool kBias>
+__global__ __launch_bounds__(kPfThreads) void paged_votes_few_kernel(PagedVotes c) {
+  votes_few_body<T, D, kCap, kBias>(c);
+}
+
 // ---- host side
 static int votes_keys(const actqkv_shape& sh) { return sh.dtype == ACTQKV_F32 ? PwShape<float, 64>::kKeys : PwShape<uint16_t, 64>::kKeys; }
 
@@ -350,10 +521,32 @@ static void launch_votes(const PagedVotes& c, hipStream_t stream) {
   else launch(paged_votes_kernel<T, D, false, false>);
 }
 
+template <typename T, int D>
+static bool launch_votes_few(PagedVotes c, hipStream_t stream) {
+  const int group = c.a.n_q_heads / c.a.n_kv_heads;
+  if (int64_t(std::min(c.w.rows, c.a.t.max_new)) * group > kPfRows<T, D>) return false;
+  const bool cap = c.a.f.cap_in > 0.f, bias = c.a.f.slopes != nullptr;
+  const int64_t pairs = int64_t(c.a.n_kv_heads) * c.a.t.batch;
+  c.key_tiles = int(std::min<int64_t>((c.a.t.max_pages * int64_t(kBlock / 32) + kPfWaves - 1) / kPfWaves, (kPfWgs + pairs - 1) / pairs));
+  auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(unsigned(c.a.n_kv_heads) * c.key_tiles, c.a.t.batch), dim3(kPfThreads), 0, stream, c);
+  };
+  if (cap && bias) launch(paged_votes_few_kernel<T, D, true, true>);
+  else if (cap) launch(paged_votes_few_kernel<T, D, true, false>);
+  else if (bias) launch(paged_votes_few_kernel<T, D, false, true>);
+  else launch(paged_votes_few_kernel<T, D, false, false>);
+  return true;
+}
+
 int launch_paged_votes(const actqkv_shape& sh, const PagedAttn& p, const PagedWeights& w, const Workspace& ws, hipStream_t stream) {
   PagedVotes c;
   c.a = p;
   c.w = w;
+  c.pieces = 1;
+  c.part = nullptr;
+  const bool few = sh.dtype == ACTQKV_F32 ? (sh.head_dim == 64 ? launch_votes_few<float, 64>(c, stream) : launch_votes_few<float, 128>(c, stream))
+                                          : (sh.head_dim == 64 ? launch_votes_few<uint16_t, 64>(c, stream) : launch_votes_few<uint16_t, 128>(c, stream));
+  if (few) return hip_status("paged attention weights");
   const int keys = votes_keys(sh);
   c.key_tiles = (p.t.max_pages * kBlock + keys - 1) / keys;
   const int64_t items = int64_t(c.key_tiles) * p.n_kv_heads * p.t.batch;
