@@ -590,3 +590,19 @@ def test_a_call_that_says_how_many_rows_it_brings():
         got.append((out, lse, w))
     assert all(torch.equal(a, c) for a, c in zip(*got))
     run_attention(b, runner=made_for)
+
+
+@pytest.mark.parametrize("shape,rows", [("llama", 64), ("g8_64", 64), ("fp32_64", 64), ("fp32_g8", 16)])
+@pytest.mark.parametrize("more", [0, 1])
+@pytest.mark.parametrize("kind", ["plain", "all", "cap_slopes_end"])
+def test_weights_of_as_many_rows_as_stay_staged(shape, rows, more, kind):
+    """At and above the number of voting rows up to which they are staged once."""
+    r = rows + more
+    b = Batch(shape_of(*SHAPES[shape]), [(r + 5, 400), (1, 200), (0, 3), (r, r), (2, 131)], 109, extra_rows=(1, 0))
+    run_attention(b, kind, 11, weight_rows=r)
+
+
+def test_weights_of_a_long_sequence_among_many():
+    """One wavefront's keys of more than 64 steps: 64 short sequences of 16 KV heads leave few workgroups for the long one."""
+    b = Batch(shape_of(16, 16, 64, "bf16"), [(1, 3)] * 40 + [(20, 17000)] + [(2, 5)] * 23, 113, extra_entries=0)
+    run_attention(b, weight_rows=3)
