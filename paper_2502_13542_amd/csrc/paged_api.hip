@@ -22,12 +22,14 @@ static int launch_paged_attention(const actqkv_shape& sh, PagedAttn p, const Pag
   ACTQKV_TRY(sh.dtype == ACTQKV_F32 ? launch_paged_chunk_f32(sh, p, ws, stream) : launch_paged_chunk(sh, p, ws, stream));
   return weights != nullptr ? launch_paged_votes(sh, p, *weights, ws, stream) : ACTQKV_OK;
 }
-// Enough for every call of at most these sizes.
+// Enough for every call of at most these sizes: of few rows a sequence, none of them takes the chunks' kernels.
 static size_t paged_workspace_bytes(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages) {
-  const size_t chunk = sh.dtype == ACTQKV_F32 ? paged_chunk_f32_scratch_most(sh, batch, n_rows, max_new, max_pages)
-                                              : paged_chunk_scratch_most(sh, batch, n_rows, max_new, max_pages);
-  const size_t step = paged_step_scratch_most(sh, batch, max_new, max_pages);
-  return kCounterBytes + align_up(std::max({step, chunk, paged_votes_scratch_most(sh)}), 256);
+  size_t most = paged_step_scratch_most(sh, batch, max_new, max_pages);
+  if (!paged_step_supported(sh, max_new))
+    most = std::max({most, paged_votes_scratch_most(sh),
+                     sh.dtype == ACTQKV_F32 ? paged_chunk_f32_scratch_most(sh, batch, n_rows, max_new, max_pages)
+                                            : paged_chunk_scratch_most(sh, batch, n_rows, max_new, max_pages)});
+  return kCounterBytes + align_up(most, 256);
 }
 
 constexpr int kMaxPages = (1 << 30) / kBlock;     // 2^30 tokens: of a sequence, and in the pool

@@ -239,3 +239,10 @@ def test_the_runner_checks_the_rows_a_call_says_it_brings(max_new):
         r.attend(b.q, **t, out=out, max_new=max_new)
     with pytest.raises(B.ActQKVError, match="max_new"):
         r.attend_weigh(b.q, **t, out=out, lse=lse, weight_rows=1, weights=w, max_new=max_new)
+
+
+def test_workspace_of_steps_holds_no_pieces_of_chunks():
+    """64 steps of 32 heads at 8192 tokens: kept scores (32 x 8192 x 4 bytes each) and at most 2048 parts of 16 rows."""
+    cs = B.c_shape(LLAMA)
+    assert B.paged_workspace_bytes(cs, 64, 64, 1, 64) <= 64 * 32 * 8192 * 4 + 2048 * 16 * 130 * 4 + 65536
+    assert B.paged_workspace_bytes(cs, 64, 64 * 5, 5, 64) >= B.paged_workspace_bytes(cs, 64, 64 * 4, 4, 64)
