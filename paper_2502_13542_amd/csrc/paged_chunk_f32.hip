@@ -377,7 +377,7 @@ __device__ __forceinline__ void chunk_f32_body(const PagedChunkF32& c) {
   if (p.lse != nullptr && half == 0) p.lse[at] = (m_run + log2f(l_tot)) * kLn2;
 }
 template <int D, bool kCap, bool kBias>
-__global__ __launch_bounds__(kP4Threads, 2) void paged_chunk_f32_kernel(PagedChunkF32 c) {
+__global__ __launch_bounds__(kP4Threads, D == 64 ? 2 : 1) void paged_chunk_f32_kernel(PagedChunkF32 c) {
   chunk_f32_body<D, kCap, kBias>(c);
 }
 
@@ -393,7 +393,7 @@ static int chunk_f32_tiles(const actqkv_shape& sh, int batch, int n_rows, int ma
 static int chunk_f32_splits(const actqkv_shape& sh, const PagedAttn& p, int tiles) {
   const int64_t items = int64_t(tiles) * sh.n_kv_heads;
   const int keys = 4096 / sh.head_dim;
-  const double tile_us = sh.head_dim == 64 ? 2.9 : 3.8;
+  const double tile_us = sh.head_dim == 64 ? 2.9 : 3.2;
   int64_t longest = int64_t(p.t.max_pages) * (kBlock / keys);
   if (p.f.window > 0) longest = std::min<int64_t>(longest, (int64_t(p.f.window) + kP4Rows) / keys + 2);
   if (p.f.row_first != nullptr) longest = (longest + 2) / 3;      // (of documents a part, nobody knows which)
