@@ -5,9 +5,11 @@
 // A workgroup of 4 wavefronts owns 128 query rows that share a KV head (numbered position by position, the G heads side by
 // side), a wavefront 32 of them.  A tile is 4096 / D keys of a page, 16 KB of keys and 16 KB of values: every wavefront brings a quarter
 // of each into registers while the tile before is worked on, and cuts it into parts in LDS (48 KB, one tile) between two barriers.
-// Two workgroups share a compute unit.  2 x 2048 rows at 8192 tokens, 8 query and 2 KV heads of 64: 372 us (160 TFLOP/s), of 128: 862 (139);
-// bound by the vector work of cutting and softmax beside the products.  Keys that no row of the workgroup sees enter as zeros, whatever their slots hold.  Where
-// the query tiles do not fill the chip the tiles are cut into pieces that a second launch merges.
+// With 64 channels two workgroups share a compute unit; with 128 one has all of its registers (two, with 73 in scratch, were 10 % slower).
+// 2 x 2048 rows at 8192 tokens, 8 query and 2 KV heads of 64: 366 us (164 TFLOP/s), of 128: 774 (155); bound by the vector work of cutting
+// and softmax and by operand reads beside the products.  (Two tiles in LDS, cut between the products of the one before: 64 channels
+// 422, 128 810; three sums of the scores in turn, 128 channels: 803.)  Keys that no row of the workgroup sees enter as zeros, whatever
+// their slots hold.  Where the query tiles do not fill the chip the tiles are cut into pieces that a second launch merges.
 #include "f32_parts.h"
 #include "mfma_util.h"
 #include "paged.h"
@@ -386,8 +388,8 @@ static int chunk_f32_tiles(const actqkv_shape& sh, int batch, int n_rows, int ma
   const int64_t group = sh.n_q_heads / sh.n_kv_heads, seqs = std::min(batch, n_rows);
   return int(std::min(seqs * ((int64_t(max_new) * group + kP4Rows - 1) / kP4Rows), int64_t(n_rows) * group / kP4Rows + seqs));
 }
-// Pieces of a query tile's keys, by these figures, in us: a tile of keys 2.9 (128 channels 3.8), 1.9 times that where two workgroups
-// share a compute unit (of the first rows of a prompt few pieces have keys, and of several sequences some are short); a launch
+// Pieces of a query tile's keys, by these figures, in us: a tile of keys 2.9 (128 channels 3.2), 1.9 times that where two workgroups
+// share a compute unit, or one waits for another (of the first rows of a prompt few pieces have keys, and of several sequences some are short); a launch
 // to merge 4, and 0.4 a piece.  8 query and 2 KV heads of 64, us with so many pieces: 2 x 2048 rows at 8192 tokens 1 398, 2 361; 2048
 // at 2048 2 63, 4 46; 2 x 512 at 4096 4 68, 8 63; 4 x 33 at 2000 16 20, 32 23; 128 at 16384 16 63, 32 46, 64 52.
 static int chunk_f32_splits(const actqkv_shape& sh, const PagedAttn& p, int tiles) {
