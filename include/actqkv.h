@@ -651,7 +651,7 @@ int actqkv_paged_append(const actqkv_shape* shape, int batch, int n_rows, int ma
  *                                                       row's document begins); window 0: none
  *     end   = min(row_end[row], n_ctx)                  row_end [n_rows] int32 (of a prefix mask: max(p + 1, prefix length));
  *                                                       NULL: p + 1
- *   out      [n_rows][H][D] = softmax over the keys seen, times their values; 0 for a row that sees none.
+ *   out      [n_rows][H][D] = softmax over the keys seen, times their values; 0 for a row that sees none.  Not over an input.
  *   lse      [n_rows][H] fp32, natural-log sum of exp of the scores (-infinity for a row that sees none); may be NULL.
  * Errors: EINVAL (null, sizes, softcap outside its range, window < 0), ESHAPE, EALIGN, EWORKSPACE. */
 int actqkv_paged_attention(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q,
