@@ -106,14 +106,15 @@ struct PagedForm {
 // Positions [lo, hi) that a row at position pos of a sequence of n tokens sees (hi <= lo: none).
 struct PagedSpan {
   int lo, hi;
-  // one comparison a key, unsigned: a second one costs scalar registers for its mask, which 32 of them do not have
+  // one comparison a key, unsigned: a second one costs scalar registers for its mask, which 32 of them do not have.  (Neither
+  // bound is negative, so that their difference fits.)
   __device__ __forceinline__ uint32_t length() const { return uint32_t(max(hi - lo, 0)); }
 };
 __device__ __forceinline__ bool span_holds(int key_less_lo, uint32_t length) { return uint32_t(key_less_lo) < length; }
 __device__ __forceinline__ PagedSpan paged_span(const PagedForm& f, int row, int pos, int n) {
   PagedSpan v{0, 0};
   if (pos < 0) return v;                         // more rows than tokens: the row is not in the cache
-  v.hi = f.row_end != nullptr ? min(f.row_end[row], n) : pos + 1;
+  v.hi = f.row_end != nullptr ? max(min(f.row_end[row], n), 0) : pos + 1;
   if (f.row_first != nullptr) v.lo = max(f.row_first[row], 0);
   if (f.window > 0) v.lo = max(v.lo, pos - f.window + 1);
   return v;

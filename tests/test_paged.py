@@ -606,3 +606,20 @@ def test_weights_of_a_long_sequence_among_many():
     """One wavefront's keys of more than 64 steps: 64 short sequences of 16 KV heads leave few workgroups for the long one."""
     b = Batch(shape_of(16, 16, 64, "bf16"), [(1, 3)] * 40 + [(20, 17000)] + [(2, 5)] * 23, 113, extra_entries=0)
     run_attention(b, weight_rows=3)
+
+
+@pytest.mark.parametrize("shape", ["llama", "g8_64", "fp32_64", "fp32_g3"])
+@pytest.mark.parametrize("batch", ["few", "steps", "chunks", "long_tail"])
+@pytest.mark.parametrize("start", ["first", "window", "both"])
+def test_rows_that_end_at_the_least_number(shape, batch, start):
+    """row_end of -2^31 and its neighbours beside a first position above 0: the row sees nothing, whatever the rows beside it see."""
+    b = Batch(shape_of(*SHAPES[shape]), BATCHES[batch], 127, extra_rows=(1, 1))
+    pos = b.positions()
+    f = dict(row_end=pos + 1)
+    f["row_end"][::2] = np.resize([-(2 ** 31), -(2 ** 31) + 1, -(2 ** 31) + 40, -1, 0], len(pos[::2]))
+    if start != "window":
+        f["row_first"] = np.maximum(pos - 50, 0)
+        f["row_first"][::4] = np.resize([2 ** 31 - 1, 1, 60, 2 ** 30], len(pos[::4]))
+    if start != "first":
+        f["window"] = 30
+    run_attention(b, f, weight_rows=40)
