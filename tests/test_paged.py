@@ -623,3 +623,47 @@ def test_rows_that_end_at_the_least_number(shape, batch, start):
     if start != "first":
         f["window"] = 30
     run_attention(b, f, weight_rows=40)
+
+
+CLAMPED = [2 ** 31 - 1, -(2 ** 31), 17, 256]     # more tokens than the pages hold; none; fewer than rows; all that the pages hold
+
+
+def clamped_batch(shape):
+    """Sequences with such lengths on the device, and on the host what they are taken as; no page is two sequences'."""
+    b = Batch(shape_of(*SHAPES[shape]), [(5, 200), (3, 130), (40, 256), (2, 256)], 131, extra_rows=(1, 2), extra_entries=0, garbage=None)
+    b.n_ctx = np.clip(CLAMPED, 0, b.max_pages * BS)
+    b.seqs = [(m, n) for (m, _), n in zip(b.seqs, b.n_ctx)]
+    raw = torch.tensor(CLAMPED, dtype=torch.int32, device=DEV)
+    b.dev = lambda dev=DEV: dict(Batch.dev(b, dev), n_ctx=raw.clone())
+    return b
+
+
+@pytest.mark.parametrize("shape", ["llama", "g8_64", "fp32_64", "fp32_g3"])
+@pytest.mark.parametrize("kind", ["plain", "all"])
+def test_clamped_lengths_give_what_the_lengths_they_stand_for_give(shape, kind):
+    """The bounds are those of the lengths after clamping: zeros in the place of the results are far outside."""
+    b = clamped_batch(shape)
+    out, lse, w_out, want = run_attention(b, kind, 13, weight_rows=3)
+    rows = np.arange(b.row_start[0], b.row_start[-1])
+    assert b.n_ctx.tolist() == [256, 0, 17, 256]
+    with pytest.raises(AssertionError, match="out off"):
+        check_out(b, want, torch.zeros_like(out), lse, rows)
+    with pytest.raises(AssertionError):
+        check_out(b, want, out, torch.where(torch.isinf(lse), lse, 0.0), rows)
+    if kind == "plain":                           # of 40 rows of 17 tokens the last 17 see some, of the sequence of none no row
+        assert (~np.isneginf(want["lse"][rows]).all(1)).sum() == 5 + 17 + 2
+    few = Batch(b.shape, [(2, 200), (1, 130), (2, 256), (2, 256)], 137, extra_entries=0, garbage=None)      # the kernels for few rows
+    few.seqs = [(m, n) for (m, _), n in zip(few.seqs, b.n_ctx)]
+    few.n_ctx, few.dev = b.n_ctx, lambda dev=DEV: dict(Batch.dev(few, dev), n_ctx=b.dev()["n_ctx"])
+    run_attention(few, kind, 13, weight_rows=3)
+
+
+@pytest.mark.parametrize("shape", list(SHAPES))
+def test_append_at_clamped_lengths(shape):
+    b = clamped_batch(shape)
+    t = b.dev()
+    b.runner().append(b.k_new.to(DEV), b.v_new.to(DEV), t["row_start"], t["n_ctx"], t["pages"], t["k_pages"], t["v_pages"])
+    torch.cuda.synchronize()
+    k, v = po.append(f64(b.k_new), f64(b.v_new), b.row_start, b.n_ctx, b.pages, f64(b.k_pages), f64(b.v_pages))
+    assert (k != f64(b.k_pages)).any((1, 3)).sum() == 5 + 17 + 2           # tokens that have new keys
+    assert np.array_equal(f64(t["k_pages"]), k) and np.array_equal(f64(t["v_pages"]), v)
