@@ -667,3 +667,73 @@ def test_append_at_clamped_lengths(shape):
     k, v = po.append(f64(b.k_new), f64(b.v_new), b.row_start, b.n_ctx, b.pages, f64(b.k_pages), f64(b.v_pages))
     assert (k != f64(b.k_pages)).any((1, 3)).sum() == 5 + 17 + 2           # tokens that have new keys
     assert np.array_equal(f64(t["k_pages"]), k) and np.array_equal(f64(t["v_pages"]), v)
+
+
+@pytest.mark.parametrize("shape", ["llama", "g8_64", "fp32_64"])
+@pytest.mark.parametrize("in_place", [True, False])
+def test_replayed_graph_from_pools_as_they_were(shape, in_place):
+    """Every replay starts from the pools and weights that the eager calls started from, with new keys, values and queries, so that
+    a graph without the append, the weights or the move, or with old inputs, ends with other pools."""
+    sh = shape_of(*SHAPES[shape])
+    hk, budget = sh.n_kv_heads, 140
+    b = Batch(sh, [(1, 600), (4, 300), (90, 90), (2, 131)], 139, spare_pages=10, garbage=None)
+    r, t = b.runner(), b.dev()
+    to = torch.tensor([[b.free.pop(), b.free.pop()] for _ in b.seqs], dtype=torch.int32, device=DEV)
+    given = [t["k_pages"], t["v_pages"], torch.rand(b.batch, hk, b.max_pages * BS, device=DEV)]
+    kp, vp, w = (x.clone() for x in given)
+    q, kn, vn = b.q.to(DEV), b.k_new.to(DEV), b.v_new.to(DEV)
+    out, lse = torch.zeros_like(q), torch.zeros(b.n_rows, sh.n_q_heads, device=DEV)
+    to_w = torch.zeros(b.batch, hk, 2 * BS, device=DEV)
+    kept, n_kept = torch.zeros(b.batch, hk, budget, dtype=torch.int32, device=DEV), torch.zeros(b.batch, dtype=torch.int32, device=DEV)
+    results = (out, lse, to_w, kept, n_kept)
+
+    def step():
+        table = (t["row_start"], t["n_ctx"], t["pages"], kp, vp)
+        r.append(kn, vn, *table)
+        r.attend_weigh(q, *table, out, lse, 3, w)
+        r.evict(*table[1:], w, 2, 30, budget, kept, n_kept, **({} if in_place else dict(to_pages=to, to_weights=to_w)))
+
+    def start():
+        for x, x0 in zip((kp, vp, w), given):
+            x.copy_(x0)
+        for x in results:
+            x.zero_()
+
+    def state():
+        torch.cuda.synchronize()
+        return [x.clone() for x in (kp, vp, w, *results)]
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    last = None
+    for n_ctx in ([600, 300, 90, 131], [130, 299, 90, 140], [5, 141, 90, 142], [600, 17, 95, 256]):
+        t["n_ctx"].copy_(torch.tensor(n_ctx, dtype=torch.int32))
+        for x in (q, kn, vn):
+            x.copy_(torch.randn(x.shape).to(x.dtype))
+        start()
+        step()
+        want = state()
+        for a, x0 in zip(want, given):
+            assert not torch.equal(a, x0)
+        assert last is None or not any(torch.equal(a, c) for a, c in zip(want[:4], last))
+        last = want
+        for _ in range(2):
+            start()
+            graph.replay()
+            assert all(torch.equal(a, c) for a, c in zip(state(), want))
+        # what the pools hold by the definitions: the new tokens, then the move
+        k, v = po.append(f64(kn), f64(vn), b.row_start, n_ctx, b.pages, f64(given[0]), f64(given[1]))
+        k_end, v_end, kept_end = f64(want[0]), f64(want[1]), want[6].cpu().numpy()
+        cut = np.asarray(n_ctx) > budget
+        for s in range(b.batch):
+            for h in range(hk):
+                old = kept_end[s, h][kept_end[s, h] >= 0]
+                assert len(old) == min(n_ctx[s], budget) and cut[s] == (old[-1] >= budget)
+                dst = b.pages[s] if in_place else to[s].cpu().numpy()
+                new = np.arange(len(old))
+                src = b.pages[s][old // BS]
+                assert np.array_equal(k_end[dst[new // BS], h, new % BS], k[src, h, old % BS])
+                assert np.array_equal(v_end[dst[new // BS], h, :, new % BS], v[src, h, :, old % BS])
