@@ -991,11 +991,14 @@ class PagedRunner:
 
     def evict(self, n_ctx, pages, k_pages, v_pages, weights, keep_first: int, keep_last: int, budget: int, kept, n_kept,
               to_pages=None, to_weights=None, stream=None) -> None:
-        """Leaves every sequence `budget` tokens per KV head: in place, with the weights, or (to_pages) in other pages, with the
-        weights in to_weights.  kept [batch][Hk][budget], n_kept [batch]."""
+        """Leaves every sequence `budget` tokens per KV head: in place (to_pages None, or `pages` itself), and then their weights in
+        `weights` unless to_weights is given; or in other pages, and their weights in to_weights.  kept [batch][Hk][budget], n_kept [batch].
+        Other pages are none of those in `pages`: a copy of the table, or of a part of it, is not a way to say in place (tokens
+        would be written over others that have yet to move, which the numbers, on the device, do not tell the host)."""
         batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, v_pages)
-        if to_pages is None:
-            to_pages, to_weights = pages, weights if to_weights is None else to_weights
+        if to_pages is None or to_pages.data_ptr() == pages.data_ptr():
+            to_pages = pages if to_pages is None else to_pages
+            to_weights = weights if to_weights is None else to_weights
         rows = batch * self.shape.n_kv_heads
         self._per_row(rows * weights.shape[-1], weights)
         self._per_row(rows * budget, kept)

@@ -737,3 +737,24 @@ def test_replayed_graph_from_pools_as_they_were(shape, in_place):
                 src = b.pages[s][old // BS]
                 assert np.array_equal(k_end[dst[new // BS], h, new % BS], k[src, h, old % BS])
                 assert np.array_equal(v_end[dst[new // BS], h, :, new % BS], v[src, h, :, old % BS])
+
+
+@pytest.mark.parametrize("shape", ["llama", "fp32_64"])
+def test_evict_in_place_by_the_table_itself(shape):
+    """to_pages as `pages`: keys, values and weights move as with None, and the next eviction goes by weights that have moved."""
+    sh = shape_of(*SHAPES[shape])
+    b = Batch(sh, [(0, 900), (0, 140), (0, 513)], 149, garbage=None)
+    r, t = b.runner(), b.dev()
+    w = torch.rand(b.batch, sh.n_kv_heads, b.max_pages * BS, generator=torch.Generator().manual_seed(2))
+    wd, n_ctx = w.to(DEV), t["n_ctx"]
+    n, k, v, want_w = b.n_ctx, f64(b.k_pages), f64(b.v_pages), w.numpy()
+    for budget in (400, 150):
+        kept = torch.zeros(b.batch, sh.n_kv_heads, budget, dtype=torch.int32, device=DEV)
+        n_kept = torch.zeros(b.batch, dtype=torch.int32, device=DEV)
+        r.evict(n_ctx, t["pages"], t["k_pages"], t["v_pages"], wd, 3, 20, budget, kept, n_kept, to_pages=t["pages"])
+        torch.cuda.synchronize()
+        want_kept, n, k, v, want_w = po.evict(n, b.pages, k, v, want_w, 3, 20, budget, b.pages, want_w)
+        n_ctx = n_kept
+        assert np.array_equal(kept.cpu().numpy(), want_kept) and np.array_equal(n_kept.cpu().numpy(), n)
+        assert np.array_equal(wd.cpu().numpy(), want_w)
+        assert np.array_equal(f64(t["k_pages"]), k) and np.array_equal(f64(t["v_pages"]), v)

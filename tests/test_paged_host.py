@@ -246,3 +246,21 @@ def test_workspace_of_steps_holds_no_pieces_of_chunks():
     cs = B.c_shape(LLAMA)
     assert B.paged_workspace_bytes(cs, 64, 64, 1, 64) <= 64 * 32 * 8192 * 4 + 2048 * 16 * 130 * 4 + 65536
     assert B.paged_workspace_bytes(cs, 64, 64 * 5, 5, 64) >= B.paged_workspace_bytes(cs, 64, 64 * 4, 4, 64)
+
+
+def test_in_place_eviction_takes_the_weights_along(monkeypatch):
+    """Both ways to say in place, None and the table itself (or a view of it), move the account with the tokens."""
+    b = Batch(shape_of(4, 2, 64, "fp32"), [(0, 400), (0, 200)], 3)
+    r, t = b.runner("cpu"), b.dev("cpu")
+    w, other = torch.zeros(2, 2, b.max_pages * BS), torch.zeros(2, 2, b.max_pages * BS)
+    kept, n_kept = torch.zeros(2, 2, 50, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    calls = []
+    monkeypatch.setattr(B, "paged_evict", lambda *a: calls.append(dict(to_pages=a[13], to_weights=a[15], stride=a[16])))
+    pages = t["pages"]
+    for to_pages in (None, pages, pages.view(-1).view(pages.shape)):
+        for to_weights, gets in ((None, w), (other, other)):
+            r.evict(t["n_ctx"], pages, t["k_pages"], t["v_pages"], w, 1, 1, 50, kept, n_kept, to_pages=to_pages, to_weights=to_weights)
+            c = calls.pop()
+            assert c["to_pages"].data_ptr() == pages.data_ptr() and c["to_weights"] is gets and c["stride"] == b.max_pages * BS
+    r.evict(t["n_ctx"], pages, t["k_pages"], t["v_pages"], w, 1, 1, 50, kept, n_kept, to_pages=pages.clone())
+    assert calls.pop()["to_weights"] is None      # other pages: nothing is written unless it is said where
