@@ -145,12 +145,15 @@ def measured_traffic(workload):
 
 def traffic_fields(workload, mean_blocks_selected=None):
     """roofline.traffic: the stored counter bytes, as long as they were taken on the kernels that
-    are being timed (same hash of csrc/) and on a pass that selected about as many blocks."""
+    are being timed (same hash of their sources) and on a pass that selected about as many blocks."""
     t = measured_traffic(workload)
     if not t:
         return {"traffic": None, "traffic_note": "no counter run stored for this workload"}
     import bench_traffic
-    now = bench_traffic.source_hash()
+    try:
+        now = bench_traffic.source_hash(t["kernels"])
+    except ValueError as e:            # (a kernel of another name)
+        now = str(e)
     if t.get("source_hash") != now:
         return {"traffic": None,
                 "traffic_note": f"stored counters were taken on other kernel sources ({t.get('source_hash')}, "

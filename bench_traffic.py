@@ -4,7 +4,7 @@ with --pmc WRITE_SIZE, CSV output) into HBM bytes per kernel dispatch.
 Each counter is scaled by what it reads for the library's plain copy kernel of known size,
 which runs first in such a pass.  Writes a short text summary and updates bench_traffic.json
 next to this file, which bench.py reports as roofline.traffic as long as the kernels' sources
-are the ones the counters were taken with (a hash of csrc/ is stored with the bytes).
+are the ones the counters were taken with (a hash of them is stored with the bytes).
 
     python bench_traffic.py --workload c3_128k \
         --fetch <dir>/f_counter_collection.csv --write <dir>/w_counter_collection.csv \
@@ -21,20 +21,43 @@ import csv
 import hashlib
 import json
 import os
+import re
 from collections import defaultdict
 
 HERE = os.path.dirname(os.path.abspath(__file__))
+CSRC = os.path.join(HERE, "paper_2502_13542_amd", "csrc")
 
 
-def source_hash() -> str:
-    """Hash of the kernels' sources: the stored traffic is only reported for these."""
-    d = os.path.join(HERE, "paper_2502_13542_amd", "csrc")
+def kernel_sources(kernels, csrc: str = CSRC) -> list:
+    """The files that these kernels are made of: those that define them, with their launches, and what these include of csrc/
+    (the library's public header has declarations of every call and is none of them)."""
+    def text(name):
+        with open(os.path.join(csrc, name), encoding="utf-8") as f:
+            return f.read()
+
+    todo = []
+    for kernel in kernels:
+        defines = re.compile(r"__global__[^;{]*\b" + re.escape(kernel) + r"\s*\(")
+        found = [n for n in sorted(os.listdir(csrc)) if n.endswith(".hip") and defines.search(text(n))]
+        if not found:
+            raise ValueError(f"no source file defines {kernel}")
+        todo += found
+    files = set()
+    while todo:
+        name = todo.pop()
+        if name not in files:
+            files.add(name)
+            todo += [n for n in re.findall(r'^\s*#include "([^"/]+)"', text(name), flags=re.M) if os.path.exists(os.path.join(csrc, n))]
+    return sorted(files)
+
+
+def source_hash(kernels, csrc: str = CSRC) -> str:
+    """Hash of these kernels' sources: their stored traffic is only reported for these."""
     h = hashlib.sha256()
-    for name in sorted(os.listdir(d)):
-        if name.endswith((".hip", ".h")):
-            h.update(name.encode())
-            with open(os.path.join(d, name), "rb") as f:
-                h.update(f.read())
+    for name in kernel_sources(kernels, csrc):
+        h.update(name.encode())
+        with open(os.path.join(csrc, name), "rb") as f:
+            h.update(f.read())
     return h.hexdigest()[:16]
 
 
@@ -95,7 +118,7 @@ def main() -> int:
               f"counter unit (1024 = the counters' nominal KiB).", "",
               "| kernel | dispatches | fetch MB / dispatch | write MB / dispatch |", "|---|---|---|---|"]
     for name in sorted(set(fetch) | set(write)):
-        if name == "copy_bytes_kernel" or not any(k in name for k in OURS):
+        if name == "copy_bytes_kernel" or not name.startswith(OURS):
             continue
         fv, wv = fetch.get(name, []), write.get(name, [])
         n = max(len(fv), len(wv), 1)
@@ -133,7 +156,7 @@ def main() -> int:
         data = {}
     data[args.workload] = {"fetch_bytes_per_launch": f_bytes, "write_bytes_per_launch": w_bytes,
                            "launches": launches, "fetch_scale": f_scale, "write_scale": w_scale,
-                           "kernels": parts, "source_hash": source_hash(), "pass": info}
+                           "kernels": parts, "source_hash": source_hash(parts), "pass": info}
     with open(jpath, "w") as f:
         json.dump(data, f, indent=1, sort_keys=True)
         f.write("\n")

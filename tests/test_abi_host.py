@@ -560,3 +560,41 @@ def test_side_streams_have_a_queue_each(monkeypatch, queues, beside, want):
     monkeypatch.setattr(H, "runs_beside", lambda st, busy, src, host: st.queue != busy.queue, raising=False)
     there = [SimpleNamespace(queue=x) for x in beside]
     assert [st.queue for st in H.side_streams(len(want), "cuda", there)] == want
+
+
+# ---------------------------------------------------------------- stored counters
+def test_stored_traffic_goes_by_the_sources_of_its_own_kernels(tmp_path):
+    """bench.py reports counters for as long as the kernels they were taken on stay as they are, whatever other files do."""
+    import json
+    import shutil
+    import bench_traffic as T
+    csrc = str(tmp_path / "csrc")
+    shutil.copytree(T.CSRC, csrc)
+
+    def change(name):
+        with open(os.path.join(csrc, name), "a") as f:
+            f.write("// a line more\n")
+
+    with open(os.path.join(ROOT, "bench_traffic.json")) as f:
+        stored = json.load(f)
+    assert set(stored) == set(T.ATTENTION)
+    for workload, (_, kernels) in T.ATTENTION.items():
+        assert stored[workload]["kernels"] == kernels
+        files = T.kernel_sources(kernels, csrc)
+        assert {"common.h", "launch.h", "select_body.h"} < set(files) and not any(n.startswith("paged") for n in files)
+        before = T.source_hash(kernels, csrc)
+        assert before == T.source_hash(kernels)
+        for name in ("paged.h", "paged_step.hip", "gather.hip"):
+            change(name)
+        with open(os.path.join(csrc, "new_kernels.hip"), "w") as f:
+            f.write('#include "common.h"\n')
+        assert T.source_hash(kernels, csrc) == before
+        for name in files:
+            change(name)
+            now = T.source_hash(kernels, csrc)
+            assert now != before, name
+            before = now
+        shutil.rmtree(csrc)
+        shutil.copytree(T.CSRC, csrc)
+    with pytest.raises(ValueError):
+        T.kernel_sources(["no_such_kernel"])
