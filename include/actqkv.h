@@ -631,7 +631,9 @@ int actqkv_copy_bytes(void* dst, const void* src, size_t bytes, void* stream);
 
 /* Bytes of workspace of the paged calls that take one, for calls of at most batch sequences, n_rows rows, max_new rows of a
  * sequence and max_pages pages.  As for the other calls: zero-filled once, and calls that share one ordered on one stream (a graph
- * that was captured with it is a call). */
+ * that was captured with it is a call).  Most of it are the scores that the account of weight keeps where a call brings few
+ * rows: 4 bytes for every query head, row (of at most 16 / G) and token of batch tables of max_pages pages (64 sequences of up
+ * to 32768 tokens, 32 and 8 heads, chunks: 1.07 GB of 1.09). */
 size_t actqkv_paged_workspace_bytes(const actqkv_shape* shape, int batch, int n_rows, int max_new, int max_pages);
 
 /* Keys and values of the new tokens into their pages.
@@ -680,7 +682,8 @@ int actqkv_paged_attention_weights(const actqkv_shape* shape, int batch, int n_r
  * and weights (of a token without a page: as zeros); a shorter sequence keeps everything, in place untouched.
  *   weights  [batch][Hk][weight_stride] fp32, weight_stride >= max_pages * Bs.
  *   to_pages device int32 [batch][to_max_pages]: the pages the kept tokens move to, none of which is a page of `pages`; NULL,
- *            or the array `pages` itself: in place (to_max_pages = max_pages), for sequences that share no page.
+ *            or the array `pages` itself: in place (to_max_pages = max_pages), for sequences that share no page.  A copy of
+ *            `pages`, or of a part of it, is neither: tokens would be written over others that have yet to move.
  *   to_weights  [batch][Hk][to_weight_stride], to_weight_stride >= to_max_pages * Bs; the kept tokens' weights, and 0 up to entry
  *            to_max_pages * Bs; may be `weights` with the same stride; NULL: not written.
  *   kept     [batch][Hk][budget] int32: the old positions, ascending; -1 behind the last.

@@ -3,9 +3,9 @@
 // A workgroup takes half of the channels of the new tokens of one (sequence, KV head) that fall into one page: the keys go as
 // they are, the values through LDS, two neighbouring tokens a word, so that a channel's row of the page is written in 16-byte
 // stores where eight (fp32: four) neighbouring tokens are new.  All loads of a thread are in flight before the first store.
-// Bound by HBM, a step by its launch.  32 query, 8 KV heads of 128, bf16: a token of each of 64 sequences 5.2 us (all channels in one
-// workgroup, tokens one by one: 5.8), 15.4k tokens of 16 sequences, 126 MB in and out, 35 us = 3.6 TB/s either way; a plain copy of
-// as many bytes takes 26.
+// Bound by HBM, a step by its launch.  32 query, 8 KV heads of 128, bf16: a token of each of 64 sequences 5.4 to 5.6 us, 15.4k tokens of
+// 16 sequences, 126 MB in and out, 35 to 36 us = 3.6 TB/s; a plain copy of as many bytes takes 26: here all is one round of
+// workgroups, whose first reads nothing overlaps.  (All channels in one workgroup: 5.1 to 5.7 and 34.)
 #include "paged.h"
 
 namespace actqkv {

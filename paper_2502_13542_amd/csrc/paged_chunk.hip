@@ -15,7 +15,7 @@
 // (1.66e-3 of it each, 2.3e-3 together); keeping what it leaves as a second term costs half as many products again.
 //
 // Bound by power with whole pages: 2 x 2048 rows at 16K tokens, 32 query and 8 KV heads of 128, 906 to 954 us (1.08 to 1.14 PFLOP/s, the
-// matrix pipe busy in 61 % of the cycles at 1.7 GHz; an 8192^3 library product 1.25 to 1.33), under a cap by vector instructions (21 % more).
+// matrix pipe busy in 61 % of the cycles at 1.7 GHz; an 8192^3 library product 1.25 to 1.33), under a cap by vector instructions (21 % more; with 256 rows and 128 channels 6 registers are in scratch then, 7 with slopes too).
 //
 // Every row sees a span of positions.  A page that all rows of a wavefront see whole takes the path without a mask, one that
 // none sees is skipped, and the walk is over the union of the spans: a window or documents cost what they cover.

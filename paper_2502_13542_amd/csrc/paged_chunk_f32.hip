@@ -6,7 +6,7 @@
 // side), a wavefront 32 of them.  A tile is 4096 / D keys of a page, 16 KB of keys and 16 KB of values: every wavefront brings a quarter
 // of each into registers while the tile before is worked on, and cuts it into parts in LDS (48 KB, one tile) between two barriers.
 // With 64 channels two workgroups share a compute unit; with 128 one has all of its registers (two, with 73 in scratch, were 10 % slower).
-// 2 x 2048 rows at 8192 tokens, 8 query and 2 KV heads of 64: 366 us (164 TFLOP/s), of 128: 774 (155); bound by the vector work of cutting
+// 2 x 2048 rows at 8192 tokens, 8 query and 2 KV heads of 64: 353 to 366 us (164 to 170 TFLOP/s), of 128: 774 (155); bound by the vector work of cutting
 // and softmax and by operand reads beside the products.  (Two tiles in LDS, cut between the products of the one before: 64 channels
 // 422, 128 810; three sums of the scores in turn, 128 channels: 803.)  Keys that no row of the workgroup sees enter as zeros, whatever
 // their slots hold.  Where the query tiles do not fill the chip the tiles are cut into pieces that a second launch merges.

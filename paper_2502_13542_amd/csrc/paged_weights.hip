@@ -12,7 +12,8 @@
 //
 // Rows with spans of their own are walked from the first to the last that sees any of the workgroup's keys (documents, as many rows
 // and tokens as above at 8192: with the attention 239 us instead of 340).  A cap is the polynomial of the attention's where a wavefront's
-// scores are small, a bias two instructions on positions relative to the workgroup's first key.
+// scores are small, a bias two instructions on positions relative to the workgroup's first key.  (With 128 channels in bf16 6 registers are in
+// scratch under a cap, 17 with a bias too.)
 //
 // Where keys alone do not fill the chip, the rows are cut into pieces whose sums a second launch adds up, in order.  Sums of
 // 16 rows are added to the running sum, not single terms: its rounding would pass 1e-6 after some thousand.
