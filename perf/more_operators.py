@@ -1,0 +1,574 @@
+"""More operators on the paged cache, as cases that can be timed and compared with their plain forms.
+
+  rotate   keys and values of a ragged batch's new tokens into the pages of its sequences, keys rotated by their position on
+           the way, and the queries with them
+  append8  the same into pages held in 8 bits (e4m3), with a scale for each page and KV head, keys and values apart
+  attend8  attention of the new tokens over such pages: whole prompts, chunks and single tokens, with the score forms
+  sparse   attention of single and drafted tokens over the pages that a cheap score selects for each of them: the bounds of
+           the keys of the pages with new tokens, the selection by those of all pages, the attention over the selected ones
+
+Pages hold 128 tokens: keys [page][Hk][128][D], values transposed, [page][Hk][D][128].  Row i of a sequence with m
+new tokens and n tokens in all is at position n - m + i; a sequence's rows are row_start[s] .. row_start[s + 1] - 1.
+A rotation is a table of cosines and sines, [positions][2][R / 2], of the first R channels.
+"""
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda"
+BS = 128
+E4M3 = torch.float8_e4m3fn
+MOST_E4M3, LEAST_EXPONENT = 448.0, -100
+
+# (query heads, KV heads, channels per head, storage) of the layers that are in use
+LAYERS = [(32, 8, 128, "bf16"), (28, 4, 128, "bf16"), (8, 2, 128, "bf16"), (8, 2, 64, "bf16"), (8, 2, 64, "fp32")]
+
+MOST_PAIRS = 2 * 32 * 2048 * 16384      # (query, head, key) triples of the largest chunk
+MOST_CACHE = 16 * 32768 * 8 * 128 * 2   # cached elements (keys alone, times two for fp32) of the largest batch
+
+
+def _case(op, layer, batch, new, ctx, ragged=True, rotary=0, interleaved=False, far=False, softcap=0.0, window=0, slopes=False,
+          mask="causal", k_sel=0, keep_first=0, keep_last=0, name=None):
+    hq, hkv, d, dtype = layer
+    c = dict(op=op, hq=hq, hkv=hkv, d=d, dtype=dtype, batch=batch, new=new, ctx=ctx, ragged=ragged, rotary=rotary,
+             interleaved=interleaved, far=far, softcap=softcap, window=window, slopes=slopes, mask=mask, k_sel=k_sel,
+             keep_first=keep_first, keep_last=keep_last)
+    return c if name is None else dict(c, name=name)
+
+
+def listed():
+    llama, g7, small, small64, fp32 = LAYERS
+    return [
+        # the smallest call: the next token of one chat, small fp32 model that rotates half of its channels
+        _case("rotate", fp32, 1, 1, 700, ragged=False, rotary=32, interleaved=True, name="rotate_step_b1_fp32"),
+        # a decode step of a served batch; what is left of longer chats after evictions, so that positions are not slots
+        _case("rotate", llama, 64, 1, 8192, rotary=128, far=True, name="rotate_step_b64"),
+        # prompts that arrive in chunks of different lengths
+        _case("rotate", llama, 16, 2048, 8192, rotary=128, name="rotate_chunk_b16"),
+        # a decode step into an 8-bit cache
+        _case("append8", llama, 64, 1, 8192, rotary=128, name="append8_step_b64"),
+        # chunks into an 8-bit cache, of a layer that keeps no positions in its keys
+        _case("append8", g7, 12, 2000, 6000, name="append8_chunk_b12"),
+        # the next token of one short chat, small fp32 model
+        _case("attend8", fp32, 1, 1, 700, ragged=False, name="attend8_step_b1_fp32"),
+        # a served batch at up to 32K cached tokens, a token each
+        _case("attend8", llama, 16, 1, 32768, name="attend8_step_b16_32k"),
+        # two long prompts, a chunk of 2048 tokens of each on what is cached of them
+        _case("attend8", llama, 2, 2048, 16384, ragged=False, name="attend8_chunk_2k_at_16k"),
+        # a serving step that mixes chunks and single tokens, in a layer with capped scores and a sliding window
+        _case("attend8", g7, 12, 500, 9000, softcap=50.0, window=4096, name="attend8_mixed_cap_window"),
+        # a prefix that sees all of itself, fp32 queries
+        _case("attend8", fp32, 3, 1111, 1500, mask="prefix", name="attend8_prefix_fp32"),
+        # a served batch at up to 32K cached tokens, a token each, that looks at 4096 of them
+        _case("sparse", llama, 16, 1, 32768, k_sel=32, keep_first=1, keep_last=4, name="sparse_step_b16_32k"),
+        # four drafted tokens on one long document
+        _case("sparse", small, 1, 4, 131072, ragged=False, k_sel=48, keep_first=1, keep_last=2, name="sparse_drafts_b1_128k"),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(max(lo, hi))))))
+
+
+def draw(rng):
+    op = rng.choice(["rotate", "rotate", "append8", "append8", "attend8", "attend8", "attend8", "sparse", "sparse"])
+    layer = rng.choice(LAYERS)
+    hq, hkv, d, dtype = layer
+    size = 2 if dtype == "fp32" else 1
+    batch = _log(rng, 1, 48)
+    most = MOST_CACHE // (size * batch * hkv * d)
+    ctx = _log(rng, 1, min(131072 if op == "sparse" else 32768, most))
+    if op in ("rotate", "append8"):
+        rotary = rng.choice([d, d, d // 2, 16 * rng.randint(1, d // 16)])
+        if op == "append8" and rng.random() < 0.25:
+            rotary = 0
+        return _case(op, layer, batch, _log(rng, 1, min(ctx, 2048, 32768 // batch)), ctx, rotary=rotary,
+                     interleaved=rng.random() < 0.4, far=rng.random() < 0.3)
+    c = dict(softcap=rng.choice([0.0, 0.0, 0.0, 30.0, 50.0]), window=rng.choice([0, 0, 0, _log(rng, 1, 8192)]),
+             slopes=rng.random() < 0.25)
+    if op == "sparse":
+        k_sel = _log(rng, 1, 96)
+        first = rng.randint(0, min(2, k_sel - 1))
+        new = min(ctx, rng.choice([1, 1, 1, rng.randint(2, 8), _log(rng, 8, max(8, 512 // batch))]))
+        c["window"] = 0                                        # (a window leaves nothing to select)
+        return _case(op, layer, batch, new, ctx, k_sel=k_sel, keep_first=first, keep_last=rng.randint(1, max(1, min(4, k_sel - first))), **c)
+    new = 1 if rng.random() < 0.35 else _log(rng, 1, min(ctx, 2048, max(1, MOST_PAIRS // (2 * size * batch * hq * ctx))))
+    return _case(op, layer, batch, new, ctx, mask=rng.choice(["causal", "causal", "document", "prefix"]), **c)
+
+
+def _lengths(c):
+    """(new tokens, tokens in all) of every sequence, by the sizes alone."""
+    news, ctxs = [], []
+    for s in range(c["batch"]):
+        f = (s * 7919 % 97) / 97.0 if c["ragged"] and s else 1.0       # the first one has the full sizes
+        ctx = max(1, int(round(c["ctx"] * (0.25 + 0.75 * f))))
+        new = 1 if c["ragged"] and s % 3 == 2 else max(1, int(round(c["new"] * (0.1 + 0.9 * f))))
+        news.append(min(new, ctx))
+        ctxs.append(ctx)
+    return news, ctxs
+
+
+def prepare(case, seed):
+    c = dict(case)
+    hq, hkv, d, batch, op = c["hq"], c["hkv"], c["d"], c["batch"], c["op"]
+    td = torch.float32 if c["dtype"] == "fp32" else torch.bfloat16
+    g = torch.Generator(device=DEV).manual_seed(int(seed) % (1 << 60))
+    cpu = torch.Generator().manual_seed(int(seed) % (1 << 60))
+    i32 = dict(dtype=torch.int32, device=DEV)
+
+    def randn(*shape, dtype=td):
+        return torch.randn(*shape, generator=g, device=DEV, dtype=dtype)
+
+    news, ctxs = _lengths(c)
+    counts = [-(-n // BS) for n in ctxs]
+    n_pages = sum(counts) + 3                                          # a few that belong to nobody
+    order = torch.randperm(n_pages, generator=cpu).tolist()
+    table = [[order.pop() for _ in range(n)] + [-1] * (max(counts) - n) for n in counts]
+    starts = [0]
+    for m in news:
+        starts.append(starts[-1] + m)
+    rows = starts[-1]
+    st = dict(case=c, batch=batch, n_rows=rows, max_new=max(news), max_pages=max(counts), n_pages=n_pages,
+              n_ctx=torch.tensor(ctxs, **i32), row_start=torch.tensor(starts, **i32), pages=torch.tensor(table, **i32))
+    seq = torch.repeat_interleave(torch.arange(batch), torch.tensor(news))
+    pos = torch.tensor(ctxs)[seq] - torch.tensor(news)[seq] + torch.arange(rows) - torch.tensor(starts)[seq]
+    # some channels are larger than the others, in keys far more than in values
+    loud = 1.0 + 7.0 * (torch.rand(hkv, d, generator=g, device=DEV) < 0.04)
+    if op in ("rotate", "append8"):
+        tokens = torch.exp(0.7 * torch.randn(rows, 1, 1, generator=g, device=DEV))      # and some tokens than others
+        st["k_new"] = (randn(rows, hkv, d).float() * loud * tokens).to(td)
+        st["v_new"] = (randn(rows, hkv, d).float() * tokens).to(td)
+        st["rotation"] = st["row_pos"] = st["q"] = st["q_out"] = None
+        if c["rotary"]:
+            shift = torch.randint(0, 65536 if c["far"] else 1, (batch,), generator=cpu)  # tokens that left the cache before
+            n_positions = max(ctxs) + int(shift.max())
+            inv = 500000.0 ** (-torch.arange(0, c["rotary"], 2, dtype=torch.float64) / c["rotary"])
+            angle = torch.arange(n_positions, dtype=torch.float64, device=DEV)[:, None] * inv.to(DEV)
+            st["rotation"] = torch.stack([angle.cos(), angle.sin()], 1).float()
+            if c["far"]:
+                st["row_pos"] = (pos + shift[seq]).to(**i32)
+            st["q"] = randn(rows, hq, d)
+            st["q_out"] = torch.empty_like(st["q"])
+    if op == "rotate":
+        st["k_pages"], st["v_pages"] = randn(n_pages, hkv, BS, d), randn(n_pages, hkv, d, BS)
+    if op in ("append8", "attend8"):
+        u = randn(hkv, d, dtype=torch.float32)
+        first = torch.tensor([row[0] for row in table], device=DEV)
+        for name, shape in (("k", (n_pages, hkv, BS, d)), ("v", (n_pages, hkv, d, BS))):
+            x = randn(*shape, dtype=torch.bfloat16)
+            if name == "k":
+                x *= loud[:, None].bfloat16()
+                # a direction of the queries that the first key of every sequence answers to: most heads look at it
+                x[first, :, 0] = (x[first, :, 0].float() + 1.5 * u).bfloat16()
+            scale = torch.exp2(torch.randint(-8, -5, (n_pages, hkv), generator=g, device=DEV).float())
+            x *= (1.0 / scale)[:, :, None, None].bfloat16()
+            st[name + "_pages"] = x.clamp_(-MOST_E4M3, MOST_E4M3).to(E4M3)
+            st[name + "_scales"] = scale
+    if op == "sparse":
+        # the keys of a page have a direction in common, and every query looks for those of a few pages
+        topic = randn(n_pages, hkv, d, dtype=torch.float32)
+        st["k_pages"] = randn(n_pages, hkv, BS, d)
+        st["k_pages"] += (0.8 * topic).to(td)[:, :, None]
+        st["v_pages"] = randn(n_pages, hkv, d, BS)
+        wanted = (torch.rand(rows, 6, generator=cpu) * torch.tensor(counts)[seq][:, None]).long()
+        of = torch.tensor(table)[seq[:, None], wanted].to(DEV)
+        look = topic[of].mean(1).repeat_interleave(hq // hkv, 1)
+        st["q"] = (randn(rows, hq, d).float() + 2.0 * look).to(td)
+        bounds = torch.stack([st["k_pages"].amin(2), st["k_pages"].amax(2)], 2)          # [page][Hk][2][D]
+        for s, (m, n) in enumerate(zip(news, ctxs)):                                     # but not yet of pages with new tokens
+            bounds[table[s][(n - m) // BS : counts[s]]] = 0
+        st["bounds"] = bounds.contiguous()
+        st["idx"] = torch.empty(rows, hkv, c["k_sel"], **i32)
+        st["n_sel"] = torch.empty(rows, hkv, **i32)
+        st["scores"] = torch.empty(rows, hkv, st["max_pages"], dtype=torch.float32, device=DEV)
+    if op == "attend8":
+        st["q"] = (randn(rows, hq, d).float() + 0.4 * u.repeat_interleave(hq // hkv, 0)).to(td)
+    if op in ("attend8", "sparse"):
+        st["out"] = torch.empty(rows, hq, d, dtype=td, device=DEV)
+        st["lse"] = torch.empty(rows, hq, dtype=torch.float32, device=DEV)
+        st["slopes"] = st["row_first"] = st["row_end"] = None
+        if c["slopes"]:
+            st["slopes"] = torch.tensor([2.0 ** (-8.0 * (h + 1) / hq) for h in range(hq)], dtype=torch.float32, device=DEV)
+        if c["mask"] == "document":       # a document begins at about every 900th token; one row in 64 is padding that sees nothing
+            begins = torch.rand(batch, max(ctxs), generator=cpu) < 1.0 / 900
+            begins[:, 0] = True
+            began = torch.cummax(torch.where(begins, torch.arange(max(ctxs)), 0), 1).values[seq, pos]
+            pad = torch.rand(rows, generator=cpu) < 1.0 / 64
+            st["row_first"] = torch.where(pad, torch.tensor(ctxs)[seq], began).to(**i32)
+        if c["mask"] == "prefix":
+            prefix = (torch.tensor(ctxs) * (0.3 + 0.7 * torch.rand(batch, generator=cpu))).long()
+            st["row_end"] = torch.maximum(pos + 1, prefix[seq]).to(**i32)
+    return st
+
+
+# ---------------------------------------------------------------- plain forms
+def _places(st):
+    """Sequence and position of every row."""
+    row = torch.arange(st["n_rows"], device=DEV)
+    start = st["row_start"].long()
+    seq = torch.searchsorted(start, row, right=True) - 1
+    pos = st["n_ctx"].long()[seq] - (start[seq + 1] - row)
+    return seq, pos
+
+
+def _rotated(st, x, pos):
+    """x with its first R channels rotated, in the type that the table's product with it is computed in (64 bits, of an 8-bit cache:
+    a value next to a border between two codes goes to the right one)."""
+    r = st["case"]["rotary"]
+    wide = torch.float64 if st["case"]["op"] == "append8" else torch.float32
+    x = x.to(wide)
+    at = pos if st["row_pos"] is None else st["row_pos"].long()
+    turn = st["rotation"][at].to(wide)
+    cos, sin = turn[:, None, 0], turn[:, None, 1]
+    if st["case"]["interleaved"]:
+        a, b = x[..., 0:r:2], x[..., 1:r:2]
+        return torch.cat([torch.stack([a * cos - b * sin, b * cos + a * sin], -1).flatten(-2), x[..., r:]], -1)
+    a, b = x[..., : r // 2], x[..., r // 2 : r]
+    return torch.cat([a * cos - b * sin, b * cos + a * sin, x[..., r:]], -1)
+
+
+def _append(st):
+    seq, pos = _places(st)
+    page = st["pages"].long()[seq, pos // BS]
+    k, v, got = st["k_new"].float(), st["v_new"].float(), {}
+    if st["rotation"] is not None:
+        k = _rotated(st, st["k_new"], pos).float()
+        got["q"] = _rotated(st, st["q"], pos).to(st["q"].dtype)
+    if st["case"]["op"] == "rotate":
+        st["k_pages"][page, :, pos % BS] = k.to(st["k_pages"].dtype)
+        st["v_pages"][page, :, :, pos % BS] = st["v_new"]
+        return {**got, "k_pages": st["k_pages"], "v_pages": st["v_pages"]}
+    # the pages with new tokens: what they hold already, before which slot
+    m, n = st["row_start"].long().diff(), st["n_ctx"].long()
+    held = (n - m)[:, None] - torch.arange(st["max_pages"], device=DEV) * BS              # [batch][max_pages]
+    touched = (held < BS) & (held + m[:, None] > 0) & (st["pages"] >= 0)
+    to, old = st["pages"].long()[touched], held[touched].clamp(min=0)
+    place = torch.zeros(st["n_pages"], dtype=torch.long, device=DEV)
+    place[to] = torch.arange(to.numel(), device=DEV)
+    slot = torch.arange(BS, device=DEV)
+    fresh = torch.zeros(to.numel(), BS, dtype=torch.bool, device=DEV)
+    fresh[place[page], pos % BS] = True
+    for name, new in (("k", k), ("v", v)):
+        pages, scales = st[name + "_pages"], st[name + "_scales"]
+        x = torch.zeros(to.numel(), st["case"]["hkv"], BS, st["case"]["d"], device=DEV)
+        x[place[page], :, pos % BS] = new
+        e = torch.log2(x.abs().amax((2, 3)).double() / MOST_E4M3).ceil().clamp(min=LEAST_EXPONENT)
+        was = torch.log2(scales[to].double()).round()
+        e = torch.where((old > 0)[:, None], torch.maximum(e, was), e)
+        by, again = (torch.exp2(y).float()[:, :, None, None] for y in (-e, was - e))
+        codes = pages.view(torch.uint8)[to].view(E4M3).float()
+        codes = codes if name == "k" else codes.transpose(2, 3)
+        held_now = torch.where((slot < old[:, None])[:, None, :, None], codes * again, codes)
+        x = torch.where(fresh[:, None, :, None], x * by, held_now).to(E4M3)
+        pages.view(torch.uint8)[to] = (x if name == "k" else x.transpose(2, 3)).contiguous().view(torch.uint8)
+        scales[to] = torch.exp2(e).float()
+    return {**got, "k_pages": st["k_pages"], "v_pages": st["v_pages"], "k_scales": st["k_scales"], "v_scales": st["v_scales"]}
+
+
+def _attend(st, chosen=None):
+    """Attention over the pages; chosen [n_rows][Hk][max_pages]: the pages that a row looks at."""
+    c = st["case"]
+    batch, hq, hkv, d, most = c["batch"], c["hq"], c["hkv"], c["d"], st["max_new"]
+    group, keys = hq // hkv, st["max_pages"] * BS
+    seq, pos = _places(st)
+    row = torch.arange(st["n_rows"], device=DEV)
+    at = row - st["row_start"].long()[seq]                              # place of a row in its sequence
+    q = torch.zeros(batch, most, hq, d, device=DEV)
+    q[seq, at] = st["q"].float()
+    pages = st["pages"].long().clamp(min=0)
+    if c["op"] == "attend8":
+        k = st["k_pages"].view(torch.uint8)[pages].view(E4M3).float() * st["k_scales"][pages][..., None, None]
+        v = st["v_pages"].view(torch.uint8)[pages].view(E4M3).float() * st["v_scales"][pages][..., None, None]
+    else:
+        k, v = st["k_pages"][pages].float(), st["v_pages"][pages].float()
+    k = k.permute(0, 2, 1, 3, 4).reshape(batch, hkv, keys, d)
+    v = v.permute(0, 2, 1, 4, 3).reshape(batch, hkv, keys, d)
+    q = q.reshape(batch, most, hkv, group, d).permute(0, 2, 1, 3, 4).reshape(batch, hkv, most * group, d)
+    s = torch.matmul(q, k.transpose(2, 3).contiguous()) / math.sqrt(d)
+    s = s.reshape(batch, hkv, most, group, keys)
+    if c["softcap"] > 0:
+        s = torch.tanh(s / c["softcap"]) * c["softcap"]
+    j = torch.arange(keys, device=DEV)
+    p = torch.zeros(batch, most, dtype=torch.long, device=DEV)
+    p[seq, at] = pos
+    if st["slopes"] is not None:
+        far = (p[:, :, None] - j).abs().float()
+        s = s - st["slopes"].reshape(1, hkv, 1, group, 1) * far[:, None, :, None, :]
+    lo, hi = torch.zeros_like(p), torch.zeros_like(p)                   # padded rows see nothing
+    lo[seq, at] = torch.zeros_like(pos) if st["row_first"] is None else st["row_first"].long()
+    hi[seq, at] = pos + 1 if st["row_end"] is None else st["row_end"].long()
+    if c["window"] > 0:
+        lo = torch.maximum(lo, p - c["window"] + 1)
+    seen = ((j >= lo[:, :, None]) & (j < hi[:, :, None]))[:, None, :, None, :]
+    if chosen is not None:
+        by_row = torch.zeros(batch, most, hkv, st["max_pages"], dtype=torch.bool, device=DEV)
+        by_row[seq, at] = chosen
+        seen = seen & by_row.permute(0, 2, 1, 3).repeat_interleave(BS, 3)[:, :, :, None]
+    s = torch.where(seen, s, float("-inf"))
+    top = s.amax(-1, keepdim=True)
+    e = torch.exp(s - torch.where(top == float("-inf"), 0.0, top))
+    total = e.sum(-1, keepdim=True)
+    e = e / torch.where(total == 0, 1.0, total)
+    lse = (top + torch.log(total)).squeeze(-1)
+    o = torch.matmul(e.reshape(batch, hkv, most * group, keys), v).reshape(batch, hkv, most, group, d)
+    o = o.permute(0, 2, 1, 3, 4).reshape(batch, most, hq, d)[seq, at]
+    return {"out": o.to(st["out"].dtype), "lse": lse.permute(0, 2, 1, 3).reshape(batch, most, hq)[seq, at]}
+
+
+def _sparse(st):
+    c = st["case"]
+    seq, pos = _places(st)
+    # the bounds of the pages with new tokens
+    m, n = st["row_start"].long().diff(), st["n_ctx"].long()
+    first = torch.arange(st["max_pages"], device=DEV) * BS
+    touched = (first + BS > (n - m)[:, None]) & (first < n[:, None]) & (m > 0)[:, None]
+    to = st["pages"].long()[touched]
+    there = (torch.arange(BS, device=DEV) < (n[:, None] - first)[touched][:, None])[:, None, :, None]
+    k = st["k_pages"][to].float()
+    st["bounds"][to] = torch.stack([torch.where(there, k, float("inf")).amin(2), torch.where(there, k, float("-inf")).amax(2)], 2).to(st["bounds"].dtype)
+    # scores in 64 bits: two pages may be next to each other where the selection ends
+    hkv, group = c["hkv"], c["hq"] // c["hkv"]
+    pages = st["pages"].long()
+    lo, hi = (st["bounds"][:, :, i][pages.clamp(min=0)].double().permute(0, 2, 3, 1) for i in (0, 1))     # [batch][Hk][D][max_pages]
+    q = st["q"].double().reshape(-1, hkv, group, c["d"])
+    most = st["max_new"]
+    at = torch.arange(st["n_rows"], device=DEV) - st["row_start"].long()[seq]
+    qs = torch.zeros(c["batch"], most, hkv, group, c["d"], dtype=torch.float64, device=DEV)
+    qs[seq, at] = q
+    qs = qs.permute(0, 2, 1, 3, 4).reshape(c["batch"], hkv, most * group, c["d"])
+    score = torch.matmul(qs.clamp(min=0), hi.contiguous()) + torch.matmul(qs.clamp(max=0), lo.contiguous())
+    score = score.reshape(c["batch"], hkv, most, group, -1).amax(3).permute(0, 2, 1, 3)[seq, at].float()     # [n_rows][Hk][max_pages]
+    b = torch.arange(st["max_pages"], device=DEV)
+    last = pos // BS
+    seen = (b <= last[:, None]) & (pages[seq] >= 0)
+    score = torch.where(seen[:, None], score, float("-inf"))
+    always = (b < c["keep_first"]) | (b > last[:, None] - c["keep_last"])
+    rank = torch.where((seen & always)[:, None], float("inf"), score)
+    best = torch.sort(rank, dim=-1, descending=True, stable=True).indices[..., : c["k_sel"]]
+    chosen = torch.zeros_like(rank, dtype=torch.bool).scatter_(2, best, True) & seen[:, None]
+    n_sel = chosen.sum(-1)
+    idx = torch.sort(torch.where(chosen, b, st["max_pages"]), dim=-1).values[..., : c["k_sel"]]
+    idx = torch.nn.functional.pad(idx, (0, c["k_sel"] - idx.shape[-1]), value=st["max_pages"])
+    idx = torch.where(idx < st["max_pages"], idx, -1)
+    return {**_attend(st, chosen), "idx": idx.int(), "n_sel": n_sel.int(), "scores": score, "bounds": st["bounds"]}
+
+
+# ---------------------------------------------------------------- the framework's calls
+def _runner(st):
+    """What a program that calls these operators keeps: the layer's shape and a workspace."""
+    if "runner" not in st:
+        from paper_2502_13542_amd import harness
+        from paper_2502_13542_amd.synth import LayerShape
+        c = st["case"]
+        shape = LayerShape(c["hq"], c["hkv"], c["d"], BS, 4, 128, 512, c["dtype"])
+        st["runner"] = harness.PagedRunner(shape, st["batch"], st["n_rows"], st["max_new"], st["max_pages"], DEV)
+    return st["runner"]
+
+
+def _own(st):
+    c, r = st["case"], _runner(st)
+    cache = (st["pages"], st["k_pages"], st["v_pages"])
+    if c["op"] in ("rotate", "append8"):
+        turn = dict(rotation=st["rotation"], q=st["q"], q_out=st["q_out"], row_pos=st["row_pos"], interleaved=c["interleaved"])
+        if c["op"] == "rotate":
+            r.append_rotated(st["k_new"], st["v_new"], st["row_start"], st["n_ctx"], *cache, **turn)
+            return {"q": st["q_out"], "k_pages": st["k_pages"], "v_pages": st["v_pages"]}
+        r.append_8bit(st["k_new"], st["v_new"], st["row_start"], st["n_ctx"], *cache, st["k_scales"], st["v_scales"], **turn)
+        got = {} if st["q"] is None else {"q": st["q_out"]}
+        return {**got, "k_pages": st["k_pages"], "v_pages": st["v_pages"], "k_scales": st["k_scales"], "v_scales": st["v_scales"]}
+    form = dict(softcap=c["softcap"], window=c["window"], slopes=st["slopes"], row_first=st["row_first"], row_end=st["row_end"])
+    if c["op"] == "attend8":
+        r.attend_8bit(st["q"], st["row_start"], st["n_ctx"], *cache, st["k_scales"], st["v_scales"], st["out"], st["lse"], **form)
+        return {"out": st["out"], "lse": st["lse"]}
+    r.key_bounds(st["n_ctx"], *cache[:2], st["bounds"], row_start=st["row_start"], n_rows=st["n_rows"])
+    r.select_pages(st["q"], st["row_start"], st["n_ctx"], st["pages"], st["bounds"], c["keep_first"], c["keep_last"], st["scores"],
+                   st["idx"], st["n_sel"])
+    r.attend_selected(st["q"], st["row_start"], st["n_ctx"], *cache, st["idx"], st["n_sel"], st["out"], st["lse"], **form)
+    return {"out": st["out"], "lse": st["lse"], "idx": st["idx"], "n_sel": st["n_sel"], "scores": st["scores"], "bounds": st["bounds"]}
+
+
+def run(state):
+    if own:
+        return _own(state)
+    op = state["case"]["op"]
+    if op in ("rotate", "append8"):
+        return _append(state)
+    return _sparse(state) if op == "sparse" else _attend(state)
+
+
+# ---------------------------------------------------------------- what a pass cannot do without
+def _bounds(c):
+    """Of every sequence: its new tokens, its tokens, and how many (row, key) pairs its rows see at most, by the sizes."""
+    for m, n in zip(*_lengths(c)):
+        p = [n - m + i for i in range(m)]
+        win = c["window"] or n
+        if c["mask"] == "prefix":                      # a prefix of about two thirds
+            seen = sum(min(max(x + 1, int(0.65 * n)) - max(0, x - win + 1), n) for x in p)
+        elif c["mask"] == "document":                  # documents of about 900 tokens: half of one is behind a row
+            seen = sum(min(x + 1, win, 900) for x in p)
+        else:
+            seen = sum(min(x + 1, win) for x in p)
+        first = max(0, p[0] - win + 1) if p else 0
+        yield m, n, seen, n - first
+
+
+def work(case):
+    c = dict(case)
+    e = 4 if c["dtype"] == "fp32" else 2
+    hq, hkv, d = c["hq"], c["hkv"], c["d"]
+    held = 1 if c["op"] in ("append8", "attend8") else e
+    news, ctxs = _lengths(c)
+    if c["op"] in ("rotate", "append8"):
+        rows = sum(news)
+        turn = c["rotary"] > 0
+        bytes_ = rows * (2 * hkv * d * (e + held) + turn * (2 * hq * d * e + 4 * c["rotary"]))
+        if c["op"] == "append8":                       # one scale of keys and values for each page with new tokens
+            bytes_ += 8 * hkv * sum((n - 1) // BS - (n - m) // BS + 1 for m, n in zip(news, ctxs))
+        return {"bytes": bytes_, "flops": rows * (hkv + hq) * c["rotary"] * 3}
+    bytes_, flops = 0, 0
+    if c["op"] == "sparse":
+        for m, n in zip(news, ctxs):
+            pages = -(-n // BS)
+            looked = min(n, c["k_sel"] * BS)
+            bytes_ += 2 * m * hq * d * e + m * hq * 4 + hkv * (pages * (2 * d * e + 4 * m) + 2 * looked * d * e + 4 * m * c["k_sel"])
+            flops += m * hq * d * (4 * pages + 4 * looked)
+        return {"bytes": bytes_, "flops": flops}
+    for m, n, seen, cached in _bounds(c):
+        bytes_ += 2 * m * hq * d * e + m * hq * 4 + 2 * cached * hkv * d + 8 * hkv * -(-cached // BS)
+        flops += 4 * hq * d * seen
+    return {"bytes": bytes_, "flops": flops}
+
+
+# ---------------------------------------------------------------- from the definitions, in 64 bits
+def _round_e4m3(x):
+    """The nearest value with 4 significant bits, down to 2^-9; of two the one with an even last bit."""
+    _, exponent = torch.frexp(x)
+    unit = torch.exp2((exponent - 1).clamp(min=-6).double() - 3)
+    return torch.round(x / unit) * unit
+
+
+def _turned(x, cos, sin, interleaved):
+    y = x.clone()
+    half = cos.shape[-1]
+    for i in range(half):
+        a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + half)
+        y[..., a] = x[..., a] * cos[:, None, i] - x[..., b] * sin[:, None, i]
+        y[..., b] = x[..., b] * cos[:, None, i] + x[..., a] * sin[:, None, i]
+    return y
+
+
+def _exact_append(c, st):
+    news, ctxs = _lengths(c)
+    starts, tables = st["row_start"].tolist(), st["pages"].tolist()
+    k, v = st["k_new"].double(), st["v_new"].double()
+    got = {}
+    if c["rotary"]:
+        where = torch.cat([torch.arange(n - m, n, device=DEV) for m, n in zip(news, ctxs)]) if st["row_pos"] is None else st["row_pos"].long()
+        cos, sin = (st["rotation"][where, i].double() for i in (0, 1))
+        k = _turned(k, cos, sin, c["interleaved"])
+        got["q"] = _turned(st["q"].double(), cos, sin, c["interleaved"])
+    pools = {"k": st["k_pages"].double(), "v": st["v_pages"].double().transpose(2, 3)}
+    scales = {} if c["op"] == "rotate" else {"k": st["k_scales"].double(), "v": st["v_scales"].double()}
+    for s in range(c["batch"]):
+        m, n = news[s], ctxs[s]
+        for i in range((n - m) // BS, (n - 1) // BS + 1):
+            lo, hi = max(n - m, i * BS), min(n, (i + 1) * BS)
+            page, had = tables[s][i], lo - i * BS
+            for name, new in (("k", k), ("v", v)):
+                x = new[starts[s] + lo - (n - m) : starts[s] + hi - (n - m)].transpose(0, 1)          # [Hk][tokens][D]
+                to = pools[name][page]
+                if not scales:
+                    to[:, had : had + hi - lo] = x
+                    continue
+                x = x.float().double()                  # (a rotated key is rounded to 32 bits before it is held in 8)
+                # the least power of two whose 448-fold no value exceeds: |x| = f 2^p with f in [1/2, 1), and 448 = 7/8 2^9
+                f, p = torch.frexp(x.abs().amax((1, 2)))
+                e = torch.where(f > 0, p - 9 + (f > 0.875).int(), torch.full_like(p, LEAST_EXPONENT)).clamp(min=LEAST_EXPONENT).double()
+                was = torch.log2(scales[name][page])
+                if had:
+                    e = torch.maximum(e, was)
+                    to[:, :had] = _round_e4m3(to[:, :had] * torch.exp2(was - e)[:, None, None])
+                to[:, had : had + hi - lo] = _round_e4m3(x * torch.exp2(-e)[:, None, None])
+                scales[name][page] = torch.exp2(e)
+    got["k_pages"], got["v_pages"] = pools["k"], pools["v"].transpose(2, 3).contiguous()
+    if scales:
+        got["k_scales"], got["v_scales"] = scales["k"], scales["v"]
+    return got
+
+
+def exact(case, seed):
+    c = dict(case)
+    st = prepare(case, seed)
+    if c["op"] in ("rotate", "append8"):
+        return _exact_append(c, st)
+    kp, vp = st["k_pages"], st["v_pages"]
+    hq, hkv, d = c["hq"], c["hkv"], c["d"]
+    news, ctxs = _lengths(c)
+    starts, tables = st["row_start"].tolist(), st["pages"].tolist()
+    group = hq // hkv
+    f64 = dict(dtype=torch.float64, device=DEV)
+    out = torch.zeros(st["n_rows"], hq, d, **f64)
+    lse = torch.full((st["n_rows"], hq), float("-inf"), **f64)
+    got = {"out": out, "lse": lse}
+    if c["op"] == "sparse":
+        got["idx"] = torch.full((st["n_rows"], hkv, c["k_sel"]), -1, dtype=torch.int32)
+        got["n_sel"] = torch.zeros(st["n_rows"], hkv, dtype=torch.int32)
+        got["scores"] = torch.full((st["n_rows"], hkv, st["max_pages"]), float("-inf"), **f64)
+        got["bounds"] = st["bounds"].double()
+    for s in range(c["batch"]):
+        m, n = news[s], ctxs[s]
+        own_pages = torch.tensor([x for x in tables[s] if x >= 0], device=DEV)
+        pos = torch.arange(n - m, n, device=DEV)
+        rows = slice(starts[s], starts[s] + m)
+        first = torch.zeros_like(pos) if st["row_first"] is None else st["row_first"][rows].long()
+        end = pos + 1 if st["row_end"] is None else st["row_end"][rows].long()
+        if c["window"]:
+            first = torch.maximum(first, pos + 1 - c["window"])
+        key = torch.arange(n, device=DEV)
+        hidden = (key[None] < first[:, None]) | (key[None] >= end[:, None])
+        for kh in range(hkv):
+            heads = slice(kh * group, (kh + 1) * group)
+            k, v = (x[:, kh].double()[own_pages] for x in (kp, vp))
+            if c["op"] == "attend8":
+                k = k * st["k_scales"][own_pages, kh].double()[:, None, None]
+                v = v * st["v_scales"][own_pages, kh].double()[:, None, None]
+            v = v.transpose(1, 2)                                                                      # [pages][128][D]
+            k, v = k.reshape(-1, d)[:n], v.reshape(-1, d)[:n]
+            unseen = hidden
+            if c["op"] == "sparse":
+                limits = []
+                for b in range(len(own_pages)):
+                    if (b + 1) * BS > n - m:
+                        got["bounds"][own_pages[b], kh, 0] = k[b * BS : (b + 1) * BS].amin(0)
+                        got["bounds"][own_pages[b], kh, 1] = k[b * BS : (b + 1) * BS].amax(0)
+                    limits.append(got["bounds"][own_pages[b], kh])
+                limits = torch.stack(limits)                                                           # [pages][2][D]
+                unseen = hidden.clone()
+                for i in range(m):
+                    p = n - m + i
+                    x = st["q"][starts[s] + i, heads].double()                                         # [G][D]
+                    visible = p // BS + 1
+                    score = torch.maximum(x[:, None] * limits[None, :visible, 0], x[:, None] * limits[None, :visible, 1]).sum(-1).amax(0).float()
+                    got["scores"][starts[s] + i, kh, :visible] = score.double()
+                    values = score.tolist()
+                    kept = [b for b in range(visible) if b < c["keep_first"] or b >= visible - c["keep_last"]]
+                    ranked = kept + sorted(set(range(visible)) - set(kept), key=lambda b: (-values[b], b))
+                    chosen = sorted(ranked[: c["k_sel"]])
+                    got["idx"][starts[s] + i, kh, : len(chosen)] = torch.tensor(chosen, dtype=torch.int32)
+                    got["n_sel"][starts[s] + i, kh] = len(chosen)
+                    looked = torch.zeros(len(own_pages), dtype=torch.bool, device=DEV)
+                    looked[chosen] = True
+                    unseen[i] |= ~looked.repeat_interleave(BS)[:n]
+            for h in range(kh * group, (kh + 1) * group):
+                z = st["q"][rows, h].double() @ k.t().contiguous() * d ** -0.5
+                if c["softcap"]:
+                    z = c["softcap"] * torch.tanh(z / c["softcap"])
+                if st["slopes"] is not None:
+                    z = z - st["slopes"][h].double() * (pos[:, None] - key[None]).abs()
+                z = z.masked_fill(unseen, float("-inf"))
+                norm = torch.logsumexp(z, 1)
+                out[rows, h] = torch.exp(z - torch.where(norm.isinf(), 0.0, norm)[:, None]) @ v
+                lse[rows, h] = norm
+    return got
