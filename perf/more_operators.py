@@ -375,12 +375,12 @@ def _own(st):
         if c["op"] == "rotate":
             r.append_rotated(st["k_new"], st["v_new"], st["row_start"], st["n_ctx"], *cache, **turn)
             return {"q": st["q_out"], "k_pages": st["k_pages"], "v_pages": st["v_pages"]}
-        r.append_8bit(st["k_new"], st["v_new"], st["row_start"], st["n_ctx"], *cache, st["k_scales"], st["v_scales"], **turn)
+        r.append_quantised(st["k_new"], st["v_new"], st["row_start"], st["n_ctx"], *cache, st["k_scales"], st["v_scales"], **turn)
         got = {} if st["q"] is None else {"q": st["q_out"]}
         return {**got, "k_pages": st["k_pages"], "v_pages": st["v_pages"], "k_scales": st["k_scales"], "v_scales": st["v_scales"]}
     form = dict(softcap=c["softcap"], window=c["window"], slopes=st["slopes"], row_first=st["row_first"], row_end=st["row_end"])
     if c["op"] == "attend8":
-        r.attend_8bit(st["q"], st["row_start"], st["n_ctx"], *cache, st["k_scales"], st["v_scales"], st["out"], st["lse"], **form)
+        r.attend_quantised(st["q"], st["row_start"], st["n_ctx"], *cache, st["k_scales"], st["v_scales"], st["out"], st["lse"], **form)
         return {"out": st["out"], "lse": st["lse"]}
     r.key_bounds(st["n_ctx"], *cache[:2], st["bounds"], row_start=st["row_start"], n_rows=st["n_rows"])
     r.select_pages(st["q"], st["row_start"], st["n_ctx"], st["pages"], st["bounds"], c["keep_first"], c["keep_last"], st["scores"],
