@@ -50,7 +50,7 @@
 extern "C" {
 #endif
 
-#define ACTQKV_VERSION 108
+#define ACTQKV_VERSION 109
 
 enum {
   ACTQKV_OK = 0,
@@ -694,6 +694,83 @@ int actqkv_paged_evict(const actqkv_shape* shape, int batch, const int32_t* n_ct
                        void* k_pages, void* v_pages, int n_pages, const float* weights, int64_t weight_stride,
                        int keep_first, int keep_last, int budget, const int32_t* to_pages, int to_max_pages,
                        float* to_weights, int64_t to_weight_stride, int32_t* kept, int32_t* n_kept, void* stream);
+
+/* Append with rotation: actqkv_paged_append with the keys turned by their position on the way, and the queries turned with them.
+ *   The first rotary_dim channels (a multiple of 16 up to D) of every head are taken in pairs (a, b): channels (i, i + rotary_dim / 2),
+ *   or (2 i, 2 i + 1) where interleaved is 1.  Pair i of a row at place t becomes (a c - b s, b c + a s), formed in fp32 and rounded
+ *   once; the other channels and the values stay as they are.
+ *   rotation  [n_positions][2][rotary_dim / 2] fp32, 16-byte aligned: the cosines c, then the sines s, of place t (times a factor, where
+ *            a model has one).
+ *   row_pos  [n_rows] int32, may be NULL: the rows' places.  NULL: their positions in the cache (after an eviction those are slots, and
+ *            the places are the caller's to count).  Clamped to 0 .. n_positions - 1.
+ *   q, q_out [n_rows][H][D], storage dtype; both NULL: keys alone.  q_out may be q.  Of a row without a page for its key q_out is written all the same;
+ *            of a row at a negative position, or of no sequence, it is not.
+ * Errors: as actqkv_paged_append; ESHAPE (rotary_dim), EINVAL (interleaved, n_positions, one of q and q_out). */
+int actqkv_paged_append_rotated(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q, const void* k_new,
+                                const void* v_new, const int32_t* row_start, const int32_t* n_ctx, const int32_t* pages,
+                                int max_pages, void* k_pages, void* v_pages, int n_pages, const float* rotation, int n_positions,
+                                int rotary_dim, int interleaved, const int32_t* row_pos, void* q_out, void* stream);
+
+/* Pages in 8 bits: half of the bytes of bf16, and of what a step reads.
+ *     k_pages  [n_pages][Hk][Bs][D]     v_pages  [n_pages][Hk][D][Bs]     e4m3 codes (4 bits of exponent, 3 of the significand; up to 448), a byte each
+ *     k_scales, v_scales  [n_pages][Hk] fp32, powers of two: a token's value is its code times the scale of its page and KV head.
+ * Append: the scale of a page is 2^e with the least e >= -100 for which the largest |x| it is given is at most 448 2^e (infinities and NaN aside, which are
+ * held as NaN: they must not be in a token that somebody sees).  A page whose first slot is among the new tokens starts anew; otherwise
+ * its scale stays, unless a new token needs a larger one: then the codes of its older tokens are rounded to that.  Codes are the nearest
+ * ones, ties to even.  Absolute values are at most 2^126.
+ *   rotation, n_positions, rotary_dim, interleaved, row_pos, q, q_out  as of actqkv_paged_append_rotated, but keys are formed in 64 bits
+ *            and rounded to fp32 before they become codes; rotation NULL: none (rotary_dim 0; q, q_out and row_pos NULL).
+ * Only the new tokens' slots, and older ones of a page whose scale grows, are written: no page that another sequence shares may be one of a
+ * sequence's with new tokens.  Errors: as actqkv_paged_append_rotated. */
+int actqkv_paged_append_quantised(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q, const void* k_new,
+                             const void* v_new, const int32_t* row_start, const int32_t* n_ctx, const int32_t* pages,
+                             int max_pages, void* k_pages, void* v_pages, int n_pages, float* k_scales, float* v_scales,
+                             const float* rotation, int n_positions, int rotary_dim, int interleaved, const int32_t* row_pos,
+                             void* q_out, void* stream);
+
+/* actqkv_paged_attention over pages in 8 bits, with the same forms, workspace and errors: attention over the values that codes and scales stand
+ * for, which enter the products exactly.  q and out have the storage dtype; in fp32, queries times softmax_scale are at most 2^126. */
+int actqkv_paged_attention_quantised(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q,
+                                const int32_t* row_start, const int32_t* n_ctx, const int32_t* pages, int max_pages,
+                                const void* k_pages, const void* v_pages, int n_pages, const float* k_scales,
+                                const float* v_scales, float softcap, int window, const float* slopes, const int32_t* row_first,
+                                const int32_t* row_end, void* out, float* lse, void* workspace, size_t ws_bytes, void* stream);
+
+/* Sparse attention: every row looks at the pages that a cheap score selects for it.  Pages are in the storage dtype.
+ *
+ * Bounds of the keys of a page: bounds [n_pages][Hk][2][D], storage dtype: of every channel the least key of the page's tokens, then the largest
+ * (of the tokens that n_ctx counts).
+ *   row_start  NULL: of all pages of every sequence (n_rows and max_new are not looked at then); otherwise of the pages that hold a new
+ *            token, after an append.
+ * Errors: EINVAL, ESHAPE, EALIGN. */
+int actqkv_paged_key_bounds(const actqkv_shape* shape, int batch, int n_rows, int max_new, const int32_t* row_start,
+                            const int32_t* n_ctx, const int32_t* pages, int max_pages, const void* k_pages, int n_pages,
+                            void* bounds, void* stream);
+
+/* Selection.  The row at position p sees the pages b = 0 .. p / Bs of its sequence that are in the pool.
+ *   scores [n_rows][Hk][score_stride] fp32, score_stride >= max_pages: of page b
+ *            max over the G query heads of  sum over the channels of max(q lo, q hi)
+ *            with the page's bounds lo, hi, in 64 bits rounded to fp32: at least every <q, k> in the page, of any of the heads.  -infinity for pages that the
+ *            row does not see, up to entry max_pages - 1.
+ *   idx    [n_rows][Hk][k_sel] int32: the pages that are selected, ascending, -1 behind the last: the first keep_first and the last keep_last of 0 .. p / Bs
+ *            (keep_first + keep_last <= k_sel), and those with the largest scores of the others (equal scores: the lower page), k_sel in all, or every page that
+ *            the row sees if there are no more.
+ *   n_sel  [n_rows][Hk] int32: how many.
+ * Rows that belong to no sequence are not written; of a row at a negative position nothing is selected.  n_rows * Hk is at most 2^22.
+ * Errors: EINVAL, ESHAPE, EALIGN. */
+int actqkv_paged_select_pages(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q, const int32_t* row_start,
+                              const int32_t* n_ctx, const int32_t* pages, int max_pages, const void* bounds, int n_pages, int k_sel,
+                              int keep_first, int keep_last, float* scores, int64_t score_stride, int32_t* idx, int32_t* n_sel,
+                              void* stream);
+
+/* actqkv_paged_attention of rows that see, of the positions they would see there, those in their selected pages alone: idx and n_sel as above (or the
+ * caller's own; a page in a list twice counts twice, entries outside the sequence's pages are skipped).  Every row reads its own pages: meant for single tokens and a few
+ * drafted ones; rows of a long chunk share nothing.  Workspace and errors as there; n_rows * Hk is at most 2^22. */
+int actqkv_paged_attention_selected(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q,
+                                    const int32_t* row_start, const int32_t* n_ctx, const int32_t* pages, int max_pages,
+                                    const void* k_pages, const void* v_pages, int n_pages, const int32_t* idx, const int32_t* n_sel,
+                                    int k_sel, float softcap, int window, const float* slopes, const int32_t* row_first,
+                                    const int32_t* row_end, void* out, float* lse, void* workspace, size_t ws_bytes, void* stream);
 
 /* How an attention call of batch windows of m >= 2 tokens in bf16 is cut up (host only, nothing is launched): cut[0] query rows of
  * a workgroup, cut[1] query tiles of a window and KV head, cut[2] pieces they are in altogether (equal: not cut; the tiles are

@@ -124,3 +124,146 @@ def evict(n_ctx, pages, k_pages, v_pages, weights, keep_first, keep_last, budget
                     k[to_page[t], h, to_slot[t]] = k_pages[page[o], h, slot[o]] if there else 0.0
                     v[to_page[t], h, :, to_slot[t]] = v_pages[page[o], h, :, slot[o]] if there else 0.0
     return kept, n_kept, k, v, w
+
+
+# ---------------------------------------------------------------- rotation
+def rotate(x, table, places, interleaved):
+    """x [rows][heads][D] with its first R channels turned by rows `places` (clamped) of table [n][2][R / 2]; and what an error
+    bound needs: the sum of the absolute values of the two products of every channel."""
+    at = np.clip(np.asarray(places), 0, len(table) - 1)
+    cos, sin = table[at, 0][:, None], table[at, 1][:, None]
+    half = table.shape[2]
+    a = np.arange(half) * 2 if interleaved else np.arange(half)
+    b = a + 1 if interleaved else a + half
+    y, size = x.copy(), np.abs(x)
+    y[..., a], y[..., b] = x[..., a] * cos - x[..., b] * sin, x[..., b] * cos + x[..., a] * sin
+    size[..., a] = np.abs(x[..., a] * cos) + np.abs(x[..., b] * sin)
+    size[..., b] = np.abs(x[..., b] * cos) + np.abs(x[..., a] * sin)
+    return y, size
+
+
+# ---------------------------------------------------------------- pages in 8 bits
+def round_e4m3(x):
+    """The nearest e4m3 value of |x| <= 448, ties to the even code; not a number where x is none or infinite."""
+    x = np.asarray(x, np.float64)
+    _, p = np.frexp(np.where(np.isfinite(x), x, 0.0))
+    unit = np.exp2(np.maximum(p - 1, -6) - 3.0)
+    return np.where(np.isfinite(x), np.rint(x / unit) * unit, np.nan)
+
+
+def scale_exponent(x):
+    """The least e >= -100 for which the largest finite |x| is at most 448 2^e."""
+    finite = np.abs(x[np.isfinite(x)])
+    top = finite.max() if finite.size else 0.0
+    e = -100
+    while top > 448.0 * 2.0 ** e:
+        e += 1
+    return e
+
+
+def quantised_append(k_new, v_new, row_start, n_ctx, pages, k_codes, v_codes, k_scales, v_scales):
+    """The pools of code values and the scales after the call; k_new and v_new are what is to be held (rotated, and fp32 values)."""
+    kc, vc, ks, vs = k_codes.copy(), v_codes.copy(), k_scales.copy(), v_scales.copy()
+    for s in range(len(n_ctx)):
+        r0, r1 = rows_of(row_start, len(k_new), s)
+        n = min(max(int(n_ctx[s]), 0), pages.shape[1] * BS)
+        pos0 = n - (r1 - r0)
+        for i in range(max(pos0, 0) // BS, -(-n // BS)):
+            lo, hi, page = max(pos0, i * BS, 0), min(n, (i + 1) * BS), int(pages[s][i])
+            if r1 == r0 or hi <= lo or not 0 <= page < len(kc):
+                continue
+            had, new = lo - i * BS, slice(r0 + lo - pos0, r0 + hi - pos0)
+            for codes, scales, x in ((kc, ks, k_new), (vc.swapaxes(2, 3), vs, v_new)):
+                for h in range(codes.shape[1]):
+                    e = scale_exponent(x[new, h])
+                    if had:
+                        old = int(np.log2(scales[page, h]))
+                        e = max(e, old)
+                        codes[page, h, :had] = round_e4m3(codes[page, h, :had] * 2.0 ** (old - e))
+                    codes[page, h, had: had + hi - lo] = round_e4m3(x[new, h] * 2.0 ** -e)
+                    scales[page, h] = 2.0 ** e
+    return kc, vc, ks, vs
+
+
+# ---------------------------------------------------------------- selected pages
+def key_bounds(n_ctx, pages, k_pages, bounds, news=None):
+    """bounds [n_pages][Hk][2][D] after the call: of all pages, or of those with the last news[s] tokens of a sequence."""
+    b = bounds.copy()
+    for s in range(len(n_ctx)):
+        n = min(max(int(n_ctx[s]), 0), pages.shape[1] * BS)
+        first = 0 if news is None else max(n - news[s], 0) // BS
+        for i in range(first, -(-n // BS)):
+            page = int(pages[s][i])
+            if 0 <= page < len(k_pages) and (news is None or news[s] > 0):
+                k = k_pages[page, :, : min(n - i * BS, BS)]
+                b[page, :, 0], b[page, :, 1] = k.min(1), k.max(1)
+    return b
+
+
+def page_scores(q, bounds, page):
+    """Score of a page for one row: q [H][D]; [Hk], rounded to fp32."""
+    hk = bounds.shape[1]
+    x = q.reshape(hk, -1, q.shape[-1])
+    return np.maximum(x * bounds[page, :, :1], x * bounds[page, :, 1:]).sum(-1).max(1).astype(np.float32)
+
+
+def select_pages(q, row_start, n_ctx, pages, bounds, k_sel, keep_first, keep_last):
+    """scores [rows][Hk][max_pages], and the selected pages as lists [row][Hk] (None for rows of no sequence)."""
+    hk, max_pages = bounds.shape[1], pages.shape[1]
+    scores = np.full((len(q), hk, max_pages), -np.inf, np.float32)
+    chosen = [None] * len(q)
+    for s in range(len(n_ctx)):
+        r0, r1 = rows_of(row_start, len(q), s)
+        n = min(max(int(n_ctx[s]), 0), max_pages * BS)
+        for r in range(r0, r1):
+            p = n - (r1 - r0) + (r - r0)
+            last = p // BS if p >= 0 else -1
+            seen = [b for b in range(last + 1) if 0 <= pages[s][b] < len(bounds)]
+            for b in seen:
+                scores[r, :, b] = page_scores(q[r], bounds, int(pages[s][b]))
+            chosen[r] = []
+            for h in range(hk):
+                always = [b for b in seen if b < keep_first or b > last - keep_last]
+                others = sorted(set(seen) - set(always), key=lambda b: (-scores[r, h, b], b))
+                chosen[r].append(sorted((always + others)[:k_sel]))
+    return scores, chosen
+
+
+def attention_selected(q, row_start, n_ctx, pages, k_pages, v_pages, chosen, scale, **form):
+    """attention, where row r and KV head h see the positions of the pages chosen[r][h] alone (a page listed twice counts twice)."""
+    hk_n, group = k_pages.shape[1], q.shape[1] // k_pages.shape[1]
+    got = dict(out=np.full(q.shape, np.nan), lse=np.full(q.shape[:2], np.nan), mass=np.zeros(q.shape), size=np.zeros(q.shape[:2]))
+    slopes, first, end = (form.pop(x, None) for x in ("slopes", "row_first", "row_end"))
+    softcap, window = form.pop("softcap", 0.0), form.pop("window", 0)
+    assert not form
+    for s in range(len(n_ctx)):
+        r0, r1 = rows_of(row_start, len(q), s)
+        n = min(max(int(n_ctx[s]), 0), pages.shape[1] * BS)
+        for r in range(r0, r1):
+            p = n - (r1 - r0) + (r - r0)
+            hi = p + 1 if end is None else min(int(end[r]), n)
+            lo = 0 if first is None else max(0, int(first[r]))
+            if window > 0:
+                lo = max(lo, p - window + 1)
+            for h in range(hk_n):
+                j = np.array([b * BS + t for b in chosen[r][h] if 0 <= b < pages.shape[1] for t in range(BS)], int)
+                j = j[(j >= lo) & (j < hi)] if p >= 0 else j[:0]
+                page = pages[s][j // BS]
+                there = (page >= 0) & (page < len(k_pages))
+                j, page = j[there], page[there]
+                k, v = k_pages[page, h, j % BS], v_pages[page, h, :, j % BS]
+                for x in range(h * group, (h + 1) * group):
+                    if len(j) == 0:
+                        got["out"][r, x], got["lse"][r, x] = 0.0, -np.inf
+                        continue
+                    z, big = scale * (k @ q[r, x]), scale * (np.abs(k) @ np.abs(q[r, x]))
+                    if softcap > 0:
+                        z = softcap * np.tanh(z / softcap)
+                    if slopes is not None:
+                        z, big = z - slopes[x] * np.abs(p - j), big + slopes[x] * np.abs(p - j)
+                    e = np.exp(z - z.max())
+                    prob = e / e.sum()
+                    got["lse"][r, x] = z.max() + np.log(e.sum())
+                    got["out"][r, x], got["mass"][r, x] = prob @ v, prob @ np.abs(v)
+                    got["size"][r, x] = (big * (prob > 1e-12)).max()
+    return got

@@ -96,6 +96,16 @@ SIGNATURES = {
     "actqkv_paged_attention_weights": (_i, [_shp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _i, ctypes.c_float, _i, _vp, _vp,
                                             _vp, _vp, _vp, _i, _vp, _vp, _i64, _vp, _sz, _vp]),
     "actqkv_paged_evict": (_i, [_shp, _i, _vp, _vp, _i, _vp, _vp, _i, _vp, _i64, _i, _i, _i, _vp, _i, _vp, _i64, _vp, _vp, _vp]),
+    "actqkv_paged_append_rotated": (_i, [_shp, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _vp, _i, _vp, _i, _i, _i, _vp,
+                                         _vp, _vp]),
+    "actqkv_paged_append_quantised": (_i, [_shp, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _vp, _i, _vp, _vp, _vp, _i, _i,
+                                           _i, _vp, _vp, _vp]),
+    "actqkv_paged_attention_quantised": (_i, [_shp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _i, _vp, _vp, ctypes.c_float, _i,
+                                              _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "actqkv_paged_key_bounds": (_i, [_shp, _i, _i, _i, _vp, _vp, _vp, _i, _vp, _i, _vp, _vp]),
+    "actqkv_paged_select_pages": (_i, [_shp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _i, _i, _i, _i, _vp, _i64, _vp, _vp, _vp]),
+    "actqkv_paged_attention_selected": (_i, [_shp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _i, _vp, _vp, _i, ctypes.c_float,
+                                             _i, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "actqkv_last_error": (ctypes.c_char_p, []),
     "actqkv_prefill_cut": (_i, [_shp, _i, _i, _i, _i, _vp]),
     "actqkv_version": (_i, []),
@@ -385,3 +395,51 @@ def paged_evict(shape: CShape, batch: int, n_ctx, pages, max_pages: int, k_pages
     """The tokens with the least attention weight leave the cache; see the header."""
     _calls().paged_evict(shape, batch, n_ctx, pages, max_pages, k_pages, v_pages, n_pages, weights, weight_stride, keep_first,
                          keep_last, budget, to_pages, to_max_pages, to_weights, to_weight_stride, kept, n_kept, stream)
+
+
+def paged_append_rotated(shape: CShape, batch: int, n_rows: int, max_new: int, q, k_new, v_new, row_start, n_ctx, pages,
+                         max_pages: int, k_pages, v_pages, n_pages: int, rotation, n_positions: int, rotary_dim: int,
+                         interleaved: bool, row_pos, q_out, stream=None) -> None:
+    """Append with the keys, and the queries with them, turned by their position; see the header."""
+    _calls().paged_append_rotated(shape, batch, n_rows, max_new, q, k_new, v_new, row_start, n_ctx, pages, max_pages, k_pages,
+                                  v_pages, n_pages, rotation, n_positions, rotary_dim, int(interleaved), row_pos, q_out, stream)
+
+
+def paged_append_quantised(shape: CShape, batch: int, n_rows: int, max_new: int, q, k_new, v_new, row_start, n_ctx, pages,
+                      max_pages: int, k_pages, v_pages, n_pages: int, k_scales, v_scales, rotation, n_positions: int,
+                      rotary_dim: int, interleaved: bool, row_pos, q_out, stream=None) -> None:
+    """Append into pages in 8 bits, with or without a rotation; see the header."""
+    _calls().paged_append_quantised(shape, batch, n_rows, max_new, q, k_new, v_new, row_start, n_ctx, pages, max_pages, k_pages,
+                               v_pages, n_pages, k_scales, v_scales, rotation, n_positions, rotary_dim, int(interleaved), row_pos,
+                               q_out, stream)
+
+
+def paged_attention_quantised(shape: CShape, batch: int, n_rows: int, max_new: int, q, row_start, n_ctx, pages, max_pages: int, k_pages,
+                         v_pages, n_pages: int, k_scales, v_scales, out, lse, workspace, softcap: float = 0.0, window: int = 0,
+                         slopes=None, row_first=None, row_end=None, stream=None) -> None:
+    """Attention over pages in 8 bits; see the header."""
+    _calls().paged_attention_quantised(shape, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, k_pages, v_pages, n_pages,
+                                  k_scales, v_scales, softcap, window, slopes, row_first, row_end, out, lse, workspace, stream)
+
+
+def paged_key_bounds(shape: CShape, batch: int, n_rows: int, max_new: int, row_start, n_ctx, pages, max_pages: int, k_pages,
+                     n_pages: int, bounds, stream=None) -> None:
+    """Least and largest key of every channel of a page; see the header."""
+    _calls().paged_key_bounds(shape, batch, n_rows, max_new, row_start, n_ctx, pages, max_pages, k_pages, n_pages, bounds, stream)
+
+
+def paged_select_pages(shape: CShape, batch: int, n_rows: int, max_new: int, q, row_start, n_ctx, pages, max_pages: int, bounds,
+                       n_pages: int, k_sel: int, keep_first: int, keep_last: int, scores, score_stride: int, idx, n_sel,
+                       stream=None) -> None:
+    """The pages that each row looks at, by their bounds; see the header."""
+    _calls().paged_select_pages(shape, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, bounds, n_pages, k_sel,
+                                keep_first, keep_last, scores, score_stride, idx, n_sel, stream)
+
+
+def paged_attention_selected(shape: CShape, batch: int, n_rows: int, max_new: int, q, row_start, n_ctx, pages, max_pages: int,
+                             k_pages, v_pages, n_pages: int, idx, n_sel, k_sel: int, out, lse, workspace, softcap: float = 0.0,
+                             window: int = 0, slopes=None, row_first=None, row_end=None, stream=None) -> None:
+    """Attention of rows over the pages selected for each; see the header."""
+    _calls().paged_attention_selected(shape, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, k_pages, v_pages,
+                                      n_pages, idx, n_sel, k_sel, softcap, window, slopes, row_first, row_end, out, lse, workspace,
+                                      stream)

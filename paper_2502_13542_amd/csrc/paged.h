@@ -94,6 +94,21 @@ __device__ __forceinline__ bool paged_find_tile(const PagedTable& t, int tile, i
   return false;
 }
 
+// The sequence that brings row `row`, or -1 (the same in all lanes).
+__device__ __forceinline__ int paged_seq_of_row(const PagedTable& t, int row) {
+  const int lane = threadIdx.x & 63;
+  for (int s0 = 0; s0 < t.batch; s0 += 64) {
+    bool mine = false;
+    if (s0 + lane < t.batch) {
+      const PagedSeq q = paged_seq(t, s0 + lane);
+      mine = row >= q.row0 && row < q.row0 + q.m;
+    }
+    const unsigned long long any = __ballot(mine);
+    if (any != 0) return s0 + __ffsll(any) - 1;
+  }
+  return -1;
+}
+
 // How scores are formed and which keys a row sees.
 struct PagedForm {
   const int32_t* row_first;  // [n_rows] or NULL
@@ -218,6 +233,8 @@ struct PagedAttn {
   const void* v_pages;
   void* out;                 // [n_rows][H][D]
   float* lse;                // [n_rows][H] or NULL
+  const float* k_scales;     // [n_pages][Hk], of pages in 8 bits
+  const float* v_scales;
 };
 __device__ __forceinline__ SpanOfRows span_of_rows(const PagedSpan& v) {
   return SpanOfRows{half_min(v.lo), half_max(v.hi), half_max(v.lo), half_min(v.hi)};
@@ -234,6 +251,12 @@ bool paged_step_supported(const actqkv_shape& sh, int max_new);
 size_t paged_step_scratch_most(const actqkv_shape& sh, int batch, int max_new, int max_pages);
 int launch_paged_step(const actqkv_shape& sh, const PagedAttn& p, const PagedWeights* weights, const Workspace& ws,
                       hipStream_t stream);
+int launch_paged8_chunk(const actqkv_shape& sh, const PagedAttn& p, const Workspace& ws, hipStream_t stream);
+int launch_paged8_chunk_f32(const actqkv_shape& sh, const PagedAttn& p, const Workspace& ws, hipStream_t stream);
+int launch_paged8_step(const actqkv_shape& sh, const PagedAttn& p, const Workspace& ws, hipStream_t stream);
+size_t paged_selected_scratch_most(const actqkv_shape& sh, int n_rows);
+int launch_paged_selected(const actqkv_shape& sh, const PagedAttn& p, const int32_t* idx, const int32_t* n_sel, int k_sel,
+                          const Workspace& ws, hipStream_t stream);
 size_t paged_chunk_scratch_most(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages);
 int launch_paged_chunk(const actqkv_shape& sh, const PagedAttn& p, const Workspace& ws, hipStream_t stream);
 size_t paged_chunk_f32_scratch_most(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages);
@@ -242,6 +265,21 @@ size_t paged_votes_scratch_most(const actqkv_shape& sh);
 int launch_paged_votes(const actqkv_shape& sh, const PagedAttn& p, const PagedWeights& w, const Workspace& ws, hipStream_t stream);
 int launch_paged_append(const actqkv_shape& sh, const PagedTable& t, const void* k_new, const void* v_new,
                         void* k_pages, void* v_pages, hipStream_t stream);
+// Rotation of keys and queries by their position (paged_rotate.h).
+struct PagedRotation {
+  const float* table;        // [n_positions][2][dims / 2]: cosines, sines; NULL: none (dims 0)
+  int n_positions, dims;
+  bool interleaved;
+  const int32_t* row_pos;    // [n_rows] or NULL: the rows' own positions
+};
+int launch_paged_append_rotated(const actqkv_shape& sh, const PagedTable& t, const PagedRotation& r, const void* q, const void* k_new,
+                                const void* v_new, void* k_pages, void* v_pages, void* q_out, hipStream_t stream);
+int launch_paged_append_quantised(const actqkv_shape& sh, const PagedTable& t, const PagedRotation& r, const void* q, const void* k_new,
+                             const void* v_new, uint8_t* k_pages, uint8_t* v_pages, float* k_scales, float* v_scales, void* q_out,
+                             hipStream_t stream);
+int launch_paged_bounds(const actqkv_shape& sh, const PagedTable& t, const void* k_pages, void* bounds, hipStream_t stream);
+int launch_paged_select(const actqkv_shape& sh, const PagedTable& t, const void* q, const void* bounds, int k_sel, int keep_first,
+                        int keep_last, float* scores, int64_t stride, int32_t* idx, int32_t* n_sel, hipStream_t stream);
 struct PagedEvict {
   PagedTable t;
   void* k_pages;

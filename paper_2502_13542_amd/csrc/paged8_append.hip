@@ -1,0 +1,224 @@
+// Keys and values of a ragged batch's new tokens into pages held in 8 bits (e4m3.h), the keys turned by their position on the way if
+// a rotation is given, and the queries with them.
+//
+// A workgroup takes the new tokens of one (sequence, KV head) that fall into one page, its keys or its values: it holds them in
+// registers, finds the largest of them and with it the page's scale, 2^e with the least e that leaves all of them within 448 2^e.  A
+// page that held tokens before keeps its scale, unless the new ones need a larger one: then its old codes are rounded to that.  Rotated keys are
+// formed in 64 bits and rounded to fp32 before they become codes, so that a key next to the border between two codes goes to
+// the right one.  Values go through LDS four neighbouring tokens a word.  Bound by HBM, a step by its launch.
+#include "e4m3.h"
+#include "paged_rotate.h"
+
+namespace actqkv {
+
+struct PagedAppend8 {
+  PagedTable t;
+  PagedRotation r;
+  const void *k_new, *v_new, *q;           // q may be NULL
+  void* q_out;
+  uint8_t *k_pages, *v_pages;
+  float *k_scales, *v_scales;              // [n_pages][Hk]
+  int n_kv_heads, group;
+  int slices, pages;
+};
+// The new tokens of a page: slots [j0, j0 + n), the first of them row `row`.
+struct NewTokens {
+  int page, j0, n, row, pos;
+};
+
+// The scale's exponent: of the new values' largest, and of the old one where the page held tokens; `again`: the factor of the old
+// codes, 1 where nothing changes.
+__device__ __forceinline__ int page_exponent(float most, const NewTokens& w, float* scale, float* red, float& again) {
+  most = block_max(most, red);
+  int e = e4m3_exponent_for(most);
+  again = 1.f;
+  if (w.j0 > 0) {
+    const int old = e4m3_exponent(*scale);
+    again = pow2f(max(old - max(old, e), -126));
+    e = max(old, e);
+  }
+  __syncthreads();                                // (everybody has read the old one)
+  if (threadIdx.x == 0) *scale = pow2f(e);
+  return e;
+}
+
+template <typename T, int D>
+__device__ __forceinline__ void append8_keys(const PagedAppend8& a, const NewTokens& w, int hk, float* red) {
+  constexpr int V = Vec<T>::N, kPairs = D / (2 * V), kRows = kTurnThreads / kPairs, kEach = kBlock / kRows;
+  typedef typename Vec<T>::raw raw_t;
+  const int p = threadIdx.x % kPairs, j = threadIdx.x / kPairs;       // of the new tokens, j, j + kRows, ...
+  const TurnPair at = turn_pair<V>(a.r, p);
+  const T* from = static_cast<const T*>(a.k_new) + (size_t(w.row) * a.n_kv_heads + hk) * D;
+  raw_t x[kEach][2];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int tok = i * kRows + j;
+    if (tok < w.n) {
+      x[i][0] = Vec<T>::load_raw(from + size_t(tok) * a.n_kv_heads * D + at.a);
+      x[i][1] = Vec<T>::load_raw(from + size_t(tok) * a.n_kv_heads * D + at.b);
+    }
+  }
+  float k[kEach][2][V], most = 0.f;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int tok = i * kRows + j;
+    if (tok < w.n) {
+      Vec<T>::widen(x[i][0], k[i][0]);
+      Vec<T>::widen(x[i][1], k[i][1]);
+      if (at.turns) {
+        TurnBy<V> by;
+        by.load(a.r, w.row + tok, w.pos + tok, p);
+        turn<double, V>(by, a.r.interleaved, k[i][0], k[i][1]);
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) most = largest(largest(most, k[i][0][e]), k[i][1][e]);
+    }
+  }
+  const size_t tile = (size_t(w.page) * a.n_kv_heads + hk) * (kBlock * D);
+  float again;
+  const float by = pow2f(-page_exponent(most, w, a.k_scales + size_t(w.page) * a.n_kv_heads + hk, red, again));
+  if (again != 1.f) {
+    for (int i = threadIdx.x; i < w.j0 * (D / 16); i += kTurnThreads) {
+      u32x4* to = reinterpret_cast<u32x4*>(a.k_pages + tile) + i;
+      u32x4 c = *to;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c[e] = e4m3_again(c[e], again);
+      *to = c;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int tok = i * kRows + j;
+    if (tok < w.n) {
+      uint8_t* to = a.k_pages + tile + size_t(w.j0 + tok) * D;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < V; e += 4)
+          *reinterpret_cast<uint32_t*>(to + (h ? at.b : at.a) + e) =
+              e4m3_pack(k[i][h][e] * by, k[i][h][e + 1] * by, k[i][h][e + 2] * by, k[i][h][e + 3] * by);
+    }
+  }
+}
+
+constexpr int kV8Pad = kBlock / 4 + 1;           // words of a channel in LDS
+template <typename T, int D>
+__device__ __forceinline__ void append8_values(const PagedAppend8& a, const NewTokens& w, int hk, float* red, uint32_t* vt) {
+  constexpr int V = Vec<T>::N, kChunks = D / V, kEach = kBlock / 4 * kChunks / kTurnThreads;
+  typedef typename Vec<T>::raw raw_t;
+  const T* from = static_cast<const T*>(a.v_new) + (size_t(w.row) * a.n_kv_heads + hk) * D;
+  raw_t x[kEach][4];
+  float most = 0.f;
+#pragma unroll
+  for (int n = 0; n < kEach; ++n) {
+    const int i = n * kTurnThreads + threadIdx.x, j = i / kChunks * 4 - w.j0, c = i % kChunks;
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+      x[n][h] = j + h >= 0 && j + h < w.n ? Vec<T>::load_raw(from + size_t(j + h) * a.n_kv_heads * D + c * V) : raw_t{};
+  }
+#pragma unroll
+  for (int n = 0; n < kEach; ++n)
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      float v[V];
+      Vec<T>::widen(x[n][h], v);
+#pragma unroll
+      for (int e = 0; e < V; ++e) most = largest(most, v[e]);
+    }
+  uint8_t* tile = a.v_pages + (size_t(w.page) * a.n_kv_heads + hk) * (kBlock * D);
+  float again;
+  const float by = pow2f(-page_exponent(most, w, a.v_scales + size_t(w.page) * a.n_kv_heads + hk, red, again));
+#pragma unroll
+  for (int n = 0; n < kEach; ++n) {
+    const int i = n * kTurnThreads + threadIdx.x, j = i / kChunks * 4 - w.j0, c = i % kChunks;
+    if (j + 3 < 0 || j >= w.n) continue;
+    float v[4][V];
+#pragma unroll
+    for (int h = 0; h < 4; ++h) Vec<T>::widen(x[n][h], v[h]);
+#pragma unroll
+    for (int e = 0; e < V; ++e) vt[(c * V + e) * kV8Pad + i / kChunks] = e4m3_pack(v[0][e] * by, v[1][e] * by, v[2][e] * by, v[3][e] * by);
+  }
+  __syncthreads();
+  const int end = w.j0 + w.n, g0 = again != 1.f ? 0 : w.j0 / 16, groups = (end - 1) / 16 - g0 + 1;
+  for (int i = threadIdx.x; i < D * groups; i += kTurnThreads) {
+    const int d = i / groups, j = (g0 + i - d * groups) * 16;
+    const uint32_t* words = vt + d * kV8Pad + j / 4;
+    uint8_t* to = tile + size_t(d) * kBlock + j;
+    if (j >= w.j0 && j + 16 <= end) {
+      *reinterpret_cast<u32x4*>(to) = u32x4{words[0], words[1], words[2], words[3]};
+    } else if (again != 1.f) {
+      u32x4 c = *reinterpret_cast<const u32x4*>(to);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int slot = j + 4 * e;
+        uint32_t old = 0, fresh = 0;             // masks of the word's bytes
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          old |= slot + b < w.j0 ? 0xffu << (8 * b) : 0u;
+          fresh |= slot + b >= w.j0 && slot + b < end ? 0xffu << (8 * b) : 0u;
+        }
+        c[e] = (c[e] & ~(old | fresh)) | (e4m3_again(c[e], again) & old) | (fresh != 0 ? words[e] & fresh : 0u);
+      }
+      *reinterpret_cast<u32x4*>(to) = c;
+    } else {
+      for (int b = max(w.j0 - j, 0); b < min(16, end - j); ++b) to[b] = uint8_t(words[b / 4] >> (8 * (b % 4)));
+    }
+  }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kTurnThreads) void paged8_append_kernel(PagedAppend8 a) {
+  __shared__ uint32_t vt[D * kV8Pad];            // [channel][four slots]
+  __shared__ float red[32];
+  const int hk = blockIdx.x >> 1, role = blockIdx.x & 1, s = blockIdx.z;
+  const PagedSeq seq = paged_seq(a.t, s);
+  if (seq.m == 0) return;
+  const int pos0 = seq.n - seq.m, first = max(pos0, 0) / kBlock;
+  for (int y = blockIdx.y; y < a.pages + (a.slices + 1) / 2; y += gridDim.y) {
+    if (y >= a.pages) {
+      const int slice = (y - a.pages) * 2 + role;
+      turn_rows<T, D, false>(a.t, a.r, seq, s, hk, a.n_kv_heads, a.group, slice, nullptr, nullptr, static_cast<const T*>(a.q),
+                             static_cast<T*>(a.q_out));
+      continue;
+    }
+    const int index = first + y, lo = max(max(pos0, 0), index * kBlock), hi = min(seq.n, index * kBlock + kBlock);
+    if (hi <= lo) continue;                      // (index < max_pages: hi > index * kBlock)
+    const NewTokens w{paged_page(a.t, s, index), lo - index * kBlock, hi - lo, seq.row0 + lo - pos0, lo};
+    if (w.page < 0) continue;
+    if (role == 0) append8_keys<T, D>(a, w, hk, red);
+    else append8_values<T, D>(a, w, hk, red, vt);
+    __syncthreads();
+  }
+}
+
+int launch_paged_append_quantised(const actqkv_shape& sh, const PagedTable& t, const PagedRotation& r, const void* q, const void* k_new,
+                             const void* v_new, uint8_t* k_pages, uint8_t* v_pages, float* k_scales, float* v_scales, void* q_out,
+                             hipStream_t stream) {
+  PagedAppend8 a;
+  a.t = t;
+  a.r = r;
+  a.q = q;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.q_out = q_out;
+  a.k_pages = k_pages;
+  a.v_pages = v_pages;
+  a.k_scales = k_scales;
+  a.v_scales = v_scales;
+  a.n_kv_heads = sh.n_kv_heads;
+  a.group = sh.n_q_heads / sh.n_kv_heads;
+  a.slices = q != nullptr ? turn_slices(sh, t.max_new) : 0;
+  a.pages = std::min(t.max_pages, (t.max_new + kBlock - 2) / kBlock + 1);
+  const dim3 grid(2 * sh.n_kv_heads, std::min(a.pages + (a.slices + 1) / 2, kTurnMostY), t.batch);
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kTurnThreads), 0, stream, a); };
+  if (sh.dtype == ACTQKV_F32) {
+    if (sh.head_dim == 64) launch(paged8_append_kernel<float, 64>);
+    else launch(paged8_append_kernel<float, 128>);
+  } else {
+    if (sh.head_dim == 64) launch(paged8_append_kernel<uint16_t, 64>);
+    else launch(paged8_append_kernel<uint16_t, 128>);
+  }
+  return hip_status("paged append (8 bits)");
+}
+
+}  // namespace actqkv

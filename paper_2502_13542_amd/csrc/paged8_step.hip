@@ -1,0 +1,39 @@
+// Attention over a paged cache in 8 bits of sequences that bring few rows (paged_step_body.h has the kernel, paged8_shape.h the operands
+// of an item, a page of 128 keys: as many bytes on their way as of 64 keys in 16 bits).
+#include "paged8_shape.h"
+#include "paged_step_body.h"
+
+namespace actqkv {
+
+template <typename T, int D, bool kCap, bool kBias>
+__global__ __launch_bounds__(kStThreads) void paged8_step_kernel(PagedStep st) {
+  step_body<Step8Shape<T, D>, T, D, kCap, kBias, false>(st);
+}
+template <typename T, int D>
+static void launch_step8(const PagedStep& st, hipStream_t stream) {
+  const bool cap = st.a.f.cap_in > 0.f, bias = st.a.f.slopes != nullptr;
+  auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(st.n_wg, st.a.n_kv_heads, st.a.t.batch), dim3(kStThreads), 0, stream, st);
+  };
+  if (cap && bias) launch(paged8_step_kernel<T, D, true, true>);
+  else if (cap) launch(paged8_step_kernel<T, D, true, false>);
+  else if (bias) launch(paged8_step_kernel<T, D, false, true>);
+  else launch(paged8_step_kernel<T, D, false, false>);
+}
+int launch_paged8_step(const actqkv_shape& sh, const PagedAttn& p, const Workspace& ws, hipStream_t stream) {
+  PagedStep st = {};
+  st.a = p;
+  st.n_wg = step_workgroups(int64_t(p.t.batch) * sh.n_kv_heads, p.t.max_pages, step_least(kBlock, sh.head_dim, 1));
+  st.part = reinterpret_cast<uint32_t*>(ws.scratch_f32());
+  st.counters = ws.counters();
+  if (sh.dtype == ACTQKV_F32) {
+    if (sh.head_dim == 64) launch_step8<float, 64>(st, stream);
+    else launch_step8<float, 128>(st, stream);
+  } else {
+    if (sh.head_dim == 64) launch_step8<uint16_t, 64>(st, stream);
+    else launch_step8<uint16_t, 128>(st, stream);
+  }
+  return hip_status("paged attention (8 bits, few rows)");
+}
+
+}  // namespace actqkv

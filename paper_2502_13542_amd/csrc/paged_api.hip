@@ -9,22 +9,24 @@ namespace actqkv {
 // Which kernels a call takes: few rows per sequence or chunks, by the storage type; the votes behind them.
 static int launch_paged_attention(const actqkv_shape& sh, PagedAttn p, const PagedWeights* weights, const Workspace& ws,
                                   hipStream_t stream) {
-  if (paged_step_supported(sh, p.t.max_new)) return launch_paged_step(sh, p, weights, ws, stream);
+  const bool byte = p.k_scales != nullptr;                        // (an 8-bit cache has no account)
+  if (paged_step_supported(sh, p.t.max_new)) return byte ? launch_paged8_step(sh, p, ws, stream) : launch_paged_step(sh, p, weights, ws, stream);
   // Sequences of a batch that bring few rows go through the step kernel, in a launch of their own of about 15 us, if they may
   // be so many that their pages, read for a query tile each, would take longer (2 us a page and workgroup).
   const int group = sh.n_q_heads / sh.n_kv_heads, few_rows = 16 / group;
   const int64_t more = std::max<int64_t>(0, int64_t(p.t.n_rows) - int64_t(p.t.batch) * few_rows);
   const int64_t few_most = p.t.batch - (more + p.t.max_new - 1) / p.t.max_new;
   if (few_most * p.t.max_pages * sh.n_kv_heads * 2 > int64_t(20) * kChipCus) {
-    ACTQKV_TRY(launch_paged_step(sh, p, nullptr, ws, stream));
+    ACTQKV_TRY(byte ? launch_paged8_step(sh, p, ws, stream) : launch_paged_step(sh, p, nullptr, ws, stream));
     p.t.few = 16;
   }
+  if (byte) return sh.dtype == ACTQKV_F32 ? launch_paged8_chunk_f32(sh, p, ws, stream) : launch_paged8_chunk(sh, p, ws, stream);
   ACTQKV_TRY(sh.dtype == ACTQKV_F32 ? launch_paged_chunk_f32(sh, p, ws, stream) : launch_paged_chunk(sh, p, ws, stream));
   return weights != nullptr ? launch_paged_votes(sh, p, *weights, ws, stream) : ACTQKV_OK;
 }
 // Enough for every call of at most these sizes: of few rows a sequence, none of them takes the chunks' kernels.
 static size_t paged_workspace_bytes(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages) {
-  size_t most = paged_step_scratch_most(sh, batch, max_new, max_pages);
+  size_t most = std::max(paged_step_scratch_most(sh, batch, max_new, max_pages), paged_selected_scratch_most(sh, n_rows));
   if (!paged_step_supported(sh, max_new))
     most = std::max({most, paged_votes_scratch_most(sh),
                      sh.dtype == ACTQKV_F32 ? paged_chunk_f32_scratch_most(sh, batch, n_rows, max_new, max_pages)
@@ -58,11 +60,47 @@ static int check_rows(int n_rows, int max_new) {
   return ACTQKV_OK;
 }
 
+// Lists of selected pages: of every (row, KV head) k_sel entries.
+struct PagedChosen {
+  const int32_t *idx, *n_sel;
+  int k_sel;
+};
+static int check_k_sel(const actqkv_shape* shape, int n_rows, int k_sel) {
+  if (k_sel < 1) return set_error(ACTQKV_EINVAL, "k_sel %d < 1", k_sel);
+  if (k_sel > kMaxPages) return set_error(ACTQKV_ESHAPE, "k_sel %d > %d", k_sel, kMaxPages);
+  // (a launch has less than 2^32 threads: 512 for a row and KV head)
+  if (int64_t(n_rows) * shape->n_kv_heads > 1 << 22)
+    return set_error(ACTQKV_ESHAPE, "%d rows of %d KV heads > 2^22", n_rows, shape->n_kv_heads);
+  return ACTQKV_OK;
+}
+// Rotation of `dims` channels by a table; table NULL: none, where that is allowed.
+static int check_rotation(const actqkv_shape* shape, bool required, const void* q, const float* rotation, int n_positions, int rotary_dim,
+                          int interleaved, const int32_t* row_pos, const void* q_out, PagedRotation* r) {
+  *r = PagedRotation{nullptr, 0, 0, false, nullptr};
+  if (rotation == nullptr && !required) {
+    if (q != nullptr || q_out != nullptr || row_pos != nullptr || rotary_dim != 0)
+      return set_error(ACTQKV_EINVAL, "q, q_out, row_pos or rotary_dim without a rotation");
+    return ACTQKV_OK;
+  }
+  ACTQKV_REQUIRE_PTR(rotation);
+  if (n_positions < 1) return set_error(ACTQKV_EINVAL, "n_positions %d < 1", n_positions);
+  if (rotary_dim < 16 || rotary_dim > shape->head_dim || rotary_dim % 16 != 0)
+    return set_error(ACTQKV_ESHAPE, "rotary_dim %d is not a multiple of 16 up to head_dim %d", rotary_dim, shape->head_dim);
+  if (interleaved != 0 && interleaved != 1) return set_error(ACTQKV_EINVAL, "interleaved %d is neither 0 nor 1", interleaved);
+  ACTQKV_OPTIONAL_SMALL(row_pos, 4);
+  ACTQKV_OPTIONAL_PTR(q);
+  ACTQKV_OPTIONAL_PTR(q_out);
+  if ((q == nullptr) != (q_out == nullptr)) return set_error(ACTQKV_EINVAL, "q without q_out, or q_out without q");
+  *r = PagedRotation{rotation, n_positions, rotary_dim, interleaved != 0, row_pos};
+  return ACTQKV_OK;
+}
+
 static int attention_call(const char* name, const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q,
                           const int32_t* row_start, const int32_t* n_ctx, const int32_t* pages, int max_pages,
                           const void* k_pages, const void* v_pages, int n_pages, float softcap, int window,
                           const float* slopes, const int32_t* row_first, const int32_t* row_end, void* out, float* lse,
-                          const PagedWeights* weights, void* workspace, size_t ws_bytes, void* stream) {
+                          const PagedWeights* weights, const float* k_scales, const float* v_scales, const PagedChosen* chosen,
+                          void* workspace, size_t ws_bytes, void* stream) {
   ACTQKV_TRY(check_table(shape, batch, n_ctx, pages, max_pages, k_pages, v_pages, n_pages));
   ACTQKV_TRY(check_rows(n_rows, max_new));
   // (a launch has less than 2^32 threads: 512 for 64 (row, query head) pairs or, of the account, 128 tokens of a KV head)
@@ -90,6 +128,12 @@ static int attention_call(const char* name, const actqkv_shape* shape, int batch
       return set_error(ACTQKV_EINVAL, "weight_stride %lld < %d pages of %d tokens", (long long)weights->stride, max_pages, kBlock);
     if (weights->stride % 4 != 0) return set_error(ACTQKV_EALIGN, "weight_stride must be a multiple of 4");
   }
+  if (chosen != nullptr) {
+    const int32_t *idx = chosen->idx, *n_sel = chosen->n_sel;
+    ACTQKV_TRY(check_k_sel(shape, n_rows, chosen->k_sel));
+    ACTQKV_REQUIRE_SMALL(idx, 4);
+    ACTQKV_REQUIRE_SMALL(n_sel, 4);
+  }
   if (workspace == nullptr || !aligned16(workspace))
     return set_error(ACTQKV_EWORKSPACE, "workspace is NULL or not 16-byte aligned");
   const size_t need = paged_workspace_bytes(*shape, batch, n_rows, max_new, max_pages);
@@ -106,6 +150,11 @@ static int attention_call(const char* name, const actqkv_shape* shape, int batch
   p.v_pages = v_pages;
   p.out = out;
   p.lse = lse;
+  p.k_scales = k_scales;
+  p.v_scales = v_scales;
+  if (chosen != nullptr)
+    return launch_paged_selected(*shape, p, chosen->idx, chosen->n_sel, chosen->k_sel, Workspace{workspace, ws_bytes},
+                                 static_cast<hipStream_t>(stream));
   return launch_paged_attention(*shape, p, weights, Workspace{workspace, ws_bytes}, static_cast<hipStream_t>(stream));
 }
 
@@ -143,8 +192,8 @@ int actqkv_paged_attention(const actqkv_shape* shape, int batch, int n_rows, int
                            const float* slopes, const int32_t* row_first, const int32_t* row_end, void* out, float* lse,
                            void* workspace, size_t ws_bytes, void* stream) {
   return attention_call("paged_attention", shape, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, k_pages,
-                        v_pages, n_pages, softcap, window, slopes, row_first, row_end, out, lse, nullptr, workspace,
-                        ws_bytes, stream);
+                        v_pages, n_pages, softcap, window, slopes, row_first, row_end, out, lse, nullptr, nullptr, nullptr,
+                        nullptr, workspace, ws_bytes, stream);
 }
 
 int actqkv_paged_attention_weights(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q,
@@ -155,8 +204,102 @@ int actqkv_paged_attention_weights(const actqkv_shape* shape, int batch, int n_r
                                    int64_t weight_stride, void* workspace, size_t ws_bytes, void* stream) {
   const PagedWeights w{weight_rows, weights_in, weights_out, weight_stride};
   return attention_call("paged_attention_weights", shape, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages,
-                        k_pages, v_pages, n_pages, softcap, window, slopes, row_first, row_end, out, lse, &w, workspace,
-                        ws_bytes, stream);
+                        k_pages, v_pages, n_pages, softcap, window, slopes, row_first, row_end, out, lse, &w, nullptr, nullptr,
+                        nullptr, workspace, ws_bytes, stream);
+}
+
+int actqkv_paged_append_rotated(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q, const void* k_new,
+                                const void* v_new, const int32_t* row_start, const int32_t* n_ctx, const int32_t* pages,
+                                int max_pages, void* k_pages, void* v_pages, int n_pages, const float* rotation, int n_positions,
+                                int rotary_dim, int interleaved, const int32_t* row_pos, void* q_out, void* stream) {
+  ACTQKV_TRY(check_table(shape, batch, n_ctx, pages, max_pages, k_pages, v_pages, n_pages));
+  ACTQKV_TRY(check_rows(n_rows, max_new));
+  ACTQKV_REQUIRE_PTR(k_new);
+  ACTQKV_REQUIRE_PTR(v_new);
+  ACTQKV_REQUIRE_SMALL(row_start, 4);
+  PagedRotation r;
+  ACTQKV_TRY(check_rotation(shape, true, q, rotation, n_positions, rotary_dim, interleaved, row_pos, q_out, &r));
+  const PagedTable t{row_start, n_ctx, pages, batch, n_rows, max_new, max_pages, n_pages, 0};
+  return launch_paged_append_rotated(*shape, t, r, q, k_new, v_new, k_pages, v_pages, q_out, static_cast<hipStream_t>(stream));
+}
+
+int actqkv_paged_append_quantised(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q, const void* k_new,
+                             const void* v_new, const int32_t* row_start, const int32_t* n_ctx, const int32_t* pages,
+                             int max_pages, void* k_pages, void* v_pages, int n_pages, float* k_scales, float* v_scales,
+                             const float* rotation, int n_positions, int rotary_dim, int interleaved, const int32_t* row_pos,
+                             void* q_out, void* stream) {
+  ACTQKV_TRY(check_table(shape, batch, n_ctx, pages, max_pages, k_pages, v_pages, n_pages));
+  ACTQKV_TRY(check_rows(n_rows, max_new));
+  ACTQKV_REQUIRE_PTR(k_new);
+  ACTQKV_REQUIRE_PTR(v_new);
+  ACTQKV_REQUIRE_SMALL(row_start, 4);
+  ACTQKV_REQUIRE_SMALL(k_scales, 4);
+  ACTQKV_REQUIRE_SMALL(v_scales, 4);
+  if (k_scales == v_scales) return set_error(ACTQKV_EINVAL, "k_scales is v_scales");
+  PagedRotation r;
+  ACTQKV_TRY(check_rotation(shape, false, q, rotation, n_positions, rotary_dim, interleaved, row_pos, q_out, &r));
+  const PagedTable t{row_start, n_ctx, pages, batch, n_rows, max_new, max_pages, n_pages, 0};
+  return launch_paged_append_quantised(*shape, t, r, q, k_new, v_new, static_cast<uint8_t*>(k_pages), static_cast<uint8_t*>(v_pages),
+                                  k_scales, v_scales, q_out, static_cast<hipStream_t>(stream));
+}
+
+int actqkv_paged_attention_quantised(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q,
+                                const int32_t* row_start, const int32_t* n_ctx, const int32_t* pages, int max_pages,
+                                const void* k_pages, const void* v_pages, int n_pages, const float* k_scales,
+                                const float* v_scales, float softcap, int window, const float* slopes, const int32_t* row_first,
+                                const int32_t* row_end, void* out, float* lse, void* workspace, size_t ws_bytes, void* stream) {
+  ACTQKV_TRY(check_shape(shape));
+  ACTQKV_REQUIRE_SMALL(k_scales, 4);
+  ACTQKV_REQUIRE_SMALL(v_scales, 4);
+  return attention_call("paged_attention_quantised", shape, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, k_pages,
+                        v_pages, n_pages, softcap, window, slopes, row_first, row_end, out, lse, nullptr, k_scales, v_scales,
+                        nullptr, workspace, ws_bytes, stream);
+}
+
+int actqkv_paged_key_bounds(const actqkv_shape* shape, int batch, int n_rows, int max_new, const int32_t* row_start,
+                            const int32_t* n_ctx, const int32_t* pages, int max_pages, const void* k_pages, int n_pages,
+                            void* bounds, void* stream) {
+  ACTQKV_TRY(check_table(shape, batch, n_ctx, pages, max_pages, k_pages, k_pages, n_pages));
+  if (row_start != nullptr) ACTQKV_TRY(check_rows(n_rows, max_new));
+  ACTQKV_OPTIONAL_SMALL(row_start, 4);
+  ACTQKV_REQUIRE_PTR(bounds);
+  if (bounds == k_pages) return set_error(ACTQKV_EINVAL, "bounds is k_pages");
+  const PagedTable t{row_start, n_ctx, pages, batch, n_rows, max_new, max_pages, n_pages, 0};
+  return launch_paged_bounds(*shape, t, k_pages, bounds, static_cast<hipStream_t>(stream));
+}
+
+int actqkv_paged_select_pages(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q, const int32_t* row_start,
+                              const int32_t* n_ctx, const int32_t* pages, int max_pages, const void* bounds, int n_pages, int k_sel,
+                              int keep_first, int keep_last, float* scores, int64_t score_stride, int32_t* idx, int32_t* n_sel,
+                              void* stream) {
+  ACTQKV_TRY(check_shape(shape));
+  ACTQKV_REQUIRE_PTR(bounds);
+  ACTQKV_TRY(check_table(shape, batch, n_ctx, pages, max_pages, bounds, bounds, n_pages));
+  ACTQKV_TRY(check_rows(n_rows, max_new));
+  ACTQKV_TRY(check_k_sel(shape, n_rows, k_sel));
+  if (keep_first < 0 || keep_last < 0 || int64_t(keep_first) + keep_last > k_sel)
+    return set_error(ACTQKV_EINVAL, "keep_first %d, keep_last %d negative or together more than k_sel %d", keep_first, keep_last, k_sel);
+  ACTQKV_REQUIRE_PTR(q);
+  ACTQKV_REQUIRE_SMALL(row_start, 4);
+  ACTQKV_REQUIRE_SMALL(scores, 4);
+  if (score_stride < max_pages)
+    return set_error(ACTQKV_EINVAL, "score_stride %lld < max_pages %d", (long long)score_stride, max_pages);
+  ACTQKV_REQUIRE_SMALL(idx, 4);
+  ACTQKV_REQUIRE_SMALL(n_sel, 4);
+  const PagedTable t{row_start, n_ctx, pages, batch, n_rows, max_new, max_pages, n_pages, 0};
+  return launch_paged_select(*shape, t, q, bounds, k_sel, keep_first, keep_last, scores, score_stride, idx, n_sel,
+                             static_cast<hipStream_t>(stream));
+}
+
+int actqkv_paged_attention_selected(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q,
+                                    const int32_t* row_start, const int32_t* n_ctx, const int32_t* pages, int max_pages,
+                                    const void* k_pages, const void* v_pages, int n_pages, const int32_t* idx, const int32_t* n_sel,
+                                    int k_sel, float softcap, int window, const float* slopes, const int32_t* row_first,
+                                    const int32_t* row_end, void* out, float* lse, void* workspace, size_t ws_bytes, void* stream) {
+  const PagedChosen chosen{idx, n_sel, k_sel};
+  return attention_call("paged_attention_selected", shape, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, k_pages,
+                        v_pages, n_pages, softcap, window, slopes, row_first, row_end, out, lse, nullptr, nullptr, nullptr, &chosen,
+                        workspace, ws_bytes, stream);
 }
 
 int actqkv_paged_evict(const actqkv_shape* shape, int batch, const int32_t* n_ctx, const int32_t* pages, int max_pages,

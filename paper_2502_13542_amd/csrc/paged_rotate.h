@@ -1,0 +1,125 @@
+// Rotation of keys and queries by their position, on the way into the paged cache.
+//
+// The first `dims` of a head's channels are taken in pairs (a, b), channels (i, i + dims / 2) or, interleaved, (2 i, 2 i + 1), and pair i
+// of a row becomes (a cos - b sin, b cos + a sin) with row `position` of a table [n_positions][2][dims / 2] of cosines, then sines.
+//
+// A thread turns two 16-byte chunks of a head, the same two of several heads of a row: cosines and sines are read once for all of them.
+#pragma once
+
+#include "paged.h"
+
+namespace actqkv {
+
+constexpr int kTurnThreads = 256;
+constexpr int kTurnMostY = 32768;          // workgroups along y: more work goes round
+
+// Chunks a thread's pair is made of: their first channels, and whether they turn (behind `dims` they are just two neighbours).
+struct TurnPair {
+  int a, b;
+  bool turns;
+};
+template <int V>
+__device__ __forceinline__ TurnPair turn_pair(const PagedRotation& r, int p) {
+  TurnPair c;
+  c.turns = p * (2 * V) < r.dims;
+  const bool apart = c.turns && !r.interleaved;
+  c.a = apart ? p * V : 2 * p * V;
+  c.b = apart ? r.dims / 2 + p * V : c.a + V;
+  return c;
+}
+// Cosines and sines of a thread's V pairs at the row's position (clamped to the table).
+template <int V>
+struct TurnBy {
+  alignas(16) float c[V];
+  alignas(16) float s[V];
+  __device__ __forceinline__ void load(const PagedRotation& r, int row, int pos, int p) {
+    const int at = min(max(r.row_pos != nullptr ? r.row_pos[row] : pos, 0), r.n_positions - 1);
+    const float* from = r.table + size_t(at) * r.dims + p * V;
+#pragma unroll
+    for (int i = 0; i < V; i += 4) {
+      *reinterpret_cast<f32x4*>(c + i) = *reinterpret_cast<const f32x4*>(from + i);
+      *reinterpret_cast<f32x4*>(s + i) = *reinterpret_cast<const f32x4*>(from + r.dims / 2 + i);
+    }
+  }
+};
+// W: the type the products are formed in.
+template <typename W, int V>
+__device__ __forceinline__ void turn(const TurnBy<V>& by, bool interleaved, float (&a)[V], float (&b)[V]) {
+  auto one = [](float& x, float& y, float c, float s) {
+    const W x0 = x, y0 = y, c0 = c, s0 = s;
+    x = float(x0 * c0 - y0 * s0);
+    y = float(y0 * c0 + x0 * s0);
+  };
+  if (interleaved) {
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+      one(a[2 * i], a[2 * i + 1], by.c[i], by.s[i]);
+      one(b[2 * i], b[2 * i + 1], by.c[V / 2 + i], by.s[V / 2 + i]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) one(a[i], b[i], by.c[i], by.s[i]);
+  }
+}
+__device__ __forceinline__ f32x4 narrow(const float (&x)[4], f32x4*) { return f32x4{x[0], x[1], x[2], x[3]}; }
+__device__ __forceinline__ u32x4 narrow(const float (&x)[8], u32x4*) {
+  return u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+}
+
+// Slice `slice` of a sequence's rows: their query heads of KV head hk, and their keys (kKeys), turned.  Products in fp32, each result
+// rounded once to the storage type.
+template <typename T, int D, bool kKeys>
+__device__ __forceinline__ void turn_rows(const PagedTable& t, const PagedRotation& r, const PagedSeq& seq, int s, int hk, int n_kv_heads,
+                                          int group, int slice, const T* k_new, T* k_pages, const T* q, T* q_out) {
+  constexpr int V = Vec<T>::N, kPairs = D / (2 * V), kRows = kTurnThreads / kPairs, kHeads = 4;
+  typedef typename Vec<T>::raw raw_t;
+  const int i = slice * kRows + threadIdx.x / kPairs, p = threadIdx.x % kPairs;
+  const int pos = seq.n - seq.m + i, row = seq.row0 + i;
+  if (i >= seq.m || pos < 0) return;             // (a row at a negative position is not in the cache)
+  const TurnPair at = turn_pair<V>(r, p);
+  TurnBy<V> by;
+  if (at.turns) by.load(r, row, pos, p);
+  auto move = [&](raw_t x, raw_t y, T* to) {
+    if (at.turns) {
+      float a[V], b[V];
+      Vec<T>::widen(x, a);
+      Vec<T>::widen(y, b);
+      turn<float, V>(by, r.interleaved, a, b);
+      x = narrow(a, static_cast<raw_t*>(nullptr));
+      y = narrow(b, static_cast<raw_t*>(nullptr));
+    }
+    *reinterpret_cast<raw_t*>(to + at.a) = x;
+    *reinterpret_cast<raw_t*>(to + at.b) = y;
+  };
+  raw_t ka, kb;
+  int page = -1;
+  if (kKeys) {
+    const T* from = k_new + (size_t(row) * n_kv_heads + hk) * D;
+    ka = Vec<T>::load_raw(from + at.a);
+    kb = Vec<T>::load_raw(from + at.b);
+    page = paged_page(t, s, pos / kBlock);
+  }
+  if (q != nullptr) {
+    const size_t head0 = (size_t(row) * n_kv_heads + hk) * group * D;
+    for (int h0 = 0; h0 < group; h0 += kHeads) {
+      raw_t x[kHeads], y[kHeads];
+#pragma unroll
+      for (int h = 0; h < kHeads; ++h) {
+        const T* from = q + head0 + min(h0 + h, group - 1) * D;
+        x[h] = Vec<T>::load_raw(from + at.a);
+        y[h] = Vec<T>::load_raw(from + at.b);
+      }
+#pragma unroll
+      for (int h = 0; h < kHeads; ++h)
+        if (h0 + h < group) move(x[h], y[h], q_out + head0 + (h0 + h) * D);
+    }
+  }
+  if (kKeys && page >= 0) move(ka, kb, k_pages + ((size_t(page) * n_kv_heads + hk) * kBlock + pos % kBlock) * D);
+}
+// Rows of a slice, and slices of a sequence of at most max_new rows.
+inline int turn_slices(const actqkv_shape& sh, int max_new) {
+  const int rows = kTurnThreads / (sh.head_dim / (sh.dtype == ACTQKV_F32 ? 8 : 16));
+  return (max_new + rows - 1) / rows;
+}
+
+}  // namespace actqkv

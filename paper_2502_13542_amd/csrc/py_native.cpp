@@ -10,6 +10,7 @@
 // (a ctypes structure, by its buffer), integers, floats, int32 and fp32 tensors.  Parameters that
 // are plain `void*` take their meaning from a string, one letter per such parameter:
 //   s  tensor of the shape's storage type        b  tensor of bf16, whatever the shape says
+//   e  tensor of e4m3 (float8_e4m3fn)
 //   h  like s, but pinned host memory will do    w  workspace (a size_t parameter follows: its bytes)
 //   p  address (an integer)                      q  stream, None for the current one
 // A string that begins with @ is of a call whose tensors all have to be on the current device (where it launches).
@@ -91,6 +92,7 @@ struct Args {
     switch (*kinds++) {
       case 's': return tensor(storage(), false, false);
       case 'b': return tensor(c10::kBFloat16, false, false);
+      case 'e': return tensor(c10::kFloat8_e4m3fn, false, false);
       case 'h': return tensor(storage(), false, true);
       case 'w': return tensor(c10::kByte, true, false);
       case 'p': {
@@ -240,7 +242,13 @@ template <typename... P> struct Entry<int(P...)> {
   X(paged_append, "@ssssq")                                      \
   X(paged_attention, "@sssswq")                                  \
   X(paged_attention_weights, "@sssswq")                          \
-  X(paged_evict, "@ssq")
+  X(paged_evict, "@ssq")                                         \
+  X(paged_append_rotated, "@ssssssq")                            \
+  X(paged_append_quantised, "@ssseesq")                               \
+  X(paged_attention_quantised, "@seeswq")                             \
+  X(paged_key_bounds, "@ssq")                                    \
+  X(paged_select_pages, "@ssq")                                  \
+  X(paged_attention_selected, "@sssswq")
 
 #define ACTQKV_DEFINE(name, kinds)                                                          \
   Entry<decltype(actqkv_##name)> entry_##name;                                              \

@@ -1010,3 +1010,113 @@ class PagedRunner:
             self._per_row(rows * to_stride, to_weights)
         B.paged_evict(self.cs, batch, n_ctx, pages, max_pages, k_pages, v_pages, n_pages, weights, weights.shape[-1],
                       keep_first, keep_last, budget, to_pages, to_pages.shape[-1], to_weights, to_stride, kept, n_kept, stream)
+
+    # ---- rotation on the way into the cache
+    def _turn(self, n_rows: int, rotation, q, q_out, row_pos, interleaved) -> Tuple[int, int, bool]:
+        """n_positions, rotary_dim and interleaved of a call."""
+        self._per_row(n_rows * self.shape.n_q_heads * self.shape.head_dim, q, q_out)
+        self._per_row(n_rows, row_pos)
+        if rotation is None:
+            return 0, 0, False
+        if rotation.dim() != 3 or rotation.shape[1] != 2:
+            raise B.ActQKVError(-1, "rotation is not [n_positions][2][rotary_dim / 2]")
+        return rotation.shape[0], 2 * rotation.shape[2], bool(interleaved)
+
+    def append_rotated(self, k_new, v_new, row_start, n_ctx, pages, k_pages, v_pages, rotation, q=None, q_out=None, row_pos=None,
+                       interleaved: bool = False, stream=None, max_new=None) -> None:
+        """append, the keys turned by their position, and the queries q [n_rows][H][D] into q_out (q itself: in place; q None:
+        keys alone).  rotation [n_positions][2][rotary_dim / 2] fp32: cosines, sines; row_pos [n_rows]: places of the rows that
+        are not their positions in the cache."""
+        batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, v_pages)
+        n_rows, max_new = self._rows(batch, row_start, k_new, self.shape.n_kv_heads, max_new, v_new)
+        turn = self._turn(n_rows, rotation, q, q_out, row_pos, interleaved)
+        if n_rows == 0:
+            return
+        B.paged_append_rotated(self.cs, batch, n_rows, max_new, q, k_new, v_new, row_start, n_ctx, pages, max_pages, k_pages,
+                               v_pages, n_pages, rotation, *turn, row_pos, q_out, stream)
+
+    # ---- pages in 8 bits
+    def _scales(self, n_pages: int, k_scales, v_scales) -> None:
+        self._per_row(n_pages * self.shape.n_kv_heads, k_scales, v_scales)
+
+    def append_quantised(self, k_new, v_new, row_start, n_ctx, pages, k_pages, v_pages, k_scales, v_scales, rotation=None, q=None,
+                    q_out=None, row_pos=None, interleaved: bool = False, stream=None, max_new=None) -> None:
+        """Keys and values of the new tokens into pages of e4m3 codes (float8_e4m3fn pools) with the scales [n_pages][Hk] fp32;
+        rotation and what comes with it as in append_rotated, None: keys as they are."""
+        batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, v_pages)
+        self._scales(n_pages, k_scales, v_scales)
+        n_rows, max_new = self._rows(batch, row_start, k_new, self.shape.n_kv_heads, max_new, v_new)
+        turn = self._turn(n_rows, rotation, q, q_out, row_pos, interleaved)
+        if n_rows == 0:
+            return
+        B.paged_append_quantised(self.cs, batch, n_rows, max_new, q, k_new, v_new, row_start, n_ctx, pages, max_pages, k_pages, v_pages,
+                            n_pages, k_scales, v_scales, rotation, *turn, row_pos, q_out, stream)
+
+    def attend_quantised(self, q, row_start, n_ctx, pages, k_pages, v_pages, k_scales, v_scales, out, lse=None, softcap: float = 0.0,
+                    window: int = 0, slopes=None, row_first=None, row_end=None, stream=None, max_new=None) -> None:
+        """attend over pages in 8 bits."""
+        batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, v_pages)
+        self._scales(n_pages, k_scales, v_scales)
+        n_rows, max_new = self._attending(batch, row_start, q, out, lse, slopes, row_first, row_end, max_new)
+        if n_rows == 0:
+            return
+        B.paged_attention_quantised(self.cs, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, k_pages, v_pages, n_pages,
+                               k_scales, v_scales, out, lse, self.workspace, softcap, window, slopes, row_first, row_end, stream)
+
+    def _attending(self, batch, row_start, q, out, lse, slopes, row_first, row_end, max_new) -> Tuple[int, int]:
+        n_rows, max_new = self._rows(batch, row_start, q, self.shape.n_q_heads, max_new, out)
+        self._per_row(n_rows, row_first, row_end)
+        self._per_row(n_rows * self.shape.n_q_heads, lse)
+        self._per_row(self.shape.n_q_heads, slopes)
+        return n_rows, max_new
+
+    # ---- attention over selected pages
+    def key_bounds(self, n_ctx, pages, k_pages, bounds, row_start=None, n_rows: int = 0, stream=None, max_new=None) -> None:
+        """bounds [n_pages][Hk][2][D], the least and the largest key of every channel: of the pages with new tokens (the n_rows rows
+        that row_start deals out), or of all pages (row_start None)."""
+        batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, k_pages)
+        self._per_row(n_pages * self.shape.n_kv_heads * 2 * self.shape.head_dim, bounds)
+        if row_start is not None:
+            max_new = self.max_new if max_new is None else max_new
+            if not 1 <= max_new <= self.max_new:
+                raise B.ActQKVError(-1, f"max_new {max_new}: made for {self.max_new}")
+            if not 0 <= n_rows <= self.n_rows:
+                raise B.ActQKVError(-1, f"{n_rows} rows: made for {self.n_rows}")
+            self._per_row(batch + 1, row_start)
+            if n_rows == 0:
+                return
+            max_new = min(max_new, n_rows)
+        B.paged_key_bounds(self.cs, batch, n_rows, max_new or 0, row_start, n_ctx, pages, max_pages, k_pages, n_pages, bounds, stream)
+
+    def select_pages(self, q, row_start, n_ctx, pages, bounds, keep_first: int, keep_last: int, scores, idx, n_sel, stream=None,
+                     max_new=None) -> None:
+        """The pages that each row looks at: idx [n_rows][Hk][k_sel], ascending, and n_sel [n_rows][Hk], by the scores
+        [n_rows][Hk][at least max_pages] that the pages' bounds give them."""
+        batch, max_pages = pages.shape
+        n_pages = bounds.shape[0]
+        rows = self.shape.n_kv_heads
+        if batch > self.batch or max_pages > self.max_pages:
+            raise B.ActQKVError(-1, f"{batch} sequences of {max_pages} pages: made for {self.batch} of {self.max_pages}")
+        self._per_row(batch, n_ctx)
+        self._per_row(n_pages * rows * 2 * self.shape.head_dim, bounds)
+        n_rows, max_new = self._rows(batch, row_start, q, self.shape.n_q_heads, max_new)
+        self._per_row(n_rows * rows, n_sel)
+        self._per_row(n_rows * rows * idx.shape[-1], idx)
+        self._per_row(n_rows * rows * scores.shape[-1], scores)
+        if n_rows == 0:
+            return
+        B.paged_select_pages(self.cs, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, bounds, n_pages, idx.shape[-1],
+                             keep_first, keep_last, scores, scores.shape[-1], idx, n_sel, stream)
+
+    def attend_selected(self, q, row_start, n_ctx, pages, k_pages, v_pages, idx, n_sel, out, lse=None, softcap: float = 0.0,
+                        window: int = 0, slopes=None, row_first=None, row_end=None, stream=None, max_new=None) -> None:
+        """attend, of rows that see their selected pages alone."""
+        batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, v_pages)
+        n_rows, max_new = self._attending(batch, row_start, q, out, lse, slopes, row_first, row_end, max_new)
+        self._per_row(n_rows * self.shape.n_kv_heads, n_sel)
+        self._per_row(n_rows * self.shape.n_kv_heads * idx.shape[-1], idx)
+        if n_rows == 0:
+            return
+        B.paged_attention_selected(self.cs, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, k_pages, v_pages, n_pages,
+                                   idx, n_sel, idx.shape[-1], out, lse, self.workspace, softcap, window, slopes, row_first, row_end,
+                                   stream)
