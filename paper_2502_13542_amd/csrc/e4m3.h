@@ -21,6 +21,8 @@ __device__ __forceinline__ int e4m3_exponent_for(float most) {
   const uint32_t bits = __float_as_uint(most);
   return max(int(bits >> 23) - 127 - 8 + int((bits & 0x7fffffu) > 0x600000u), kLeastE4m3);
 }
+// The largest value that a scale 2^e is the least for (448 2^e, but of the largest e what fp32 has).
+__device__ __forceinline__ float e4m3_most(int e) { return e < kMostE4m3 ? 1.75f * pow2f(e + 8) : __uint_as_float(0x7f7fffffu); }
 __device__ __forceinline__ uint32_t e4m3_pack(float x0, float x1, float x2, float x3) {
   const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(x0, x1, 0, false);
   return __builtin_amdgcn_cvt_pk_fp8_f32(x2, x3, lo, true);

@@ -26,25 +26,23 @@ struct NewTokens {
   int page, j0, n, row, pos;
 };
 
-// The scale's exponent: of the new values' largest, and of the old one where the page held tokens; `again`: the factor of the old
-// codes, 1 where nothing changes.
-__device__ __forceinline__ int page_exponent(float most, const NewTokens& w, float* scale, float* red, float& again) {
-  most = block_max(most, red);
-  int e = e4m3_exponent_for(most);
-  again = 1.f;
-  if (w.j0 > 0) {
-    const int old = e4m3_exponent(*scale);
-    again = pow2f(max(old - max(old, e), -126));
-    e = max(old, e);
-  }
-  __syncthreads();                                // (everybody has read the old one)
+// The scale's exponent: the least that the new values' largest and, where the page held tokens, its old scale allow; `again`: the factor
+// of the old codes, 1 where nothing changes.  (The old scale goes into the maximum: all threads have read it before one writes the new one.)
+template <int kThreads>
+__device__ __forceinline__ int page_exponent(float most, const NewTokens& w, float old_scale, float* scale, float* red, float& again) {
+  const int old = e4m3_exponent(old_scale);
+  if (w.j0 > 0) most = fmaxf(most, e4m3_most(old));
+  most = kThreads == 64 ? wave_max(most) : block_max(most, red);
+  const int e = e4m3_exponent_for(most);
+  again = w.j0 > 0 ? pow2f(max(old - e, -126)) : 1.f;
   if (threadIdx.x == 0) *scale = pow2f(e);
   return e;
 }
 
-template <typename T, int D>
+// kFew: at most kTurnRows new tokens, all in one round.
+template <typename T, int D, int kThreads, bool kFew, bool kTurn>
 __device__ __forceinline__ void append8_keys(const PagedAppend8& a, const NewTokens& w, int hk, float* red) {
-  constexpr int V = Vec<T>::N, kPairs = D / (2 * V), kRows = kTurnThreads / kPairs, kEach = kBlock / kRows;
+  constexpr int V = Vec<T>::N, kPairs = D / (2 * V), kRows = kTurnRows<T, D, kThreads>, kEach = kFew ? 1 : kBlock / kRows;
   typedef typename Vec<T>::raw raw_t;
   const int p = threadIdx.x % kPairs, j = threadIdx.x / kPairs;       // of the new tokens, j, j + kRows, ...
   const TurnPair at = turn_pair<V>(a.r, p);
@@ -58,27 +56,31 @@ __device__ __forceinline__ void append8_keys(const PagedAppend8& a, const NewTok
       x[i][1] = Vec<T>::load_raw(from + size_t(tok) * a.n_kv_heads * D + at.b);
     }
   }
-  float k[kEach][2][V], most = 0.f;
+  if (w.page < 0) return;
+  float* scale = a.k_scales + size_t(w.page) * a.n_kv_heads + hk;
+  const float old_scale = *scale;
+  // (turned keys are held in fp32; others are widened twice, which leaves room for twice as many workgroups)
+  float k[kTurn ? kEach : 1][2][V], most = 0.f;
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
-    const int tok = i * kRows + j;
+    const int tok = i * kRows + j, at_i = kTurn ? i : 0;
     if (tok < w.n) {
-      Vec<T>::widen(x[i][0], k[i][0]);
-      Vec<T>::widen(x[i][1], k[i][1]);
-      if (at.turns) {
+      Vec<T>::widen(x[i][0], k[at_i][0]);
+      Vec<T>::widen(x[i][1], k[at_i][1]);
+      if (kTurn && at.turns) {
         TurnBy<V> by;
         by.load(a.r, w.row + tok, w.pos + tok, p);
-        turn<double, V>(by, a.r.interleaved, k[i][0], k[i][1]);
+        turn<double, V>(by, a.r.interleaved, k[at_i][0], k[at_i][1]);
       }
 #pragma unroll
-      for (int e = 0; e < V; ++e) most = largest(largest(most, k[i][0][e]), k[i][1][e]);
+      for (int e = 0; e < V; ++e) most = largest(largest(most, k[at_i][0][e]), k[at_i][1][e]);
     }
   }
   const size_t tile = (size_t(w.page) * a.n_kv_heads + hk) * (kBlock * D);
   float again;
-  const float by = pow2f(-page_exponent(most, w, a.k_scales + size_t(w.page) * a.n_kv_heads + hk, red, again));
+  const float by = pow2f(-page_exponent<kThreads>(most, w, old_scale, scale, red, again));
   if (again != 1.f) {
-    for (int i = threadIdx.x; i < w.j0 * (D / 16); i += kTurnThreads) {
+    for (int i = threadIdx.x; i < w.j0 * (D / 16); i += kThreads) {
       u32x4* to = reinterpret_cast<u32x4*>(a.k_pages + tile) + i;
       u32x4 c = *to;
 #pragma unroll
@@ -92,30 +94,37 @@ __device__ __forceinline__ void append8_keys(const PagedAppend8& a, const NewTok
     if (tok < w.n) {
       uint8_t* to = a.k_pages + tile + size_t(w.j0 + tok) * D;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2; ++h) {
+        float (&y)[V] = k[kTurn ? i : 0][h];
+        if (!kTurn) Vec<T>::widen(x[i][h], y);
 #pragma unroll
         for (int e = 0; e < V; e += 4)
-          *reinterpret_cast<uint32_t*>(to + (h ? at.b : at.a) + e) =
-              e4m3_pack(k[i][h][e] * by, k[i][h][e + 1] * by, k[i][h][e + 2] * by, k[i][h][e + 3] * by);
+          *reinterpret_cast<uint32_t*>(to + (h ? at.b : at.a) + e) = e4m3_pack(y[e] * by, y[e + 1] * by, y[e + 2] * by, y[e + 3] * by);
+      }
     }
   }
 }
 
 constexpr int kV8Pad = kBlock / 4 + 1;           // words of a channel in LDS
-template <typename T, int D>
+template <typename T, int D, int kThreads, bool kFew>
 __device__ __forceinline__ void append8_values(const PagedAppend8& a, const NewTokens& w, int hk, float* red, uint32_t* vt) {
-  constexpr int V = Vec<T>::N, kChunks = D / V, kEach = kBlock / 4 * kChunks / kTurnThreads;
+  constexpr int V = Vec<T>::N, kChunks = D / V, kWords = kBlock / 4 * kChunks, kEach = kFew || kWords < kThreads ? 1 : kWords / kThreads;
+  static_assert(!kFew || (kTurnRows<T, D, kThreads> + 6) / 4 * kChunks <= kThreads, "words of as many tokens, wherever they begin");
+  const int quad0 = kFew ? w.j0 / 4 : 0;          // the first word with a new token
   typedef typename Vec<T>::raw raw_t;
   const T* from = static_cast<const T*>(a.v_new) + (size_t(w.row) * a.n_kv_heads + hk) * D;
   raw_t x[kEach][4];
   float most = 0.f;
 #pragma unroll
   for (int n = 0; n < kEach; ++n) {
-    const int i = n * kTurnThreads + threadIdx.x, j = i / kChunks * 4 - w.j0, c = i % kChunks;
+    const int i = n * kThreads + threadIdx.x, j = (quad0 + i / kChunks) * 4 - w.j0, c = i % kChunks;
 #pragma unroll
     for (int h = 0; h < 4; ++h)
       x[n][h] = j + h >= 0 && j + h < w.n ? Vec<T>::load_raw(from + size_t(j + h) * a.n_kv_heads * D + c * V) : raw_t{};
   }
+  if (w.page < 0) return;
+  float* scale = a.v_scales + size_t(w.page) * a.n_kv_heads + hk;
+  const float old_scale = *scale;
 #pragma unroll
   for (int n = 0; n < kEach; ++n)
 #pragma unroll
@@ -127,20 +136,20 @@ __device__ __forceinline__ void append8_values(const PagedAppend8& a, const NewT
     }
   uint8_t* tile = a.v_pages + (size_t(w.page) * a.n_kv_heads + hk) * (kBlock * D);
   float again;
-  const float by = pow2f(-page_exponent(most, w, a.v_scales + size_t(w.page) * a.n_kv_heads + hk, red, again));
+  const float by = pow2f(-page_exponent<kThreads>(most, w, old_scale, scale, red, again));
 #pragma unroll
   for (int n = 0; n < kEach; ++n) {
-    const int i = n * kTurnThreads + threadIdx.x, j = i / kChunks * 4 - w.j0, c = i % kChunks;
+    const int i = n * kThreads + threadIdx.x, quad = quad0 + i / kChunks, j = quad * 4 - w.j0, c = i % kChunks;
     if (j + 3 < 0 || j >= w.n) continue;
     float v[4][V];
 #pragma unroll
     for (int h = 0; h < 4; ++h) Vec<T>::widen(x[n][h], v[h]);
 #pragma unroll
-    for (int e = 0; e < V; ++e) vt[(c * V + e) * kV8Pad + i / kChunks] = e4m3_pack(v[0][e] * by, v[1][e] * by, v[2][e] * by, v[3][e] * by);
+    for (int e = 0; e < V; ++e) vt[(c * V + e) * kV8Pad + quad] = e4m3_pack(v[0][e] * by, v[1][e] * by, v[2][e] * by, v[3][e] * by);
   }
   __syncthreads();
   const int end = w.j0 + w.n, g0 = again != 1.f ? 0 : w.j0 / 16, groups = (end - 1) / 16 - g0 + 1;
-  for (int i = threadIdx.x; i < D * groups; i += kTurnThreads) {
+  for (int i = threadIdx.x; i < D * groups; i += kThreads) {
     const int d = i / groups, j = (g0 + i - d * groups) * 16;
     const uint32_t* words = vt + d * kV8Pad + j / 4;
     uint8_t* to = tile + size_t(d) * kBlock + j;
@@ -166,8 +175,8 @@ __device__ __forceinline__ void append8_values(const PagedAppend8& a, const NewT
   }
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(kTurnThreads) void paged8_append_kernel(PagedAppend8 a) {
+template <typename T, int D, int kThreads, bool kFew, bool kTurn>
+__global__ __launch_bounds__(kThreads) void paged8_append_kernel(PagedAppend8 a) {
   __shared__ uint32_t vt[D * kV8Pad];            // [channel][four slots]
   __shared__ float red[32];
   const int hk = blockIdx.x >> 1, role = blockIdx.x & 1, s = blockIdx.z;
@@ -177,16 +186,15 @@ __global__ __launch_bounds__(kTurnThreads) void paged8_append_kernel(PagedAppend
   for (int y = blockIdx.y; y < a.pages + (a.slices + 1) / 2; y += gridDim.y) {
     if (y >= a.pages) {
       const int slice = (y - a.pages) * 2 + role;
-      turn_rows<T, D, false>(a.t, a.r, seq, s, hk, a.n_kv_heads, a.group, slice, nullptr, nullptr, static_cast<const T*>(a.q),
+      turn_rows<T, D, kThreads, false>(a.t, a.r, seq, s, hk, a.n_kv_heads, a.group, slice, nullptr, nullptr, static_cast<const T*>(a.q),
                              static_cast<T*>(a.q_out));
       continue;
     }
     const int index = first + y, lo = max(max(pos0, 0), index * kBlock), hi = min(seq.n, index * kBlock + kBlock);
     if (hi <= lo) continue;                      // (index < max_pages: hi > index * kBlock)
     const NewTokens w{paged_page(a.t, s, index), lo - index * kBlock, hi - lo, seq.row0 + lo - pos0, lo};
-    if (w.page < 0) continue;
-    if (role == 0) append8_keys<T, D>(a, w, hk, red);
-    else append8_values<T, D>(a, w, hk, red, vt);
+    if (role == 0) append8_keys<T, D, kThreads, kFew, kTurn>(a, w, hk, red);
+    else append8_values<T, D, kThreads, kFew>(a, w, hk, red, vt);
     __syncthreads();
   }
 }
@@ -207,17 +215,16 @@ int launch_paged_append_quantised(const actqkv_shape& sh, const PagedTable& t, c
   a.v_scales = v_scales;
   a.n_kv_heads = sh.n_kv_heads;
   a.group = sh.n_q_heads / sh.n_kv_heads;
-  a.slices = q != nullptr ? turn_slices(sh, t.max_new) : 0;
   a.pages = std::min(t.max_pages, (t.max_new + kBlock - 2) / kBlock + 1);
-  const dim3 grid(2 * sh.n_kv_heads, std::min(a.pages + (a.slices + 1) / 2, kTurnMostY), t.batch);
-  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kTurnThreads), 0, stream, a); };
-  if (sh.dtype == ACTQKV_F32) {
-    if (sh.head_dim == 64) launch(paged8_append_kernel<float, 64>);
-    else launch(paged8_append_kernel<float, 128>);
-  } else {
-    if (sh.head_dim == 64) launch(paged8_append_kernel<uint16_t, 64>);
-    else launch(paged8_append_kernel<uint16_t, 128>);
-  }
+  with_turn_types<kTurnThreads>(sh, t.max_new, [&](auto* type, auto dim, auto threads, auto few) {
+    typedef std::remove_pointer_t<decltype(type)> T;
+    constexpr int D = decltype(dim)::value, kThreads = decltype(threads)::value;
+    a.slices = q != nullptr ? (t.max_new + kTurnRows<T, D, kThreads> - 1) / kTurnRows<T, D, kThreads> : 0;
+    const dim3 grid(2 * sh.n_kv_heads, std::min(a.pages + (a.slices + 1) / 2, kTurnMostY), t.batch);
+    constexpr bool kFew = decltype(few)::value;
+    if (r.table != nullptr) hipLaunchKernelGGL((paged8_append_kernel<T, D, kThreads, kFew, true>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((paged8_append_kernel<T, D, kThreads, kFew, false>), grid, dim3(kThreads), 0, stream, a);
+  });
   return hip_status("paged append (8 bits)");
 }
 

@@ -20,7 +20,8 @@ struct PagedAppendRotated {
   int slices, pages;                       // of the rows and of the pages of a sequence, at most
 };
 
-template <typename T, int D>
+// kFew: at most kTurnRows new tokens, all in one round.
+template <typename T, int D, int kThreads, bool kFew>
 __device__ __forceinline__ void append_values(const PagedAppendRotated& a, const PagedSeq& q, int s, int hk, int index, int d0, T* vt) {
   constexpr int V = Vec<T>::N, kOwn = D / kArSlices, kChunks = kOwn / V, kPad = kBlock + 2;
   typedef typename Vec<T>::raw raw_t;
@@ -32,18 +33,20 @@ __device__ __forceinline__ void append_values(const PagedAppendRotated& a, const
   const int n_tok = hi - lo, j0 = lo - index * kBlock;
   const T* v_new = static_cast<const T*>(a.v_new) + (size_t(q.row0 + (lo - pos0)) * a.n_kv_heads + hk) * D + d0;
   T* tile = static_cast<T*>(a.v_pages) + (size_t(page) * a.n_kv_heads + hk) * (kBlock * D) + size_t(d0) * kBlock;
-  constexpr int kEach = kBlock / 2 * kChunks / kTurnThreads;
+  constexpr int kEach = kFew ? 1 : kBlock / 2 * kChunks / kThreads;
+  static_assert(!kFew || (kTurnRows<T, D, kThreads> / 2 + 1) * kChunks <= kThreads, "pairs of as many tokens, wherever they begin");
+  const int pair0 = kFew ? j0 / 2 : 0;                              // the first pair with a new token
   raw_t v[kEach][2];
 #pragma unroll
   for (int n = 0; n < kEach; ++n) {
-    const int i = n * kTurnThreads + threadIdx.x, j = i / kChunks * 2, c = i % kChunks;
+    const int i = n * kThreads + threadIdx.x, j = (pair0 + i / kChunks) * 2, c = i % kChunks;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
       v[n][h] = j + h >= j0 && j + h < j0 + n_tok ? Vec<T>::load_raw(v_new + size_t(j + h - j0) * a.n_kv_heads * D + c * V) : raw_t{};
   }
 #pragma unroll
   for (int n = 0; n < kEach; ++n) {
-    const int i = n * kTurnThreads + threadIdx.x, j = i / kChunks * 2, c = i % kChunks;
+    const int i = n * kThreads + threadIdx.x, j = (pair0 + i / kChunks) * 2, c = i % kChunks;
     if (j + 1 < j0 || j >= j0 + n_tok) continue;
     alignas(16) T ve[2][V];
 #pragma unroll
@@ -60,7 +63,7 @@ __device__ __forceinline__ void append_values(const PagedAppendRotated& a, const
   }
   __syncthreads();
   const int g0 = j0 / V, groups = (j0 + n_tok - 1) / V - g0 + 1;
-  for (int i = threadIdx.x; i < kOwn * groups; i += kTurnThreads) {
+  for (int i = threadIdx.x; i < kOwn * groups; i += kThreads) {
     const int d = i / groups, j = (g0 + i - d * groups) * V;
     const T* from = vt + d * kPad + j;
     T* to = tile + size_t(d) * kBlock + j;
@@ -73,8 +76,8 @@ __device__ __forceinline__ void append_values(const PagedAppendRotated& a, const
   }
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(kTurnThreads) void paged_append_rotated_kernel(PagedAppendRotated a) {
+template <typename T, int D, int kThreads, bool kFew>
+__global__ __launch_bounds__(kThreads) void paged_append_rotated_kernel(PagedAppendRotated a) {
   constexpr int kOwn = D / kArSlices;
   __shared__ __attribute__((aligned(16))) T vt[kOwn * (kBlock + 2)];   // [channel][place in the page]
   const int hk = blockIdx.x, s = blockIdx.z;
@@ -83,11 +86,11 @@ __global__ __launch_bounds__(kTurnThreads) void paged_append_rotated_kernel(Page
   const int first = max(seq.n - seq.m, 0) / kBlock;
   for (int y = blockIdx.y; y < a.slices + a.pages * kArSlices; y += gridDim.y) {
     if (y < a.slices) {
-      turn_rows<T, D, true>(a.t, a.r, seq, s, hk, a.n_kv_heads, a.group, y, static_cast<const T*>(a.k_new), static_cast<T*>(a.k_pages),
+      turn_rows<T, D, kThreads, true>(a.t, a.r, seq, s, hk, a.n_kv_heads, a.group, y, static_cast<const T*>(a.k_new), static_cast<T*>(a.k_pages),
                             static_cast<const T*>(a.q), static_cast<T*>(a.q_out));
     } else {
       const int i = y - a.slices;
-      append_values<T, D>(a, seq, s, hk, first + i / kArSlices, i % kArSlices * kOwn, vt);
+      append_values<T, D, kThreads, kFew>(a, seq, s, hk, first + i / kArSlices, i % kArSlices * kOwn, vt);
       __syncthreads();
     }
   }
@@ -106,18 +109,15 @@ int launch_paged_append_rotated(const actqkv_shape& sh, const PagedTable& t, con
   a.q_out = q_out;
   a.n_kv_heads = sh.n_kv_heads;
   a.group = sh.n_q_heads / sh.n_kv_heads;
-  a.slices = turn_slices(sh, t.max_new);
   // a sequence's rows lie in one page more than they would from a page's first slot on
   a.pages = std::min(t.max_pages, (t.max_new + kBlock - 2) / kBlock + 1);
-  const dim3 grid(sh.n_kv_heads, std::min(a.slices + a.pages * kArSlices, kTurnMostY), t.batch);
-  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kTurnThreads), 0, stream, a); };
-  if (sh.dtype == ACTQKV_F32) {
-    if (sh.head_dim == 64) launch(paged_append_rotated_kernel<float, 64>);
-    else launch(paged_append_rotated_kernel<float, 128>);
-  } else {
-    if (sh.head_dim == 64) launch(paged_append_rotated_kernel<uint16_t, 64>);
-    else launch(paged_append_rotated_kernel<uint16_t, 128>);
-  }
+  with_turn_types<kTurnThreads>(sh, t.max_new, [&](auto* type, auto dim, auto threads, auto few) {
+    typedef std::remove_pointer_t<decltype(type)> T;
+    constexpr int D = decltype(dim)::value, kThreads = decltype(threads)::value;
+    a.slices = (t.max_new + kTurnRows<T, D, kThreads> - 1) / kTurnRows<T, D, kThreads>;
+    const dim3 grid(sh.n_kv_heads, std::min(a.slices + a.pages * kArSlices, kTurnMostY), t.batch);
+    hipLaunchKernelGGL((paged_append_rotated_kernel<T, D, kThreads, decltype(few)::value>), grid, dim3(kThreads), 0, stream, a);
+  });
   return hip_status("paged append (rotated)");
 }
 

@@ -10,7 +10,9 @@
 
 namespace actqkv {
 
-constexpr int kTurnThreads = 256;
+// Threads of a workgroup: of calls whose sequences bring few rows one wavefront, which has no barriers to wait at and leaves room for the
+// other workgroups (a step of 64 sequences, 32 query and 8 KV heads of 128, turned: 6.3 us in workgroups of 256 threads, 5.0 so; into 8 bits 10.6, 6.0).
+constexpr int kTurnThreads = 256, kTurnFew = 64;
 constexpr int kTurnMostY = 32768;          // workgroups along y: more work goes round
 
 // Chunks a thread's pair is made of: their first channels, and whether they turn (behind `dims` they are just two neighbours).
@@ -68,10 +70,11 @@ __device__ __forceinline__ u32x4 narrow(const float (&x)[8], u32x4*) {
 
 // Slice `slice` of a sequence's rows: their query heads of KV head hk, and their keys (kKeys), turned.  Products in fp32, each result
 // rounded once to the storage type.
-template <typename T, int D, bool kKeys>
+template <typename T, int D, int kThreads> constexpr int kTurnRows = kThreads / (D / (2 * Vec<T>::N));   // rows of a slice
+template <typename T, int D, int kThreads, bool kKeys>
 __device__ __forceinline__ void turn_rows(const PagedTable& t, const PagedRotation& r, const PagedSeq& seq, int s, int hk, int n_kv_heads,
                                           int group, int slice, const T* k_new, T* k_pages, const T* q, T* q_out) {
-  constexpr int V = Vec<T>::N, kPairs = D / (2 * V), kRows = kTurnThreads / kPairs, kHeads = 4;
+  constexpr int V = Vec<T>::N, kPairs = D / (2 * V), kRows = kTurnRows<T, D, kThreads>, kHeads = 4;
   typedef typename Vec<T>::raw raw_t;
   const int i = slice * kRows + threadIdx.x / kPairs, p = threadIdx.x % kPairs;
   const int pos = seq.n - seq.m + i, row = seq.row0 + i;
@@ -116,10 +119,28 @@ __device__ __forceinline__ void turn_rows(const PagedTable& t, const PagedRotati
   }
   if (kKeys && page >= 0) move(ka, kb, k_pages + ((size_t(page) * n_kv_heads + hk) * kBlock + pos % kBlock) * D);
 }
-// Rows of a slice, and slices of a sequence of at most max_new rows.
-inline int turn_slices(const actqkv_shape& sh, int max_new) {
-  const int rows = kTurnThreads / (sh.head_dim / (sh.dtype == ACTQKV_F32 ? 8 : 16));
-  return (max_new + rows - 1) / rows;
+// Calls launch(T*, D, threads, few) with the types of a call: few, where every sequence's rows are at most a slice; kMost threads otherwise.
+template <int kMost, typename Launch>
+inline void with_turn_types(const actqkv_shape& sh, int max_new, Launch launch) {
+  auto by_rows = [&](auto* type, auto dim) {
+    typedef std::remove_pointer_t<decltype(type)> T;
+    constexpr int D = decltype(dim)::value;
+    if (max_new <= kTurnRows<T, D, kTurnFew>)
+      launch(type, dim, std::integral_constant<int, kTurnFew>(), std::true_type());
+    else if (max_new <= kTurnRows<T, D, kTurnThreads>)
+      launch(type, dim, std::integral_constant<int, kTurnThreads>(), std::true_type());
+    else
+      launch(type, dim, std::integral_constant<int, kMost>(), std::false_type());
+  };
+  const std::integral_constant<int, 64> d64;
+  const std::integral_constant<int, 128> d128;
+  if (sh.dtype == ACTQKV_F32) {
+    if (sh.head_dim == 64) by_rows(static_cast<float*>(nullptr), d64);
+    else by_rows(static_cast<float*>(nullptr), d128);
+  } else {
+    if (sh.head_dim == 64) by_rows(static_cast<uint16_t*>(nullptr), d64);
+    else by_rows(static_cast<uint16_t*>(nullptr), d128);
+  }
 }
 
 }  // namespace actqkv
