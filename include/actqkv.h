@@ -757,11 +757,11 @@ int actqkv_paged_key_bounds(const actqkv_shape* shape, int batch, int n_rows, in
  *            the row sees if there are no more.
  *   n_sel  [n_rows][Hk] int32: how many.
  * Rows that belong to no sequence are not written; of a row at a negative position nothing is selected.  n_rows * Hk is at most 2^22.
- * Errors: EINVAL, ESHAPE, EALIGN. */
+ * Errors: EINVAL, ESHAPE, EALIGN, EWORKSPACE. */
 int actqkv_paged_select_pages(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q, const int32_t* row_start,
                               const int32_t* n_ctx, const int32_t* pages, int max_pages, const void* bounds, int n_pages, int k_sel,
                               int keep_first, int keep_last, float* scores, int64_t score_stride, int32_t* idx, int32_t* n_sel,
-                              void* stream);
+                              void* workspace, size_t ws_bytes, void* stream);
 
 /* actqkv_paged_attention of rows that see, of the positions they would see there, those in their selected pages alone: idx and n_sel as above (or the
  * caller's own; a page in a list twice counts twice, entries outside the sequence's pages are skipped).  Every row reads its own pages: meant for single tokens and a few

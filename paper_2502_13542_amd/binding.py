@@ -103,7 +103,7 @@ SIGNATURES = {
     "actqkv_paged_attention_quantised": (_i, [_shp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _i, _vp, _vp, ctypes.c_float, _i,
                                               _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "actqkv_paged_key_bounds": (_i, [_shp, _i, _i, _i, _vp, _vp, _vp, _i, _vp, _i, _vp, _vp]),
-    "actqkv_paged_select_pages": (_i, [_shp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _i, _i, _i, _i, _vp, _i64, _vp, _vp, _vp]),
+    "actqkv_paged_select_pages": (_i, [_shp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _i, _i, _i, _i, _vp, _i64, _vp, _vp, _vp, _sz, _vp]),
     "actqkv_paged_attention_selected": (_i, [_shp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _i, _vp, _vp, _i, ctypes.c_float,
                                              _i, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "actqkv_last_error": (ctypes.c_char_p, []),
@@ -430,10 +430,10 @@ def paged_key_bounds(shape: CShape, batch: int, n_rows: int, max_new: int, row_s
 
 def paged_select_pages(shape: CShape, batch: int, n_rows: int, max_new: int, q, row_start, n_ctx, pages, max_pages: int, bounds,
                        n_pages: int, k_sel: int, keep_first: int, keep_last: int, scores, score_stride: int, idx, n_sel,
-                       stream=None) -> None:
+                       workspace, stream=None) -> None:
     """The pages that each row looks at, by their bounds; see the header."""
     _calls().paged_select_pages(shape, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, bounds, n_pages, k_sel,
-                                keep_first, keep_last, scores, score_stride, idx, n_sel, stream)
+                                keep_first, keep_last, scores, score_stride, idx, n_sel, workspace, stream)
 
 
 def paged_attention_selected(shape: CShape, batch: int, n_rows: int, max_new: int, q, row_start, n_ctx, pages, max_pages: int,

@@ -279,7 +279,8 @@ int launch_paged_append_quantised(const actqkv_shape& sh, const PagedTable& t, c
                              hipStream_t stream);
 int launch_paged_bounds(const actqkv_shape& sh, const PagedTable& t, const void* k_pages, void* bounds, hipStream_t stream);
 int launch_paged_select(const actqkv_shape& sh, const PagedTable& t, const void* q, const void* bounds, int k_sel, int keep_first,
-                        int keep_last, float* scores, int64_t stride, int32_t* idx, int32_t* n_sel, hipStream_t stream);
+                        int keep_last, float* scores, int64_t stride, int32_t* idx, int32_t* n_sel, const Workspace& ws,
+                        hipStream_t stream);
 struct PagedEvict {
   PagedTable t;
   void* k_pages;

@@ -60,6 +60,16 @@ static int check_rows(int n_rows, int max_new) {
   return ACTQKV_OK;
 }
 
+static int check_workspace(const char* name, const actqkv_shape* shape, int batch, int n_rows, int max_new, int max_pages,
+                           const void* workspace, size_t ws_bytes) {
+  if (workspace == nullptr || !aligned16(workspace))
+    return set_error(ACTQKV_EWORKSPACE, "workspace is NULL or not 16-byte aligned");
+  const size_t need = paged_workspace_bytes(*shape, batch, n_rows, max_new, max_pages);
+  if (ws_bytes < need)
+    return set_error(ACTQKV_EWORKSPACE, "workspace has %zu bytes, %s needs %zu", ws_bytes, name, need);
+  return ACTQKV_OK;
+}
+
 // Lists of selected pages: of every (row, KV head) k_sel entries.
 struct PagedChosen {
   const int32_t *idx, *n_sel;
@@ -134,11 +144,7 @@ static int attention_call(const char* name, const actqkv_shape* shape, int batch
     ACTQKV_REQUIRE_SMALL(idx, 4);
     ACTQKV_REQUIRE_SMALL(n_sel, 4);
   }
-  if (workspace == nullptr || !aligned16(workspace))
-    return set_error(ACTQKV_EWORKSPACE, "workspace is NULL or not 16-byte aligned");
-  const size_t need = paged_workspace_bytes(*shape, batch, n_rows, max_new, max_pages);
-  if (ws_bytes < need)
-    return set_error(ACTQKV_EWORKSPACE, "workspace has %zu bytes, %s needs %zu", ws_bytes, name, need);
+  ACTQKV_TRY(check_workspace(name, shape, batch, n_rows, max_new, max_pages, workspace, ws_bytes));
   const float scale = shape->softmax_scale > 0.f ? shape->softmax_scale : 1.f / std::sqrt(float(shape->head_dim));
   PagedAttn p;
   p.t = PagedTable{row_start, n_ctx, pages, batch, n_rows, max_new, max_pages, n_pages, 0};
@@ -271,7 +277,7 @@ int actqkv_paged_key_bounds(const actqkv_shape* shape, int batch, int n_rows, in
 int actqkv_paged_select_pages(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q, const int32_t* row_start,
                               const int32_t* n_ctx, const int32_t* pages, int max_pages, const void* bounds, int n_pages, int k_sel,
                               int keep_first, int keep_last, float* scores, int64_t score_stride, int32_t* idx, int32_t* n_sel,
-                              void* stream) {
+                              void* workspace, size_t ws_bytes, void* stream) {
   ACTQKV_TRY(check_shape(shape));
   ACTQKV_REQUIRE_PTR(bounds);
   ACTQKV_TRY(check_table(shape, batch, n_ctx, pages, max_pages, bounds, bounds, n_pages));
@@ -286,9 +292,10 @@ int actqkv_paged_select_pages(const actqkv_shape* shape, int batch, int n_rows, 
     return set_error(ACTQKV_EINVAL, "score_stride %lld < max_pages %d", (long long)score_stride, max_pages);
   ACTQKV_REQUIRE_SMALL(idx, 4);
   ACTQKV_REQUIRE_SMALL(n_sel, 4);
+  ACTQKV_TRY(check_workspace("paged_select_pages", shape, batch, n_rows, max_new, max_pages, workspace, ws_bytes));
   const PagedTable t{row_start, n_ctx, pages, batch, n_rows, max_new, max_pages, n_pages, 0};
   return launch_paged_select(*shape, t, q, bounds, k_sel, keep_first, keep_last, scores, score_stride, idx, n_sel,
-                             static_cast<hipStream_t>(stream));
+                             Workspace{workspace, ws_bytes}, static_cast<hipStream_t>(stream));
 }
 
 int actqkv_paged_attention_selected(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q,

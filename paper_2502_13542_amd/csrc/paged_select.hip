@@ -13,6 +13,14 @@ namespace actqkv {
 
 constexpr int kSelThreads = 256, kSelWaves = kSelThreads / 64;
 constexpr int kSelMostY = 32768;           // workgroups along y: more work goes round
+constexpr int kSelEach = 4;                // keys that a thread of the selection holds (of more pages it reads the scores again)
+constexpr int kSelWgs = 1024, kSelLeast = 64;   // workgroups that a selection is cut into, of so many pages at least
+
+template <int J>
+__device__ __forceinline__ double lane_xor64(double v) {
+  const u32x2 x = __builtin_bit_cast(u32x2, v);
+  return __builtin_bit_cast(double, u32x2{lane_xor32<J>(x.x), lane_xor32<J>(x.y)});
+}
 
 // ---- bounds
 struct PagedBounds {
@@ -76,136 +84,95 @@ struct PagedSelect {
   float* scores;                           // [n_rows][Hk][stride]
   int64_t stride;
   int32_t *idx, *n_sel;                    // [n_rows][Hk][k_sel], [n_rows][Hk]
+  int parts;                               // workgroups of a (row, KV head)
+  unsigned int* counters;                  // one of each, zero between launches
 };
-// Sequence and position of a row; false of a row that no sequence brings.
-__device__ __forceinline__ bool row_place(const PagedTable& t, int row, int& s, int& pos) {
-  s = paged_seq_of_row(t, row);
-  if (s < 0) return false;
-  const PagedSeq seq = paged_seq(t, s);
-  pos = seq.n - seq.m + (row - seq.row0);
-  return true;
-}
-template <typename T, int D>
-__global__ __launch_bounds__(kSelThreads) void paged_scores_kernel(PagedSelect a) {
-  constexpr int V = Vec<T>::N, kOwn = 16, kLanes = D / kOwn, kPages = kSelThreads / kLanes, kHeads = 4;
-  const int item = blockIdx.x, row = item / a.n_kv_heads, hk = item % a.n_kv_heads;
-  const int part = threadIdx.x % kLanes, at = threadIdx.x / kLanes;
-  int s, pos;
-  if (!row_place(a.t, row, s, pos)) return;
-  const int seen = pos >= 0 ? pos / kBlock + 1 : 0;
-  float* scores = a.scores + size_t(item) * a.stride;
-  const T* q = static_cast<const T*>(a.q) + (size_t(row) * a.n_kv_heads + hk) * a.group * D + part * kOwn;
-  for (int b0 = blockIdx.y * kPages; b0 < a.t.max_pages; b0 += gridDim.y * kPages) {
-    const int b = b0 + at;
-    const int page = b < min(seen, a.t.max_pages) ? paged_page(a.t, s, b) : -1;
-    float most = -INFINITY;
-    if (page >= 0) {
-      const T* from = static_cast<const T*>(a.bounds) + (size_t(page) * a.n_kv_heads + hk) * (2 * D) + part * kOwn;
-      float lo[kOwn], hi[kOwn];
-#pragma unroll
-      for (int i = 0; i < kOwn; i += V) {
-        Vec<T>::load(from + i, *reinterpret_cast<float(*)[V]>(lo + i));
-        Vec<T>::load(from + D + i, *reinterpret_cast<float(*)[V]>(hi + i));
-      }
-      for (int h0 = 0; h0 < a.group; h0 += kHeads) {
-        double sum[kHeads] = {};
-#pragma unroll
-        for (int h = 0; h < kHeads; ++h) {
-          const T* qh = q + min(h0 + h, a.group - 1) * D;
-          float x[kOwn];
-#pragma unroll
-          for (int i = 0; i < kOwn; i += V) Vec<T>::load(qh + i, *reinterpret_cast<float(*)[V]>(x + i));
-#pragma unroll
-          for (int i = 0; i < kOwn; ++i) sum[h] += double(x[i]) * double(x[i] > 0.f ? hi[i] : lo[i]);
-        }
-#pragma unroll
-        for (int h = 0; h < kHeads; ++h) {
-#pragma unroll
-          for (int d = 1; d < kLanes; d <<= 1) sum[h] += __shfl_xor(sum[h], d, 64);
-          most = fmaxf(most, float(sum[h]));
-        }
-      }
-      most += 0.f;                         // (no -0: equal scores have equal bits)
-    }
-    if (part == 0 && b < a.t.max_pages) scores[b] = most;
-  }
-}
-
-// A page's place in the order: 0 is no candidate, the largest one that always stays.
-__device__ __forceinline__ uint32_t page_key(const PagedSelect& a, const float* scores, int s, int b, int last) {
-  if (b > last || paged_page(a.t, s, b) < 0) return 0;
+// A page's place in the order, by its score: 0 is no candidate, the largest one that always stays.
+__device__ __forceinline__ uint32_t page_key(const PagedSelect& a, float score, int b, int last) {
+  if (score == -INFINITY) return 0;
   if (b < a.keep_first || b > last - a.keep_last) return 0xffffffffu;
-  const uint32_t bits = __float_as_uint(scores[b]), order = bits >> 31 ? ~bits : bits | 0x80000000u;
+  const uint32_t bits = __float_as_uint(score), order = bits >> 31 ? ~bits : bits | 0x80000000u;
   return min(max(order, 1u), 0xfffffffeu);
 }
-__global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagedSelect a) {
-  __shared__ int hist[256], wave_sum[kSelWaves], bin_lds, left_lds;
-  const int item = blockIdx.x, row = item / a.n_kv_heads, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int s, pos;
-  if (!row_place(a.t, row, s, pos)) return;
-  const float* scores = a.scores + size_t(item) * a.stride;
+// Of 64 lanes' counts the inclusive sums, by the data-parallel primitives.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ int dpp_add(int v) { return v + __builtin_amdgcn_update_dpp(0, v, kCtrl, kRows, 0xF, false); }
+__device__ __forceinline__ int lane_sums(int v) {
+  v = dpp_add<0x111, 0xF>(v);                    // row_shr 1, 2, 4, 8
+  v = dpp_add<0x112, 0xF>(v);
+  v = dpp_add<0x114, 0xF>(v);
+  v = dpp_add<0x118, 0xF>(v);
+  v = dpp_add<0x142, 0xA>(v);                    // row_bcast 15 into rows 1, 3, then 31 into rows 2, 3
+  return dpp_add<0x143, 0xC>(v);
+}
+// The selection of one (row, KV head) from the keys of the pages 0 .. last: key_of(i, b) is that of page b = i kSelThreads + threadIdx.x, 0
+// behind the last.
+template <typename Key>
+__device__ __forceinline__ void select_from(const PagedSelect& a, int item, int last, Key key_of) {
+  __shared__ int hist[256], wave_sum[2][kSelWaves], bin_lds, left_lds, whole_lds;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, rounds = last / kSelThreads + 1;
   int32_t* idx = a.idx + size_t(item) * a.k_sel;
-  const int last = pos >= 0 ? min(pos / kBlock, a.t.max_pages - 1) : -1;      // the last visible page
   // ---- candidates
   int n = 0;
-  for (int b = tid; b <= last; b += kSelThreads) n += page_key(a, scores, s, b, last) != 0;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) n += __shfl_xor(n, d, 64);
-  if (lane == 0) wave_sum[wave] = n;
+  for (int i = 0; i < rounds; ++i) n += __popcll(__ballot(key_of(i, i * kSelThreads + tid) != 0));
+  if (lane == 0) wave_sum[0][wave] = n;
+  hist[tid] = 0;
   __syncthreads();
   n = 0;
 #pragma unroll
-  for (int w = 0; w < kSelWaves; ++w) n += wave_sum[w];
+  for (int w = 0; w < kSelWaves; ++w) n += wave_sum[0][w];
   const int take = min(n, a.k_sel);
-  // ---- the key of the last one that is taken, and how many of its equals are
-  uint32_t key = 1, above = 0;             // digits found so far, as a key and as a mask
-  int left = take;
+  // ---- the key above which all are taken, and how many of its equals are
+  uint32_t key = 0, known = 0;                   // digits found so far, as a key and as a mask
+  int left = 0;                                  // (every candidate's key is above 0)
   if (n > take) {
-    key = 0;
+    left = take;
     for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < 256; i += kSelThreads) hist[i] = 0;
-      __syncthreads();
-      for (int b = tid; b <= last; b += kSelThreads) {
-        const uint32_t k = page_key(a, scores, s, b, last);
-        if (k != 0 && (k & above) == key) atomicAdd(&hist[k >> shift & 255u], 1);
+      for (int i = 0; i < rounds; ++i) {
+        const uint32_t k = key_of(i, i * kSelThreads + tid);
+        if (k != 0 && (k & known) == key) atomicAdd(&hist[k >> shift & 255u], 1);
       }
       __syncthreads();
-      if (wave == 0) {                     // from the top: the bin in which the count reaches `left`
+      if (wave == 0) {                           // from the top: the bin in which the count reaches `left`
         int mine[4], sum = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) mine[i] = hist[255 - (4 * lane + i)], sum += mine[i];
-        int before = wave_scan(sum) - sum;
+        int before = lane_sums(sum) - sum;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           if (before < left && before + mine[i] >= left) {
             bin_lds = 255 - (4 * lane + i);
             left_lds = left - before;
+            whole_lds = before + mine[i] == left;
           }
           before += mine[i];
         }
       }
       __syncthreads();
       key |= uint32_t(bin_lds) << shift;
-      above |= 255u << shift;
+      known |= 255u << shift;
       left = left_lds;
+      if (whole_lds != 0) {                      // all of that bin: the other digits do not matter
+        key -= key != 0;                         // (a candidate's key is not 0)
+        left = 0;
+        break;
+      }
+      hist[tid] = 0;
+      __syncthreads();
     }
-  } else {
-    left = 0;                              // every candidate's key is at least 1: all are above 0
-    key = 0;
   }
   // ---- in their order
-  int base = 0, equal = 0;                 // taken above the key, and equal to it, before this round
-  for (int b0 = 0; b0 <= last; b0 += kSelThreads) {
-    const int b = b0 + tid;
-    const uint32_t k = page_key(a, scores, s, b, last);
+  int base = 0, equal = 0;                       // taken above the key, and equal to it, before this round
+  for (int i = 0; i < rounds; ++i) {
+    const int b = i * kSelThreads + tid;
+    const uint32_t k = key_of(i, b);
     const unsigned long long gt = __ballot(k > key), eq = __ballot(k == key && k != 0), below = (1ull << lane) - 1;
-    __syncthreads();
-    if (lane == 0) wave_sum[wave] = __popcll(gt) | __popcll(eq) << 16;
-    __syncthreads();
+    if (lane == 0) wave_sum[~i & 1][wave] = __popcll(gt) | __popcll(eq) << 16;
+    __syncthreads();                             // (two rows of sums, the first one the candidates': a round writes the other one)
     int g = base, e = equal;
 #pragma unroll
     for (int w = 0; w < kSelWaves; ++w) {
-      const int sum = wave_sum[w];
+      const int sum = wave_sum[~i & 1][w];
       if (w < wave) g += sum & 0xffff, e += sum >> 16;
       base += sum & 0xffff, equal += sum >> 16;
     }
@@ -214,6 +181,87 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagedSelect a
   }
   for (int i = take + tid; i < a.k_sel; i += kSelThreads) idx[i] = -1;
   if (tid == 0) a.n_sel[item] = take;
+}
+
+// The pages of a (row, KV head) go to `parts` workgroups; the one that is done last selects.
+template <typename T, int D>
+__global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagedSelect a) {
+  constexpr int V = Vec<T>::N, kOwn = 16, kLanes = D / kOwn, kPages = kSelThreads / kLanes;
+  __shared__ int last_flag;
+  const int item = blockIdx.x / a.parts, part = blockIdx.x - item * a.parts, row = item / a.n_kv_heads, hk = item % a.n_kv_heads;
+  const int slice = threadIdx.x % kLanes, at = threadIdx.x / kLanes;
+  const int s = paged_seq_of_row(a.t, row);
+  if (s < 0) return;
+  const PagedSeq seq = paged_seq(a.t, s);
+  const int pos = seq.n - seq.m + (row - seq.row0);
+  const int last = pos >= 0 ? pos / kBlock : -1;     // the last page that the row sees (below max_pages: pos < n)
+  uint32_t* scores = reinterpret_cast<uint32_t*>(a.scores) + size_t(item) * a.stride;
+  const T* q = static_cast<const T*>(a.q) + (size_t(row) * a.n_kv_heads + hk) * a.group * D + slice * kOwn;
+  constexpr int kAtOnce = 2;
+  for (int b0 = part * (kAtOnce * kPages); b0 <= last; b0 += a.parts * (kAtOnce * kPages)) {
+    int page[kAtOnce];
+    float lo[kAtOnce][kOwn], hi[kAtOnce][kOwn], most[kAtOnce];
+#pragma unroll
+    for (int n = 0; n < kAtOnce; ++n) page[n] = b0 + n * kPages + at <= last ? paged_page(a.t, s, b0 + n * kPages + at) : -1;
+#pragma unroll
+    for (int n = 0; n < kAtOnce; ++n) {
+      const T* from = static_cast<const T*>(a.bounds) + (size_t(max(page[n], 0)) * a.n_kv_heads + hk) * (2 * D) + slice * kOwn;
+      most[n] = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kOwn; i += V) {
+        Vec<T>::load(from + i, *reinterpret_cast<float(*)[V]>(lo[n] + i));
+        Vec<T>::load(from + D + i, *reinterpret_cast<float(*)[V]>(hi[n] + i));
+      }
+    }
+    for (int h = 0; h < a.group; ++h) {
+      float x[kOwn];
+#pragma unroll
+      for (int i = 0; i < kOwn; i += V) Vec<T>::load(q + h * D + i, *reinterpret_cast<float(*)[V]>(x + i));
+#pragma unroll
+      for (int n = 0; n < kAtOnce; ++n) {
+        double sum[2] = {};
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+          const float b = x[i] > 0.f ? hi[n][i] : lo[n][i];
+          if constexpr (sizeof(T) == 2) sum[i & 1] += double(x[i] * b);      // (a product of two bf16 is exact)
+          else sum[i & 1] += double(x[i]) * double(b);
+        }
+        double all = sum[0] + sum[1];
+        all += lane_xor64<1>(all);
+        all += lane_xor64<2>(all);
+        if (kLanes == 8) all += lane_xor64<4>(all);
+        most[n] = fmaxf(most[n], float(all));
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < kAtOnce; ++n) {
+      const int b = b0 + n * kPages + at;
+      // (adding 0 leaves no -0: equal scores have equal bits)
+      if (slice == 0 && b <= last) st_agent(scores + b, __float_as_uint(page[n] >= 0 ? most[n] + 0.f : -INFINITY));
+    }
+  }
+  for (int b = last + 1 + part * kSelThreads + threadIdx.x; b < a.t.max_pages; b += a.parts * kSelThreads)
+    scores[b] = __float_as_uint(-INFINITY);
+  if (a.parts > 1) {
+    if (!last_of_group(a.counters + item, unsigned(a.parts), &last_flag)) return;
+  } else {
+    __builtin_amdgcn_s_waitcnt(0);         // (this wavefront's scores have been acknowledged)
+    __syncthreads();
+  }
+  auto from_memory = [&](int, int b) { return b <= last ? page_key(a, __uint_as_float(ld_agent(scores + b)), b, last) : 0u; };
+  if (last < kSelThreads * kSelEach) {
+    uint32_t k[kSelEach];
+#pragma unroll
+    for (int i = 0; i < kSelEach; ++i) k[i] = from_memory(i, i * kSelThreads + threadIdx.x);
+    select_from(a, item, last, [&](int i, int) {
+      uint32_t of = k[0];
+#pragma unroll
+      for (int j = 1; j < kSelEach; ++j) of = i == j ? k[j] : of;
+      return of;
+    });
+  } else {
+    select_from(a, item, last, from_memory);
+  }
 }
 
 // ---- host side
@@ -236,7 +284,7 @@ int launch_paged_bounds(const actqkv_shape& sh, const PagedTable& t, const void*
   return hip_status("paged key bounds");
 }
 int launch_paged_select(const actqkv_shape& sh, const PagedTable& t, const void* q, const void* bounds, int k_sel, int keep_first,
-                        int keep_last, float* scores, int64_t stride, int32_t* idx, int32_t* n_sel, hipStream_t stream) {
+                        int keep_last, float* scores, int64_t stride, int32_t* idx, int32_t* n_sel, const Workspace& ws, hipStream_t stream) {
   PagedSelect a;
   a.t = t;
   a.q = q;
@@ -250,18 +298,17 @@ int launch_paged_select(const actqkv_shape& sh, const PagedTable& t, const void*
   a.stride = stride;
   a.idx = idx;
   a.n_sel = n_sel;
-  const unsigned items = unsigned(t.n_rows) * sh.n_kv_heads;
-  const int pages = kSelThreads / (sh.head_dim / 16);
-  const dim3 grid(items, std::min((t.max_pages + pages - 1) / pages, kSelMostY));
-  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kSelThreads), 0, stream, a); };
+  const int64_t items = int64_t(t.n_rows) * sh.n_kv_heads;
+  a.parts = items > int64_t(kTicketCounters) ? 1 : int(std::max<int64_t>(1, std::min<int64_t>((t.max_pages + kSelLeast - 1) / kSelLeast, kSelWgs / items)));
+  a.counters = ws.counters();
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned(items) * a.parts), dim3(kSelThreads), 0, stream, a); };
   if (sh.dtype == ACTQKV_F32) {
-    if (sh.head_dim == 64) launch(paged_scores_kernel<float, 64>);
-    else launch(paged_scores_kernel<float, 128>);
+    if (sh.head_dim == 64) launch(paged_select_kernel<float, 64>);
+    else launch(paged_select_kernel<float, 128>);
   } else {
-    if (sh.head_dim == 64) launch(paged_scores_kernel<uint16_t, 64>);
-    else launch(paged_scores_kernel<uint16_t, 128>);
+    if (sh.head_dim == 64) launch(paged_select_kernel<uint16_t, 64>);
+    else launch(paged_select_kernel<uint16_t, 128>);
   }
-  hipLaunchKernelGGL(paged_select_kernel, dim3(items), dim3(kSelThreads), 0, stream, a);
   return hip_status("paged page selection");
 }
 

@@ -247,7 +247,7 @@ template <typename... P> struct Entry<int(P...)> {
   X(paged_append_quantised, "@ssseesq")                               \
   X(paged_attention_quantised, "@seeswq")                             \
   X(paged_key_bounds, "@ssq")                                    \
-  X(paged_select_pages, "@ssq")                                  \
+  X(paged_select_pages, "@sswq")                                 \
   X(paged_attention_selected, "@sssswq")
 
 #define ACTQKV_DEFINE(name, kinds)                                                          \

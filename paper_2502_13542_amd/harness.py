@@ -1106,7 +1106,7 @@ class PagedRunner:
         if n_rows == 0:
             return
         B.paged_select_pages(self.cs, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, bounds, n_pages, idx.shape[-1],
-                             keep_first, keep_last, scores, scores.shape[-1], idx, n_sel, stream)
+                             keep_first, keep_last, scores, scores.shape[-1], idx, n_sel, self.workspace, stream)
 
     def attend_selected(self, q, row_start, n_ctx, pages, k_pages, v_pages, idx, n_sel, out, lse=None, softcap: float = 0.0,
                         window: int = 0, slopes=None, row_first=None, row_end=None, stream=None, max_new=None) -> None:

@@ -139,8 +139,8 @@ def bounds(lib, cs, **kw):
 
 
 def select(lib, cs, **kw):
-    return call(lib, "select_pages", "batch n_rows max_new q rs n pages max_pages bounds n_pages k_sel keep_first keep_last scores stride idx n_sel",
-                dict(T, q=A16, bounds=A16, k_sel=4, keep_first=1, keep_last=1, scores=A16, stride=4, idx=A16, n_sel=A16), cs, kw)
+    return call(lib, "select_pages", "batch n_rows max_new q rs n pages max_pages bounds n_pages k_sel keep_first keep_last scores stride idx n_sel ws wsb",
+                dict(T, q=A16, bounds=A16, k_sel=4, keep_first=1, keep_last=1, scores=A16, stride=4, idx=A16, n_sel=A16, ws=A16, wsb=1 << 40), cs, kw)
 
 
 def selected(lib, cs, **kw):
@@ -199,7 +199,7 @@ def test_selected_refusals(lib, bad, code):
 @pytest.mark.parametrize("bad,code", [x for x in TABLE if "kp" not in x[0] and "vp" not in x[0]] + ROWS + [
     (dict(bounds=None), -1), (dict(bounds=A16 + 8), -3), (dict(q=None), -1), (dict(q=A16 + 8), -3), (dict(keep_first=-1), -1), (dict(keep_last=-1), -1),
     (dict(keep_first=3, keep_last=2), -1), (dict(keep_first=2 ** 31 - 1, keep_last=2 ** 31 - 1), -1), (dict(scores=None), -1), (dict(scores=A16 + 2), -3),
-    (dict(stride=3), -1)])
+    (dict(stride=3), -1), (dict(ws=None), -4), (dict(ws=A16 + 8), -4), (dict(wsb=64), -4)])
 def test_select_refusals(lib, bad, code):
     assert select(lib, B.c_shape(LLAMA), **bad) == code
 
