@@ -13,6 +13,7 @@ namespace actqkv {
 constexpr int kP4Threads = 256, kP4Waves = 4, kP4Rows = 32 * kP4Waves;
 constexpr int kP4Part = 8192;                     // one of the three parts of K or V^T of a tile
 constexpr int kP4MaxSplits = 32, kP4Slots = 512;  // pieces of a query tile; workgroups that fill the chip
+constexpr int kP4SlotsByte = 1024;                // of pages in 8 bits
 
 struct PagedChunkF32 {
   PagedAttn a;
@@ -425,20 +426,31 @@ inline int chunk_f32_tiles(const actqkv_shape& sh, int batch, int n_rows, int ma
 // share a compute unit, or one waits for another (of the first rows of a prompt few pieces have keys, and of several sequences some are short); a launch
 // to merge 4, and 0.4 a piece.  8 query and 2 KV heads of 64, us with so many pieces: 2 x 2048 rows at 8192 tokens 1 398, 2 361; 2048
 // at 2048 2 63, 4 46; 2 x 512 at 4096 4 68, 8 63; 4 x 33 at 2000 16 20, 32 23; 128 at 16384 16 63, 32 46, 64 52.
+// In 8 bits a tile is 1.6 and a piece 2 more, pieces may be twice as many, which evens out tiles of different length, and the factors are
+// fitted to these: 2 x 2048 rows at 8192 tokens 1 238, 2 205, 4 187, 8 196 (128 channels 490, 457, 458); 20 sequences of up to 100 rows at up to
+// 3000 1 87, 3 41, 6 38, 24 48; 2 x 512 at 4096 4 44, 8 42; 2048 at 2048 2 42, 4 34, 8 37; 128 at 16384 8 68, 16 42, 32 34 (54).
 inline int chunk_f32_splits(const actqkv_shape& sh, const PagedAttn& p, int tiles) {
   const int64_t items = int64_t(tiles) * sh.n_kv_heads;
   const int keys = 4096 / sh.head_dim;
-  const double tile_us = sh.head_dim == 64 ? 2.9 : 3.2;
+  const bool byte = p.k_scales != nullptr;
+  const double tile_us = byte ? 1.6 : sh.head_dim == 64 ? 2.9 : 3.2;
   int64_t longest = int64_t(p.t.max_pages) * (kBlock / keys);
   if (p.f.window > 0) longest = std::min<int64_t>(longest, (int64_t(p.f.window) + kP4Rows) / keys + 2);
   if (p.f.row_first != nullptr) longest = (longest + 2) / 3;      // (of documents a part, nobody knows which)
   const double own = double(p.t.max_new) / keys, average = double(longest) - std::min<double>(own, double(longest)) / 2.;
   int best = 1;
   double least = 0.;
-  for (int splits = 1; splits <= std::min<int64_t>(kP4MaxSplits, longest) && (splits == 1 || items * splits <= kP4Slots); ++splits) {
+  for (int splits = 1; splits <= std::min<int64_t>(kP4MaxSplits, longest) && (splits == 1 || items * splits <= (byte ? kP4SlotsByte : kP4Slots)); ++splits) {
     const double busy = double(items) * splits * average / double(longest) / kChipCus * (p.t.batch > 1 ? 0.8 : 1.);
     double us = double((longest + splits - 1) / splits) * tile_us * (1. + 0.9 * std::min(std::max(busy - 1., 0.), 1.));
-    if (splits > 1) us += 4. + 0.4 * splits;
+    if (byte) {                                    // the longest piece, or what a compute unit has in all
+      const double pieces = double(items) * splits * (p.t.batch > 1 ? 0.8 : 1.), share = pieces / kChipCus;
+      us = std::max((double((longest + splits - 1) / splits) * tile_us + 2.) * (1. + 0.3 * std::min(std::max(share - 1., 0.), 1.)),
+                    share * (average / splits * tile_us + 2.) * 0.6 * (p.t.batch > 1 ? 0.7 : 1.));
+      if (splits > 1) us += 4. + pieces * (sh.head_dim * kP4Rows * 8) / 3e6;
+    } else if (splits > 1) {
+      us += 4. + 0.4 * splits;
+    }
     if (splits == 1 || us < least) {
       least = us;
       best = splits;
