@@ -764,8 +764,8 @@ int actqkv_paged_select_pages(const actqkv_shape* shape, int batch, int n_rows, 
                               void* workspace, size_t ws_bytes, void* stream);
 
 /* actqkv_paged_attention of rows that see, of the positions they would see there, those in their selected pages alone: idx and n_sel as above (or the
- * caller's own; a page in a list twice counts twice, entries outside the sequence's pages are skipped).  Every row reads its own pages: meant for single tokens and a few
- * drafted ones; rows of a long chunk share nothing.  Workspace and errors as there; n_rows * Hk is at most 2^22. */
+ * caller's own, ascending, a page once; entries outside the sequence's pages are skipped).  Of single tokens and a few drafted ones every row reads its own pages;
+ * rows of longer chunks share what tiles of them read, where that is less.  Workspace and errors as there; n_rows * Hk is at most 2^22. */
 int actqkv_paged_attention_selected(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q,
                                     const int32_t* row_start, const int32_t* n_ctx, const int32_t* pages, int max_pages,
                                     const void* k_pages, const void* v_pages, int n_pages, const int32_t* idx, const int32_t* n_sel,

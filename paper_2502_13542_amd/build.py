@@ -17,7 +17,8 @@ SOURCES = ["api.hip", "probe.hip", "score.hip", "select.hip", "attn_prefill_f32.
            "decode_retrieve.hip", "attn_static.hip", "paged_api.hip", "paged_append.hip",
            "paged_append_rotated.hip", "paged8_append.hip", "paged_chunk.hip",
            "paged_chunk_f32.hip", "paged8_chunk.hip", "paged8_chunk_f32.hip", "paged_step.hip",
-           "paged8_step.hip", "paged_selected.hip", "paged_select.hip", "paged_weights.hip",
+           "paged8_step.hip", "paged_selected.hip", "paged_chosen_chunk.hip",
+           "paged_chosen_chunk_f32.hip", "paged_select.hip", "paged_weights.hip",
            "paged_evict.hip"]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

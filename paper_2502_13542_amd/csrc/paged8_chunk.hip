@@ -5,7 +5,7 @@ namespace actqkv {
 
 template <int D, int KS, bool kCap, bool kBias>
 __global__ __launch_bounds__(kPcThreads) void paged8_chunk_kernel(PagedChunk c) {
-  chunk_body<D, KS, kCap, kBias, true>(c);
+  chunk_body<D, KS, kCap, kBias, true, false>(c);
 }
 
 template <int D, int KS>
@@ -33,6 +33,7 @@ int launch_paged8_chunk(const actqkv_shape& sh, const PagedAttn& p, const Worksp
   c.tiles = cut.tiles;
   c.splits = cut.splits;
   c.part = ws.scratch_f32();
+  c.chosen = PagedBits{nullptr, 0};
   if (sh.head_dim == 64) launch_chunk8_ks<64>(cut.ks, c, stream);
   else launch_chunk8_ks<128>(cut.ks, c, stream);
   return hip_status("paged attention (8 bits, chunks)");

@@ -6,7 +6,7 @@ namespace actqkv {
 
 template <int D, bool kCap, bool kBias>
 __global__ __launch_bounds__(kP4Threads, D == 64 ? 2 : 1) void paged8_chunk_f32_kernel(PagedChunkF32 c) {
-  chunk_f32_body<D, kCap, kBias, true>(c);
+  chunk_f32_body<D, kCap, kBias, true, false>(c);
 }
 
 template <int D>
@@ -27,6 +27,7 @@ int launch_paged8_chunk_f32(const actqkv_shape& sh, const PagedAttn& p, const Wo
   c.tiles = chunk_f32_tiles(sh, p.t.batch, p.t.n_rows, p.t.max_new);
   c.splits = chunk_f32_splits(sh, p, c.tiles);
   c.part = ws.scratch_f32();
+  c.chosen = PagedBits{nullptr, 0};
   if (sh.head_dim == 64) launch_chunk8_f32<64>(c, stream);
   else launch_chunk8_f32<128>(c, stream);
   return hip_status("paged attention (8 bits, chunks, fp32)");

@@ -26,7 +26,7 @@ static int launch_paged_attention(const actqkv_shape& sh, PagedAttn p, const Pag
 }
 // Enough for every call of at most these sizes: of few rows a sequence, none of them takes the chunks' kernels.
 static size_t paged_workspace_bytes(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages) {
-  size_t most = std::max(paged_step_scratch_most(sh, batch, max_new, max_pages), paged_selected_scratch_most(sh, n_rows));
+  size_t most = std::max(paged_step_scratch_most(sh, batch, max_new, max_pages), paged_selected_scratch_most(sh, batch, n_rows, max_new, max_pages));
   if (!paged_step_supported(sh, max_new))
     most = std::max({most, paged_votes_scratch_most(sh),
                      sh.dtype == ACTQKV_F32 ? paged_chunk_f32_scratch_most(sh, batch, n_rows, max_new, max_pages)

@@ -1,0 +1,43 @@
+// Attention of chunks whose rows look at selected pages each (paged_chunk_body.h has the kernel, paged_chunk.hip its design).
+#include "paged_chunk_body.h"
+
+namespace actqkv {
+
+template <int D, int KS, bool kCap, bool kBias>
+__global__ __launch_bounds__(kPcThreads) void paged_chosen_chunk_kernel(PagedChunk c) {
+  chunk_body<D, KS, kCap, kBias, false, true>(c);
+}
+
+template <int D, int KS>
+static void launch_chosen(const PagedChunk& c, hipStream_t stream) {
+  const bool cap = c.a.f.cap_in > 0.f, bias = c.a.f.slopes != nullptr;
+  auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(unsigned(c.tiles) * c.splits * c.a.n_kv_heads), dim3(kPcThreads), 0, stream, c);
+  };
+  if (cap && bias) launch(paged_chosen_chunk_kernel<D, KS, true, true>);
+  else if (cap) launch(paged_chosen_chunk_kernel<D, KS, true, false>);
+  else if (bias) launch(paged_chosen_chunk_kernel<D, KS, false, true>);
+  else launch(paged_chosen_chunk_kernel<D, KS, false, false>);
+  launch_chunk_merge(D, KS, c, stream);
+}
+template <int D>
+static void launch_chosen_ks(int ks, const PagedChunk& c, hipStream_t stream) {
+  if (ks == 1) launch_chosen<D, 1>(c, stream);
+  else if (ks == 2) launch_chosen<D, 2>(c, stream);
+  else launch_chosen<D, 4>(c, stream);
+}
+double paged_chosen_chunk_us(const actqkv_shape& sh, const PagedAttn& p) { return chunk_cut(sh, p).us; }
+int launch_paged_chosen_chunk(const actqkv_shape& sh, const PagedAttn& p, const PagedBits& bits, const Workspace& ws, hipStream_t stream) {
+  const ChunkCut cut = chunk_cut(sh, p);
+  PagedChunk c;
+  c.a = p;
+  c.tiles = cut.tiles;
+  c.splits = cut.splits;
+  c.part = ws.scratch_f32();
+  c.chosen = bits;
+  if (sh.head_dim == 64) launch_chosen_ks<64>(cut.ks, c, stream);
+  else launch_chosen_ks<128>(cut.ks, c, stream);
+  return hip_status("paged attention (selected pages, chunks)");
+}
+
+}  // namespace actqkv

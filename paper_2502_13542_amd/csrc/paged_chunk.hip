@@ -25,7 +25,7 @@ namespace actqkv {
 
 template <int D, int KS, bool kCap, bool kBias>
 __global__ __launch_bounds__(kPcThreads) void paged_chunk_kernel(PagedChunk c) {
-  chunk_body<D, KS, kCap, kBias, false>(c);
+  chunk_body<D, KS, kCap, kBias, false, false>(c);
 }
 
 size_t paged_chunk_scratch_most(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages) {
@@ -81,6 +81,7 @@ int launch_paged_chunk(const actqkv_shape& sh, const PagedAttn& p, const Workspa
   c.tiles = cut.tiles;
   c.splits = cut.splits;
   c.part = ws.scratch_f32();
+  c.chosen = PagedBits{nullptr, 0};
   if (sh.head_dim == 64) launch_chunk_ks<64>(cut.ks, c, stream);
   else launch_chunk_ks<128>(cut.ks, c, stream);
   return hip_status("paged attention (chunks)");

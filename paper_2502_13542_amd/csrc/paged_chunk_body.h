@@ -5,6 +5,7 @@
 #include "e4m3.h"
 #include "mfma_util.h"
 #include "paged.h"
+#include "paged_bits.h"
 #include "paged_merge.h"
 
 namespace actqkv {
@@ -22,6 +23,7 @@ struct PagedChunk {
   int tiles;                 // query tiles that the launch has workgroups for (a bound)
   int splits;                // pieces of a query tile's pages
   void* part;                // pieces [tile][Hk][split]
+  PagedBits chosen;
 };
 template <int D, int KS>
 using ChunkPiece = PagedPiece<kPcWaves / KS, (D / 32 > KS ? D / 32 / KS : 1), (D / 32 < KS ? D / 32 : KS)>;
@@ -48,7 +50,8 @@ __device__ __forceinline__ void chunk_store(const PagedAttn& p, const f32x16 (&o
 // kByte: pages in 8 bits.  Their codes become bf16 between registers and LDS, once for the workgroup, and what follows is what follows
 // in 16 bits.  A page is asked for in the second half of the value products two pages ahead of it (the registers of the scores come
 // free there), and placed in LDS behind the scores of the page before it.
-template <int D, int KS, bool kCap, bool kBias, bool kByte>
+// kChosen: every row sees selected pages alone, as bits (paged_bits.h).  The workgroup walks the pages that any of its rows selected.
+template <int D, int KS, bool kCap, bool kBias, bool kByte, bool kChosen>
 __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
   constexpr int kDb = D / 32, kKs = D / 16;      // 32-channel groups of the output, 16-channel steps of a score
   constexpr int kRows = kPcRows<KS>, kRowGroups = kPcWaves / KS;
@@ -59,6 +62,7 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
   constexpr uint32_t kTileBytes = kPcTileBytes<D>;
   __shared__ __attribute__((aligned(16))) char lds_b[kPcLdsBytes<D>];
   __shared__ int span_lds[2][kPcWaves];
+  __shared__ uint32_t any_bits[kChosen ? kMostBitWords : 1];
   const PagedAttn& p = c.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, half = lane >> 5;
@@ -139,10 +143,13 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
   // the pages of 64 tiles at a time, one per lane
   int my_page = -1;
   float my_k = 1.f, my_v = 1.f;                  // their scales
+  int have = -1;                                 // selected pages: which 64 those are
   auto page_of = [&](int t) {
     const int k = t - t_begin;
-    if ((k & 63) == 0) {
-      my_page = t + lane < t_end ? paged_page(p.t, s, t + lane) : -1;
+    if (kChosen ? k >> 6 != have : (k & 63) == 0) {
+      have = k >> 6;
+      const int at = kChosen ? t_begin + (k & ~63) + lane : t + lane;
+      my_page = at < t_end ? paged_page(p.t, s, at) : -1;
       if constexpr (kByte) {
         const size_t at = size_t(max(my_page, 0)) * p.n_kv_heads + hk;
         my_k = p.k_scales[at];
@@ -166,6 +173,7 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
     none = split > 0 && split * per >= n_tiles;
     t_begin = t_first + split * per;
     t_end = min(t_first + n_tiles, t_begin + per);
+    if (kChosen) t_begin = next_chosen(any_bits, t_begin, t_end);
     if (t_begin < t_end) {
       page = page_of(t_begin);
       if constexpr (kByte) {
@@ -176,6 +184,10 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
       }
     }
   };
+  if constexpr (kChosen) {
+    const int first = qtile * kRows / group, last = (min((qtile + 1) * kRows, seq.m * group) - 1) / group;
+    any_chosen<kPcThreads>(c.chosen, seq.row0 + first, last - first + 1, hk, p.n_kv_heads, any_bits);
+  }
   const bool arrays = p.f.row_first != nullptr || p.f.row_end != nullptr;
   if (!arrays) {
     const int first = qtile * kRows / group, last = (min((qtile + 1) * kRows, seq.m * group) - 1) / group, w0 = seq.n - seq.m;
@@ -247,8 +259,18 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
   const int a_row = perm_row(n);
   uint32_t a_off0 = uint32_t(a_row) * kKRow + (uint32_t(half ^ (D == 128 ? a_row & 15 : (a_row >> 1) & 7)) << 4);
   uint32_t v_off0 = uint32_t(n) * 256 + (uint32_t(half ^ (n & 15)) << 4);
-  for (int t = t_begin; t < t_end; ++t) {
-    const int stage = (t - t_begin) & 1;
+  const uint32_t* row_bits = kChosen ? c.chosen.of(row, hk, p.n_kv_heads) : nullptr;
+  uint32_t word = 0;                             // of 32 pages, which this lane's row sees
+  int word_at = -1, step = 0;
+  for (int t = t_begin, t_next; t < t_end; t = t_next, ++step) {
+    const int stage = kChosen ? step & 1 : (t - t_begin) & 1;
+    t_next = kChosen ? next_chosen(any_bits, t + 1, t_end) : t + 1;
+    bool seen_page = true;
+    if constexpr (kChosen) {
+      if (t >> 5 != word_at) word = row_bits[word_at = t >> 5];
+      seen_page = (word >> (t & 31) & 1) != 0;
+    }
+    const uint32_t len = kChosen && !seen_page ? 0u : v_len;
     asm volatile("" : "+v"(a_off0), "+v"(v_off0));     // (XOR-ed offsets are recomputed, not kept across the loop)
     int page_after = -1;                         // 8 bits: the page behind the next one
     Scales after_by{1.f, 1.f};
@@ -258,11 +280,11 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
         after_by = scales_of(t + 2);
       }
     } else {
-      page_next = t + 1 < t_end ? page_of(t + 1) : -1;
+      page_next = t_next < t_end ? page_of(t_next) : -1;
     }
     const int kpos0 = t * kBlock, sub0 = kpos0 + kb0 * 32, sub1 = sub0 + kNg * 32;
-    const bool visible = page >= 0 && sub0 < hi_any && sub1 > lo_any;
-    const bool masked = sub0 < lo_all || sub1 > hi_all;
+    const bool visible = page >= 0 && sub0 < hi_any && sub1 > lo_any && (!kChosen || __any(seen_page) != 0);
+    const bool masked = sub0 < lo_all || sub1 > hi_all || (kChosen && !__all(seen_page));
     char* ks_ = lds_b + stage * 2 * kTileBytes;
     char* vs_ = ks_ + kTileBytes;
     if (kpos0 + kBlock > seq.n) {                // slots behind the last token: their values may be anything
@@ -348,7 +370,7 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
         for (int kb = 0; kb < kNg; ++kb)
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            acc_s[kb][i] = span_holds(ahead + (kb * 32 + 16 * (i >> 3) + (i & 7)), v_len) ? acc_s[kb][i] : kHidden;
+            acc_s[kb][i] = span_holds(ahead + (kb * 32 + 16 * (i >> 3) + (i & 7)), len) ? acc_s[kb][i] : kHidden;
       }
       // ---- online softmax, one row per lane (lanes n and n + 32 share it)
       auto v_read = [&](int j) {
@@ -495,6 +517,7 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
 //   248, 271, 380; 64 channels, 8192 at 8192 137, 100, 137, with documents 79, 52, 61
 struct ChunkCut {
   int ks, splits, tiles;
+  double us;                 // by those figures
 };
 inline int chunk_tiles(const actqkv_shape& sh, int batch, int n_rows, int max_new, int ks) {
   // every sequence's last tile may be partly empty
@@ -523,7 +546,7 @@ inline ChunkCut chunk_cut(const actqkv_shape& sh, const PagedAttn& p) {
     longest /= 3.;
     equal = alike = false;
   }
-  ChunkCut best{1, 1, 1};
+  ChunkCut best{1, 1, 1, 0.};
   double least = 0.;
   for (int i = 0; i < 3; ++i) {
     const int ks = 1 << i, tiles = chunk_tiles(sh, t.batch, t.n_rows, t.max_new, ks);
@@ -538,7 +561,7 @@ inline ChunkCut chunk_cut(const actqkv_shape& sh, const PagedAttn& p) {
       if (splits > 1) us += 4. + pieces * rows * sh.head_dim * 8. / 4e6;
       if ((i == 0 && splits == 1) || us < least) {
         least = us;
-        best = ChunkCut{ks, splits, tiles};
+        best = ChunkCut{ks, splits, tiles, us};
       }
     }
   }

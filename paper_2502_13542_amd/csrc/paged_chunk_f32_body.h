@@ -6,6 +6,7 @@
 #include "f32_parts.h"
 #include "mfma_util.h"
 #include "paged.h"
+#include "paged_bits.h"
 #include "paged_merge.h"
 
 namespace actqkv {
@@ -19,12 +20,14 @@ struct PagedChunkF32 {
   PagedAttn a;
   int tiles, splits;
   void* part;
+  PagedBits chosen;
 };
 template <int D> using ChunkPieceF32 = PagedPiece<kP4Waves, D / 32, 1>;
 
 // kByte: pages in 8 bits.  A code is a bf16 exactly (one part instead of three, and three products instead of six), and the queries' parts
 // are truncated, so that none exceeds bf16's range: no value is without parts.
-template <int D, bool kCap, bool kBias, bool kByte>
+// kChosen: every row sees selected pages alone, as bits (paged_bits.h); tiles of pages that no row of the workgroup selected are left out.
+template <int D, bool kCap, bool kBias, bool kByte, bool kChosen>
 __device__ __forceinline__ void chunk_f32_body(const PagedChunkF32& c) {
   constexpr int kParts = kByte ? 1 : 3, kVPart0 = kParts;      // parts of a key, and of a value behind them
   constexpr int kKeys = 4096 / D;                   // keys of a tile: 64 or 32
@@ -36,6 +39,7 @@ __device__ __forceinline__ void chunk_f32_body(const PagedChunkF32& c) {
   // whether a wavefront brought values above kFfMax: [K, V^T][wavefront]
   __shared__ __attribute__((aligned(16))) uint32_t no_parts[2][kP4Waves];
   __shared__ int span_lds[2][kP4Waves];
+  __shared__ uint32_t any_bits[kChosen ? kMostBitWords : 1];
   const PagedAttn& p = c.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, half = lane >> 5;
@@ -83,7 +87,20 @@ __device__ __forceinline__ void chunk_f32_body(const PagedChunkF32& c) {
     Piece::store_none(Piece::at(c.part, tile * p.n_kv_heads + hk, c.splits, split, wave), -INFINITY, 0.f, lane);
     return;
   }
-  const int t_begin = t_first + split * per, t_end = min(t_first + n_tiles, t_begin + per);
+  int t_begin = t_first + split * per, t_end = min(t_first + n_tiles, t_begin + per);
+  auto next_tile = [&](int t) {                     // the first tile from t on that some row sees
+    if constexpr (kChosen) {
+      if (t >= t_end) return t_end;
+      const int page = next_chosen(any_bits, t / kPerPage, (t_end + kPerPage - 1) / kPerPage);
+      return min(page == t / kPerPage ? t : page * kPerPage, t_end);
+    }
+    return t;
+  };
+  if constexpr (kChosen) {
+    const int first = qtile * kP4Rows / group, last = (min((qtile + 1) * kP4Rows, seq.m * group) - 1) / group;
+    any_chosen<kP4Threads>(c.chosen, seq.row0 + first, last - first + 1, hk, p.n_kv_heads, any_bits);
+    t_begin = next_tile(t_begin);
+  }
 
   // ---- tiles: a wavefront brings a quarter of the rows of K and of V^T into registers, 4 x 1 KB each
   constexpr int kKPer = 1024 / (4 * D), kVPer = 1024 / (4 * kKeys);   // rows of 1 KB in memory
@@ -255,18 +272,29 @@ __device__ __forceinline__ void chunk_f32_body(const PagedChunkF32& c) {
   float m_run = -INFINITY, l_run = 0.f;                      // the row's maximum (log2 units), this lane's share of the sum
 
   const int kn = perm_row(n);                                // the key of this lane's row in the first product
-  for (int t = t_begin; t < t_end; ++t) {
+  const uint32_t* row_bits = kChosen ? c.chosen.of(row, hk, p.n_kv_heads) : nullptr;
+  uint32_t word = 0;                                         // of 32 pages, which this lane's row sees
+  int word_at = -1;
+  for (int t = t_begin, t_next; t < t_end; t = t_next) {
+    t_next = kChosen ? next_tile(t + 1) : t + 1;
+    bool seen_page = true;
+    if constexpr (kChosen) {
+      const int of = t / kPerPage;
+      if (of >> 5 != word_at) word = row_bits[word_at = of >> 5];
+      seen_page = (word >> (of & 31) & 1) != 0;
+    }
+    const uint32_t len = kChosen && !seen_page ? 0u : v_len;
     const int key0 = now.key0, lo = now.lo, hi = now.hi;
     const size_t at_page = now.at;
     if (t > t_begin) __syncthreads();                        // everybody is done with the tile before
     store_tile(now);
     __syncthreads();
-    if (t + 1 < t_end) {
-      now = tile_at(t + 1);
+    if (t_next < t_end) {
+      now = tile_at(t_next);
       fetch_tile(now);
     }
-    if (!(hi > lo && lo < hi_any && hi > lo_any)) continue;  // none of the wavefront's rows sees any of it
-    const bool masked = key0 < lo_all || key0 + kKeys > hi_all;
+    if (!(hi > lo && lo < hi_any && hi > lo_any) || (kChosen && !__any(seen_page))) continue;  // none of the wavefront's rows sees any of it
+    const bool masked = key0 < lo_all || key0 + kKeys > hi_all || (kChosen && !__all(seen_page));
     bool k_large = q_large, v_large = false;
     if constexpr (!kByte) {
       const u32x4 of_k = *reinterpret_cast<const u32x4*>(no_parts[0]), of_v = *reinterpret_cast<const u32x4*>(no_parts[1]);
@@ -326,7 +354,7 @@ __device__ __forceinline__ void chunk_f32_body(const PagedChunkF32& c) {
       for (int gg = 0; gg < kG; ++gg)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          acc_s[gg][i] = span_holds(ahead + (gg * 32 + 16 * (i >> 3) + (i & 7)), v_len) ? acc_s[gg][i] : -INFINITY;
+          acc_s[gg][i] = span_holds(ahead + (gg * 32 + 16 * (i >> 3) + (i & 7)), len) ? acc_s[gg][i] : -INFINITY;
     }
     float mx = acc_s[0][0];
 #pragma unroll
@@ -429,7 +457,7 @@ inline int chunk_f32_tiles(const actqkv_shape& sh, int batch, int n_rows, int ma
 // In 8 bits a tile is 1.6 and a piece 2 more, pieces may be twice as many, which evens out tiles of different length, and the factors are
 // fitted to these: 2 x 2048 rows at 8192 tokens 1 238, 2 205, 4 187, 8 196 (128 channels 490, 457, 458); 20 sequences of up to 100 rows at up to
 // 3000 1 87, 3 41, 6 38, 24 48; 2 x 512 at 4096 4 44, 8 42; 2048 at 2048 2 42, 4 34, 8 37; 128 at 16384 8 68, 16 42, 32 34 (54).
-inline int chunk_f32_splits(const actqkv_shape& sh, const PagedAttn& p, int tiles) {
+inline int chunk_f32_splits(const actqkv_shape& sh, const PagedAttn& p, int tiles, double* took = nullptr) {
   const int64_t items = int64_t(tiles) * sh.n_kv_heads;
   const int keys = 4096 / sh.head_dim;
   const bool byte = p.k_scales != nullptr;
@@ -456,6 +484,7 @@ inline int chunk_f32_splits(const actqkv_shape& sh, const PagedAttn& p, int tile
       best = splits;
     }
   }
+  if (took != nullptr) *took = least;
   return best;
 }
 // The merge of a call's pieces, where there are several (paged_chunk_f32.hip).

@@ -1,8 +1,21 @@
 // Attention of rows that look at selected pages each (paged_step_body.h has the kernel): a (row, KV head) of its own per group of
 // workgroups, its items the halves of the pages in the row's list.
+//
+// That reads every list, from the L2s and the memory-side cache where rows share pages: 8 to 9 TB/s at best.  Rows of a chunk share most of
+// theirs, and where reading every page of the sequence once for a tile of rows takes less, the chunks' kernels do that, with the lists as bits
+// (paged_bits.h).  us of lists | so, 32 query and 8 KV heads of 128, 96 pages a row at 100K tokens: 512 rows 2773 | 762 (all pages: 802), 64 391 | 144, 16 132 | 97;
+// 8 x 64 rows, 32 pages at 16K 946 | 181; fp32, 8 and 2 heads of 64, 512 rows, 16 pages at 8K 145 | 91.  16 sequences' single tokens at up to 32K, 32 pages each: 49 us = 5.4
+// TB/s from memory.
+#include "checks.h"
+#include "paged_bits.h"
 #include "paged_step_body.h"
 
 namespace actqkv {
+
+double paged_chosen_chunk_us(const actqkv_shape& sh, const PagedAttn& p);
+double paged_chosen_chunk_f32_us(const actqkv_shape& sh, const PagedAttn& p);
+int launch_paged_chosen_chunk(const actqkv_shape& sh, const PagedAttn& p, const PagedBits& bits, const Workspace& ws, hipStream_t stream);
+int launch_paged_chosen_chunk_f32(const actqkv_shape& sh, const PagedAttn& p, const PagedBits& bits, const Workspace& ws, hipStream_t stream);
 
 template <typename T, int D, bool kCap, bool kBias>
 __global__ __launch_bounds__(kStThreads) void paged_selected_kernel(PagedStep st) {
@@ -18,8 +31,50 @@ static void launch_selected(const PagedStep& st, hipStream_t stream) {
   else if (bias) launch(paged_selected_kernel<T, D, false, true>);
   else launch(paged_selected_kernel<T, D, false, false>);
 }
-size_t paged_selected_scratch_most(const actqkv_shape& sh, int n_rows) {
-  return step_part_most(sh, int64_t(n_rows) * sh.n_kv_heads);
+
+// The lists as bits: a wavefront a (row, KV head), 64 words and 64 entries at a time.
+constexpr int kPbThreads = 256;
+__global__ __launch_bounds__(kPbThreads) void paged_bits_kernel(PagedStep st, uint32_t* bits, int words) {
+  const PagedTable& t = st.a.t;
+  const int lane = threadIdx.x & 63, hk_n = st.a.n_kv_heads;
+  const int64_t item = int64_t(blockIdx.x) * (kPbThreads / 64) + (threadIdx.x >> 6);
+  if (item >= int64_t(t.n_rows) * hk_n) return;
+  const int32_t* idx = st.idx + size_t(item) * st.k_sel;
+  const int n = min(max(st.n_sel[item], 0), st.k_sel);
+  for (int w0 = 0; w0 < words; w0 += 64) {
+    uint32_t word = 0;
+    for (int l0 = 0; l0 < n; l0 += 64) {
+      const int e = l0 + lane < n ? idx[l0 + lane] : -1;
+      for (int j = 0; j < min(n - l0, 64); ++j) {
+        const int page = __builtin_amdgcn_readlane(e, j);
+        if (page >= 0 && page < t.max_pages && page >> 5 == w0 + lane) word |= 1u << (page & 31);
+      }
+    }
+    if (w0 + lane < words) bits[size_t(item) * words + w0 + lane] = word;
+  }
+}
+constexpr size_t kMostBitBytes = size_t(256) << 20;        // of a call whose lists are taken as bits
+static size_t bit_bytes(const actqkv_shape& sh, int n_rows, int max_pages) {
+  return size_t(n_rows) * sh.n_kv_heads * ((max_pages + 31) / 32) * sizeof(uint32_t);
+}
+static size_t chunk_scratch(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages) {
+  return align_up(sh.dtype == ACTQKV_F32 ? paged_chunk_f32_scratch_most(sh, batch, n_rows, max_new, max_pages)
+                                         : paged_chunk_scratch_most(sh, batch, n_rows, max_new, max_pages), 256);
+}
+size_t paged_selected_scratch_most(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages) {
+  const size_t parts = step_part_most(sh, int64_t(n_rows) * sh.n_kv_heads);
+  if (paged_step_supported(sh, max_new)) return parts;
+  return std::max(parts, chunk_scratch(sh, batch, n_rows, max_new, max_pages) +
+                             std::min(kMostBitBytes, bit_bytes(sh, n_rows, std::min(max_pages, 32 * kMostBitWords))));
+}
+// Whether the chunks' kernels take a call: by what they say they take for all pages, and the lists at 8 TB/s.
+static bool selected_by_chunks(const actqkv_shape& sh, const PagedAttn& p, int k_sel) {
+  if (paged_step_supported(sh, p.t.max_new) || p.t.max_pages > 32 * kMostBitWords ||
+      bit_bytes(sh, p.t.n_rows, p.t.max_pages) > kMostBitBytes)
+    return false;
+  const bool f32 = sh.dtype == ACTQKV_F32;
+  const double lists = double(p.t.n_rows) * sh.n_kv_heads * std::min(k_sel, p.t.max_pages) * 2. * kBlock * sh.head_dim * (f32 ? 4. : 2.);
+  return (f32 ? paged_chosen_chunk_f32_us(sh, p) : paged_chosen_chunk_us(sh, p)) + 8. < lists / 8e6;
 }
 int launch_paged_selected(const actqkv_shape& sh, const PagedAttn& p, const int32_t* idx, const int32_t* n_sel, int k_sel,
                           const Workspace& ws, hipStream_t stream) {
@@ -34,6 +89,16 @@ int launch_paged_selected(const actqkv_shape& sh, const PagedAttn& p, const int3
   st.idx = idx;
   st.n_sel = n_sel;
   st.k_sel = k_sel;
+  if (selected_by_chunks(sh, p, k_sel)) {
+    const PagedTable& t = p.t;
+    uint32_t* bits = reinterpret_cast<uint32_t*>(ws.scratch_f32()) + chunk_scratch(sh, t.batch, t.n_rows, t.max_new, t.max_pages) / sizeof(uint32_t);
+    const int words = (t.max_pages + 31) / 32;
+    const int64_t items = int64_t(t.n_rows) * sh.n_kv_heads;
+    hipLaunchKernelGGL(paged_bits_kernel, dim3(unsigned((items + kPbThreads / 64 - 1) / (kPbThreads / 64))), dim3(kPbThreads), 0, stream, st, bits, words);
+    ACTQKV_TRY(hip_status("paged attention (selected pages as bits)"));
+    return f32 ? launch_paged_chosen_chunk_f32(sh, p, PagedBits{bits, words}, ws, stream)
+               : launch_paged_chosen_chunk(sh, p, PagedBits{bits, words}, ws, stream);
+  }
   if (f32) {
     if (sh.head_dim == 64) launch_selected<float, 64>(st, stream);
     else launch_selected<float, 128>(st, stream);

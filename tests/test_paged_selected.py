@@ -186,16 +186,52 @@ def test_selected_forms(shape, kind):
 
 
 @pytest.mark.parametrize("shape", ["llama", "fp32_64"])
-def test_selected_without_pages_twice_the_same_and_at_clamped_lengths(shape):
+def test_selected_without_pages_and_at_clamped_lengths(shape):
     b = Batch(shape_of(*SHAPES[shape]), LONG["drafts"], 21)
     b.pages[0, [0, 3, 11]], b.pages[1, 0] = -1, b.n_pages
     chosen = some_pages(b, 6, 3)
-    chosen[0][0], chosen[1][0], chosen[2][0] = [2, 2, 5], [0, 3], []
-    chosen[3][0] = [2 ** 30, 4, -5, 2 ** 31 - 1]
+    chosen[0][0], chosen[1][0], chosen[2][0] = [2, 5], [0, 3], []
+    chosen[3][0] = [-5, -1, 4, 2 ** 30, 2 ** 31 - 1]
     run_selected(b, chosen, 6)
     c = clamped_batch(shape)
     c.positions = lambda: Batch.positions(c)
     run_selected(c, [[[0, 1]] * c.shape.n_kv_heads if c.row_start[0] <= r < c.row_start[-1] else None for r in range(c.n_rows)], 2)
+
+
+# Calls that the chunks' kernels take, in every cut of theirs (128 pages a row: reading every list takes far longer); tables wider than the sequences
+CHUNKS = [("llama", [(300, 2600), (64, 700), (1, 300), (0, 5), (130, 130)], 0, 128), ("g7", [(100, 5000), (70, 900)], 3, 128), ("mha64", [(500, 4000), (300, 300)], 0, 128),
+          ("g8_64", [(260, 6000)], 30, 128), ("fp32_64", [(300, 2600), (64, 700), (1, 300)], 0, 128), ("fp32_g3", [(200, 3000), (3, 500)], 0, 128),
+          ("fp32_g8", [(130, 3300)], 9, 128), ("g5_64", [(128, 9000), (40, 4200)], 0, 128)]
+
+
+@pytest.mark.parametrize("case", range(len(CHUNKS)))
+@pytest.mark.parametrize("kind", ["plain", "cap", "slopes", "all", "first", "window"])
+def test_selected_of_chunks(case, kind):
+    shape, seqs, more, k_sel = CHUNKS[case]
+    b = Batch(shape_of(*SHAPES[shape]), seqs, 31 + case, extra_rows=(2, 1), extra_entries=more)
+    if kind == "plain":
+        b.pages[0, 3], b.pages[0, 1] = -1, b.n_pages
+    chosen = some_pages(b, min(k_sel, 9), 8)
+    for r in range(0, b.n_rows, 5):
+        if chosen[r] is not None:
+            chosen[r][0] = list(range(max(b.positions()[r], 0) // BS + 1))       # all that the row sees
+    run_selected(b, chosen, k_sel, kind, 9)
+
+
+def test_selected_of_chunks_takes_the_kernels_of_chunks():
+    """The same call with rows few enough for lists, and with many: within the same bounds (as above), and the second one far less than its lists."""
+    sh = shape_of(*SHAPES["llama"])
+    b = Batch(sh, [(256, 8000)], 33, garbage=None)
+    every = [[list(range(p // BS + 1))] * sh.n_kv_heads for p in b.positions()]
+    t, q, r = b.dev(), b.q.to(DEV), b.runner()
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device=DEV)
+    idx = i32([[h + [-1] * (b.max_pages - len(h)) for h in row] for row in every])
+    n_sel = (idx >= 0).sum(-1).int()
+    outs = [torch.zeros_like(q) for _ in range(2)]
+    r.attend_selected(q, t["row_start"], t["n_ctx"], t["pages"], t["k_pages"], t["v_pages"], idx, n_sel, outs[0])
+    r.attend(q, t["row_start"], t["n_ctx"], t["pages"], t["k_pages"], t["v_pages"], outs[1])
+    torch.cuda.synchronize()
+    assert torch.equal(*outs)                     # (all pages selected: the chunks' attention, bit for bit)
 
 
 @pytest.mark.parametrize("shape", ["llama", "fp32_g3", "g7"])
