@@ -919,10 +919,11 @@ class PagedRunner:
         ws = B.paged_workspace_bytes(self.cs, batch, n_rows, max_new, max_pages)
         self.workspace = torch.zeros(ws, dtype=torch.uint8, device=device)
         self._page = shape.n_kv_heads * shape.block_size * shape.head_dim
+        self._q_row = shape.n_q_heads * shape.head_dim
 
     def _table(self, n_ctx, pages, k_pages, v_pages) -> Tuple[int, int, int]:
         batch, max_pages = pages.shape
-        n_pages = k_pages.shape[0]
+        n_pages = k_pages.size(0)
         if batch > self.batch or max_pages > self.max_pages:
             raise B.ActQKVError(-1, f"{batch} sequences of {max_pages} pages: made for {self.batch} of {self.max_pages}")
         if n_ctx.numel() != batch:
@@ -932,7 +933,7 @@ class PagedRunner:
         return batch, max_pages, n_pages
 
     def _rows(self, batch: int, row_start, rows, heads: int, max_new, *same) -> Tuple[int, int]:
-        n_rows = rows.shape[0]
+        n_rows = rows.size(0)
         max_new = self.max_new if max_new is None else max_new
         if not 1 <= max_new <= self.max_new:
             raise B.ActQKVError(-1, f"max_new {max_new}: made for {self.max_new}")
@@ -940,8 +941,9 @@ class PagedRunner:
             raise B.ActQKVError(-1, f"row_start has {row_start.numel()} entries for {batch} sequences")
         if n_rows > self.n_rows:
             raise B.ActQKVError(-1, f"{n_rows} rows: made for {self.n_rows}")
+        size = n_rows * heads * self.shape.head_dim
         for t in (rows, *same):
-            if t.numel() != n_rows * heads * self.shape.head_dim:
+            if t.numel() != size:
                 raise B.ActQKVError(-1, f"tensor of {t.numel()} elements, expected {n_rows} rows of {heads} heads")
         return n_rows, min(max_new, n_rows)
 
@@ -1012,15 +1014,18 @@ class PagedRunner:
                       keep_first, keep_last, budget, to_pages, to_pages.shape[-1], to_weights, to_stride, kept, n_kept, stream)
 
     # ---- rotation on the way into the cache
-    def _turn(self, n_rows: int, rotation, q, q_out, row_pos, interleaved) -> Tuple[int, int, bool]:
-        """n_positions, rotary_dim and interleaved of a call."""
-        self._per_row(n_rows * self.shape.n_q_heads * self.shape.head_dim, q, q_out)
-        self._per_row(n_rows, row_pos)
+    def _turn(self, n_rows: int, rotation, q, q_out, row_pos) -> Tuple[int, int]:
+        """n_positions and rotary_dim of a call."""
+        if q is not None and q.numel() != n_rows * self._q_row or q_out is not None and q_out.numel() != n_rows * self._q_row:
+            raise B.ActQKVError(-1, f"q or q_out is not {n_rows} rows of {self.shape.n_q_heads} heads")
+        if row_pos is not None and row_pos.numel() != n_rows:
+            raise B.ActQKVError(-1, f"row_pos has {row_pos.numel()} entries for {n_rows} rows")
         if rotation is None:
-            return 0, 0, False
-        if rotation.dim() != 3 or rotation.shape[1] != 2:
+            return 0, 0
+        turn = rotation.shape
+        if len(turn) != 3 or turn[1] != 2:
             raise B.ActQKVError(-1, "rotation is not [n_positions][2][rotary_dim / 2]")
-        return rotation.shape[0], 2 * rotation.shape[2], bool(interleaved)
+        return turn[0], 2 * turn[2]
 
     def append_rotated(self, k_new, v_new, row_start, n_ctx, pages, k_pages, v_pages, rotation, q=None, q_out=None, row_pos=None,
                        interleaved: bool = False, stream=None, max_new=None) -> None:
@@ -1029,11 +1034,11 @@ class PagedRunner:
         are not their positions in the cache."""
         batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, v_pages)
         n_rows, max_new = self._rows(batch, row_start, k_new, self.shape.n_kv_heads, max_new, v_new)
-        turn = self._turn(n_rows, rotation, q, q_out, row_pos, interleaved)
+        n_positions, rotary = self._turn(n_rows, rotation, q, q_out, row_pos)
         if n_rows == 0:
             return
         B.paged_append_rotated(self.cs, batch, n_rows, max_new, q, k_new, v_new, row_start, n_ctx, pages, max_pages, k_pages,
-                               v_pages, n_pages, rotation, *turn, row_pos, q_out, stream)
+                               v_pages, n_pages, rotation, n_positions, rotary, interleaved, row_pos, q_out, stream)
 
     # ---- pages in 8 bits
     def _scales(self, n_pages: int, k_scales, v_scales) -> None:
@@ -1046,11 +1051,11 @@ class PagedRunner:
         batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, v_pages)
         self._scales(n_pages, k_scales, v_scales)
         n_rows, max_new = self._rows(batch, row_start, k_new, self.shape.n_kv_heads, max_new, v_new)
-        turn = self._turn(n_rows, rotation, q, q_out, row_pos, interleaved)
+        n_positions, rotary = self._turn(n_rows, rotation, q, q_out, row_pos)
         if n_rows == 0:
             return
         B.paged_append_quantised(self.cs, batch, n_rows, max_new, q, k_new, v_new, row_start, n_ctx, pages, max_pages, k_pages, v_pages,
-                            n_pages, k_scales, v_scales, rotation, *turn, row_pos, q_out, stream)
+                            n_pages, k_scales, v_scales, rotation, n_positions, rotary, interleaved, row_pos, q_out, stream)
 
     def attend_quantised(self, q, row_start, n_ctx, pages, k_pages, v_pages, k_scales, v_scales, out, lse=None, softcap: float = 0.0,
                     window: int = 0, slopes=None, row_first=None, row_end=None, stream=None, max_new=None) -> None:
@@ -1065,9 +1070,12 @@ class PagedRunner:
 
     def _attending(self, batch, row_start, q, out, lse, slopes, row_first, row_end, max_new) -> Tuple[int, int]:
         n_rows, max_new = self._rows(batch, row_start, q, self.shape.n_q_heads, max_new, out)
-        self._per_row(n_rows, row_first, row_end)
-        self._per_row(n_rows * self.shape.n_q_heads, lse)
-        self._per_row(self.shape.n_q_heads, slopes)
+        if row_first is not None or row_end is not None:
+            self._per_row(n_rows, row_first, row_end)
+        if lse is not None:
+            self._per_row(n_rows * self.shape.n_q_heads, lse)
+        if slopes is not None:
+            self._per_row(self.shape.n_q_heads, slopes)
         return n_rows, max_new
 
     # ---- attention over selected pages
@@ -1093,30 +1101,32 @@ class PagedRunner:
         """The pages that each row looks at: idx [n_rows][Hk][k_sel], ascending, and n_sel [n_rows][Hk], by the scores
         [n_rows][Hk][at least max_pages] that the pages' bounds give them."""
         batch, max_pages = pages.shape
-        n_pages = bounds.shape[0]
+        n_pages = bounds.size(0)
         rows = self.shape.n_kv_heads
         if batch > self.batch or max_pages > self.max_pages:
             raise B.ActQKVError(-1, f"{batch} sequences of {max_pages} pages: made for {self.batch} of {self.max_pages}")
         self._per_row(batch, n_ctx)
         self._per_row(n_pages * rows * 2 * self.shape.head_dim, bounds)
         n_rows, max_new = self._rows(batch, row_start, q, self.shape.n_q_heads, max_new)
-        self._per_row(n_rows * rows, n_sel)
-        self._per_row(n_rows * rows * idx.shape[-1], idx)
-        self._per_row(n_rows * rows * scores.shape[-1], scores)
+        k_sel, stride = idx.size(-1), scores.size(-1)
+        rows *= n_rows
+        if n_sel.numel() != rows or idx.numel() != rows * k_sel or scores.numel() != rows * stride:
+            raise B.ActQKVError(-1, f"n_sel, idx or scores is not of {n_rows} rows of {self.shape.n_kv_heads} KV heads")
         if n_rows == 0:
             return
-        B.paged_select_pages(self.cs, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, bounds, n_pages, idx.shape[-1],
-                             keep_first, keep_last, scores, scores.shape[-1], idx, n_sel, self.workspace, stream)
+        B.paged_select_pages(self.cs, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, bounds, n_pages, k_sel,
+                             keep_first, keep_last, scores, stride, idx, n_sel, self.workspace, stream)
 
     def attend_selected(self, q, row_start, n_ctx, pages, k_pages, v_pages, idx, n_sel, out, lse=None, softcap: float = 0.0,
                         window: int = 0, slopes=None, row_first=None, row_end=None, stream=None, max_new=None) -> None:
         """attend, of rows that see their selected pages alone."""
         batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, v_pages)
         n_rows, max_new = self._attending(batch, row_start, q, out, lse, slopes, row_first, row_end, max_new)
-        self._per_row(n_rows * self.shape.n_kv_heads, n_sel)
-        self._per_row(n_rows * self.shape.n_kv_heads * idx.shape[-1], idx)
+        k_sel, rows = idx.size(-1), n_rows * self.shape.n_kv_heads
+        if n_sel.numel() != rows or idx.numel() != rows * k_sel:
+            raise B.ActQKVError(-1, f"n_sel or idx is not of {n_rows} rows of {self.shape.n_kv_heads} KV heads")
         if n_rows == 0:
             return
         B.paged_attention_selected(self.cs, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, k_pages, v_pages, n_pages,
-                                   idx, n_sel, idx.shape[-1], out, lse, self.workspace, softcap, window, slopes, row_first, row_end,
+                                   idx, n_sel, k_sel, out, lse, self.workspace, softcap, window, slopes, row_first, row_end,
                                    stream)

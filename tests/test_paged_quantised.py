@@ -207,6 +207,37 @@ def test_append_rotated(shape, rotary, interleaved):
         run_append(b, min(rotary, sh.head_dim), interleaved, far=i != 1, with_q=i != 2)
 
 
+def test_append_of_more_rows_than_a_launch_has_workgroups_for():
+    """As many rows as a call may bring, of one sequence: the workgroups go round.  (Checked on the device, exactly.)"""
+    sh = shape_of(1, 1, 64, "bf16")
+    m = 2 ** 22
+    n, max_pages = m + 77, m // BS + 1
+    g = torch.Generator(device=DEV).manual_seed(3)
+    k, v = (torch.randn(m, 1, 64, generator=g, device=DEV, dtype=torch.bfloat16) for _ in range(2))
+    pools = [torch.zeros(s, dtype=torch.uint8, device=DEV).view(E4M3) for s in ((max_pages, 1, BS, 64), (max_pages, 1, 64, BS))]
+    pools += [torch.full((max_pages, 1), 2.0 ** -9, device=DEV) for _ in range(2)]
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device=DEV)
+    pages = torch.randperm(max_pages, device=DEV).int()[None].contiguous()
+    H.PagedRunner(sh, 1, m, m, max_pages).append_quantised(k, v, i32([0, m]), i32([n]), pages, *pools)
+    torch.cuda.synchronize()
+    order = pages[0].long()
+    for x, codes, scales in ((k, pools[0], pools[2]), (v, pools[1].transpose(2, 3), pools[3])):
+        full = torch.cat([torch.zeros(77, 64, device=DEV), x[:, 0].float(), torch.zeros(max_pages * BS - n, 64, device=DEV)]).reshape(max_pages, BS, 64)
+        e = torch.ceil(torch.log2(full.abs().amax((1, 2)).double() / 448))
+        e[0] = max(e[0], torch.tensor(-9.0, device=DEV, dtype=torch.float64))
+        assert torch.equal(scales[order, 0], torch.exp2(e).float())
+        want = (full * torch.exp2(-e).float()[:, None, None]).to(E4M3)
+        assert torch.equal(codes[:, 0].float()[order], want.float())
+
+
+@pytest.mark.parametrize("layer", [(16, 1, 128, "bf16"), (16, 1, 64, "fp32"), (48, 3, 64, "bf16"), (5, 1, 128, "fp32")])
+def test_other_groups(layer):
+    for batch in ("steps", "chunks"):
+        b = quantise(Batch(shape_of(*layer), BATCHES[batch], 32, extra_rows=(1, 1)), 9)
+        run_append(loud(b, 4), 48, True)
+        run_attention(b)
+
+
 @pytest.mark.parametrize("shape", ["llama", "fp32_64"])
 def test_append_of_the_scales_edges(shape):
     """Largest values at and next to 448 times a power of two, zeros, subnormals, infinities and NaN, scales that hold anything."""

@@ -91,6 +91,12 @@ def test_rotated_in_place_and_keys_alone(shape, batch):
     run(b, 64, interleaved=True, keys_alone=True)
 
 
+@pytest.mark.parametrize("layer", [(16, 1, 128, "bf16"), (16, 1, 64, "fp32"), (48, 3, 64, "bf16"), (5, 1, 128, "fp32")])
+def test_rotated_of_other_groups(layer):
+    run(Batch(shape_of(*layer), BATCHES["chunks"], 6, extra_rows=(1, 1)), 32, interleaved=True)
+    run(Batch(shape_of(*layer), BATCHES["steps"], 6), 64)
+
+
 def test_rotated_without_pages_and_at_clamped_lengths():
     b = Batch(shape_of(*SHAPES["llama"]), BATCHES["chunks"], 9, garbage=None)
     b.pages[0, 1] = b.n_pages                     # no page: keys go nowhere, queries are turned
@@ -100,9 +106,31 @@ def test_rotated_without_pages_and_at_clamped_lengths():
         run(clamped_batch(shape), 64)
 
 
-def test_rotated_of_more_rows_than_workgroups_go_round():
-    """Few slices a launch: the workgroups go round (a prompt of 5000 rows beside one of 3)."""
-    run(Batch(shape_of(2, 1, 64, "bf16"), [(5000, 5100), (3, 3)], 11, extra_entries=0), 64)
+def test_rotated_of_more_rows_than_a_launch_has_workgroups_for():
+    """2.3 million rows of one sequence: the workgroups go round.  (Checked on the device, in 64 bits.)"""
+    sh = shape_of(1, 1, 64, "bf16")
+    m, n = 2_300_000, 2_300_077
+    max_pages = -(-n // BS)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    k, v, q = (torch.randn(m, 1, 64, generator=g, device=DEV, dtype=torch.bfloat16) for _ in range(3))
+    kp, vp = torch.zeros(max_pages, 1, BS, 64, dtype=torch.bfloat16, device=DEV), torch.zeros(max_pages, 1, 64, BS, dtype=torch.bfloat16, device=DEV)
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device=DEV)
+    table = table_of(64, 50).to(DEV)
+    places = torch.randint(0, 50, (m,), dtype=torch.int32, device=DEV)
+    pages = torch.randperm(max_pages, device=DEV).int()[None].contiguous()
+    H.PagedRunner(sh, 1, m, m, max_pages).append_rotated(k, v, i32([0, m]), i32([n]), pages, kp, vp, table, q=q, q_out=q, row_pos=places)
+    torch.cuda.synchronize()
+    pos = torch.arange(n - m, n, device=DEV)
+    page = pages[0, pos // BS].long()
+    assert torch.equal(vp[page, 0, :, pos % BS], v[:, 0])
+    cos, sin = (table[places.long(), i].double() for i in (0, 1))
+    a, b = k[:, 0, :32].double(), k[:, 0, 32:].double()
+    want = torch.cat([a * cos - b * sin, b * cos + a * sin], -1)
+    size = torch.cat([(a * cos).abs() + (b * sin).abs(), (b * cos).abs() + (a * sin).abs()], -1)
+    bound = 2 * E32 * size
+    bound = bound + E16 * (want.abs() + bound)
+    assert ((kp[page, 0, pos % BS].double() - want).abs() <= bound).all()
+    assert (kp.reshape(max_pages, -1).abs().sum(1) > 0).sum() == -(-n // BS) - (n - m) // BS
 
 
 def test_rotated_on_a_side_stream_and_through_a_larger_runner():

@@ -135,6 +135,38 @@ def test_select_from_many_pages(shape):
     run_select(Batch(sh, [(2, 1000), (1, 33000)], 15, extra_entries=3000, garbage=None), 300, 0, 0)
 
 
+@pytest.mark.parametrize("layer", [(4, 1, 64, "bf16"), (2, 2, 64, "fp32")])
+@pytest.mark.parametrize("k_sel,first,last", [(64, 1, 4), (1500, 0, 0), (7, 0, 0)])
+@pytest.mark.parametrize("kind", ["random", "equal"])
+def test_select_from_more_pages_than_threads_hold_keys(layer, k_sel, first, last, kind):
+    """More than 1024 visible pages: the scores are read again in each round."""
+    b = Batch(shape_of(*layer), [(2, 150000), (1, 131073), (1, 131072)], 16, extra_entries=1, garbage=None)
+    bounds = torch.randn(b.n_pages, layer[1], 2, layer[2], generator=torch.Generator().manual_seed(1)).sort(2).values.to(b.shape.torch_dtype)
+    if kind == "equal":
+        bounds = bounds[torch.arange(b.n_pages) % 3].contiguous()
+    run_select(b, k_sel, first, last, bounds.to(DEV))
+
+
+@pytest.mark.parametrize("layer", [(16, 1, 128, "bf16"), (16, 1, 64, "fp32"), (48, 3, 64, "bf16"), (5, 1, 128, "fp32")])
+def test_other_groups(layer):
+    b = Batch(shape_of(*layer), LONG["drafts"], 18, extra_rows=(1, 1))
+    run_select(b, 5, 1, 1)
+    run_selected(b, some_pages(b, 6, 4), 6, "all", 5)
+
+
+def test_bounds_of_more_pages_than_a_launch_has_workgroups_for():
+    sh = shape_of(1, 1, 64, "bf16")
+    max_pages = 33000
+    k = torch.randn(max_pages, 1, BS, 64, dtype=torch.bfloat16, device=DEV)
+    bounds = torch.zeros(max_pages, 1, 2, 64, dtype=torch.bfloat16, device=DEV)
+    pages = torch.randperm(max_pages, device=DEV).int()[None].contiguous()
+    n = torch.tensor([max_pages * BS - 5], dtype=torch.int32, device=DEV)
+    H.PagedRunner(sh, 1, 1, 1, max_pages).key_bounds(n, pages, k, bounds)
+    torch.cuda.synchronize()
+    k[pages[0, -1].long(), :, -5:] = k[pages[0, -1].long(), :, :1]
+    assert torch.equal(bounds[:, :, 0], k.amin(2)) and torch.equal(bounds[:, :, 1], k.amax(2))
+
+
 def run_selected(b, chosen, k_sel, kind="plain", seed=0, runner=None, garbage=True, **kw):
     """Attention over given lists; what is behind n_sel in a list is anything."""
     f = form_of(b, kind, seed)
