@@ -91,7 +91,7 @@ def test_rotated_in_place_and_keys_alone(shape, batch):
     run(b, 64, interleaved=True, keys_alone=True)
 
 
-@pytest.mark.parametrize("layer", [(16, 1, 128, "bf16"), (16, 1, 64, "fp32"), (48, 3, 64, "bf16"), (5, 1, 128, "fp32")])
+@pytest.mark.parametrize("layer", [(8, 1, 128, "bf16"), (7, 1, 64, "fp32"), (48, 6, 64, "bf16"), (5, 1, 128, "fp32")])
 def test_rotated_of_other_groups(layer):
     run(Batch(shape_of(*layer), BATCHES["chunks"], 6, extra_rows=(1, 1)), 32, interleaved=True)
     run(Batch(shape_of(*layer), BATCHES["steps"], 6), 64)

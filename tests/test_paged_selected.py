@@ -147,7 +147,7 @@ def test_select_from_more_pages_than_threads_hold_keys(layer, k_sel, first, last
     run_select(b, k_sel, first, last, bounds.to(DEV))
 
 
-@pytest.mark.parametrize("layer", [(16, 1, 128, "bf16"), (16, 1, 64, "fp32"), (48, 3, 64, "bf16"), (5, 1, 128, "fp32")])
+@pytest.mark.parametrize("layer", [(8, 1, 128, "bf16"), (7, 1, 64, "fp32"), (48, 6, 64, "bf16"), (5, 1, 128, "fp32")])
 def test_other_groups(layer):
     b = Batch(shape_of(*layer), LONG["drafts"], 18, extra_rows=(1, 1))
     run_select(b, 5, 1, 1)
