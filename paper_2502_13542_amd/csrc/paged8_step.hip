@@ -23,7 +23,7 @@ static void launch_step8(const PagedStep& st, hipStream_t stream) {
 int launch_paged8_step(const actqkv_shape& sh, const PagedAttn& p, const Workspace& ws, hipStream_t stream) {
   PagedStep st = {};
   st.a = p;
-  st.n_wg = step_workgroups(int64_t(p.t.batch) * sh.n_kv_heads, p.t.max_pages, step_least(kBlock, sh.head_dim, 1));
+  st.n_wg = step_workgroups(int64_t(p.t.batch) * sh.n_kv_heads, p.t.max_pages, step_least(kBlock, sh.head_dim, 1), 4);
   st.part = reinterpret_cast<uint32_t*>(ws.scratch_f32());
   st.counters = ws.counters();
   if (sh.dtype == ACTQKV_F32) {

@@ -281,12 +281,13 @@ __device__ __forceinline__ void step_body(const PagedStep& st) {
 
 // ---- host side
 // Workgroups per (sequence, KV head), or row and KV head, of `items` items at most: as many as fill the compute units once, and more only
-// where a wavefront still has eight items, which evens out sequences of different length; every one adds a part to merge.  us with
+// where a wavefront still has `each` items, which evens out sequences of different length; every one adds a part to merge.  us with
 // 256 | 1024 workgroups, 32 query and 8 KV heads: 1 sequence at 32K tokens 28 | 41, 4 at 8K 24 | 30, 8 at up to 16K 83 | 88, 16
-// at up to 32K 300 | 264 (those take the 1024).
-inline int step_workgroups(int64_t pairs, int64_t items, int64_t least) {
+// at up to 32K 300 | 264 (those take the 1024).  Of 8-bit pages, as many bytes of twice as many keys, eight items are 154 us there, four 148,
+// two 167.
+inline int step_workgroups(int64_t pairs, int64_t items, int64_t least, int each = 8) {
   if (pairs > int64_t(kTicketCounters)) return 1;
-  const int64_t fill = (kChipCus + pairs - 1) / pairs, even = std::min(items / (8 * kStWaves), (kStepWgs + pairs - 1) / pairs);
+  const int64_t fill = (kChipCus + pairs - 1) / pairs, even = std::min(items / (each * kStWaves), (kStepWgs + pairs - 1) / pairs);
   return int(std::max<int64_t>(1, std::min({std::max(fill, even), (items + least - 1) / least, int64_t(64)})));
 }
 // Partial results of at most kStepWgs + pairs workgroups.
