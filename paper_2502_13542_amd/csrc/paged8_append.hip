@@ -93,13 +93,21 @@ __device__ __forceinline__ void append8_keys(const PagedAppend8& a, const NewTok
     const int tok = i * kRows + j;
     if (tok < w.n) {
       uint8_t* to = a.k_pages + tile + size_t(w.j0 + tok) * D;
+      typedef std::conditional_t<V == 8, u32x2, uint32_t> codes_t;      // of a chunk
+      typedef std::conditional_t<V == 8, u32x4, u32x2> pair_t;
+      uint32_t c[2][V / 4];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         float (&y)[V] = k[kTurn ? i : 0][h];
         if (!kTurn) Vec<T>::widen(x[i][h], y);
 #pragma unroll
-        for (int e = 0; e < V; e += 4)
-          *reinterpret_cast<uint32_t*>(to + (h ? at.b : at.a) + e) = e4m3_pack(y[e] * by, y[e + 1] * by, y[e + 2] * by, y[e + 3] * by);
+        for (int e = 0; e < V; e += 4) c[h][e / 4] = e4m3_pack(y[e] * by, y[e + 1] * by, y[e + 2] * by, y[e + 3] * by);
+      }
+      if (at.b == at.a + V) {
+        *reinterpret_cast<pair_t*>(to + at.a) = __builtin_bit_cast(pair_t, c);
+      } else {
+        *reinterpret_cast<codes_t*>(to + at.a) = __builtin_bit_cast(codes_t, c[0]);
+        *reinterpret_cast<codes_t*>(to + at.b) = __builtin_bit_cast(codes_t, c[1]);
       }
     }
   }
