@@ -56,6 +56,17 @@ __device__ __forceinline__ int wave_scan(int v) {
   return v;
 }
 
+// Of 64 lanes' counts the inclusive sums, by the data-parallel primitives.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ int dpp_add(int v) { return v + __builtin_amdgcn_update_dpp(0, v, kCtrl, kRows, 0xF, false); }
+__device__ __forceinline__ int lane_sums(int v) {
+  v = dpp_add<0x111, 0xF>(v);                    // row_shr 1, 2, 4, 8
+  v = dpp_add<0x112, 0xF>(v);
+  v = dpp_add<0x114, 0xF>(v);
+  v = dpp_add<0x118, 0xF>(v);
+  v = dpp_add<0x142, 0xA>(v);                    // row_bcast 15 into rows 1, 3, then 31 into rows 2, 3
+  return dpp_add<0x143, 0xC>(v);
+}
 // The least and the largest over each half of the lanes, by the data-parallel primitives (through LDS, as a shuffle, a step is 60 ns).
 __device__ __forceinline__ int half_min(int v) {
   v = min(v, int(lane_xor32<1>(uint32_t(v))));

@@ -19,7 +19,7 @@ struct PagedAppend8 {
   uint8_t *k_pages, *v_pages;
   float *k_scales, *v_scales;              // [n_pages][Hk]
   int n_kv_heads, group;
-  int slices, pages;
+  TurnItems items;                         // (of a page: its keys, its values)
 };
 // The new tokens of a page: slots [j0, j0 + n), the first of them row `row`.
 struct NewTokens {
@@ -187,21 +187,20 @@ template <typename T, int D, int kThreads, bool kFew, bool kTurn>
 __global__ __launch_bounds__(kThreads) void paged8_append_kernel(PagedAppend8 a) {
   __shared__ uint32_t vt[D * kV8Pad];            // [channel][four slots]
   __shared__ float red[32];
-  const int hk = blockIdx.x >> 1, role = blockIdx.x & 1, s = blockIdx.z;
-  const PagedSeq seq = paged_seq(a.t, s);
-  if (seq.m == 0) return;
-  const int pos0 = seq.n - seq.m, first = max(pos0, 0) / kBlock;
-  for (int y = blockIdx.y; y < a.pages + (a.slices + 1) / 2; y += gridDim.y) {
-    if (y >= a.pages) {
-      const int slice = (y - a.pages) * 2 + role;
-      turn_rows<T, D, kThreads, false>(a.t, a.r, seq, s, hk, a.n_kv_heads, a.group, slice, nullptr, nullptr, static_cast<const T*>(a.q),
-                             static_cast<T*>(a.q_out));
+  for (int i = blockIdx.x; i < a.items.total; i += gridDim.x) {
+    const int hk = i % a.n_kv_heads;
+    TurnItem it;
+    if (!turn_item(a.t, a.items, i / a.n_kv_heads, it)) return;
+    const PagedSeq seq = paged_seq(a.t, it.s);
+    if (it.slice >= 0) {
+      turn_rows<T, D, kThreads, false>(a.t, a.r, seq, it.s, hk, a.n_kv_heads, a.group, it.slice, nullptr, nullptr, static_cast<const T*>(a.q),
+                                       static_cast<T*>(a.q_out));
       continue;
     }
-    const int index = first + y, lo = max(max(pos0, 0), index * kBlock), hi = min(seq.n, index * kBlock + kBlock);
-    if (hi <= lo) continue;                      // (index < max_pages: hi > index * kBlock)
-    const NewTokens w{paged_page(a.t, s, index), lo - index * kBlock, hi - lo, seq.row0 + lo - pos0, lo};
-    if (role == 0) append8_keys<T, D, kThreads, kFew, kTurn>(a, w, hk, red);
+    const int pos0 = seq.n - seq.m, index = max(pos0, 0) / kBlock + it.page;
+    const int lo = max(max(pos0, 0), index * kBlock), hi = min(seq.n, index * kBlock + kBlock);
+    const NewTokens w{paged_page(a.t, it.s, index), lo - index * kBlock, hi - lo, seq.row0 + lo - pos0, lo};
+    if (it.part == 0) append8_keys<T, D, kThreads, kFew, kTurn>(a, w, hk, red);
     else append8_values<T, D, kThreads, kFew>(a, w, hk, red, vt);
     __syncthreads();
   }
@@ -223,12 +222,13 @@ int launch_paged_append_quantised(const actqkv_shape& sh, const PagedTable& t, c
   a.v_scales = v_scales;
   a.n_kv_heads = sh.n_kv_heads;
   a.group = sh.n_q_heads / sh.n_kv_heads;
-  a.pages = std::min(t.max_pages, (t.max_new + kBlock - 2) / kBlock + 1);
-  with_turn_types<kTurnThreads>(sh, t.max_new, [&](auto* type, auto dim, auto threads, auto few) {
+  with_turn_types<kTurnThreads>(sh, t, [&](auto* type, auto dim, auto threads, auto few, int least, int most) {
     typedef std::remove_pointer_t<decltype(type)> T;
     constexpr int D = decltype(dim)::value, kThreads = decltype(threads)::value;
-    a.slices = q != nullptr ? (t.max_new + kTurnRows<T, D, kThreads> - 1) / kTurnRows<T, D, kThreads> : 0;
-    const dim3 grid(2 * sh.n_kv_heads, std::min(a.pages + (a.slices + 1) / 2, kTurnMostY), t.batch);
+    const int rows = q != nullptr ? kTurnRows<T, D, kThreads> : 0;
+    a.items = turn_items(sh, t, rows, 2, least, most);
+    if (a.items.total == 0) return;
+    const dim3 grid(std::min(a.items.total, kTurnMostWgs));
     constexpr bool kFew = decltype(few)::value;
     if (r.table != nullptr) hipLaunchKernelGGL((paged8_append_kernel<T, D, kThreads, kFew, true>), grid, dim3(kThreads), 0, stream, a);
     else hipLaunchKernelGGL((paged8_append_kernel<T, D, kThreads, kFew, false>), grid, dim3(kThreads), 0, stream, a);

@@ -17,7 +17,7 @@ struct PagedAppendRotated {
   const void *k_new, *v_new, *q;           // q may be NULL
   void *k_pages, *v_pages, *q_out;
   int n_kv_heads, group;
-  int slices, pages;                       // of the rows and of the pages of a sequence, at most
+  TurnItems items;
 };
 
 // kFew: at most kTurnRows new tokens, all in one round.
@@ -80,17 +80,16 @@ template <typename T, int D, int kThreads, bool kFew>
 __global__ __launch_bounds__(kThreads) void paged_append_rotated_kernel(PagedAppendRotated a) {
   constexpr int kOwn = D / kArSlices;
   __shared__ __attribute__((aligned(16))) T vt[kOwn * (kBlock + 2)];   // [channel][place in the page]
-  const int hk = blockIdx.x, s = blockIdx.z;
-  const PagedSeq seq = paged_seq(a.t, s);
-  if (seq.m == 0) return;
-  const int first = max(seq.n - seq.m, 0) / kBlock;
-  for (int y = blockIdx.y; y < a.slices + a.pages * kArSlices; y += gridDim.y) {
-    if (y < a.slices) {
-      turn_rows<T, D, kThreads, true>(a.t, a.r, seq, s, hk, a.n_kv_heads, a.group, y, static_cast<const T*>(a.k_new), static_cast<T*>(a.k_pages),
-                            static_cast<const T*>(a.q), static_cast<T*>(a.q_out));
+  for (int i = blockIdx.x; i < a.items.total; i += gridDim.x) {
+    const int hk = i % a.n_kv_heads;
+    TurnItem it;
+    if (!turn_item(a.t, a.items, i / a.n_kv_heads, it)) return;
+    const PagedSeq seq = paged_seq(a.t, it.s);
+    if (it.slice >= 0) {
+      turn_rows<T, D, kThreads, true>(a.t, a.r, seq, it.s, hk, a.n_kv_heads, a.group, it.slice, static_cast<const T*>(a.k_new),
+                                      static_cast<T*>(a.k_pages), static_cast<const T*>(a.q), static_cast<T*>(a.q_out));
     } else {
-      const int i = y - a.slices;
-      append_values<T, D, kThreads, kFew>(a, seq, s, hk, first + i / kArSlices, i % kArSlices * kOwn, vt);
+      append_values<T, D, kThreads, kFew>(a, seq, it.s, hk, max(seq.n - seq.m, 0) / kBlock + it.page, it.part * kOwn, vt);
       __syncthreads();
     }
   }
@@ -109,14 +108,13 @@ int launch_paged_append_rotated(const actqkv_shape& sh, const PagedTable& t, con
   a.q_out = q_out;
   a.n_kv_heads = sh.n_kv_heads;
   a.group = sh.n_q_heads / sh.n_kv_heads;
-  // a sequence's rows lie in one page more than they would from a page's first slot on
-  a.pages = std::min(t.max_pages, (t.max_new + kBlock - 2) / kBlock + 1);
-  with_turn_types<kTurnThreads>(sh, t.max_new, [&](auto* type, auto dim, auto threads, auto few) {
+  with_turn_types<kTurnThreads>(sh, t, [&](auto* type, auto dim, auto threads, auto few, int least, int most) {
     typedef std::remove_pointer_t<decltype(type)> T;
-    constexpr int D = decltype(dim)::value, kThreads = decltype(threads)::value;
-    a.slices = (t.max_new + kTurnRows<T, D, kThreads> - 1) / kTurnRows<T, D, kThreads>;
-    const dim3 grid(sh.n_kv_heads, std::min(a.slices + a.pages * kArSlices, kTurnMostY), t.batch);
-    hipLaunchKernelGGL((paged_append_rotated_kernel<T, D, kThreads, decltype(few)::value>), grid, dim3(kThreads), 0, stream, a);
+    constexpr int D = decltype(dim)::value, kThreads = decltype(threads)::value, kRows = kTurnRows<T, D, kThreads>;
+    a.items = turn_items(sh, t, kRows, kArSlices, least, most);
+    if (a.items.total == 0) return;
+    hipLaunchKernelGGL((paged_append_rotated_kernel<T, D, kThreads, decltype(few)::value>), dim3(std::min(a.items.total, kTurnMostWgs)),
+                       dim3(kThreads), 0, stream, a);
   });
   return hip_status("paged append (rotated)");
 }

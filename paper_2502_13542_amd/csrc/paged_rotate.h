@@ -13,7 +13,70 @@ namespace actqkv {
 // Threads of a workgroup: of calls whose sequences bring few rows one wavefront, which has no barriers to wait at and leaves room for the
 // other workgroups (a step of 64 sequences, 32 query and 8 KV heads of 128, turned: 6.3 us in workgroups of 256 threads, 5.0 so; into 8 bits 10.6, 6.0).
 constexpr int kTurnThreads = 256, kTurnFew = 64;
-constexpr int kTurnMostY = 32768;          // workgroups along y: more work goes round
+constexpr int kTurnMostWgs = 1 << 22;      // workgroups of a launch: more work goes round
+constexpr int kTurnApart = 256;            // (sequence, KV head) pairs of few rows that are worth a launch
+
+// The work of a call is dealt out in items of a KV head: a sequence has slices of its rows and pages with new tokens, as many as it needs
+// (a workgroup for every one that the longest could have would be 784 thousand for a chunk of 2048 tokens beside 1000 steps of 8 KV heads).
+struct TurnItems {
+  int rows, per_page;                      // of a slice (0: no slices); items of a page
+  int least, most;                         // new tokens of the sequences that this launch is for
+  int total;                               // of all sequences, at most, times the KV heads
+};
+__host__ __device__ inline int turn_pages(int pos0, int n) { return n > pos0 ? (n - 1) / kBlock - pos0 / kBlock + 1 : 0; }
+inline TurnItems turn_items(const actqkv_shape& sh, const PagedTable& t, int rows, int per_page, int least, int most) {
+  const int64_t seqs = std::min(t.batch, t.n_rows / least), n_rows = std::min<int64_t>(t.n_rows, seqs * most);
+  int64_t items = per_page * std::min<int64_t>(seqs * std::min(t.max_pages, (most + kBlock - 2) / kBlock + 1), n_rows / kBlock + 2 * seqs);
+  if (rows > 0) items += std::min<int64_t>(seqs * ((most + rows - 1) / rows), n_rows / rows + seqs);
+  return TurnItems{rows, per_page, least, most, int(items * sh.n_kv_heads)};
+}
+// Item `item` of a KV head: a sequence, and a slice of its rows, or (from `slices` on) a part of a page; false behind the last one.
+struct TurnItem {
+  int s, slice, page, part;                // slice or page -1
+};
+// (kSeqs: sequences of a lane.  A search of 1000 sequences is 4 rounds of loads, of 64 one.)
+template <int kSeqs>
+__device__ __forceinline__ bool turn_item_of(const PagedTable& t, const TurnItems& of, int item, TurnItem& it) {
+  const int lane = threadIdx.x & 63;
+  for (int s0 = 0; s0 < t.batch; s0 += 64 * kSeqs) {
+    int slices[kSeqs], n[kSeqs], all = 0;
+#pragma unroll
+    for (int k = 0; k < kSeqs; ++k) {
+      const int s = s0 + lane * kSeqs + k;
+      const PagedSeq q = paged_seq(t, min(s, t.batch - 1));
+      const bool some = s < t.batch && q.m >= of.least && q.m <= of.most;
+      slices[k] = some && of.rows > 0 ? (q.m + of.rows - 1) / of.rows : 0;
+      n[k] = some ? slices[k] + of.per_page * turn_pages(max(q.n - q.m, 0), q.n) : 0;
+      all += n[k];
+    }
+    const int sum = lane_sums(all);
+    const unsigned long long mine = __ballot(item < sum);
+    if (mine != 0) {
+      const int at = __ffsll(mine) - 1;
+      item -= __builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(all, at);
+      int k_at = 0, first = __builtin_amdgcn_readlane(slices[0], at);
+#pragma unroll
+      for (int k = 1; k < kSeqs; ++k) {
+        const int before = __builtin_amdgcn_readlane(n[k - 1], at);
+        if (k_at == k - 1 && item >= before) {
+          item -= before;
+          k_at = k;
+          first = __builtin_amdgcn_readlane(slices[k], at);
+        }
+      }
+      it.s = s0 + at * kSeqs + k_at;
+      it.slice = item < first ? item : -1;
+      it.page = item < first ? -1 : (item - first) / of.per_page;
+      it.part = (item - first) - it.page * of.per_page;
+      return true;
+    }
+    item -= __builtin_amdgcn_readlane(sum, 63);
+  }
+  return false;
+}
+__device__ __forceinline__ bool turn_item(const PagedTable& t, const TurnItems& of, int item, TurnItem& it) {
+  return t.batch <= 64 ? turn_item_of<1>(t, of, item, it) : turn_item_of<4>(t, of, item, it);
+}
 
 // Chunks a thread's pair is made of: their first channels, and whether they turn (behind `dims` they are just two neighbours).
 struct TurnPair {
@@ -119,18 +182,28 @@ __device__ __forceinline__ void turn_rows(const PagedTable& t, const PagedRotati
   }
   if (kKeys && page >= 0) move(ka, kb, k_pages + ((size_t(page) * n_kv_heads + hk) * kBlock + pos % kBlock) * D);
 }
-// Calls launch(T*, D, threads, few) with the types of a call: few, where every sequence's rows are at most a slice; kMost threads otherwise.
+// Calls launch(T*, D, threads, few, least, most) with the types of a call and the rows of the sequences that a launch is for: few, where those
+// are at most a slice; kMost threads otherwise.  Sequences of few rows beside longer ones take a launch of their own if they may be so many
+// that in large workgroups, of which a compute unit holds two, they would take longer: 999 single tokens beside a chunk of 2048, 32 query and 8 KV heads of
+// 128, in one launch 241 us and 408 into 8 bits, in two 197 and 229.
 template <int kMost, typename Launch>
-inline void with_turn_types(const actqkv_shape& sh, int max_new, Launch launch) {
+inline void with_turn_types(const actqkv_shape& sh, const PagedTable& t, Launch launch) {
   auto by_rows = [&](auto* type, auto dim) {
     typedef std::remove_pointer_t<decltype(type)> T;
-    constexpr int D = decltype(dim)::value;
-    if (max_new <= kTurnRows<T, D, kTurnFew>)
-      launch(type, dim, std::integral_constant<int, kTurnFew>(), std::true_type());
-    else if (max_new <= kTurnRows<T, D, kTurnThreads>)
-      launch(type, dim, std::integral_constant<int, kTurnThreads>(), std::true_type());
-    else
-      launch(type, dim, std::integral_constant<int, kMost>(), std::false_type());
+    constexpr int D = decltype(dim)::value, kFewest = kTurnRows<T, D, kTurnFew>, kFew = kTurnRows<T, D, kTurnThreads>;
+    const std::integral_constant<int, kTurnFew> few;
+    const std::integral_constant<int, kTurnThreads> all;
+    const std::integral_constant<int, kMost> most;
+    if (t.max_new <= kFewest) {
+      launch(type, dim, few, std::true_type(), 1, kFewest);
+      return;
+    }
+    const int64_t more = std::max<int64_t>(0, int64_t(t.n_rows) - int64_t(t.batch) * kFewest);
+    const bool apart = (t.batch - (more + t.max_new - 1) / t.max_new) * sh.n_kv_heads > kTurnApart;
+    if (apart) launch(type, dim, few, std::true_type(), 1, kFewest);
+    const int least = apart ? kFewest + 1 : 1;
+    if (t.max_new <= kFew) launch(type, dim, all, std::true_type(), least, t.max_new);
+    else launch(type, dim, most, std::false_type(), least, t.max_new);
   };
   const std::integral_constant<int, 64> d64;
   const std::integral_constant<int, 128> d128;

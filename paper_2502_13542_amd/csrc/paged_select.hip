@@ -94,17 +94,6 @@ __device__ __forceinline__ uint32_t page_key(const PagedSelect& a, float score, 
   const uint32_t bits = __float_as_uint(score), order = bits >> 31 ? ~bits : bits | 0x80000000u;
   return min(max(order, 1u), 0xfffffffeu);
 }
-// Of 64 lanes' counts the inclusive sums, by the data-parallel primitives.
-template <int kCtrl, int kRows>
-__device__ __forceinline__ int dpp_add(int v) { return v + __builtin_amdgcn_update_dpp(0, v, kCtrl, kRows, 0xF, false); }
-__device__ __forceinline__ int lane_sums(int v) {
-  v = dpp_add<0x111, 0xF>(v);                    // row_shr 1, 2, 4, 8
-  v = dpp_add<0x112, 0xF>(v);
-  v = dpp_add<0x114, 0xF>(v);
-  v = dpp_add<0x118, 0xF>(v);
-  v = dpp_add<0x142, 0xA>(v);                    // row_bcast 15 into rows 1, 3, then 31 into rows 2, 3
-  return dpp_add<0x143, 0xC>(v);
-}
 // The selection of one (row, KV head) from the keys of the pages 0 .. last: key_of(i, b) is that of page b = i kSelThreads + threadIdx.x, 0
 // behind the last.
 template <typename Key>

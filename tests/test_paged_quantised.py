@@ -12,7 +12,7 @@ from paper_2502_13542_amd import harness as H
 
 from paged_utils import BS, Batch, f64, shape_of
 from test_paged import BATCHES, CUTS, FORMS, SHAPES, check_out, clamped_batch, form_of, on_device
-from test_paged_rotated import bound_of, table_of
+from test_paged_rotated import MIXED, bound_of, table_of
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -196,6 +196,12 @@ def test_append(shape, batch, kind):
         if m and (n - m) % BS:
             assert torch.isfinite(b.ks[b.pages[s, (n - m) // BS]]).all()
     run_append(loud(b, 3) if kind == "loud" else b)
+
+
+@pytest.mark.parametrize("shape", ["llama", "mha64", "fp32_g3"])
+@pytest.mark.parametrize("seqs", MIXED)
+def test_append_of_steps_beside_chunks(shape, seqs):
+    run_append(loud(quantise(Batch(shape_of(*SHAPES[shape]), seqs, 8, extra_rows=(1, 2), extra_entries=0), 9), 3), 64)
 
 
 @pytest.mark.parametrize("shape", list(SHAPES))

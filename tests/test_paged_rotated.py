@@ -97,6 +97,17 @@ def test_rotated_of_other_groups(layer):
     run(Batch(shape_of(*layer), BATCHES["steps"], 6), 64)
 
 
+MIXED = [[(1, 30)] * 40 + [(100, 300), (8, 200), (9, 140)] + [(2, 129)] * 17 + [(0, 3), (40, 40)],      # more than a launch takes along, and an odd one among them
+         [(int(m), int(m + n)) for m, n in zip(np.random.default_rng(3).integers(0, 12, 150), np.random.default_rng(4).integers(0, 140, 150))]]
+
+
+@pytest.mark.parametrize("shape", ["llama", "mha64", "fp32_g3"])
+@pytest.mark.parametrize("seqs", MIXED)
+def test_rotated_steps_beside_chunks(shape, seqs):
+    run(Batch(shape_of(*SHAPES[shape]), seqs, 8, extra_rows=(1, 2), extra_entries=0), 64)
+    run(Batch(shape_of(*SHAPES[shape]), [(1, 60)] * 400 + [(33, 100)], 8, extra_entries=0), 64)
+
+
 def test_rotated_without_pages_and_at_clamped_lengths():
     b = Batch(shape_of(*SHAPES["llama"]), BATCHES["chunks"], 9, garbage=None)
     b.pages[0, 1] = b.n_pages                     # no page: keys go nowhere, queries are turned
