@@ -1,11 +1,13 @@
-"""Builds libactqkv.so (HIP, gfx950) with one hipcc call and the Python extension module that calls
-it with one g++ call, both next to this file."""
+"""Builds libactqkv.so (HIP, gfx950) with hipcc, a call for each source, and the Python extension module that
+calls it with one g++ call, both next to this file."""
 from __future__ import annotations
 
 import os
 import shutil
 import subprocess
 import sysconfig
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -21,7 +23,7 @@ SOURCES = ["api.hip", "probe.hip", "score.hip", "select.hip", "attn_prefill_f32.
            "paged_chosen_chunk_f32.hip", "paged_select.hip", "paged_weights.hip",
            "paged_evict.hip"]
 
-FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          # packed fp32 instructions are kept out of the generated code
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function"]
@@ -38,19 +40,24 @@ def _native_command() -> list:
 
 
 def build(verbose: bool = False) -> str:
+    """Compiles every source, a few at a time, and links them."""
     hipcc = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
-    commands = [[hipcc] + FLAGS + [os.path.join(CSRC, s) for s in SOURCES] + ["-o", LIB], _native_command()]
-    if verbose:
-        print("\n".join(" ".join(c) for c in commands))
-    running = [subprocess.Popen(c, stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True) for c in commands]
     noise = "is not a recognized feature for this target"
-    failed = []
-    for c, r in zip(commands, running):
-        err = "\n".join(l for l in r.communicate()[1].splitlines() if noise not in l)
-        if r.returncode != 0:
-            failed.append(os.path.basename(c[0]) + " failed:\n" + err)
-        elif verbose and err.strip():
-            print(err)
+    with tempfile.TemporaryDirectory() as objects, ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+        made = [os.path.join(objects, s + ".o") for s in SOURCES]
+        commands = [_native_command()] + [[hipcc] + FLAGS + ["-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, made)]
+        link = [hipcc] + FLAGS + ["-shared"] + made + ["-o", LIB]
+
+        def run(c):
+            if verbose:
+                print(" ".join(c))
+            r = subprocess.run(c, stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True)
+            err = "\n".join(l for l in r.stderr.splitlines() if noise not in l)
+            if verbose and err.strip():
+                print(err)
+            return "" if r.returncode == 0 else os.path.basename(c[0]) + " failed:\n" + err
+
+        failed = [f for f in pool.map(run, commands) if f] or [f for f in [run(link)] if f]
     if failed:
         raise RuntimeError("\n".join(failed))
     return LIB
