@@ -1,5 +1,7 @@
 // Attention of chunks and prompts over a paged cache in 8 bits, fp32 queries (paged_chunk_f32_body.h has the kernel, paged_chunk_f32.hip its
-// design).
+// design).  Bound by a wavefront's chain of products, softmax and cutting of the probabilities into parts: a tile is 1.6 us where the matrix instructions
+// are 0.64.  2 x 2048 rows at 8192 tokens, 8 query and 2 KV heads of 64, 187 to 197 us (over fp32 353 to 366), of 128 458 (774); a prefix of three prompts of
+// up to 1500 tokens 24.5 and 6 of merging.  (Two tiles in LDS, a barrier a tile: the same with 64 channels, 3 % slower with 128.)
 #include "paged_chunk_f32_body.h"
 
 namespace actqkv {

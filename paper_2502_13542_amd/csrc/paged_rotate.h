@@ -11,7 +11,7 @@
 namespace actqkv {
 
 // Threads of a workgroup: of calls whose sequences bring few rows one wavefront, which has no barriers to wait at and leaves room for the
-// other workgroups (a step of 64 sequences, 32 query and 8 KV heads of 128, turned: 6.3 us in workgroups of 256 threads, 5.0 so; into 8 bits 10.6, 6.0).
+// other workgroups (a step of 64 sequences, 32 query and 8 KV heads of 128, turned: 6.3 us in workgroups of 256 threads, 5.0 so; into 8 bits 10.6, 5.9).
 constexpr int kTurnThreads = 256, kTurnFew = 64;
 constexpr int kTurnMostWgs = 1 << 22;      // workgroups of a launch: more work goes round
 constexpr int kTurnApart = 256;            // (sequence, KV head) pairs of few rows that are worth a launch
@@ -195,7 +195,7 @@ inline void with_turn_types(const actqkv_shape& sh, const PagedTable& t, Launch 
     const std::integral_constant<int, kTurnThreads> all;
     const std::integral_constant<int, kMost> most;
     if (t.max_new <= kFewest) {
-      launch(type, dim, few, std::true_type(), 1, kFewest);
+      launch(type, dim, few, std::true_type(), 1, t.max_new);
       return;
     }
     const int64_t more = std::max<int64_t>(0, int64_t(t.n_rows) - int64_t(t.batch) * kFewest);
