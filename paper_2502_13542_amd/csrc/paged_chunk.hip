@@ -34,7 +34,7 @@ size_t paged_chunk_scratch_most(const actqkv_shape& sh, int batch, int n_rows, i
   for (int ks = 1; ks <= 4; ks *= 2)
     most = std::max(most, size_t(std::min(kPcMaxSplits, max_pages)) * sh.n_kv_heads * chunk_tiles(sh, batch, n_rows, max_new, ks) *
                               chunk_piece_bytes(sh, ks));
-  return std::min(most, kPcMostPieces * chunk_piece_bytes(sh, 1));
+  return std::min(most, kPcMostPiecesByte * chunk_piece_bytes(sh, 1));
 }
 
 template <int D, int KS>

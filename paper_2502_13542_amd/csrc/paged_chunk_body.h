@@ -12,6 +12,7 @@ namespace actqkv {
 
 constexpr int kPcThreads = 512, kPcWaves = kPcThreads / 64;
 constexpr int kPcMaxSplits = 32;
+constexpr size_t kPcMostPiecesByte = 1024; // the same of pages in 8 bits: 138 MB
 constexpr size_t kPcMostPieces = 512;      // pieces of 256 rows, or as many bytes of smaller ones, that a call leaves to be merged: 69 MB
 template <int KS> constexpr int kPcRows = 32 * kPcWaves / KS;
 template <int D> constexpr int kPcTileBytes = kBlock * D * 2;            // the keys or the values of a page
@@ -515,6 +516,9 @@ __device__ __forceinline__ void chunk_body(const PagedChunk& c) {
 //   2 x 2048 rows at 16K tokens, 32 query and 8 KV heads of 128: KS 1 908, 2 1036, 4 1563; 1 x 2048 at 2048 59, 52, 75; 8 x 512 at 512
 //   49, 59, 86; 512 at 512 21.5, 16.6, 14.4; 12 sequences of up to 500 with a window, 28 and 4 heads 291, 259, 354; 4 of up to 777
 //   248, 271, 380; 64 channels, 8192 at 8192 137, 100, 137, with documents 79, 52, 61
+// In 8 bits the pages of fewer rows cost more (each is converted by the workgroup), pieces may be twice as many, and the factors are fitted to 14 calls
+// at all cuts, of which the chosen one is 2 % from the best on average: 12 sequences of up to 500 rows under a cap and a window KS 1 289, in two 259, KS 2
+// 289; without, 380, 341, 379; 22 of up to 215 at up to 18K KS 1 472, in three 204, in eight 180.
 struct ChunkCut {
   int ks, splits, tiles;
   double us;                 // by those figures
@@ -533,7 +537,9 @@ inline size_t chunk_piece_bytes(const actqkv_shape& sh, int ks) {
   return sh.head_dim == 64 ? chunk_piece_bytes<64>(ks) : chunk_piece_bytes<128>(ks);
 }
 inline ChunkCut chunk_cut(const actqkv_shape& sh, const PagedAttn& p) {
-  constexpr double kPageUs[2][3] = {{3.5, 2.0, 1.5}, {2.1, 1.45, 1.0}}, kItemUs = 5.;
+  constexpr double kPageUs[2][2][3] = {{{3.5, 2.0, 1.5}, {2.1, 1.45, 1.0}}, {{3.5, 2.3, 1.75}, {2.1, 1.45, 1.0}}};
+  const bool byte = p.k_scales != nullptr;
+  const double item_us = byte ? 4. : 5.;
   const PagedTable& t = p.t;
   // pages of the longest tile and of an average one: of a prompt half of its own on average; of documents a part, nobody knows which
   double longest = t.max_pages, own = double(t.max_new) / kBlock;
@@ -541,6 +547,10 @@ inline ChunkCut chunk_cut(const actqkv_shape& sh, const PagedAttn& p) {
   double average = longest - std::min(own, longest) / 2.;
   bool equal = p.f.window > 0 ? longest < t.max_pages : own * 4. < longest;
   bool alike = average > 0.8 * longest;          // (pieces of tiles are more so than the tiles)
+  if (byte && t.batch > 1) {
+    average *= 0.6;
+    alike = false;
+  }
   if (p.f.row_first != nullptr) {
     average = longest / 8.;
     longest /= 3.;
@@ -550,15 +560,16 @@ inline ChunkCut chunk_cut(const actqkv_shape& sh, const PagedAttn& p) {
   double least = 0.;
   for (int i = 0; i < 3; ++i) {
     const int ks = 1 << i, tiles = chunk_tiles(sh, t.batch, t.n_rows, t.max_new, ks);
-    const double rows = kPcRows<1> / ks, page = kPageUs[sh.head_dim == 64][i];
+    const double rows = kPcRows<1> / ks, page = kPageUs[byte][sh.head_dim == 64][i] * (byte && p.f.cap_in > 0.f ? 1.2 : 1.);
     // of several sequences' last tiles half are empty, on average
     const double likely = t.batch == 1 ? tiles : std::min<double>(tiles, double(t.n_rows) * (sh.n_q_heads / sh.n_kv_heads) / rows + t.batch / 2.);
     for (int splits = 1; splits <= std::min(kPcMaxSplits, t.max_pages); ++splits) {
-      if (splits > 1 && size_t(tiles) * sh.n_kv_heads * splits * chunk_piece_bytes(sh, ks) > kPcMostPieces * chunk_piece_bytes(sh, 1)) break;
+      if (splits > 1 && size_t(tiles) * sh.n_kv_heads * splits * chunk_piece_bytes(sh, ks) > (byte ? kPcMostPiecesByte : kPcMostPieces) * chunk_piece_bytes(sh, 1)) break;
       const double pieces = likely * sh.n_kv_heads * splits, rounds = pieces / kChipCus;
-      double us = std::ceil(longest / splits) * page + kItemUs;
-      us = equal || (splits > 1 && alike) ? std::ceil(rounds) * us : std::max(us, rounds * (average / splits * page + kItemUs));
-      if (splits > 1) us += 4. + pieces * rows * sh.head_dim * 8. / 4e6;
+      double us = std::ceil(longest / splits) * page + item_us;
+      us = equal || (splits > 1 && alike) ? std::ceil(rounds) * us
+                                          : std::max(us, rounds * (average / splits * page + item_us) + (byte ? 0.3 * us : 0.));
+      if (splits > 1) us += 4. + pieces * rows * sh.head_dim * 8. / (byte ? 3e6 : 4e6);
       if ((i == 0 && splits == 1) || us < least) {
         least = us;
         best = ChunkCut{ks, splits, tiles, us};
