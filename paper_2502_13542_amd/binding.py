@@ -144,6 +144,13 @@ def _calls():
     return _native
 
 
+def check_sizes(*sizes) -> None:
+    """check_sizes(tensor, elements, tensor, elements, ...): raises unless every tensor that is not None has as many."""
+    bad = (_native or _calls()).numels(*sizes)
+    if bad >= 0:
+        raise ActQKVError(-1, f"tensor of {sizes[2 * bad].numel()} elements, expected {sizes[2 * bad + 1]} (tensor {bad} of this call's sizes)")
+
+
 def _check(rc: int) -> None:
     if rc != 0:
         raise ActQKVError(rc, load_library().actqkv_last_error().decode())

@@ -276,8 +276,26 @@ PyObject* py_load(PyObject*, PyObject* args) {
   Py_RETURN_NONE;
 }
 
+// numels(tensor, elements, tensor, elements, ...): the number of the first tensor that has another number of elements, or -1.  None has any.
+PyObject* py_numels(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  for (Py_ssize_t i = 0; i + 1 < n; i += 2) {
+    if (args[i] == Py_None) continue;
+    if (!THPVariable_Check(args[i])) {
+      PyErr_SetString(PyExc_TypeError, "expected a tensor or None");
+      return nullptr;
+    }
+    const long long want = PyLong_AsLongLong(args[i + 1]);
+    if (want == -1 && PyErr_Occurred()) return nullptr;
+    if (THPVariable_Unpack(args[i]).numel() != want) return PyLong_FromSsize_t(i / 2);
+  }
+  return PyLong_FromLong(-1);
+  END_HANDLE_TH_ERRORS
+}
+
 #define ACTQKV_METHOD(name, kinds) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_##name)), METH_FASTCALL, nullptr},
 PyMethodDef g_methods[] = {ACTQKV_ENTRIES(ACTQKV_METHOD){"load", py_load, METH_VARARGS, nullptr},
+                           {"numels", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_numels)), METH_FASTCALL, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

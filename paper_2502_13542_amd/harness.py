@@ -919,11 +919,11 @@ class PagedRunner:
         ws = B.paged_workspace_bytes(self.cs, batch, n_rows, max_new, max_pages)
         self.workspace = torch.zeros(ws, dtype=torch.uint8, device=device)
         self._page = shape.n_kv_heads * shape.block_size * shape.head_dim
-        self._q_row = shape.n_q_heads * shape.head_dim
+        self._q_row, self._kv_row = shape.n_q_heads * shape.head_dim, shape.n_kv_heads * shape.head_dim
 
     def _table(self, n_ctx, pages, k_pages, v_pages) -> Tuple[int, int, int]:
         batch, max_pages = pages.shape
-        n_pages = k_pages.size(0)
+        n_pages = k_pages.shape[0]
         if batch > self.batch or max_pages > self.max_pages:
             raise B.ActQKVError(-1, f"{batch} sequences of {max_pages} pages: made for {self.batch} of {self.max_pages}")
         if n_ctx.numel() != batch:
@@ -933,7 +933,7 @@ class PagedRunner:
         return batch, max_pages, n_pages
 
     def _rows(self, batch: int, row_start, rows, heads: int, max_new, *same) -> Tuple[int, int]:
-        n_rows = rows.size(0)
+        n_rows = rows.shape[0]
         max_new = self.max_new if max_new is None else max_new
         if not 1 <= max_new <= self.max_new:
             raise B.ActQKVError(-1, f"max_new {max_new}: made for {self.max_new}")
@@ -941,9 +941,8 @@ class PagedRunner:
             raise B.ActQKVError(-1, f"row_start has {row_start.numel()} entries for {batch} sequences")
         if n_rows > self.n_rows:
             raise B.ActQKVError(-1, f"{n_rows} rows: made for {self.n_rows}")
-        size = n_rows * heads * self.shape.head_dim
         for t in (rows, *same):
-            if t.numel() != size:
+            if t.numel() != n_rows * heads * self.shape.head_dim:
                 raise B.ActQKVError(-1, f"tensor of {t.numel()} elements, expected {n_rows} rows of {heads} heads")
         return n_rows, min(max_new, n_rows)
 
@@ -1013,13 +1012,24 @@ class PagedRunner:
         B.paged_evict(self.cs, batch, n_ctx, pages, max_pages, k_pages, v_pages, n_pages, weights, weights.shape[-1],
                       keep_first, keep_last, budget, to_pages, to_pages.shape[-1], to_weights, to_stride, kept, n_kept, stream)
 
-    # ---- rotation on the way into the cache
-    def _turn(self, n_rows: int, rotation, q, q_out, row_pos) -> Tuple[int, int]:
-        """n_positions and rotary_dim of a call."""
-        if q is not None and q.numel() != n_rows * self._q_row or q_out is not None and q_out.numel() != n_rows * self._q_row:
-            raise B.ActQKVError(-1, f"q or q_out is not {n_rows} rows of {self.shape.n_q_heads} heads")
-        if row_pos is not None and row_pos.numel() != n_rows:
-            raise B.ActQKVError(-1, f"row_pos has {row_pos.numel()} entries for {n_rows} rows")
+    # ---- rotation on the way into the cache, pages in 8 bits, selected pages: a call's sizes are compared in one go (a step takes the
+    # device 4 to 6 us, and each question to a tensor the host 0.1 to 0.2)
+    def _limits(self, pages, n_rows: int, max_new) -> Tuple[int, int, int]:
+        """batch, max_pages and the most rows of a sequence of this call."""
+        batch, max_pages = pages.shape
+        if batch > self.batch or max_pages > self.max_pages:
+            raise B.ActQKVError(-1, f"{batch} sequences of {max_pages} pages: made for {self.batch} of {self.max_pages}")
+        if max_new is None:
+            max_new = self.max_new
+        elif not 1 <= max_new <= self.max_new:
+            raise B.ActQKVError(-1, f"max_new {max_new}: made for {self.max_new}")
+        if n_rows > self.n_rows:
+            raise B.ActQKVError(-1, f"{n_rows} rows: made for {self.n_rows}")
+        return batch, max_pages, max_new if max_new < n_rows else n_rows
+
+    @staticmethod
+    def _table_of_turns(rotation) -> Tuple[int, int]:
+        """n_positions and rotary_dim of a rotation."""
         if rotation is None:
             return 0, 0
         turn = rotation.shape
@@ -1032,86 +1042,66 @@ class PagedRunner:
         """append, the keys turned by their position, and the queries q [n_rows][H][D] into q_out (q itself: in place; q None:
         keys alone).  rotation [n_positions][2][rotary_dim / 2] fp32: cosines, sines; row_pos [n_rows]: places of the rows that
         are not their positions in the cache."""
-        batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, v_pages)
-        n_rows, max_new = self._rows(batch, row_start, k_new, self.shape.n_kv_heads, max_new, v_new)
-        n_positions, rotary = self._turn(n_rows, rotation, q, q_out, row_pos)
+        n_pages, n_rows = k_pages.size(0), k_new.size(0)
+        batch, max_pages, max_new = self._limits(pages, n_rows, max_new)
+        pool, new, queries = n_pages * self._page, n_rows * self._kv_row, n_rows * self._q_row
+        B.check_sizes(n_ctx, batch, row_start, batch + 1, k_pages, pool, v_pages, pool, k_new, new, v_new, new, q, queries, q_out, queries,
+                      row_pos, n_rows)
+        n_positions, rotary = self._table_of_turns(rotation)
         if n_rows == 0:
             return
         B.paged_append_rotated(self.cs, batch, n_rows, max_new, q, k_new, v_new, row_start, n_ctx, pages, max_pages, k_pages,
                                v_pages, n_pages, rotation, n_positions, rotary, interleaved, row_pos, q_out, stream)
 
-    # ---- pages in 8 bits
-    def _scales(self, n_pages: int, k_scales, v_scales) -> None:
-        self._per_row(n_pages * self.shape.n_kv_heads, k_scales, v_scales)
-
     def append_quantised(self, k_new, v_new, row_start, n_ctx, pages, k_pages, v_pages, k_scales, v_scales, rotation=None, q=None,
-                    q_out=None, row_pos=None, interleaved: bool = False, stream=None, max_new=None) -> None:
+                         q_out=None, row_pos=None, interleaved: bool = False, stream=None, max_new=None) -> None:
         """Keys and values of the new tokens into pages of e4m3 codes (float8_e4m3fn pools) with the scales [n_pages][Hk] fp32;
         rotation and what comes with it as in append_rotated, None: keys as they are."""
-        batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, v_pages)
-        self._scales(n_pages, k_scales, v_scales)
-        n_rows, max_new = self._rows(batch, row_start, k_new, self.shape.n_kv_heads, max_new, v_new)
-        n_positions, rotary = self._turn(n_rows, rotation, q, q_out, row_pos)
+        n_pages, n_rows = k_pages.size(0), k_new.size(0)
+        batch, max_pages, max_new = self._limits(pages, n_rows, max_new)
+        pool, new, queries, scales = n_pages * self._page, n_rows * self._kv_row, n_rows * self._q_row, n_pages * self.shape.n_kv_heads
+        B.check_sizes(n_ctx, batch, row_start, batch + 1, k_pages, pool, v_pages, pool, k_scales, scales, v_scales, scales, k_new, new,
+                      v_new, new, q, queries, q_out, queries, row_pos, n_rows)
+        n_positions, rotary = self._table_of_turns(rotation)
         if n_rows == 0:
             return
         B.paged_append_quantised(self.cs, batch, n_rows, max_new, q, k_new, v_new, row_start, n_ctx, pages, max_pages, k_pages, v_pages,
-                            n_pages, k_scales, v_scales, rotation, n_positions, rotary, interleaved, row_pos, q_out, stream)
+                                 n_pages, k_scales, v_scales, rotation, n_positions, rotary, interleaved, row_pos, q_out, stream)
 
     def attend_quantised(self, q, row_start, n_ctx, pages, k_pages, v_pages, k_scales, v_scales, out, lse=None, softcap: float = 0.0,
-                    window: int = 0, slopes=None, row_first=None, row_end=None, stream=None, max_new=None) -> None:
+                         window: int = 0, slopes=None, row_first=None, row_end=None, stream=None, max_new=None) -> None:
         """attend over pages in 8 bits."""
-        batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, v_pages)
-        self._scales(n_pages, k_scales, v_scales)
-        n_rows, max_new = self._attending(batch, row_start, q, out, lse, slopes, row_first, row_end, max_new)
+        n_pages, n_rows = k_pages.size(0), q.size(0)
+        batch, max_pages, max_new = self._limits(pages, n_rows, max_new)
+        pool, queries, heads, scales = n_pages * self._page, n_rows * self._q_row, self.shape.n_q_heads, n_pages * self.shape.n_kv_heads
+        B.check_sizes(n_ctx, batch, row_start, batch + 1, k_pages, pool, v_pages, pool, k_scales, scales, v_scales, scales, q, queries,
+                      out, queries, lse, n_rows * heads, slopes, heads, row_first, n_rows, row_end, n_rows)
         if n_rows == 0:
             return
         B.paged_attention_quantised(self.cs, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, k_pages, v_pages, n_pages,
-                               k_scales, v_scales, out, lse, self.workspace, softcap, window, slopes, row_first, row_end, stream)
+                                    k_scales, v_scales, out, lse, self.workspace, softcap, window, slopes, row_first, row_end, stream)
 
-    def _attending(self, batch, row_start, q, out, lse, slopes, row_first, row_end, max_new) -> Tuple[int, int]:
-        n_rows, max_new = self._rows(batch, row_start, q, self.shape.n_q_heads, max_new, out)
-        if row_first is not None or row_end is not None:
-            self._per_row(n_rows, row_first, row_end)
-        if lse is not None:
-            self._per_row(n_rows * self.shape.n_q_heads, lse)
-        if slopes is not None:
-            self._per_row(self.shape.n_q_heads, slopes)
-        return n_rows, max_new
-
-    # ---- attention over selected pages
     def key_bounds(self, n_ctx, pages, k_pages, bounds, row_start=None, n_rows: int = 0, stream=None, max_new=None) -> None:
         """bounds [n_pages][Hk][2][D], the least and the largest key of every channel: of the pages with new tokens (the n_rows rows
         that row_start deals out), or of all pages (row_start None)."""
-        batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, k_pages)
-        self._per_row(n_pages * self.shape.n_kv_heads * 2 * self.shape.head_dim, bounds)
-        if row_start is not None:
-            max_new = self.max_new if max_new is None else max_new
-            if not 1 <= max_new <= self.max_new:
-                raise B.ActQKVError(-1, f"max_new {max_new}: made for {self.max_new}")
-            if not 0 <= n_rows <= self.n_rows:
-                raise B.ActQKVError(-1, f"{n_rows} rows: made for {self.n_rows}")
-            self._per_row(batch + 1, row_start)
-            if n_rows == 0:
-                return
-            max_new = min(max_new, n_rows)
-        B.paged_key_bounds(self.cs, batch, n_rows, max_new or 0, row_start, n_ctx, pages, max_pages, k_pages, n_pages, bounds, stream)
+        n_pages = k_pages.size(0)
+        if n_rows < 0:
+            raise B.ActQKVError(-1, f"{n_rows} rows")
+        batch, max_pages, max_new = self._limits(pages, n_rows, max_new)
+        B.check_sizes(n_ctx, batch, row_start, batch + 1, k_pages, n_pages * self._page, bounds, n_pages * 2 * self._kv_row)
+        if row_start is not None and n_rows == 0:
+            return
+        B.paged_key_bounds(self.cs, batch, n_rows, max_new, row_start, n_ctx, pages, max_pages, k_pages, n_pages, bounds, stream)
 
     def select_pages(self, q, row_start, n_ctx, pages, bounds, keep_first: int, keep_last: int, scores, idx, n_sel, stream=None,
                      max_new=None) -> None:
         """The pages that each row looks at: idx [n_rows][Hk][k_sel], ascending, and n_sel [n_rows][Hk], by the scores
         [n_rows][Hk][at least max_pages] that the pages' bounds give them."""
-        batch, max_pages = pages.shape
-        n_pages = bounds.size(0)
-        rows = self.shape.n_kv_heads
-        if batch > self.batch or max_pages > self.max_pages:
-            raise B.ActQKVError(-1, f"{batch} sequences of {max_pages} pages: made for {self.batch} of {self.max_pages}")
-        self._per_row(batch, n_ctx)
-        self._per_row(n_pages * rows * 2 * self.shape.head_dim, bounds)
-        n_rows, max_new = self._rows(batch, row_start, q, self.shape.n_q_heads, max_new)
-        k_sel, stride = idx.size(-1), scores.size(-1)
-        rows *= n_rows
-        if n_sel.numel() != rows or idx.numel() != rows * k_sel or scores.numel() != rows * stride:
-            raise B.ActQKVError(-1, f"n_sel, idx or scores is not of {n_rows} rows of {self.shape.n_kv_heads} KV heads")
+        n_pages, n_rows, k_sel, stride = bounds.size(0), q.size(0), idx.size(-1), scores.size(-1)
+        batch, max_pages, max_new = self._limits(pages, n_rows, max_new)
+        lists = n_rows * self.shape.n_kv_heads
+        B.check_sizes(n_ctx, batch, row_start, batch + 1, bounds, n_pages * 2 * self._kv_row, q, n_rows * self._q_row, n_sel, lists,
+                      idx, lists * k_sel, scores, lists * stride)
         if n_rows == 0:
             return
         B.paged_select_pages(self.cs, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, bounds, n_pages, k_sel,
@@ -1120,13 +1110,12 @@ class PagedRunner:
     def attend_selected(self, q, row_start, n_ctx, pages, k_pages, v_pages, idx, n_sel, out, lse=None, softcap: float = 0.0,
                         window: int = 0, slopes=None, row_first=None, row_end=None, stream=None, max_new=None) -> None:
         """attend, of rows that see their selected pages alone."""
-        batch, max_pages, n_pages = self._table(n_ctx, pages, k_pages, v_pages)
-        n_rows, max_new = self._attending(batch, row_start, q, out, lse, slopes, row_first, row_end, max_new)
-        k_sel, rows = idx.size(-1), n_rows * self.shape.n_kv_heads
-        if n_sel.numel() != rows or idx.numel() != rows * k_sel:
-            raise B.ActQKVError(-1, f"n_sel or idx is not of {n_rows} rows of {self.shape.n_kv_heads} KV heads")
+        n_pages, n_rows, k_sel = k_pages.size(0), q.size(0), idx.size(-1)
+        batch, max_pages, max_new = self._limits(pages, n_rows, max_new)
+        pool, queries, heads, lists = n_pages * self._page, n_rows * self._q_row, self.shape.n_q_heads, n_rows * self.shape.n_kv_heads
+        B.check_sizes(n_ctx, batch, row_start, batch + 1, k_pages, pool, v_pages, pool, n_sel, lists, idx, lists * k_sel, q, queries,
+                      out, queries, lse, n_rows * heads, slopes, heads, row_first, n_rows, row_end, n_rows)
         if n_rows == 0:
             return
         B.paged_attention_selected(self.cs, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, k_pages, v_pages, n_pages,
-                                   idx, n_sel, k_sel, out, lse, self.workspace, softcap, window, slopes, row_first, row_end,
-                                   stream)
+                                   idx, n_sel, k_sel, out, lse, self.workspace, softcap, window, slopes, row_first, row_end, stream)
