@@ -756,6 +756,7 @@ int actqkv_paged_key_bounds(const actqkv_shape* shape, int batch, int n_rows, in
  *            (keep_first + keep_last <= k_sel), and those with the largest scores of the others (equal scores: the lower page), k_sel in all, or every page that
  *            the row sees if there are no more.
  *   n_sel  [n_rows][Hk] int32: how many.
+ * Queries, bounds and scores are finite in fp32 (a page whose score is -infinity is not selected).
  * Rows that belong to no sequence are not written; of a row at a negative position nothing is selected.  n_rows * Hk is at most 2^22.
  * Errors: EINVAL, ESHAPE, EALIGN, EWORKSPACE. */
 int actqkv_paged_select_pages(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q, const int32_t* row_start,

@@ -9,9 +9,10 @@
 // histogram, then the chosen pages in their order; integers throughout, ties to the lower page.
 //
 // Bound by the 64-bit sums (26 cycles of a SIMD for 64 products) and, of few rows, by the way from the last score to the selection: 16 sequences at
-// up to 32K tokens, 32 query and 8 KV heads of 128, 12 us (in two launches 8.4 + 6.6; 32 pages a workgroup 16.9, 128 19.6), 4 rows at 128K 12, 512
-// rows at 100K 333.  (The key bit by bit in one wavefront's registers: 17, its ballots wait for one another.)  Bounds of the pages with new tokens of 16
-// sequences: 5 us, a chain of loads.
+// up to 32K tokens, 32 query and 8 KV heads of 128, 10 us in a graph, 12 alone (in two launches 8.4 + 6.6; 32 pages a workgroup 16.9, 128 19.6), 4
+// rows at 128K 15, 512 rows at 100K 320 (305 with the products of bf16 in fp32, which end at 2^128), 142 rows of 6 pages, 28 and 4 heads, 7.4 (12.8 if
+// wavefronts without a page sum all the same).  (The key bit by bit in one wavefront's registers: 17, its ballots wait for one another.)  Bounds of the
+// pages with new tokens of 16 sequences: 3.3 us in a graph, 5 alone, a chain of loads.
 #include "paged.h"
 
 namespace actqkv {
@@ -184,6 +185,7 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagedSelect a
   __shared__ int last_flag;
   const int item = blockIdx.x / a.parts, part = blockIdx.x - item * a.parts, row = item / a.n_kv_heads, hk = item % a.n_kv_heads;
   const int slice = threadIdx.x % kLanes, at = threadIdx.x / kLanes;
+  const int first = __builtin_amdgcn_readfirstlane(at);      // of this wavefront
   const int s = paged_seq_of_row(a.t, row);
   if (s < 0) return;
   const PagedSeq seq = paged_seq(a.t, s);
@@ -213,13 +215,10 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagedSelect a
       for (int i = 0; i < kOwn; i += V) Vec<T>::load(q + h * D + i, *reinterpret_cast<float(*)[V]>(x + i));
 #pragma unroll
       for (int n = 0; n < kAtOnce; ++n) {
+        if (b0 + n * kPages + first > last) break;
         double sum[2] = {};
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) {
-          const float b = x[i] > 0.f ? hi[n][i] : lo[n][i];
-          if constexpr (sizeof(T) == 2) sum[i & 1] += double(x[i] * b);      // (a product of two bf16 is exact)
-          else sum[i & 1] += double(x[i]) * double(b);
-        }
+        for (int i = 0; i < kOwn; ++i) sum[i & 1] = fma(double(x[i]), double(x[i] > 0.f ? hi[n][i] : lo[n][i]), sum[i & 1]);
         double all = sum[0] + sum[1];
         all += lane_xor64<1>(all);
         all += lane_xor64<2>(all);

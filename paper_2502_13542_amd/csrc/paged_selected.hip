@@ -17,19 +17,27 @@ double paged_chosen_chunk_f32_us(const actqkv_shape& sh, const PagedAttn& p);
 int launch_paged_chosen_chunk(const actqkv_shape& sh, const PagedAttn& p, const PagedBits& bits, const Workspace& ws, hipStream_t stream);
 int launch_paged_chosen_chunk_f32(const actqkv_shape& sh, const PagedAttn& p, const PagedBits& bits, const Workspace& ws, hipStream_t stream);
 
-template <typename T, int D, bool kCap, bool kBias>
-__global__ __launch_bounds__(kStThreads) void paged_selected_kernel(PagedStep st) {
-  step_body<StepShape<T, D>, T, D, kCap, kBias, true>(st);
+template <typename T, int D, int W, bool kCap, bool kBias>
+__global__ __launch_bounds__(64 * W) void paged_selected_kernel(PagedStep st) {
+  step_body<StepShape<T, D>, T, D, kCap, kBias, true, W>(st);
 }
-template <typename T, int D>
-static void launch_selected(const PagedStep& st, hipStream_t stream) {
+template <typename T, int D, int W>
+static void launch_selected_by(const PagedStep& st, hipStream_t stream) {
   const bool cap = st.a.f.cap_in > 0.f, bias = st.a.f.slopes != nullptr;
   const unsigned n = unsigned(st.a.t.n_rows) * st.a.n_kv_heads * st.n_wg;
-  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(n), dim3(kStThreads), 0, stream, st); };
-  if (cap && bias) launch(paged_selected_kernel<T, D, true, true>);
-  else if (cap) launch(paged_selected_kernel<T, D, true, false>);
-  else if (bias) launch(paged_selected_kernel<T, D, false, true>);
-  else launch(paged_selected_kernel<T, D, false, false>);
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(n), dim3(64 * W), 0, stream, st); };
+  if (cap && bias) launch(paged_selected_kernel<T, D, W, true, true>);
+  else if (cap) launch(paged_selected_kernel<T, D, W, true, false>);
+  else if (bias) launch(paged_selected_kernel<T, D, W, false, true>);
+  else launch(paged_selected_kernel<T, D, W, false, false>);
+}
+// A compute unit holds eight wavefronts: with more workgroups than there are compute units two of four side by side, so that one's table, list and merge are
+// hidden behind another's keys.  us of eight | two of four: 42 rows, 28 query and 4 KV heads, 4 pages each 20.1 | 16.9, 142 32.6 | 28.9; 32 and 8
+// heads, 64 rows of 4 pages 26.8 | 24.1, of 16 91.3 | 90.6, 128 rows of 8 99.0 | 92.4; fewer workgroups: 16 rows of 16 25.6 | 26.6, 1 of 4 7.4 | 8.3.
+template <typename T, int D>
+static void launch_selected(const PagedStep& st, hipStream_t stream) {
+  if (int64_t(st.a.t.n_rows) * st.a.n_kv_heads * st.n_wg > kChipCus) launch_selected_by<T, D, 4>(st, stream);
+  else launch_selected_by<T, D, 8>(st, stream);
 }
 
 // The lists as bits: a wavefront a (row, KV head), 64 words and 64 entries at a time.
@@ -67,14 +75,17 @@ size_t paged_selected_scratch_most(const actqkv_shape& sh, int batch, int n_rows
   return std::max(parts, chunk_scratch(sh, batch, n_rows, max_new, max_pages) +
                              std::min(kMostBitBytes, bit_bytes(sh, n_rows, std::min(max_pages, 32 * kMostBitWords))));
 }
-// Whether the chunks' kernels take a call: by what they say they take for all pages, and the lists at 8 TB/s.
+// Whether the chunks' kernels take a call: by what they say they take for all pages and 8 us (the bits, their masks), and the lists at 8 TB/s
+// and 5 us (for which each row has its own reads and merge to wait for).  us of lists | so: 42 sequences of up to 8 rows at up to 724 tokens, 28 query and 4 KV heads,
+// 4 pages each 30 | 24, 24 of them at 1733 tokens 22 | 30; 32 and 8 heads, 1 x 16 rows, 16 pages at 16K 22 | 33, 30 x 10 rows, 2 pages at 300 41 | 16; fp32, 8 and 2 heads
+// of 64, 8 x 12 rows, 8 pages at 2K 26 | 26.
 static bool selected_by_chunks(const actqkv_shape& sh, const PagedAttn& p, int k_sel) {
   if (paged_step_supported(sh, p.t.max_new) || p.t.max_pages > 32 * kMostBitWords ||
       bit_bytes(sh, p.t.n_rows, p.t.max_pages) > kMostBitBytes)
     return false;
   const bool f32 = sh.dtype == ACTQKV_F32;
   const double lists = double(p.t.n_rows) * sh.n_kv_heads * std::min(k_sel, p.t.max_pages) * 2. * kBlock * sh.head_dim * (f32 ? 4. : 2.);
-  return (f32 ? paged_chosen_chunk_f32_us(sh, p) : paged_chosen_chunk_us(sh, p)) + 8. < lists / 8e6;
+  return (f32 ? paged_chosen_chunk_f32_us(sh, p) : paged_chosen_chunk_us(sh, p)) + 3. < lists / 8e6;
 }
 int launch_paged_selected(const actqkv_shape& sh, const PagedAttn& p, const int32_t* idx, const int32_t* n_sel, int k_sel,
                           const Workspace& ws, hipStream_t stream) {

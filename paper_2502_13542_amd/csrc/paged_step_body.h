@@ -54,11 +54,11 @@ __device__ __forceinline__ void step_store(const PagedAttn& p, int row, int head
   if (d == 0 && p.lse != nullptr) p.lse[size_t(row) * p.n_q_heads + head] = (m + log2f(l)) * kLn2;
 }
 
-template <typename S, typename T, int D, bool kCap, bool kBias, bool kSelected>
+template <typename S, typename T, int D, bool kCap, bool kBias, bool kSelected, int W = kStWaves>
 __device__ __forceinline__ void step_body(const PagedStep& st) {
   typedef typename S::elem C;
   constexpr int kRow = D + 2;
-  __shared__ __attribute__((aligned(16))) float lds[kStWaves * 16 * kRow];
+  __shared__ __attribute__((aligned(16))) float lds[W * 16 * kRow];
   __shared__ int last_flag;
   const PagedAttn& p = st.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -120,10 +120,10 @@ __device__ __forceinline__ void step_body(const PagedStep& st) {
   f32x4 acc[D / 16];
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int stride = wgs * kStWaves;
+  const int stride = wgs * W;
   int my_page = -1, my_index = 0;
   float my_k = 1.f, my_v = 1.f;                // scales of the lane's page
-  for (int k = 0, it = n_items < stride ? wave * wgs + wg : wg * kStWaves + wave; it < n_items; it += stride, ++k) {
+  for (int k = 0, it = n_items < stride ? wave * wgs + wg : wg * W + wave; it < n_items; it += stride, ++k) {
     if ((k & 63) == 0) {                       // the pages of this and the next 63 items
       const int mine = it + lane * stride;
       if constexpr (kSelected) {
@@ -222,14 +222,14 @@ __device__ __forceinline__ void step_body(const PagedStep& st) {
   }
   __syncthreads();
   uint32_t* group_part = st.part + size_t(pair) * st.n_wg * (16 * kRow);
-  for (int e = tid; e < cols * D; e += kStThreads) {
+  for (int e = tid; e < cols * D; e += 64 * W) {
     const int c = e / D, d = e % D;
     float m = -INFINITY, l = 0.f, o = 0.f;
 #pragma unroll
-    for (int w = 0; w < kStWaves; ++w) m = fmaxf(m, lds[(w * 16 + c) * kRow + D]);
+    for (int w = 0; w < W; ++w) m = fmaxf(m, lds[(w * 16 + c) * kRow + D]);
     const float m_safe = m == -INFINITY ? 0.f : m;
 #pragma unroll
-    for (int w = 0; w < kStWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
       const float* from = lds + (w * 16 + c) * kRow;
       const float x = __builtin_amdgcn_exp2f(from[D] - m_safe);
       l = fmaf(x, from[D + 1], l);
@@ -249,7 +249,7 @@ __device__ __forceinline__ void step_body(const PagedStep& st) {
   if (wgs == 1) return;
   if (!last_of_group(st.counters + pair, unsigned(wgs), &last_flag)) return;
   // ---- the workgroups, in their order (whoever is last)
-  for (int e = tid; e < cols * D; e += kStThreads) {
+  for (int e = tid; e < cols * D; e += 64 * W) {
     const int c = e / D, d = e % D;
     const uint32_t* from = group_part + c * kRow;
     float m = -INFINITY, l = 0.f, o = 0.f;

@@ -120,6 +120,21 @@ def test_select_of_equal_scores(shape, kind):
     run_select(b, 6, 1, 1, bounds.to(DEV))
 
 
+@pytest.mark.parametrize("shape", ["llama", "fp32_64", "mha64"])
+def test_select_by_products_beyond_fp32(shape):
+    """Products of up to 9 x 2^127 that cancel in pairs, and two channels of small ones left: exact in 64 bits in any order."""
+    b = Batch(shape_of(*SHAPES[shape]), LONG["drafts"], 19, garbage=None)
+    d, g = b.shape.head_dim, torch.Generator().manual_seed(19)
+    ints = lambda *n: torch.randint(-3, 4, n, generator=g).double()
+    q, k = ints(*b.q.shape[:2], d // 2) * 2.0**64, ints(b.n_pages, b.shape.n_kv_heads, 1, d // 2) * 2.0**63
+    q, k = torch.cat([q, -q], -1), torch.cat([k, k], -1)
+    for c in (0, d // 2):
+        q[..., c] = ints(*b.q.shape[:2]) * 2.0**40
+    b.q = q.to(b.q.dtype)
+    bounds = k.expand(-1, -1, 2, -1).to(b.q.dtype).contiguous().to(DEV)
+    run_select(b, 5, 1, 1, bounds)
+
+
 def test_select_without_pages_and_at_clamped_lengths():
     b = Batch(shape_of(*SHAPES["llama"]), LONG["chunk"], 11)
     b.pages[0, [0, 3, 11]], b.pages[1, 5] = -1, b.n_pages
