@@ -33,10 +33,12 @@ static void launch_selected_by(const PagedStep& st, hipStream_t stream) {
 }
 // A compute unit holds eight wavefronts: with more workgroups than there are compute units two of four side by side, so that one's table, list and merge are
 // hidden behind another's keys.  us of eight | two of four: 42 rows, 28 query and 4 KV heads, 4 pages each 20.1 | 16.9, 142 32.6 | 28.9; 32 and 8
-// heads, 64 rows of 4 pages 26.8 | 24.1, of 16 91.3 | 90.6, 128 rows of 8 99.0 | 92.4; fewer workgroups: 16 rows of 16 25.6 | 26.6, 1 of 4 7.4 | 8.3.
+// heads, 64 rows of 4 pages 26.8 | 24.1, of 16 91.3 | 90.6, 128 rows of 8 99.0 | 92.4; fewer workgroups: 16 rows of 16 25.6 | 26.6, 1 of 4 7.4 | 8.3.  Of long
+// lists only where that fills them: fp32, 8 and 2 heads of 64, 32 pages, 140 rows 114 | 144, 200 rows of 16 87 | 85.
 template <typename T, int D>
-static void launch_selected(const PagedStep& st, hipStream_t stream) {
-  if (int64_t(st.a.t.n_rows) * st.a.n_kv_heads * st.n_wg > kChipCus) launch_selected_by<T, D, 4>(st, stream);
+static void launch_selected(const PagedStep& st, int64_t items, hipStream_t stream) {
+  const int64_t wgs = int64_t(st.a.t.n_rows) * st.a.n_kv_heads * st.n_wg;
+  if (wgs > kChipCus && (items <= 16 * st.n_wg || 2 * wgs >= 3 * kChipCus)) launch_selected_by<T, D, 4>(st, stream);
   else launch_selected_by<T, D, 8>(st, stream);
 }
 
@@ -93,8 +95,8 @@ int launch_paged_selected(const actqkv_shape& sh, const PagedAttn& p, const int3
   const int keys = f32 ? 4096 / sh.head_dim : 64;
   PagedStep st = {};
   st.a = p;
-  st.n_wg = step_workgroups(int64_t(p.t.n_rows) * sh.n_kv_heads, int64_t(std::min(k_sel, p.t.max_pages)) * (kBlock / keys),
-                            step_least(keys, sh.head_dim, f32 ? 4 : 2));
+  const int64_t halves = int64_t(std::min(k_sel, p.t.max_pages)) * (kBlock / keys);
+  st.n_wg = step_workgroups(int64_t(p.t.n_rows) * sh.n_kv_heads, halves, step_least(keys, sh.head_dim, f32 ? 4 : 2));
   st.part = reinterpret_cast<uint32_t*>(ws.scratch_f32());
   st.counters = ws.counters();
   st.idx = idx;
@@ -111,11 +113,11 @@ int launch_paged_selected(const actqkv_shape& sh, const PagedAttn& p, const int3
                : launch_paged_chosen_chunk(sh, p, PagedBits{bits, words}, ws, stream);
   }
   if (f32) {
-    if (sh.head_dim == 64) launch_selected<float, 64>(st, stream);
-    else launch_selected<float, 128>(st, stream);
+    if (sh.head_dim == 64) launch_selected<float, 64>(st, halves, stream);
+    else launch_selected<float, 128>(st, halves, stream);
   } else {
-    if (sh.head_dim == 64) launch_selected<uint16_t, 64>(st, stream);
-    else launch_selected<uint16_t, 128>(st, stream);
+    if (sh.head_dim == 64) launch_selected<uint16_t, 64>(st, halves, stream);
+    else launch_selected<uint16_t, 128>(st, halves, stream);
   }
   return hip_status("paged attention (selected pages)");
 }
