@@ -739,7 +739,7 @@ int actqkv_paged_attention_quantised(const actqkv_shape* shape, int batch, int n
 /* Sparse attention: every row looks at the pages that a cheap score selects for it.  Pages are in the storage dtype.
  *
  * Bounds of the keys of a page: bounds [n_pages][Hk][2][D], storage dtype: of every channel the least key of the page's tokens, then the largest
- * (of the tokens that n_ctx counts).
+ * (of the tokens that n_ctx counts: the same number for all sequences of the call that share the page).
  *   row_start  NULL: of all pages of every sequence (n_rows and max_new are not looked at then); otherwise of the pages that hold a new
  *            token, after an append.
  * Errors: EINVAL, ESHAPE, EALIGN. */
