@@ -5,14 +5,15 @@
 // The score of a page for a row and KV head is the largest of that over the G query heads.  Products and sums are in 64 bits and the result is
 // rounded to fp32, so that the selection does not depend on the order of a sum.
 //
-// Scores: a lane has 16 channels of a page, D / 16 lanes a page.  Selection: the key of the last page that stays by four digits of a radix
-// histogram, then the chosen pages in their order; integers throughout, ties to the lower page.
+// Scores: a lane has 16 channels of a page, D / 16 lanes a page.  Selection: the key of the last page that stays by a radix histogram, eight bits at a
+// time from the highest in which keys differ, then the chosen pages in their order; integers throughout, ties to the lower page.
 //
 // Bound by the 64-bit sums (26 cycles of a SIMD for 64 products) and, of few rows, by the way from the last score to the selection: 16 sequences at
 // up to 32K tokens, 32 query and 8 KV heads of 128, 10 us in a graph, 12 alone (in two launches 8.4 + 6.6; 32 pages a workgroup 16.9, 128 19.6), 4
-// rows at 128K 15, 512 rows at 100K 320 (305 with the products of bf16 in fp32, which end at 2^128), 142 rows of 6 pages, 28 and 4 heads, 7.4 (12.8 if
-// wavefronts without a page sum all the same).  (The key bit by bit in one wavefront's registers: 17, its ballots wait for one another.)  Bounds of the
-// pages with new tokens of 16 sequences: 3.3 us in a graph, 5 alone, a chain of loads.
+// rows at 128K 14.6 in a graph (15.4 with all four digits and three barriers for each), 512 rows at 100K 322 (305 with the products of bf16 in fp32,
+// which end at 2^128), 142 rows of 6 pages, 28 and 4 heads, 7.4 (12.8 if wavefronts without a page sum all the same).  (The key bit by bit in one
+// wavefront's registers: 17, its ballots wait for one another.)  Bounds of the pages with new tokens of 16 sequences: 3.3 us in a graph, 5 alone, a
+// chain of loads.
 #include "paged.h"
 
 namespace actqkv {
@@ -104,75 +105,116 @@ __device__ __forceinline__ uint32_t page_key(const PagedSelect& a, float score, 
 // behind the last.
 template <typename Key>
 __device__ __forceinline__ void select_from(const PagedSelect& a, int item, int last, Key key_of) {
-  __shared__ int hist[256], wave_sum[2][kSelWaves], bin_lds, left_lds, whole_lds;
+  constexpr int kDigits = 4, kAlways = 3;
+  __shared__ int hist[kDigits][256], wave_sum[2][kSelEach][kSelWaves];
+  __shared__ uint32_t wave_bits[kAlways + 1][kSelWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, rounds = last / kSelThreads + 1;
   int32_t* idx = a.idx + size_t(item) * a.k_sel;
-  // ---- candidates
-  int n = 0;
-  for (int i = 0; i < rounds; ++i) n += __popcll(__ballot(key_of(i, i * kSelThreads + tid) != 0));
-  if (lane == 0) wave_sum[0][wave] = n;
-  hist[tid] = 0;
-  __syncthreads();
-  n = 0;
+  // ---- candidates, those that always stay, and the bits in which the others differ
+  uint32_t any = 0, all = ~0u;
+  int n = 0, always = 0;
+  for (int i = 0; i < rounds; ++i) {
+    const uint32_t k = key_of(i, i * kSelThreads + tid);
+    n += __popcll(__ballot(k != 0));
+    always += __popcll(__ballot(k == ~0u));
+    if (k != 0 && k != ~0u) any |= k, all &= k;
+  }
+  if (last >= a.k_sel) {                         // (otherwise all stay)
+    any |= lane_xor32<1>(any), all &= lane_xor32<1>(all);
+    any |= lane_xor32<2>(any), all &= lane_xor32<2>(all);
+    any |= lane_xor32<4>(any), all &= lane_xor32<4>(all);
+    any |= lane_xor32<8>(any), all &= lane_xor32<8>(all);
+    any |= lane_xor32<16>(any), all &= lane_xor32<16>(all);
+    any |= lane_xor32<32>(any), all &= lane_xor32<32>(all);
 #pragma unroll
-  for (int w = 0; w < kSelWaves; ++w) n += wave_sum[0][w];
+    for (int i = 0; i < kDigits; ++i) hist[i][tid] = 0;
+  }
+  if (lane == 0) {
+    wave_bits[0][wave] = any;
+    wave_bits[1][wave] = all;
+    wave_bits[2][wave] = n;
+    wave_bits[kAlways][wave] = always;
+  }
+  __syncthreads();
+  n = always = 0;
+#pragma unroll
+  for (int w = 0; w < kSelWaves; ++w) {
+    any |= wave_bits[0][w];
+    all &= wave_bits[1][w];
+    n += int(wave_bits[2][w]);
+    always += int(wave_bits[kAlways][w]);
+  }
   const int take = min(n, a.k_sel);
-  // ---- the key above which all are taken, and how many of its equals are
-  uint32_t key = 0, known = 0;                   // digits found so far, as a key and as a mask
-  int left = 0;                                  // (every candidate's key is above 0)
+  // ---- the key above which all are taken, and how many of its equals are: from the highest bit in which keys differ, eight at a time
+  uint32_t key = 0;                              // (every candidate's key is above 0)
+  int left = 0;
   if (n > take) {
-    left = take;
-    for (int shift = 24; shift >= 0; shift -= 8) {
+    const uint32_t differ = any & ~all;          // (others than those that always stay: more of them than are left to take)
+    left = take - always;
+    int top = left > 0 ? 32 - __clz(differ) : 0;               // bits that are not known yet
+    uint32_t known = top < 32 ? ~0u << top : 0u;
+    key = left > 0 ? all & known : 0xfffffffeu;
+    for (int digit = 0; top > 0; ++digit) {
+      const int shift = max(top - 8, 0);
       for (int i = 0; i < rounds; ++i) {
         const uint32_t k = key_of(i, i * kSelThreads + tid);
-        if (k != 0 && (k & known) == key) atomicAdd(&hist[k >> shift & 255u], 1);
+        if (k != 0 && k != ~0u && (k & known) == key) atomicAdd(&hist[digit][k >> shift & 255u], 1);
       }
       __syncthreads();
-      if (wave == 0) {                           // from the top: the bin in which the count reaches `left`
-        int mine[4], sum = 0;
+      // from the top: the bin in which the count reaches `left` (each wavefront for itself)
+      int mine[4], sum = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) mine[i] = hist[255 - (4 * lane + i)], sum += mine[i];
-        int before = lane_sums(sum) - sum;
+      for (int i = 0; i < 4; ++i) mine[i] = hist[digit][255 - (4 * lane + i)], sum += mine[i];
+      int before = lane_sums(sum) - sum, bin = 0, rest = 0, whole = 0;
+      const unsigned long long here = __ballot(before < left && before + sum >= left);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (before < left && before + mine[i] >= left) {
-            bin_lds = 255 - (4 * lane + i);
-            left_lds = left - before;
-            whole_lds = before + mine[i] == left;
-          }
-          before += mine[i];
+      for (int i = 0; i < 4; ++i) {
+        if (before < left && before + mine[i] >= left) {
+          bin = 255 - (4 * lane + i);
+          rest = left - before;
+          whole = before + mine[i] == left;
         }
+        before += mine[i];
       }
-      __syncthreads();
-      key |= uint32_t(bin_lds) << shift;
+      const int at = __ffsll(here) - 1;
+      key |= uint32_t(__builtin_amdgcn_readlane(bin, at)) << shift;
       known |= 255u << shift;
-      left = left_lds;
-      if (whole_lds != 0) {                      // all of that bin: the other digits do not matter
+      left = __builtin_amdgcn_readlane(rest, at);
+      top = shift;
+      if (__builtin_amdgcn_readlane(whole, at) != 0) {      // all of that bin: the other digits do not matter
         key -= key != 0;                         // (a candidate's key is not 0)
         left = 0;
         break;
       }
-      hist[tid] = 0;
-      __syncthreads();
     }
   }
   // ---- in their order
-  int base = 0, equal = 0;                       // taken above the key, and equal to it, before this round
-  for (int i = 0; i < rounds; ++i) {
-    const int b = i * kSelThreads + tid;
-    const uint32_t k = key_of(i, b);
-    const unsigned long long gt = __ballot(k > key), eq = __ballot(k == key && k != 0), below = (1ull << lane) - 1;
-    if (lane == 0) wave_sum[~i & 1][wave] = __popcll(gt) | __popcll(eq) << 16;
-    __syncthreads();                             // (two rows of sums, the first one the candidates': a round writes the other one)
-    int g = base, e = equal;
+  int base = 0, equal = 0;                       // taken above the key, and equal to it, before these rounds
+  for (int i0 = 0, turn = 0; i0 < rounds; i0 += kSelEach, turn ^= 1) {
+    uint32_t k[kSelEach];
+    unsigned long long gt[kSelEach], eq[kSelEach];
 #pragma unroll
-    for (int w = 0; w < kSelWaves; ++w) {
-      const int sum = wave_sum[~i & 1][w];
-      if (w < wave) g += sum & 0xffff, e += sum >> 16;
-      base += sum & 0xffff, equal += sum >> 16;
+    for (int i = 0; i < kSelEach; ++i) {
+      if (i0 + i >= rounds) break;
+      k[i] = key_of(i0 + i, (i0 + i) * kSelThreads + tid);
+      gt[i] = __ballot(k[i] > key), eq[i] = __ballot(k[i] == key && k[i] != 0);
+      if (lane == 0) wave_sum[turn][i][wave] = __popcll(gt[i]) | __popcll(eq[i]) << 16;
     }
-    g += __popcll(gt & below), e += __popcll(eq & below);
-    if (k > key || (k == key && k != 0 && e < left)) idx[g + min(e, left)] = b;
+    __syncthreads();                             // (two sets of sums: these rounds write the one that the rounds before do not read)
+    const unsigned long long below = (1ull << lane) - 1;
+#pragma unroll
+    for (int i = 0; i < kSelEach; ++i) {
+      if (i0 + i >= rounds) break;
+      int g = base, e = equal;
+#pragma unroll
+      for (int w = 0; w < kSelWaves; ++w) {
+        const int sum = wave_sum[turn][i][w];
+        if (w < wave) g += sum & 0xffff, e += sum >> 16;
+        base += sum & 0xffff, equal += sum >> 16;
+      }
+      g += __popcll(gt[i] & below), e += __popcll(eq[i] & below);
+      if (k[i] > key || (k[i] == key && k[i] != 0 && e < left)) idx[g + min(e, left)] = (i0 + i) * kSelThreads + tid;
+    }
   }
   for (int i = take + tid; i < a.k_sel; i += kSelThreads) idx[i] = -1;
   if (tid == 0) a.n_sel[item] = take;
