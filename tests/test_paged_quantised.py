@@ -100,6 +100,14 @@ def test_steps_and_chunks_of_a_wide_table(shape, kind):
                                  extra_rows=(1, 2), extra_entries=60 if shape == "llama" else 450), 4), kind, 9)
 
 
+@pytest.mark.parametrize("shape,n", [("g7", 44), ("llama", 64), ("mha64", 200), ("fp32_64", 300), ("fp32_g3", 250)])
+@pytest.mark.parametrize("kind", ["plain", "cap", "slopes", "all"])
+def test_steps_of_many_short_sequences(shape, n, kind):
+    """More (sequence, KV head) pairs than compute units, of few pages: smaller workgroups."""
+    seqs = [(i % 7 != 3, 1 + 97 * i % 724) for i in range(n)]
+    run_attention(quantise(Batch(shape_of(*SHAPES[shape]), [(int(m), c) for m, c in seqs], 127), 21), kind, 3)
+
+
 @pytest.mark.parametrize("shape", ["g7", "fp32_64", "llama", "mha64"])
 def test_pages_of_nobody_inside_a_sequence(shape):
     b = Batch(shape_of(*SHAPES[shape]), [(3, 700), (150, 700), (1, 300), (1, 260)], 23)

@@ -293,6 +293,14 @@ def test_all_pages_selected_is_attention(shape):
     assert (f64(lse) - f64(dense_lse)).__abs__().max() < 1e-5
 
 
+@pytest.mark.parametrize("shape,n", [("g7", 44), ("llama", 40), ("mha64", 90), ("fp32_64", 130), ("fp32_g3", 200)])
+@pytest.mark.parametrize("kind,k_sel", [("plain", 3), ("cap", 6), ("slopes", 3), ("all", 12)])
+def test_selected_of_many_short_sequences(shape, n, kind, k_sel):
+    """More (row, KV head) pairs than compute units, of few pages: smaller workgroups."""
+    b = Batch(shape_of(*SHAPES[shape]), [(1 + (i % 5 == 2), 2 + 97 * i % 724) for i in range(n)], 29, garbage=float("inf"))
+    run_selected(b, some_pages(b, k_sel, 7), k_sel, kind, 5)
+
+
 def test_more_rows_than_counters():
     """More (row, KV head) pairs than the workspace has counters: a workgroup each."""
     b = Batch(shape_of(16, 8, 64, "bf16"), [(1, 300)] * 60 + [(90, 400)], 25, extra_entries=0)
