@@ -8,12 +8,12 @@
 // Scores: a lane has 16 channels of a page, D / 16 lanes a page.  Selection: the key of the last page that stays by a radix histogram, eight bits at a
 // time from the highest in which keys differ, then the chosen pages in their order; integers throughout, ties to the lower page.
 //
-// Bound by the 64-bit sums (26 cycles of a SIMD for 64 products) and, of few rows, by the way from the last score to the selection: 16 sequences at
-// up to 32K tokens, 32 query and 8 KV heads of 128, 10 us in a graph, 12 alone (in two launches 8.4 + 6.6; 32 pages a workgroup 16.9, 128 19.6), 4
-// rows at 128K 14.6 in a graph (15.4 with all four digits and three barriers for each), 512 rows at 100K 322 (305 with the products of bf16 in fp32,
-// which end at 2^128), 142 rows of 6 pages, 28 and 4 heads, 7.4 (12.8 if wavefronts without a page sum all the same).  (The key bit by bit in one
-// wavefront's registers: 17, its ballots wait for one another.)  Bounds of the pages with new tokens of 16 sequences: 3.3 us in a graph, 5 alone, a
-// chain of loads.
+// Bound by the 64-bit sums (26 cycles of a SIMD for 64 products, by the matrix instruction 13 where rows are many) and, of few rows, by the way from the
+// last score to the selection: 16 sequences at up to 32K tokens, 32 query and 8 KV heads of 128, 10 us in a graph, 12 alone (in two launches 8.4 + 6.6; 32
+// pages a workgroup 16.9, 128 19.6), 4 rows at 128K 14.8 in a graph (15.4 with all four digits and three barriers for each), 512 rows at 100K 151 (332 row
+// by row, 305 with the products of bf16 in fp32, which end at 2^128), 142 rows of 6 pages, 28 and 4 heads, 7.4 (12.8 if wavefronts without a page sum all
+// the same).  (The key bit by bit in one wavefront's registers: 17, its ballots wait for one another.)  Bounds of the pages with new tokens of 16
+// sequences: 3.3 us in a graph, 5 alone, a chain of loads.
 #include "paged.h"
 
 namespace actqkv {
@@ -220,8 +220,69 @@ __device__ __forceinline__ void select_from(const PagedSelect& a, int item, int 
   if (tid == 0) a.n_sel[item] = take;
 }
 
-// The pages of a (row, KV head) go to `parts` workgroups; the one that is done last selects.
+// Scores of many rows by the 64-bit matrix instruction, as sum max(q, 0) hi + min(q, 0) lo: a wavefront takes 16 pages for 16 rows of a
+// sequence, one query head after the other, and holds of each the largest.  Lane l has page and row l % 16 and the quarter l / 16 of the channels.
+// 512 rows at 100K tokens, 32 query and 8 KV heads of 128, 141 us = 46 TFLOP/s (operands widened anew for each head, in 115 registers instead of 190, 147; in
+// 128 with some in scratch 206), and the selection 19.
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+constexpr int kScRows = 16, kScPages = kSelWaves * 16;
 template <typename T, int D>
+__global__ __launch_bounds__(kSelThreads) void paged_scores_kernel(PagedSelect a) {
+  constexpr int V = Vec<T>::N, kOwn = D / 4, kChunks = kOwn / V;
+  typedef typename Vec<T>::raw raw_t;
+  const int hk = blockIdx.x % a.n_kv_heads, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int s, tile;
+  if (!paged_find_tile(a.t, blockIdx.x / a.n_kv_heads, 1, kScRows, s, tile)) return;
+  const PagedSeq seq = paged_seq(a.t, s);
+  const int own = lane & 15, quarter = lane >> 4;
+  const int i_row = min(tile * kScRows + own, seq.m - 1), pos = seq.n - seq.m + i_row, last = pos >= 0 ? pos / kBlock : -1;
+  const bool row_there = tile * kScRows + own < seq.m;
+  const int most_pos = seq.n - seq.m + min(tile * kScRows + kScRows, seq.m) - 1, tile_last = most_pos >= 0 ? most_pos / kBlock : -1;
+  const T* q = static_cast<const T*>(a.q) + (size_t(seq.row0 + i_row) * a.n_kv_heads + hk) * a.group * D + quarter * kOwn;
+  float* scores = a.scores + (size_t(seq.row0 + i_row) * a.n_kv_heads + hk) * a.stride;
+  for (int b0 = blockIdx.y * kScPages + wave * 16; b0 < a.t.max_pages; b0 += gridDim.y * kScPages) {
+    float most[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) most[r] = -INFINITY;
+    unsigned long long there = 0;
+    if (b0 <= tile_last) {
+      const int page = b0 + own <= tile_last ? paged_page(a.t, s, b0 + own) : -1;
+      there = __ballot(page >= 0);
+      const T* from = static_cast<const T*>(a.bounds) + (size_t(max(page, 0)) * a.n_kv_heads + hk) * (2 * D) + quarter * kOwn;
+      raw_t lo[kChunks], hi[kChunks];
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) lo[c] = Vec<T>::load_raw(from + c * V), hi[c] = Vec<T>::load_raw(from + D + c * V);
+      for (int h = 0; h < a.group; ++h) {
+        raw_t x[kChunks];
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) x[c] = Vec<T>::load_raw(q + h * D + c * V);
+        f64x4 up = {}, down = {};
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+          float l[V], u[V], y[V];
+          Vec<T>::widen(lo[c], l);
+          Vec<T>::widen(hi[c], u);
+          Vec<T>::widen(x[c], y);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            up = __builtin_amdgcn_mfma_f64_16x16x4f64(double(u[e]), double(fmaxf(y[e], 0.f)), up, 0, 0, 0);
+            down = __builtin_amdgcn_mfma_f64_16x16x4f64(double(l[e]), double(fminf(y[e], 0.f)), down, 0, 0, 0);
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) most[r] = fmaxf(most[r], float(up[r] + down[r]));
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {                // (register r of a lane: page 4 r + l / 16, row l % 16)
+      const int i = 4 * r + quarter, b = b0 + i;
+      if (row_there && b < a.t.max_pages) scores[b] = b <= last && (there >> i & 1) != 0 ? most[r] + 0.f : -INFINITY;
+    }
+  }
+}
+
+// The pages of a (row, KV head) go to `parts` workgroups; the one that is done last selects.  kScored: the scores are there.
+template <typename T, int D, bool kScored>
 __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagedSelect a) {
   constexpr int V = Vec<T>::N, kOwn = 16, kLanes = D / kOwn, kPages = kSelThreads / kLanes;
   __shared__ int last_flag;
@@ -234,54 +295,56 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagedSelect a
   const int pos = seq.n - seq.m + (row - seq.row0);
   const int last = pos >= 0 ? pos / kBlock : -1;     // the last page that the row sees (below max_pages: pos < n)
   uint32_t* scores = reinterpret_cast<uint32_t*>(a.scores) + size_t(item) * a.stride;
-  const T* q = static_cast<const T*>(a.q) + (size_t(row) * a.n_kv_heads + hk) * a.group * D + slice * kOwn;
-  constexpr int kAtOnce = 2;
-  for (int b0 = part * (kAtOnce * kPages); b0 <= last; b0 += a.parts * (kAtOnce * kPages)) {
-    int page[kAtOnce];
-    float lo[kAtOnce][kOwn], hi[kAtOnce][kOwn], most[kAtOnce];
+  if constexpr (!kScored) {
+    const T* q = static_cast<const T*>(a.q) + (size_t(row) * a.n_kv_heads + hk) * a.group * D + slice * kOwn;
+    constexpr int kAtOnce = 2;
+    for (int b0 = part * (kAtOnce * kPages); b0 <= last; b0 += a.parts * (kAtOnce * kPages)) {
+      int page[kAtOnce];
+      float lo[kAtOnce][kOwn], hi[kAtOnce][kOwn], most[kAtOnce];
 #pragma unroll
-    for (int n = 0; n < kAtOnce; ++n) page[n] = b0 + n * kPages + at <= last ? paged_page(a.t, s, b0 + n * kPages + at) : -1;
-#pragma unroll
-    for (int n = 0; n < kAtOnce; ++n) {
-      const T* from = static_cast<const T*>(a.bounds) + (size_t(max(page[n], 0)) * a.n_kv_heads + hk) * (2 * D) + slice * kOwn;
-      most[n] = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < kOwn; i += V) {
-        Vec<T>::load(from + i, *reinterpret_cast<float(*)[V]>(lo[n] + i));
-        Vec<T>::load(from + D + i, *reinterpret_cast<float(*)[V]>(hi[n] + i));
-      }
-    }
-    for (int h = 0; h < a.group; ++h) {
-      float x[kOwn];
-#pragma unroll
-      for (int i = 0; i < kOwn; i += V) Vec<T>::load(q + h * D + i, *reinterpret_cast<float(*)[V]>(x + i));
+      for (int n = 0; n < kAtOnce; ++n) page[n] = b0 + n * kPages + at <= last ? paged_page(a.t, s, b0 + n * kPages + at) : -1;
 #pragma unroll
       for (int n = 0; n < kAtOnce; ++n) {
-        if (b0 + n * kPages + first > last) break;
-        double sum[2] = {};
+        const T* from = static_cast<const T*>(a.bounds) + (size_t(max(page[n], 0)) * a.n_kv_heads + hk) * (2 * D) + slice * kOwn;
+        most[n] = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) sum[i & 1] = fma(double(x[i]), double(x[i] > 0.f ? hi[n][i] : lo[n][i]), sum[i & 1]);
-        double all = sum[0] + sum[1];
-        all += lane_xor64<1>(all);
-        all += lane_xor64<2>(all);
-        if (kLanes == 8) all += lane_xor64<4>(all);
-        most[n] = fmaxf(most[n], float(all));
+        for (int i = 0; i < kOwn; i += V) {
+          Vec<T>::load(from + i, *reinterpret_cast<float(*)[V]>(lo[n] + i));
+          Vec<T>::load(from + D + i, *reinterpret_cast<float(*)[V]>(hi[n] + i));
+        }
+      }
+      for (int h = 0; h < a.group; ++h) {
+        float x[kOwn];
+#pragma unroll
+        for (int i = 0; i < kOwn; i += V) Vec<T>::load(q + h * D + i, *reinterpret_cast<float(*)[V]>(x + i));
+#pragma unroll
+        for (int n = 0; n < kAtOnce; ++n) {
+          if (b0 + n * kPages + first > last) break;
+          double sum[2] = {};
+#pragma unroll
+          for (int i = 0; i < kOwn; ++i) sum[i & 1] = fma(double(x[i]), double(x[i] > 0.f ? hi[n][i] : lo[n][i]), sum[i & 1]);
+          double all = sum[0] + sum[1];
+          all += lane_xor64<1>(all);
+          all += lane_xor64<2>(all);
+          if (kLanes == 8) all += lane_xor64<4>(all);
+          most[n] = fmaxf(most[n], float(all));
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < kAtOnce; ++n) {
+        const int b = b0 + n * kPages + at;
+        // (adding 0 leaves no -0: equal scores have equal bits)
+        if (slice == 0 && b <= last) st_agent(scores + b, __float_as_uint(page[n] >= 0 ? most[n] + 0.f : -INFINITY));
       }
     }
-#pragma unroll
-    for (int n = 0; n < kAtOnce; ++n) {
-      const int b = b0 + n * kPages + at;
-      // (adding 0 leaves no -0: equal scores have equal bits)
-      if (slice == 0 && b <= last) st_agent(scores + b, __float_as_uint(page[n] >= 0 ? most[n] + 0.f : -INFINITY));
+    for (int b = last + 1 + part * kSelThreads + threadIdx.x; b < a.t.max_pages; b += a.parts * kSelThreads)
+      scores[b] = __float_as_uint(-INFINITY);
+    if (a.parts > 1) {
+      if (!last_of_group(a.counters + item, unsigned(a.parts), &last_flag)) return;
+    } else {
+      __builtin_amdgcn_s_waitcnt(0);         // (this wavefront's scores have been acknowledged)
+      __syncthreads();
     }
-  }
-  for (int b = last + 1 + part * kSelThreads + threadIdx.x; b < a.t.max_pages; b += a.parts * kSelThreads)
-    scores[b] = __float_as_uint(-INFINITY);
-  if (a.parts > 1) {
-    if (!last_of_group(a.counters + item, unsigned(a.parts), &last_flag)) return;
-  } else {
-    __builtin_amdgcn_s_waitcnt(0);         // (this wavefront's scores have been acknowledged)
-    __syncthreads();
   }
   auto from_memory = [&](int, int b) { return b <= last ? page_key(a, __uint_as_float(ld_agent(scores + b)), b, last) : 0u; };
   if (last < kSelThreads * kSelEach) {
@@ -336,13 +399,32 @@ int launch_paged_select(const actqkv_shape& sh, const PagedTable& t, const void*
   const int64_t items = int64_t(t.n_rows) * sh.n_kv_heads;
   a.parts = items > int64_t(kTicketCounters) ? 1 : int(std::max<int64_t>(1, std::min<int64_t>((t.max_pages + kSelLeast - 1) / kSelLeast, kSelWgs / items)));
   a.counters = ws.counters();
-  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned(items) * a.parts), dim3(kSelThreads), 0, stream, a); };
+  // Both ways' time by their products, of rows as they are and in tiles of 16 (and a launch more): us of one | the other, 32 query and 8 KV heads
+  // of 128: 512 rows at 100K tokens 332 | 151, 64 56 | 31, 16 23.5 | 20.1, at 16K 8.9 | 18.4, 2 x 2048 rows at 16K 462 | 234, 16 x 8 at 32K 36 | 29.5, 16 x 4
+  // 17.5 | 28; fp32, 8 and 2 heads of 64, 512 rows at 8K 14.0 | 15.5, 32 at 60K 11.9 | 15.1.
+  const int seqs = std::min(t.batch, t.n_rows), tiles = int(std::min<int64_t>(int64_t(seqs) * ((t.max_new + kScRows - 1) / kScRows), t.n_rows / kScRows + seqs));
+  const double products = double(sh.n_q_heads) * sh.head_dim * t.max_pages;     // of a row
+  const bool scored = products * t.n_rows / 4.6e6 > products * tiles * kScRows / 11.6e6 + 3.;
+  auto launch = [&](auto* type, auto dim) {
+    typedef std::remove_pointer_t<decltype(type)> T;
+    constexpr int D = decltype(dim)::value;
+    if (!scored) {
+      hipLaunchKernelGGL((paged_select_kernel<T, D, false>), dim3(unsigned(items) * a.parts), dim3(kSelThreads), 0, stream, a);
+      return;
+    }
+    a.parts = 1;
+    const dim3 grid(unsigned(tiles) * sh.n_kv_heads, std::min((t.max_pages + kScPages - 1) / kScPages, kSelMostY));
+    hipLaunchKernelGGL((paged_scores_kernel<T, D>), grid, dim3(kSelThreads), 0, stream, a);
+    hipLaunchKernelGGL((paged_select_kernel<T, D, true>), dim3(unsigned(items)), dim3(kSelThreads), 0, stream, a);
+  };
+  const std::integral_constant<int, 64> d64;
+  const std::integral_constant<int, 128> d128;
   if (sh.dtype == ACTQKV_F32) {
-    if (sh.head_dim == 64) launch(paged_select_kernel<float, 64>);
-    else launch(paged_select_kernel<float, 128>);
+    if (sh.head_dim == 64) launch(static_cast<float*>(nullptr), d64);
+    else launch(static_cast<float*>(nullptr), d128);
   } else {
-    if (sh.head_dim == 64) launch(paged_select_kernel<uint16_t, 64>);
-    else launch(paged_select_kernel<uint16_t, 128>);
+    if (sh.head_dim == 64) launch(static_cast<uint16_t*>(nullptr), d64);
+    else launch(static_cast<uint16_t*>(nullptr), d128);
   }
   return hip_status("paged page selection");
 }

@@ -120,19 +120,54 @@ def test_select_of_equal_scores(shape, kind):
     run_select(b, 6, 1, 1, bounds.to(DEV))
 
 
-@pytest.mark.parametrize("shape", ["llama", "fp32_64", "mha64"])
-def test_select_by_products_beyond_fp32(shape):
-    """Products of up to 9 x 2^127 that cancel in pairs, and two channels of small ones left: exact in 64 bits in any order."""
-    b = Batch(shape_of(*SHAPES[shape]), LONG["drafts"], 19, garbage=None)
-    d, g = b.shape.head_dim, torch.Generator().manual_seed(19)
+def beyond_fp32(b, seed):
+    """Queries and bounds whose products, of up to 9 x 2^127, cancel in pairs, and two channels of small ones left: exact in 64 bits in any order."""
+    d, g = b.shape.head_dim, torch.Generator().manual_seed(seed)
     ints = lambda *n: torch.randint(-3, 4, n, generator=g).double()
     q, k = ints(*b.q.shape[:2], d // 2) * 2.0**64, ints(b.n_pages, b.shape.n_kv_heads, 1, d // 2) * 2.0**63
     q, k = torch.cat([q, -q], -1), torch.cat([k, k], -1)
     for c in (0, d // 2):
         q[..., c] = ints(*b.q.shape[:2]) * 2.0**40
     b.q = q.to(b.q.dtype)
-    bounds = k.expand(-1, -1, 2, -1).to(b.q.dtype).contiguous().to(DEV)
-    run_select(b, 5, 1, 1, bounds)
+    return k.expand(-1, -1, 2, -1).to(b.q.dtype).contiguous().to(DEV)
+
+
+@pytest.mark.parametrize("shape", ["llama", "fp32_64", "mha64"])
+def test_select_by_products_beyond_fp32(shape):
+    b = Batch(shape_of(*SHAPES[shape]), LONG["drafts"], 19, garbage=None)
+    run_select(b, 5, 1, 1, beyond_fp32(b, 19))
+
+
+WIDE = 3000                # entries of a table whose calls by many rows take the matrix instruction
+
+
+@pytest.mark.parametrize("shape", list(SHAPES))
+@pytest.mark.parametrize("kind", ["random", "beyond", "few", "zeros", "none"])
+def test_select_of_many_rows(shape, kind):
+    seqs = LONG["chunk"] + [(0, 300), (33, 33), (16, 2100)]
+    b = Batch(shape_of(*SHAPES[shape]), seqs, 41, extra_rows=(1, 2), extra_entries=WIDE, **({} if kind in ("random", "none") else dict(garbage=None)))
+    sh, bounds = b.shape, None
+    if kind == "beyond":
+        bounds = beyond_fp32(b, 23)
+    elif kind in ("few", "zeros"):
+        bounds = torch.randn(b.n_pages, sh.n_kv_heads, 2, sh.head_dim, generator=torch.Generator().manual_seed(3)).sort(2).values.to(sh.torch_dtype)
+        bounds = bounds[torch.arange(b.n_pages) % 3].contiguous().to(DEV)
+    if kind == "zeros":
+        b.q[::2] = 0
+        b.q[1::2] = -0.0
+    if kind == "none":
+        b.pages[0, [0, 3, 11]], b.pages[1, 5], b.pages[5, 15] = -1, b.n_pages, -7
+    run_select(b, 6, 1, 1, bounds)
+
+
+def test_select_of_many_rows_at_clamped_lengths():
+    """Some rows at negative positions, lengths beyond the table."""
+    b = Batch(shape_of(*SHAPES["llama"]), [(140, 300), (120, 140), (64, 64)], 43, extra_entries=WIDE, garbage=None)
+    raw = torch.tensor([100, (b.max_pages + 5) * BS, 64], dtype=torch.int32, device=DEV)
+    b.n_ctx = np.array([100, b.max_pages * BS, 64])
+    b.seqs = [(m, n) for (m, _), n in zip(b.seqs, b.n_ctx)]
+    b.dev = lambda dev=DEV: dict(Batch.dev(b, dev), n_ctx=raw.clone())
+    run_select(b, 4, 1, 1)
 
 
 def test_select_without_pages_and_at_clamped_lengths():
