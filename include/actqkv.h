@@ -50,7 +50,7 @@
 extern "C" {
 #endif
 
-#define ACTQKV_VERSION 109
+#define ACTQKV_VERSION 110
 
 enum {
   ACTQKV_OK = 0,
@@ -630,11 +630,15 @@ int actqkv_copy_bytes(void* dst, const void* src, size_t bytes, void* stream);
  * no out-of-bounds access. */
 
 /* Bytes of workspace of the paged calls that take one, for calls of at most batch sequences, n_rows rows, max_new rows of a
- * sequence and max_pages pages.  As for the other calls: zero-filled once, and calls that share one ordered on one stream (a graph
- * that was captured with it is a call).  Most of it are the scores that the account of weight keeps where a call brings few
- * rows: 4 bytes for every query head, row (of at most 16 / G) and token of batch tables of max_pages pages (64 sequences of up
- * to 32768 tokens, 32 and 8 heads, chunks: 1.07 GB of 1.09). */
+ * sequence and max_pages pages: enough for any of them; a call is refused for less than it needs itself.  As for the other calls: zero-filled
+ * once, and calls that share one ordered on one stream (a graph that was captured with it is a call).  It is the largest of
+ *   the scores that the account of weight keeps where a call brings few rows: 4 bytes for every query head, row (of at most 16 / G) and
+ *            token of batch tables of max_pages pages (64 sequences of up to 32768 tokens, 32 and 8 heads, chunks: 1.07 GB of 1.09);
+ *   the pieces that chunks are cut into: up to 69 MB in bf16 and 35 MB in fp32, over pages in 8 bits up to twice that;
+ *   of chunks over selected pages those pieces and up to 256 MiB of bits (n_rows * Hk * max_pages / 8 bytes). */
 size_t actqkv_paged_workspace_bytes(const actqkv_shape* shape, int batch, int n_rows, int max_new, int max_pages);
+/* The same for callers of actqkv_paged_attention and actqkv_paged_attention_weights alone. */
+size_t actqkv_paged_attention_workspace_bytes(const actqkv_shape* shape, int batch, int n_rows, int max_new, int max_pages);
 
 /* Keys and values of the new tokens into their pages.
  *   k_new, v_new  [n_rows][Hk][D], storage dtype.  Only the new tokens' slots are written. */

@@ -90,6 +90,7 @@ SIGNATURES = {
     "actqkv_retrieval_attention_windows": (_i, [_shp, _i, _i, _vp, _vp, _vp, _i, _vp, _vp, _vp, _i, _vp, _vp, _vp, _sz,
                                                 _i, _vp]),
     "actqkv_paged_workspace_bytes": (_sz, [_shp, _i, _i, _i, _i]),
+    "actqkv_paged_attention_workspace_bytes": (_sz, [_shp, _i, _i, _i, _i]),
     "actqkv_paged_append": (_i, [_shp, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _i, _vp, _vp, _i, _vp]),
     "actqkv_paged_attention": (_i, [_shp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _i, ctypes.c_float, _i, _vp, _vp, _vp,
                                     _vp, _vp, _vp, _sz, _vp]),
@@ -367,6 +368,14 @@ def retrieval_attention(shape: CShape, batch: int, m: int, q, k_cache, v_cache, 
 
 def paged_workspace_bytes(shape: CShape, batch: int, n_rows: int, max_new: int, max_pages: int) -> int:
     n = load_library().actqkv_paged_workspace_bytes(ctypes.byref(shape), batch, n_rows, max_new, max_pages)
+    if n == 0:
+        raise ActQKVError(-1, last_error())
+    return n
+
+
+def paged_attention_workspace_bytes(shape: CShape, batch: int, n_rows: int, max_new: int, max_pages: int) -> int:
+    """The same for callers of paged_attention and paged_attention_weights alone."""
+    n = load_library().actqkv_paged_attention_workspace_bytes(ctypes.byref(shape), batch, n_rows, max_new, max_pages)
     if n == 0:
         raise ActQKVError(-1, last_error())
     return n

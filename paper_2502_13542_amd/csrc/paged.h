@@ -264,13 +264,15 @@ int launch_paged_step(const actqkv_shape& sh, const PagedAttn& p, const PagedWei
                       hipStream_t stream);
 int launch_paged8_chunk(const actqkv_shape& sh, const PagedAttn& p, const Workspace& ws, hipStream_t stream);
 int launch_paged8_chunk_f32(const actqkv_shape& sh, const PagedAttn& p, const Workspace& ws, hipStream_t stream);
+size_t paged8_step_scratch_most(const actqkv_shape& sh, int batch);
 int launch_paged8_step(const actqkv_shape& sh, const PagedAttn& p, const Workspace& ws, hipStream_t stream);
 size_t paged_selected_scratch_most(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages);
 int launch_paged_selected(const actqkv_shape& sh, const PagedAttn& p, const int32_t* idx, const int32_t* n_sel, int k_sel,
                           const Workspace& ws, hipStream_t stream);
-size_t paged_chunk_scratch_most(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages);
+// (byte: of pages in 8 bits, whose calls are cut into more pieces)
+size_t paged_chunk_scratch_most(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages, bool byte);
 int launch_paged_chunk(const actqkv_shape& sh, const PagedAttn& p, const Workspace& ws, hipStream_t stream);
-size_t paged_chunk_f32_scratch_most(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages);
+size_t paged_chunk_f32_scratch_most(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages, bool byte);
 int launch_paged_chunk_f32(const actqkv_shape& sh, const PagedAttn& p, const Workspace& ws, hipStream_t stream);
 size_t paged_votes_scratch_most(const actqkv_shape& sh);
 int launch_paged_votes(const actqkv_shape& sh, const PagedAttn& p, const PagedWeights& w, const Workspace& ws, hipStream_t stream);

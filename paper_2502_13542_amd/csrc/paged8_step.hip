@@ -32,6 +32,7 @@ static void launch_step8(const PagedStep& st, hipStream_t stream) {
   if ((wgs > kChipCus && pages <= 4) || (2 * wgs >= 3 * kChipCus && pages <= 16)) launch_step8_by<T, D, 4>(st, stream);
   else launch_step8_by<T, D, 8>(st, stream);
 }
+size_t paged8_step_scratch_most(const actqkv_shape& sh, int batch) { return step_part_most(sh, int64_t(batch) * sh.n_kv_heads); }
 int launch_paged8_step(const actqkv_shape& sh, const PagedAttn& p, const Workspace& ws, hipStream_t stream) {
   PagedStep st = {};
   st.a = p;

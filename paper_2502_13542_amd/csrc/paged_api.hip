@@ -24,13 +24,22 @@ static int launch_paged_attention(const actqkv_shape& sh, PagedAttn p, const Pag
   ACTQKV_TRY(sh.dtype == ACTQKV_F32 ? launch_paged_chunk_f32(sh, p, ws, stream) : launch_paged_chunk(sh, p, ws, stream));
   return weights != nullptr ? launch_paged_votes(sh, p, *weights, ws, stream) : ACTQKV_OK;
 }
-// Enough for every call of at most these sizes: of few rows a sequence, none of them takes the chunks' kernels.
-static size_t paged_workspace_bytes(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages) {
-  size_t most = std::max(paged_step_scratch_most(sh, batch, max_new, max_pages), paged_selected_scratch_most(sh, batch, n_rows, max_new, max_pages));
-  if (!paged_step_supported(sh, max_new))
-    most = std::max({most, paged_votes_scratch_most(sh),
-                     sh.dtype == ACTQKV_F32 ? paged_chunk_f32_scratch_most(sh, batch, n_rows, max_new, max_pages)
-                                            : paged_chunk_scratch_most(sh, batch, n_rows, max_new, max_pages)});
+// Calls that take a workspace; each is checked for what it needs itself.
+enum class PagedCall { kAttention, kQuantised, kSelection, kSelected };      // (kAttention: the account of weight, too)
+// Enough for every call of that kind of at most these sizes: of few rows a sequence, none of them takes the chunks' kernels.
+static size_t paged_workspace_bytes(PagedCall call, const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages) {
+  const bool byte = call == PagedCall::kQuantised;
+  size_t most = 0;
+  if (call == PagedCall::kSelected) {
+    most = paged_selected_scratch_most(sh, batch, n_rows, max_new, max_pages);
+  } else if (call != PagedCall::kSelection) {      // (a selection needs counters alone)
+    most = byte ? paged8_step_scratch_most(sh, batch) : paged_step_scratch_most(sh, batch, max_new, max_pages);
+    if (!paged_step_supported(sh, max_new)) {
+      most = std::max(most, sh.dtype == ACTQKV_F32 ? paged_chunk_f32_scratch_most(sh, batch, n_rows, max_new, max_pages, byte)
+                                                   : paged_chunk_scratch_most(sh, batch, n_rows, max_new, max_pages, byte));
+      if (!byte) most = std::max(most, paged_votes_scratch_most(sh));
+    }
+  }
   return kCounterBytes + align_up(most, 256);
 }
 
@@ -60,14 +69,25 @@ static int check_rows(int n_rows, int max_new) {
   return ACTQKV_OK;
 }
 
-static int check_workspace(const char* name, const actqkv_shape* shape, int batch, int n_rows, int max_new, int max_pages,
+static int check_workspace(PagedCall call, const char* name, const actqkv_shape* shape, int batch, int n_rows, int max_new, int max_pages,
                            const void* workspace, size_t ws_bytes) {
   if (workspace == nullptr || !aligned16(workspace))
     return set_error(ACTQKV_EWORKSPACE, "workspace is NULL or not 16-byte aligned");
-  const size_t need = paged_workspace_bytes(*shape, batch, n_rows, max_new, max_pages);
+  const size_t need = paged_workspace_bytes(call, *shape, batch, n_rows, max_new, max_pages);
   if (ws_bytes < need)
     return set_error(ACTQKV_EWORKSPACE, "workspace has %zu bytes, %s needs %zu", ws_bytes, name, need);
   return ACTQKV_OK;
+}
+
+// What a caller asks for before its calls; 0 of sizes that no call may have.
+static size_t checked_workspace_bytes(const char* name, PagedCall call, const actqkv_shape* shape, int batch, int n_rows, int max_new,
+                                      int max_pages) {
+  if (check_shape(shape) != ACTQKV_OK || check_batch(batch) != ACTQKV_OK || check_rows(n_rows, max_new) != ACTQKV_OK) return 0;
+  if (max_pages < 1 || max_pages > kMaxPages) {
+    set_error(ACTQKV_EINVAL, "%s: max_pages %d outside 1..%d", name, max_pages, kMaxPages);
+    return 0;
+  }
+  return paged_workspace_bytes(call, *shape, batch, n_rows, max_new, max_pages);
 }
 
 // Lists of selected pages: of every (row, KV head) k_sel entries.
@@ -144,7 +164,8 @@ static int attention_call(const char* name, const actqkv_shape* shape, int batch
     ACTQKV_REQUIRE_SMALL(idx, 4);
     ACTQKV_REQUIRE_SMALL(n_sel, 4);
   }
-  ACTQKV_TRY(check_workspace(name, shape, batch, n_rows, max_new, max_pages, workspace, ws_bytes));
+  const PagedCall call = chosen != nullptr ? PagedCall::kSelected : k_scales != nullptr ? PagedCall::kQuantised : PagedCall::kAttention;
+  ACTQKV_TRY(check_workspace(call, name, shape, batch, n_rows, max_new, max_pages, workspace, ws_bytes));
   const float scale = shape->softmax_scale > 0.f ? shape->softmax_scale : 1.f / std::sqrt(float(shape->head_dim));
   PagedAttn p;
   p.t = PagedTable{row_start, n_ctx, pages, batch, n_rows, max_new, max_pages, n_pages, 0};
@@ -171,13 +192,14 @@ using namespace actqkv;
 extern "C" {
 
 size_t actqkv_paged_workspace_bytes(const actqkv_shape* shape, int batch, int n_rows, int max_new, int max_pages) {
-  if (check_shape(shape) != ACTQKV_OK || check_batch(batch) != ACTQKV_OK) return 0;
-  if (check_rows(n_rows, max_new) != ACTQKV_OK) return 0;
-  if (max_pages < 1 || max_pages > kMaxPages) {
-    set_error(ACTQKV_EINVAL, "paged_workspace_bytes: max_pages %d outside 1..%d", max_pages, kMaxPages);
-    return 0;
-  }
-  return paged_workspace_bytes(*shape, batch, n_rows, max_new, max_pages);
+  size_t most = 0;
+  for (PagedCall call : {PagedCall::kAttention, PagedCall::kQuantised, PagedCall::kSelection, PagedCall::kSelected})
+    most = std::max(most, checked_workspace_bytes("paged_workspace_bytes", call, shape, batch, n_rows, max_new, max_pages));
+  return most;
+}
+
+size_t actqkv_paged_attention_workspace_bytes(const actqkv_shape* shape, int batch, int n_rows, int max_new, int max_pages) {
+  return checked_workspace_bytes("paged_attention_workspace_bytes", PagedCall::kAttention, shape, batch, n_rows, max_new, max_pages);
 }
 
 int actqkv_paged_append(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* k_new,
@@ -292,7 +314,7 @@ int actqkv_paged_select_pages(const actqkv_shape* shape, int batch, int n_rows, 
     return set_error(ACTQKV_EINVAL, "score_stride %lld < max_pages %d", (long long)score_stride, max_pages);
   ACTQKV_REQUIRE_SMALL(idx, 4);
   ACTQKV_REQUIRE_SMALL(n_sel, 4);
-  ACTQKV_TRY(check_workspace("paged_select_pages", shape, batch, n_rows, max_new, max_pages, workspace, ws_bytes));
+  ACTQKV_TRY(check_workspace(PagedCall::kSelection, "paged_select_pages", shape, batch, n_rows, max_new, max_pages, workspace, ws_bytes));
   const PagedTable t{row_start, n_ctx, pages, batch, n_rows, max_new, max_pages, n_pages, 0};
   return launch_paged_select(*shape, t, q, bounds, k_sel, keep_first, keep_last, scores, score_stride, idx, n_sel,
                              Workspace{workspace, ws_bytes}, static_cast<hipStream_t>(stream));

@@ -28,13 +28,13 @@ __global__ __launch_bounds__(kPcThreads) void paged_chunk_kernel(PagedChunk c) {
   chunk_body<D, KS, kCap, kBias, false, false>(c);
 }
 
-size_t paged_chunk_scratch_most(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages) {
+size_t paged_chunk_scratch_most(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages, bool byte) {
   if (sh.dtype != ACTQKV_BF16) return 0;
   size_t most = 0;
   for (int ks = 1; ks <= 4; ks *= 2)
     most = std::max(most, size_t(std::min(kPcMaxSplits, max_pages)) * sh.n_kv_heads * chunk_tiles(sh, batch, n_rows, max_new, ks) *
                               chunk_piece_bytes(sh, ks));
-  return std::min(most, kPcMostPiecesByte * chunk_piece_bytes(sh, 1));
+  return std::min(most, (byte ? kPcMostPiecesByte : kPcMostPieces) * chunk_piece_bytes(sh, 1));
 }
 
 template <int D, int KS>

@@ -19,11 +19,11 @@ __global__ __launch_bounds__(kP4Threads, D == 64 ? 2 : 1) void paged_chunk_f32_k
   chunk_f32_body<D, kCap, kBias, false, false>(c);
 }
 
-size_t paged_chunk_f32_scratch_most(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages) {
+size_t paged_chunk_f32_scratch_most(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages, bool byte) {
   if (sh.dtype != ACTQKV_F32) return 0;
   const int64_t pieces = std::min<int64_t>(kP4MaxSplits, int64_t(max_pages) * (kBlock / (4096 / sh.head_dim))) * sh.n_kv_heads *
                          chunk_f32_tiles(sh, batch, n_rows, max_new);
-  return size_t(std::min<int64_t>(kP4SlotsByte, pieces)) * (sh.head_dim == 64 ? ChunkPieceF32<64>::bytes() : ChunkPieceF32<128>::bytes());
+  return size_t(std::min<int64_t>(byte ? kP4SlotsByte : kP4Slots, pieces)) * (sh.head_dim == 64 ? ChunkPieceF32<64>::bytes() : ChunkPieceF32<128>::bytes());
 }
 
 void launch_chunk_f32_merge(int d, const PagedChunkF32& c, hipStream_t stream) {

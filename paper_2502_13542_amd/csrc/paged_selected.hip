@@ -68,8 +68,8 @@ static size_t bit_bytes(const actqkv_shape& sh, int n_rows, int max_pages) {
   return size_t(n_rows) * sh.n_kv_heads * ((max_pages + 31) / 32) * sizeof(uint32_t);
 }
 static size_t chunk_scratch(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages) {
-  return align_up(sh.dtype == ACTQKV_F32 ? paged_chunk_f32_scratch_most(sh, batch, n_rows, max_new, max_pages)
-                                         : paged_chunk_scratch_most(sh, batch, n_rows, max_new, max_pages), 256);
+  return align_up(sh.dtype == ACTQKV_F32 ? paged_chunk_f32_scratch_most(sh, batch, n_rows, max_new, max_pages, false)
+                                         : paged_chunk_scratch_most(sh, batch, n_rows, max_new, max_pages, false), 256);
 }
 size_t paged_selected_scratch_most(const actqkv_shape& sh, int batch, int n_rows, int max_new, int max_pages) {
   const size_t parts = step_part_most(sh, int64_t(n_rows) * sh.n_kv_heads);

@@ -911,12 +911,15 @@ class PagedRunner:
     batch, n_rows, max_new and max_pages are the most that a call brings: sequences, rows of all of them, rows of one,
     pages of one.  A call's own numbers follow from its tensors: row_start [batch + 1], n_ctx [batch], pages [batch][max_pages];
     the library's header says what they hold.  What no tensor says is the most rows that a sequence of this call brings: a call
-    that knows it (1 in a decode step) says so in max_new and takes the kernels for it."""
+    that knows it (1 in a decode step) says so in max_new and takes the kernels for it.
+    attention_only: the workspace is that of attend and attend_weigh, which is smaller; pages in 8 bits and selected pages are refused
+    where they need more."""
 
-    def __init__(self, shape: LayerShape, batch: int, n_rows: int, max_new: int, max_pages: int, device="cuda"):
+    def __init__(self, shape: LayerShape, batch: int, n_rows: int, max_new: int, max_pages: int, device="cuda", attention_only: bool = False):
         self.shape, self.batch, self.n_rows, self.max_new, self.max_pages = shape, batch, n_rows, max_new, max_pages
         self.cs = B.c_shape(shape)
-        ws = B.paged_workspace_bytes(self.cs, batch, n_rows, max_new, max_pages)
+        need = B.paged_attention_workspace_bytes if attention_only else B.paged_workspace_bytes
+        ws = need(self.cs, batch, n_rows, max_new, max_pages)
         self.workspace = torch.zeros(ws, dtype=torch.uint8, device=device)
         self._page = shape.n_kv_heads * shape.block_size * shape.head_dim
         self._q_row, self._kv_row = shape.n_q_heads * shape.head_dim, shape.n_kv_heads * shape.head_dim
