@@ -777,6 +777,17 @@ int actqkv_paged_attention_selected(const actqkv_shape* shape, int batch, int n_
                                     int k_sel, float softcap, int window, const float* slopes, const int32_t* row_first,
                                     const int32_t* row_end, void* out, float* lse, void* workspace, size_t ws_bytes, void* stream);
 
+/* How a call on pages is cut up, by its sizes (host only, nothing is launched; for tests and tuning).
+ *   call   one of ACTQKV_CUT_*; k_sel of ACTQKV_CUT_SELECTED, queries (whether q is given) of ACTQKV_CUT_APPEND_QUANTISED, softcap, window and documents
+ *          (whether row_first is given) of attention.
+ *   cut[3] attention: (row, query head) pairs of a workgroup of the chunks' kernels (0: those of few rows, or lists, take the call), wavefronts that
+ *          share a page for them, pieces of their pages; appends: items and workgroups of the largest launch (of more items the workgroups go round), launches;
+ *          selection: 16 where the scores of so many rows come from the matrix instruction, otherwise 1, workgroups of a row and KV head, launches.
+ * Errors: EINVAL, ESHAPE. */
+enum { ACTQKV_CUT_ATTENTION = 0, ACTQKV_CUT_QUANTISED = 1, ACTQKV_CUT_SELECTED = 2, ACTQKV_CUT_APPEND_ROTATED = 3, ACTQKV_CUT_APPEND_QUANTISED = 4, ACTQKV_CUT_SELECTION = 5 };
+int actqkv_paged_cut(const actqkv_shape* shape, int call, int batch, int n_rows, int max_new, int max_pages, int k_sel, int queries,
+                     float softcap, int window, int documents, int32_t* cut);
+
 /* How an attention call of batch windows of m >= 2 tokens in bf16 is cut up (host only, nothing is launched): cut[0] query rows of
  * a workgroup, cut[1] query tiles of a window and KV head, cut[2] pieces they are in altogether (equal: not cut; the tiles are
  * cut into cut[2] / cut[1] pieces, rounded down, some into one more), cut[3] 1 if a second launch merges the pieces.

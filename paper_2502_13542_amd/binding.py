@@ -107,6 +107,7 @@ SIGNATURES = {
     "actqkv_paged_select_pages": (_i, [_shp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _i, _i, _i, _i, _vp, _i64, _vp, _vp, _vp, _sz, _vp]),
     "actqkv_paged_attention_selected": (_i, [_shp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _i, _vp, _vp, _i, ctypes.c_float,
                                              _i, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "actqkv_paged_cut": (_i, [_shp, _i, _i, _i, _i, _i, _i, _i, ctypes.c_float, _i, _i, _vp]),
     "actqkv_last_error": (ctypes.c_char_p, []),
     "actqkv_prefill_cut": (_i, [_shp, _i, _i, _i, _i, _vp]),
     "actqkv_version": (_i, []),
@@ -192,6 +193,19 @@ def prefill_cut(shape: CShape, batch: int, m: int, k_cap: int, cus: int = 256) -
     """(rows of a workgroup, query tiles, pieces altogether, merged by a launch) of an attention call; see the header."""
     cut = (ctypes.c_int32 * 4)()
     if load_library().actqkv_prefill_cut(ctypes.byref(shape), batch, m, k_cap, cus, cut) != 0:
+        raise ActQKVError(-1, last_error())
+    return tuple(cut)
+
+
+PAGED_CALLS = ("attention", "attention_quantised", "attention_selected", "append_rotated", "append_quantised", "select_pages")
+
+
+def paged_cut(shape: CShape, call: str, batch: int, n_rows: int, max_new: int, max_pages: int, k_sel: int = 0, queries: bool = False,
+              softcap: float = 0.0, window: int = 0, documents: bool = False) -> tuple:
+    """How a call on pages (one of PAGED_CALLS) is cut up; see the header."""
+    cut = (ctypes.c_int32 * 3)()
+    if load_library().actqkv_paged_cut(ctypes.byref(shape), PAGED_CALLS.index(call), batch, n_rows, max_new, max_pages, k_sel, int(queries),
+                                       softcap, window, int(documents), cut) != 0:
         raise ActQKVError(-1, last_error())
     return tuple(cut)
 

@@ -278,6 +278,13 @@ size_t paged_votes_scratch_most(const actqkv_shape& sh);
 int launch_paged_votes(const actqkv_shape& sh, const PagedAttn& p, const PagedWeights& w, const Workspace& ws, hipStream_t stream);
 int launch_paged_append(const actqkv_shape& sh, const PagedTable& t, const void* k_new, const void* v_new,
                         void* k_pages, void* v_pages, hipStream_t stream);
+// How a call is cut up: cut[0 .. 2] as of actqkv_paged_cut.
+void paged_chunk_cut(const actqkv_shape& sh, const PagedAttn& p, int32_t* cut);
+void paged_chunk_f32_cut(const actqkv_shape& sh, const PagedAttn& p, int32_t* cut);
+void paged_select_cut(const actqkv_shape& sh, const PagedTable& t, int32_t* cut);
+bool paged_selected_by_chunks(const actqkv_shape& sh, const PagedAttn& p, int k_sel);
+void paged_append_rotated_cut(const actqkv_shape& sh, const PagedTable& t, int32_t* cut);
+void paged_append_quantised_cut(const actqkv_shape& sh, const PagedTable& t, bool queries, int32_t* cut);
 // Rotation of keys and queries by their position (paged_rotate.h).
 struct PagedRotation {
   const float* table;        // [n_positions][2][dims / 2]: cosines, sines; NULL: none (dims 0)

@@ -209,6 +209,19 @@ __global__ __launch_bounds__(kThreads) void paged8_append_kernel(PagedAppend8 a)
   }
 }
 
+// The items of a launch; of keys and values alone there are no slices of rows.
+struct QuantisedItems {
+  const actqkv_shape& sh;
+  const PagedTable& t;
+  bool queries;
+  template <typename T, typename Dim, typename Threads>
+  TurnItems operator()(T*, Dim, Threads, int least, int most) const {
+    return turn_items(sh, t, queries ? kTurnRows<T, Dim::value, Threads::value> : 0, 2, least, most);
+  }
+};
+void paged_append_quantised_cut(const actqkv_shape& sh, const PagedTable& t, bool queries, int32_t* cut) {
+  turn_cut<kTurnThreads>(sh, t, cut, QuantisedItems{sh, t, queries});
+}
 int launch_paged_append_quantised(const actqkv_shape& sh, const PagedTable& t, const PagedRotation& r, const void* q, const void* k_new,
                              const void* v_new, uint8_t* k_pages, uint8_t* v_pages, float* k_scales, float* v_scales, void* q_out,
                              hipStream_t stream) {
@@ -228,8 +241,7 @@ int launch_paged_append_quantised(const actqkv_shape& sh, const PagedTable& t, c
   with_turn_types<kTurnThreads>(sh, t, [&](auto* type, auto dim, auto threads, auto few, int least, int most) {
     typedef std::remove_pointer_t<decltype(type)> T;
     constexpr int D = decltype(dim)::value, kThreads = decltype(threads)::value;
-    const int rows = q != nullptr ? kTurnRows<T, D, kThreads> : 0;
-    a.items = turn_items(sh, t, rows, 2, least, most);
+    a.items = QuantisedItems{sh, t, q != nullptr}(type, dim, threads, least, most);
     if (a.items.total == 0) return;
     const dim3 grid(std::min(a.items.total, kTurnMostWgs));
     constexpr bool kFew = decltype(few)::value;

@@ -331,6 +331,45 @@ int actqkv_paged_attention_selected(const actqkv_shape* shape, int batch, int n_
                         workspace, ws_bytes, stream);
 }
 
+int actqkv_paged_cut(const actqkv_shape* shape, int call, int batch, int n_rows, int max_new, int max_pages, int k_sel, int queries,
+                     float softcap, int window, int documents, int32_t* cut) {
+  ACTQKV_TRY(check_shape(shape));
+  ACTQKV_TRY(check_batch(batch));
+  ACTQKV_TRY(check_rows(n_rows, max_new));
+  if (max_pages < 1 || max_pages > kMaxPages) return set_error(ACTQKV_EINVAL, "max_pages %d outside 1..%d", max_pages, kMaxPages);
+  if (call < ACTQKV_CUT_ATTENTION || call > ACTQKV_CUT_SELECTION) return set_error(ACTQKV_EINVAL, "call %d is none", call);
+  if (cut == nullptr) return set_error(ACTQKV_EINVAL, "cut is NULL");
+  PagedAttn p = {};
+  p.t = PagedTable{nullptr, nullptr, nullptr, batch, n_rows, max_new, max_pages, 1, 0};
+  if (call == ACTQKV_CUT_APPEND_ROTATED) {
+    paged_append_rotated_cut(*shape, p.t, cut);
+    return ACTQKV_OK;
+  }
+  if (call == ACTQKV_CUT_APPEND_QUANTISED) {
+    paged_append_quantised_cut(*shape, p.t, queries != 0, cut);
+    return ACTQKV_OK;
+  }
+  if (call == ACTQKV_CUT_SELECTION) {
+    paged_select_cut(*shape, p.t, cut);
+    return ACTQKV_OK;
+  }
+  // (the cut asks which arrays there are, not what they hold)
+  static const float scales = 1.f;
+  static const int32_t first = 0;
+  p.k_scales = p.v_scales = call == ACTQKV_CUT_QUANTISED ? &scales : nullptr;
+  p.f.row_first = documents != 0 ? &first : nullptr;
+  p.f.window = window;
+  p.f.cap_in = softcap > 0.f ? 1.f / softcap : 0.f;
+  if (call == ACTQKV_CUT_SELECTED) ACTQKV_TRY(check_k_sel(shape, n_rows, k_sel));
+  if (call == ACTQKV_CUT_SELECTED ? !paged_selected_by_chunks(*shape, p, k_sel) : paged_step_supported(*shape, max_new)) {
+    cut[0] = cut[1] = cut[2] = 0;
+    return ACTQKV_OK;
+  }
+  if (shape->dtype == ACTQKV_F32) paged_chunk_f32_cut(*shape, p, cut);
+  else paged_chunk_cut(*shape, p, cut);
+  return ACTQKV_OK;
+}
+
 int actqkv_paged_evict(const actqkv_shape* shape, int batch, const int32_t* n_ctx, const int32_t* pages, int max_pages,
                        void* k_pages, void* v_pages, int n_pages, const float* weights, int64_t weight_stride,
                        int keep_first, int keep_last, int budget, const int32_t* to_pages, int to_max_pages,

@@ -96,6 +96,18 @@ __global__ __launch_bounds__(kThreads) void paged_append_rotated_kernel(PagedApp
   }
 }
 
+// The items of a launch.
+struct RotatedItems {
+  const actqkv_shape& sh;
+  const PagedTable& t;
+  template <typename T, typename Dim, typename Threads>
+  TurnItems operator()(T*, Dim, Threads, int least, int most) const {
+    return turn_items(sh, t, kTurnRows<T, Dim::value, Threads::value>, kArSlices, least, most);
+  }
+};
+void paged_append_rotated_cut(const actqkv_shape& sh, const PagedTable& t, int32_t* cut) {
+  turn_cut<kTurnThreads>(sh, t, cut, RotatedItems{sh, t});
+}
 int launch_paged_append_rotated(const actqkv_shape& sh, const PagedTable& t, const PagedRotation& r, const void* q, const void* k_new,
                                 const void* v_new, void* k_pages, void* v_pages, void* q_out, hipStream_t stream) {
   PagedAppendRotated a;
@@ -111,8 +123,8 @@ int launch_paged_append_rotated(const actqkv_shape& sh, const PagedTable& t, con
   a.group = sh.n_q_heads / sh.n_kv_heads;
   with_turn_types<kTurnThreads>(sh, t, [&](auto* type, auto dim, auto threads, auto few, int least, int most) {
     typedef std::remove_pointer_t<decltype(type)> T;
-    constexpr int D = decltype(dim)::value, kThreads = decltype(threads)::value, kRows = kTurnRows<T, D, kThreads>;
-    a.items = turn_items(sh, t, kRows, kArSlices, least, most);
+    constexpr int D = decltype(dim)::value, kThreads = decltype(threads)::value;
+    a.items = RotatedItems{sh, t}(type, dim, threads, least, most);
     if (a.items.total == 0) return;
     hipLaunchKernelGGL((paged_append_rotated_kernel<T, D, kThreads, decltype(few)::value>), dim3(std::min(a.items.total, kTurnMostWgs)),
                        dim3(kThreads), 0, stream, a);

@@ -74,6 +74,12 @@ static void launch_chunk_ks(int ks, const PagedChunk& c, hipStream_t stream) {
   else if (ks == 2) launch_chunk<D, 2>(c, stream);
   else launch_chunk<D, 4>(c, stream);
 }
+void paged_chunk_cut(const actqkv_shape& sh, const PagedAttn& p, int32_t* cut) {
+  const ChunkCut c = chunk_cut(sh, p);
+  cut[0] = kPcRows<1> / c.ks;
+  cut[1] = c.ks;
+  cut[2] = c.splits;
+}
 int launch_paged_chunk(const actqkv_shape& sh, const PagedAttn& p, const Workspace& ws, hipStream_t stream) {
   const ChunkCut cut = chunk_cut(sh, p);
   PagedChunk c;

@@ -45,6 +45,11 @@ static void launch_chunk_f32(const PagedChunkF32& c, hipStream_t stream) {
   else launch(paged_chunk_f32_kernel<D, false, false>);
   launch_chunk_f32_merge(D, c, stream);
 }
+void paged_chunk_f32_cut(const actqkv_shape& sh, const PagedAttn& p, int32_t* cut) {
+  cut[0] = kP4Rows;
+  cut[1] = 1;
+  cut[2] = chunk_f32_splits(sh, p, chunk_f32_tiles(sh, p.t.batch, p.t.n_rows, p.t.max_new));
+}
 int launch_paged_chunk_f32(const actqkv_shape& sh, const PagedAttn& p, const Workspace& ws, hipStream_t stream) {
   PagedChunkF32 c;
   c.a = p;

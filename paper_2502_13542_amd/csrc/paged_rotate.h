@@ -215,5 +215,16 @@ inline void with_turn_types(const actqkv_shape& sh, const PagedTable& t, Launch 
     else by_rows(static_cast<uint16_t*>(nullptr), d128);
   }
 }
+// What the launches of a call have to do: items and workgroups of the largest, and how many launches there are.
+template <int kMost, typename Items>
+inline void turn_cut(const actqkv_shape& sh, const PagedTable& t, int32_t* cut, Items items_of) {
+  cut[0] = cut[1] = cut[2] = 0;
+  with_turn_types<kMost>(sh, t, [&](auto* type, auto dim, auto threads, auto, int least, int most) {
+    const int total = items_of(type, dim, threads, least, most).total;
+    cut[0] = std::max(cut[0], total);
+    cut[1] = std::max(cut[1], std::min(total, kTurnMostWgs));
+    cut[2] += total > 0;
+  });
+}
 
 }  // namespace actqkv

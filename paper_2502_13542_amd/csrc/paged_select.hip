@@ -381,6 +381,29 @@ int launch_paged_bounds(const actqkv_shape& sh, const PagedTable& t, const void*
   }
   return hip_status("paged key bounds");
 }
+// Which way a call's scores take, and the tiles of 16 rows of the matrix instruction's.
+// Both ways' time by their products, of rows as they are and in tiles of 16 (and a launch more): us of one | the other, 32 query and 8 KV heads
+// of 128: 512 rows at 100K tokens 332 | 151, 64 56 | 31, 16 23.5 | 20.1, at 16K 8.9 | 18.4, 2 x 2048 rows at 16K 462 | 234, 16 x 8 at 32K 36 | 29.5, 16 x 4
+// 17.5 | 28; fp32, 8 and 2 heads of 64, 512 rows at 8K 14.0 | 15.5, 32 at 60K 11.9 | 15.1.
+static bool select_scored(const actqkv_shape& sh, const PagedTable& t, int* tiles) {
+  const int seqs = std::min(t.batch, t.n_rows);
+  *tiles = int(std::min<int64_t>(int64_t(seqs) * ((t.max_new + kScRows - 1) / kScRows), t.n_rows / kScRows + seqs));
+  const double products = double(sh.n_q_heads) * sh.head_dim * t.max_pages;     // of a row
+  return products * t.n_rows / 4.6e6 > products * *tiles * kScRows / 11.6e6 + 3.;
+}
+// Workgroups of a (row, KV head) that scores its own pages.
+static int select_parts(const actqkv_shape& sh, const PagedTable& t) {
+  const int64_t items = int64_t(t.n_rows) * sh.n_kv_heads;
+  if (items > int64_t(kTicketCounters)) return 1;
+  return int(std::max<int64_t>(1, std::min<int64_t>((t.max_pages + kSelLeast - 1) / kSelLeast, kSelWgs / items)));
+}
+void paged_select_cut(const actqkv_shape& sh, const PagedTable& t, int32_t* cut) {
+  int tiles;
+  const bool scored = select_scored(sh, t, &tiles);
+  cut[0] = scored ? kScRows : 1;
+  cut[1] = scored ? 1 : select_parts(sh, t);
+  cut[2] = scored ? 2 : 1;
+}
 int launch_paged_select(const actqkv_shape& sh, const PagedTable& t, const void* q, const void* bounds, int k_sel, int keep_first,
                         int keep_last, float* scores, int64_t stride, int32_t* idx, int32_t* n_sel, const Workspace& ws, hipStream_t stream) {
   PagedSelect a;
@@ -397,14 +420,10 @@ int launch_paged_select(const actqkv_shape& sh, const PagedTable& t, const void*
   a.idx = idx;
   a.n_sel = n_sel;
   const int64_t items = int64_t(t.n_rows) * sh.n_kv_heads;
-  a.parts = items > int64_t(kTicketCounters) ? 1 : int(std::max<int64_t>(1, std::min<int64_t>((t.max_pages + kSelLeast - 1) / kSelLeast, kSelWgs / items)));
+  a.parts = select_parts(sh, t);
   a.counters = ws.counters();
-  // Both ways' time by their products, of rows as they are and in tiles of 16 (and a launch more): us of one | the other, 32 query and 8 KV heads
-  // of 128: 512 rows at 100K tokens 332 | 151, 64 56 | 31, 16 23.5 | 20.1, at 16K 8.9 | 18.4, 2 x 2048 rows at 16K 462 | 234, 16 x 8 at 32K 36 | 29.5, 16 x 4
-  // 17.5 | 28; fp32, 8 and 2 heads of 64, 512 rows at 8K 14.0 | 15.5, 32 at 60K 11.9 | 15.1.
-  const int seqs = std::min(t.batch, t.n_rows), tiles = int(std::min<int64_t>(int64_t(seqs) * ((t.max_new + kScRows - 1) / kScRows), t.n_rows / kScRows + seqs));
-  const double products = double(sh.n_q_heads) * sh.head_dim * t.max_pages;     // of a row
-  const bool scored = products * t.n_rows / 4.6e6 > products * tiles * kScRows / 11.6e6 + 3.;
+  int tiles;
+  const bool scored = select_scored(sh, t, &tiles);
   auto launch = [&](auto* type, auto dim) {
     typedef std::remove_pointer_t<decltype(type)> T;
     constexpr int D = decltype(dim)::value;

@@ -81,7 +81,7 @@ size_t paged_selected_scratch_most(const actqkv_shape& sh, int batch, int n_rows
 // and 5 us (for which each row has its own reads and merge to wait for).  us of lists | so: 42 sequences of up to 8 rows at up to 724 tokens, 28 query and 4 KV heads,
 // 4 pages each 30 | 24, 24 of them at 1733 tokens 22 | 30; 32 and 8 heads, 1 x 16 rows, 16 pages at 16K 22 | 33, 30 x 10 rows, 2 pages at 300 41 | 16; fp32, 8 and 2 heads
 // of 64, 8 x 12 rows, 8 pages at 2K 26 | 26.
-static bool selected_by_chunks(const actqkv_shape& sh, const PagedAttn& p, int k_sel) {
+bool paged_selected_by_chunks(const actqkv_shape& sh, const PagedAttn& p, int k_sel) {
   if (paged_step_supported(sh, p.t.max_new) || p.t.max_pages > 32 * kMostBitWords ||
       bit_bytes(sh, p.t.n_rows, p.t.max_pages) > kMostBitBytes)
     return false;
@@ -102,7 +102,7 @@ int launch_paged_selected(const actqkv_shape& sh, const PagedAttn& p, const int3
   st.idx = idx;
   st.n_sel = n_sel;
   st.k_sel = k_sel;
-  if (selected_by_chunks(sh, p, k_sel)) {
+  if (paged_selected_by_chunks(sh, p, k_sel)) {
     const PagedTable& t = p.t;
     uint32_t* bits = reinterpret_cast<uint32_t*>(ws.scratch_f32()) + chunk_scratch(sh, t.batch, t.n_rows, t.max_new, t.max_pages) / sizeof(uint32_t);
     const int words = (t.max_pages + 31) / 32;
