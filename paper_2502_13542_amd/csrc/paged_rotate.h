@@ -13,7 +13,9 @@ namespace actqkv {
 // Threads of a workgroup: of calls whose sequences bring few rows one wavefront, which has no barriers to wait at and leaves room for the
 // other workgroups (a step of 64 sequences, 32 query and 8 KV heads of 128, turned: 6.3 us in workgroups of 256 threads, 5.0 so; into 8 bits 10.6, 5.9).
 constexpr int kTurnThreads = 256, kTurnFew = 64;
-constexpr int kTurnMostWgs = 1 << 22;      // workgroups of a launch: more work goes round
+// Workgroups of a launch: of more items they go round (64 chunks of 2048 rows, 32 query and 8 KV heads of 128, 50 thousand items: 599 us, with a
+// workgroup each 594; into 8 bits 657, 674).
+constexpr int kTurnMostWgs = 1 << 15;
 constexpr int kTurnApart = 256;            // (sequence, KV head) pairs of few rows that are worth a launch
 
 // The work of a call is dealt out in items of a KV head: a sequence has slices of its rows and pages with new tokens, as many as it needs
