@@ -754,13 +754,16 @@ int actqkv_paged_key_bounds(const actqkv_shape* shape, int batch, int n_rows, in
 /* Selection.  The row at position p sees the pages b = 0 .. p / Bs of its sequence that are in the pool.
  *   scores [n_rows][Hk][score_stride] fp32, score_stride >= max_pages: of page b
  *            max over the G query heads of  sum over the channels of max(q lo, q hi)
- *            with the page's bounds lo, hi, in 64 bits rounded to fp32: at least every <q, k> in the page, of any of the heads.  -infinity for pages that the
- *            row does not see, up to entry max_pages - 1.
+ *            with the page's bounds lo, hi, in 64 bits rounded to the nearest fp32 number: but for that rounding at least every <q, k> in the page, of any of
+ *            the heads.  -infinity for pages that the row does not see, up to entry max_pages - 1.
  *   idx    [n_rows][Hk][k_sel] int32: the pages that are selected, ascending, -1 behind the last: the first keep_first and the last keep_last of 0 .. p / Bs
  *            (keep_first + keep_last <= k_sel), and those with the largest scores of the others (equal scores: the lower page), k_sel in all, or every page that
  *            the row sees if there are no more.
  *   n_sel  [n_rows][Hk] int32: how many.
- * Queries, bounds and scores are finite in fp32 (a page whose score is -infinity is not selected).
+ * The selection is that of the scores written.  The order of a score's sum depends on the sizes of the call: where 64 bits hold all products and sums exactly
+ * (bf16 of ordinary size) calls of other sizes give a row the same scores, otherwise scores that may differ by the roundings (a unit of the last place, more of
+ * sums that cancel), and then, of two pages so close where the selection ends, the other one.
+ * Queries, bounds and scores are finite in fp32 (a page whose score is -infinity is not selected; what an infinite bound gives depends on the sizes, too).
  * Rows that belong to no sequence are not written; of a row at a negative position nothing is selected.  n_rows * Hk is at most 2^22.
  * Errors: EINVAL, ESHAPE, EALIGN, EWORKSPACE. */
 int actqkv_paged_select_pages(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q, const int32_t* row_start,

@@ -2,8 +2,10 @@
 //
 // Bounds.  Of every page and KV head the least and the largest key of each channel.  With them sum_d max(q_d lo_d, q_d hi_d) is at least
 // every product <q, k> in the page: a page that holds a key that the row answers to is not missed, whatever its other keys are.
-// The score of a page for a row and KV head is the largest of that over the G query heads.  Products and sums are in 64 bits and the result is
-// rounded to fp32, so that the selection does not depend on the order of a sum.
+// The score of a page for a row and KV head is the largest of that over the G query heads.  Products (exact) and sums are in 64 bits and the result is
+// rounded to fp32, so that the order of a sum matters only where 64 bits do not hold it and it lies next to the border of two fp32 numbers: the two ways to
+// the scores below, channel by channel and as two sums of positive and of negative queries, differ by a unit of the last place then (by more where a sum cancels).  What is selected
+// follows from the scores as they are written.
 //
 // Scores: a lane has 16 channels of a page, D / 16 lanes a page.  Selection: the key of the last page that stays by a radix histogram, eight bits at a
 // time from the highest in which keys differ, then the chosen pages in their order; integers throughout, ties to the lower page.
