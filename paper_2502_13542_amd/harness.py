@@ -1084,12 +1084,14 @@ class PagedRunner:
         B.paged_attention_quantised(self.cs, batch, n_rows, max_new, q, row_start, n_ctx, pages, max_pages, k_pages, v_pages, n_pages,
                                     k_scales, v_scales, out, lse, self.workspace, softcap, window, slopes, row_first, row_end, stream)
 
-    def key_bounds(self, n_ctx, pages, k_pages, bounds, row_start=None, n_rows: int = 0, stream=None, max_new=None) -> None:
+    def key_bounds(self, n_ctx, pages, k_pages, bounds, row_start=None, n_rows=None, stream=None, max_new=None) -> None:
         """bounds [n_pages][Hk][2][D], the least and the largest key of every channel: of the pages with new tokens (the n_rows rows
         that row_start deals out), or of all pages (row_start None)."""
         n_pages = k_pages.size(0)
-        if n_rows < 0:
-            raise B.ActQKVError(-1, f"{n_rows} rows")
+        if row_start is None:
+            n_rows = 0
+        elif n_rows is None or n_rows < 0:         # (no tensor of this call says how many)
+            raise B.ActQKVError(-1, f"row_start with n_rows {n_rows}")
         batch, max_pages, max_new = self._limits(pages, n_rows, max_new)
         B.check_sizes(n_ctx, batch, row_start, batch + 1, k_pages, n_pages * self._page, bounds, n_pages * 2 * self._kv_row)
         if row_start is not None and n_rows == 0:
