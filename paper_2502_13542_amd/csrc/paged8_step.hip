@@ -7,8 +7,10 @@
 
 namespace actqkv {
 
+// (At least two wavefronts a SIMD: two workgroups of four on a compute unit.  Left to itself the compiler takes up to 290 registers for fp32 and 128
+// channels, and 258 for bf16 under a cap with slopes; so 3 to 8 of fp32 with 128 channels are in scratch, of workgroups of eight as well.)
 template <typename T, int D, int W, bool kCap, bool kBias>
-__global__ __launch_bounds__(64 * W) void paged8_step_kernel(PagedStep st) {
+__global__ __launch_bounds__(64 * W, 2) void paged8_step_kernel(PagedStep st) {
   step_body<Step8Shape<T, D>, T, D, kCap, kBias, false, W>(st);
 }
 template <typename T, int D, int W>
@@ -25,7 +27,8 @@ static void launch_step8_by(const PagedStep& st, hipStream_t stream) {
 // Many short sequences by workgroups of four wavefronts, two of them on a compute unit: more workgroups than there are compute units, of a page for each
 // wavefront, or half as many again of up to 16.  us of eight | four, 32 query and 8 KV heads of 128: 300 sequences at up to 128 tokens 47 | 30, 64 at 700
 // 20.6 | 17.4, at 2K 40 | 34, at 8K (32 a workgroup) 150 | 150, 33 at 1K 17.9 | 20.0; 28 and 4 heads, 42 at 724 (3) 17.5 | 14.4, 80 at 724 (6) 18.8 | 20.8, 80
-// at 3K 42 | 51; fp32, 8 and 2 heads of 64, 200 at 1K 15.3 | 13.7; fewer workgroups: 32 and 8 heads, 32 at 700 10.9 | 11.9.
+// at 3K 42 | 51; fp32, 8 and 2 heads of 64, 200 at 1K 15.3 | 13.7, of 128 100 at 1K 21.9 | 18.0,
+// 32 and 8 heads 300 at up to 128 62 | 36, 64 at 2K 50 | 43, 33 at 700 18.0 | 19.0; under a cap with slopes, bf16, 300 at up to 128 60 | 34, 64 at 2K 49 | 40; fewer workgroups: 32 and 8 heads, 32 at 700 10.9 | 11.9.
 template <typename T, int D>
 static void launch_step8(const PagedStep& st, hipStream_t stream) {
   const int64_t wgs = int64_t(st.a.t.batch) * st.a.n_kv_heads * st.n_wg, pages = (st.a.t.max_pages + st.n_wg - 1) / st.n_wg;

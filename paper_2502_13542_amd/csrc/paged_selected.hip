@@ -17,8 +17,9 @@ double paged_chosen_chunk_f32_us(const actqkv_shape& sh, const PagedAttn& p);
 int launch_paged_chosen_chunk(const actqkv_shape& sh, const PagedAttn& p, const PagedBits& bits, const Workspace& ws, hipStream_t stream);
 int launch_paged_chosen_chunk_f32(const actqkv_shape& sh, const PagedAttn& p, const PagedBits& bits, const Workspace& ws, hipStream_t stream);
 
+// (At least two wavefronts a SIMD: without the bound fp32 of 128 channels under a cap takes 260 registers, and one.)
 template <typename T, int D, int W, bool kCap, bool kBias>
-__global__ __launch_bounds__(64 * W) void paged_selected_kernel(PagedStep st) {
+__global__ __launch_bounds__(64 * W, 2) void paged_selected_kernel(PagedStep st) {
   step_body<StepShape<T, D>, T, D, kCap, kBias, true, W>(st);
 }
 template <typename T, int D, int W>
@@ -34,7 +35,8 @@ static void launch_selected_by(const PagedStep& st, hipStream_t stream) {
 // A compute unit holds eight wavefronts: with more workgroups than there are compute units two of four side by side, so that one's table, list and merge are
 // hidden behind another's keys.  us of eight | two of four: 42 rows, 28 query and 4 KV heads, 4 pages each 20.1 | 16.9, 142 32.6 | 28.9; 32 and 8
 // heads, 64 rows of 4 pages 26.8 | 24.1, of 16 91.3 | 90.6, 128 rows of 8 99.0 | 92.4; fewer workgroups: 16 rows of 16 25.6 | 26.6, 1 of 4 7.4 | 8.3.  Of long
-// lists only where that fills them: fp32, 8 and 2 heads of 64, 32 pages, 140 rows 114 | 144, 200 rows of 16 87 | 85.
+// lists only where that fills them: fp32, 8 and 2 heads of 64, 32 pages, 140 rows 114 | 144, 200 rows of 16 87 | 85,
+// of 128 140 rows of 8 81 | 73 (under a cap 83 | 75), 200 of 4 48 | 42, of 32 pages, 140 rows 241 | 252; 32 and 8 heads, 64 rows of 4 48 | 42, of 16 211 | 203.
 template <typename T, int D>
 static void launch_selected(const PagedStep& st, int64_t items, hipStream_t stream) {
   const int64_t wgs = int64_t(st.a.t.n_rows) * st.a.n_kv_heads * st.n_wg;
