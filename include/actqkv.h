@@ -751,7 +751,8 @@ int actqkv_paged_key_bounds(const actqkv_shape* shape, int batch, int n_rows, in
                             const int32_t* n_ctx, const int32_t* pages, int max_pages, const void* k_pages, int n_pages,
                             void* bounds, void* stream);
 
-/* Selection.  The row at position p sees the pages b = 0 .. p / Bs of its sequence that are in the pool.
+/* Selection.  The row at position p sees the pages b = 0 .. p / Bs of its sequence that are in the pool; score caps keep the order of the scores, but of slopes,
+ * windows and masks that the attention may have besides the selection knows nothing.
  *   scores [n_rows][Hk][score_stride] fp32, score_stride >= max_pages: of page b
  *            max over the G query heads of  sum over the channels of max(q lo, q hi)
  *            with the page's bounds lo, hi, in 64 bits rounded to the nearest fp32 number: but for that rounding at least every <q, k> in the page, of any of
@@ -773,7 +774,8 @@ int actqkv_paged_select_pages(const actqkv_shape* shape, int batch, int n_rows, 
 
 /* actqkv_paged_attention of rows that see, of the positions they would see there, those in their selected pages alone: idx and n_sel as above (or the
  * caller's own, ascending, a page once; entries outside the sequence's pages are skipped).  Of single tokens and a few drafted ones every row reads its own pages;
- * rows of longer chunks share what tiles of them read, where that is less.  Workspace and errors as there; n_rows * Hk is at most 2^22. */
+ * rows of longer chunks share what tiles of them read, where that is less (probabilities enter the products in bf16 then, as actqkv_paged_attention's do of chunks, of
+ * few rows as two such terms).  Errors as there; n_rows * Hk is at most 2^22. */
 int actqkv_paged_attention_selected(const actqkv_shape* shape, int batch, int n_rows, int max_new, const void* q,
                                     const int32_t* row_start, const int32_t* n_ctx, const int32_t* pages, int max_pages,
                                     const void* k_pages, const void* v_pages, int n_pages, const int32_t* idx, const int32_t* n_sel,

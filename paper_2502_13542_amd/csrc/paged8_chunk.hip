@@ -1,8 +1,7 @@
 // Attention of chunks and prompts over a paged cache in 8 bits, bf16 queries (paged_chunk_body.h has the kernel, paged_chunk.hip its design).
-// Bound as over 16 bits: 2 x 2048 rows at 16K tokens, 32 query and 8 KV heads of 128, 907 to 930 us (1.11 to 1.14 PFLOP/s; 8192^3 as a library product
-// 1.20 to 1.23), mixed rows under a cap and a window, 28 and 4 heads, 275 (262 to 274 over 16 bits): the codes' conversion, 32 instructions a wavefront and
-// page, is hidden, and the cut is the same (of ten cases at all cuts the chosen one was within 5 % of the best but one: 22 sequences of up to 215 rows at up to
-// 18K tokens 203 us, in more pieces than a workspace has room for 178).
+// Bound as over 16 bits: 2 x 2048 rows at 16K tokens, 32 query and 8 KV heads of 128, 905 to 980 us between cards (1.05 to 1.14 PFLOP/s; 8192^3 as a library
+// product 1.20 to 1.23), mixed rows under a cap and a window, 28 and 4 heads, 257 to 266 (260 over 16 bits): the codes' conversion, 32 instructions a wavefront
+// and page, is hidden.  The cut goes by figures of its own (chunk_cut).  With 256 rows, 128 channels and slopes 10 registers are in scratch.
 #include "paged_chunk_body.h"
 
 namespace actqkv {
