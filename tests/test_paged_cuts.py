@@ -1,5 +1,7 @@
 """Every way in which attention of chunks over pages in 8 bits and over selected pages is cut up: the cut of each case is asserted on the host (so that
 figures which change it are noticed here), and the case runs in it on the GPU, against the plain fp64 implementation."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -59,6 +61,26 @@ def test_the_cases_are_all_cuts_of_chunks(call):
             assert got == (256 // want[0], *want), (layer, seqs, kind)
         found.add((layer[2], want[0], want[1] > 1))
     assert found == {(d, ks, cut) for d in (64, 128) for ks in (1, 2, 4) for cut in (False, True)}
+
+
+@pytest.mark.parametrize("bad,code", [(dict(call=-1), -1), (dict(call=6), -1), (dict(batch=0), -1), (dict(max_new=0), -1), (dict(max_new=10), -1),
+                                      (dict(max_pages=0), -1), (dict(call=2, k_sel=0), -1), (dict(n_rows=2 ** 22 + 1), -2), (dict(cut=None), -1)])
+def test_cuts_refused(bad, code):
+    cut = (ctypes.c_int32 * 3)(7, 7, 7)
+    a = dict(call=0, batch=2, n_rows=9, max_new=5, max_pages=4, k_sel=4, queries=0, softcap=0.0, window=0, documents=0, cut=cut)
+    a.update(bad)
+    cs = B.c_shape(shape_of(32, 8, 128, "bf16"))
+    assert B.load_library().actqkv_paged_cut(ctypes.byref(cs), *a.values()) == code
+    assert list(cut) == [7, 7, 7]
+
+
+def test_cuts_of_few_rows_and_of_lists():
+    """Steps take the kernels of few rows, rows of short lists read those; fp32 has one kind of workgroup; a window and documents shorten what is cut."""
+    assert cut_of("attention", (32, 8, 128), [(4, 900)] * 3, 0) == (0, 0, 0) == cut_of("attention_quantised", (8, 2, 64), [(1, 900)], 0, dtype="fp32")
+    assert cut_of("attention_selected", (32, 8, 128), [(5, 900)], 0, k_sel=1) == (0, 0, 0)
+    assert cut_of("attention_quantised", (8, 2, 64), [(300, 4000)], 0, dtype="fp32")[:2] == (128, 1)
+    whole, window = (cut_of("attention", (32, 8, 128), [(300, 9000)], 0, kind)[2] for kind in ("plain", "window"))
+    assert whole > window >= 1
 
 
 def reference(b, k, v, form, chosen=None):
